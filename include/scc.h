@@ -74,7 +74,8 @@ typedef enum {
     SCC_ERR_DTYPE = -4,     /* dtype is neither SCC_F32 nor SCC_BF16 */
     SCC_ERR_WORKSPACE = -5, /* workspace missing, misaligned or smaller than the call needs */
     SCC_ERR_LAUNCH = -6,    /* the HIP runtime refused a launch (hipGetLastError != hipSuccess) */
-    SCC_ERR_SCRATCH = -7    /* scc_backward_weight_static: the problem needs more than SCC_STATIC_SCRATCH_BYTES */
+    SCC_ERR_SCRATCH = -7,   /* scc_backward_weight_static: the problem needs more than SCC_STATIC_SCRATCH_BYTES */
+    SCC_ERR_OPTION = -8     /* an activation, a number of steps or a coefficient out of its range */
 } scc_status;
 
 /* Size of the device buffer the library itself holds, per GPU, for scc_backward_weight_static. */
@@ -347,6 +348,74 @@ int scc_dw_backward_as(const void* x, const void* kdw, const void* w, const void
 int scc_backward_weight_static(const void* x, const void* dy, void* dw,
                                int N, int Cin, int Cout, int H, int W, int cg, double co,
                                scc_dtype dtype, void* stream);
+
+/*
+ * Gated layer, with which a gated feed-forward block opens: two sliding-channel convolutions of the same input with the same windows,
+ * one of them through an activation, multiplied pixel by pixel:
+ *     g = scc_forward(x, w[0]),  u = scc_forward(x, w[1]),  y = act(g) * u
+ * act(g) = g / (1 + exp(-g)) (SCC_SILU) or g * (1 + erf(g / sqrt(2))) / 2 (SCC_GELU).  cg = 1 makes both projections dense (with the
+ * channels rotated by s_k, unless co is 0 or 1).  A sequence of S tokens is a map of S x 1 pixels, single tokens are N maps of 1 x 1.
+ * x: in, N*Cin*H*W.  w: in, 2*Cout*L: the gate's weights, then the other's.  y: out, N*Cout*H*W.  g and u are binary32
+ * sums (products as in scc_forward) and never reach memory; y is rounded once.  Non-finite inputs as for scc_forward.
+ * Three paths (scc_gated_forward_path): up to 4 columns N*H*W a kernel that is a reading of the weights; else a product on the
+ * matrix cores with the weights packed into the workspace, for layers whose channels fit on chip for 32 columns (2528 in bf16, 1240 in
+ * fp32); else a plain kernel for any shape.  workspace: at least scc_gated_forward_workspace_bytes(...) bytes, 256-byte aligned,
+ * owned by the caller, contents undefined before and after; NULL where the query returns 0 (as it does for invalid arguments).
+ * Errors: as scc_forward (2*Cout*L is limited as Cout*L is there), SCC_ERR_WORKSPACE, and SCC_ERR_OPTION for an unknown activation.
+ */
+typedef enum { SCC_SILU = 0, SCC_GELU = 1 } scc_activation;
+typedef enum {
+    SCC_GATED_ANY = 0,      /* the kernel for any shape */
+    SCC_GATED_FEW = 1,      /* few columns */
+    SCC_GATED_PRODUCT = 2   /* matrix cores */
+} scc_gated_paths;
+size_t scc_gated_forward_workspace_bytes(int N, int Cin, int Cout, int H, int W, int cg, double co, scc_dtype dtype);
+int scc_gated_forward_path(int N, int Cin, int Cout, int H, int W, int cg, double co, scc_dtype dtype);
+int scc_gated_forward(const void* x, const void* w, void* y, int N, int Cin, int Cout, int H, int W, int cg, double co,
+                      scc_activation act, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of the gated layer, g and u computed again from x and w:
+ *     dg = dy * u * act'(g),  du = dy * act(g)
+ *     dx = scc_backward_input(dg, w[0]) + scc_backward_input(du, w[1]),  dw = (scc_backward_weight(x, dg), scc_backward_weight(x, du))
+ * with dx one sum over both, rounded once.  In bf16 dg and du are rounded to bf16 between the two stages, as the gradient that one
+ * layer hands the next is; not so on layers of fewer than 64 columns.  dy: in, N*Cout*H*W.  dx: out, as x.  dw: out, 2*Cout*L values of the type `grad` (rounded from
+ * binary32 sums), which may be SCC_F32 or SCC_BF16 whatever dtype is.  Two calls on the same inputs give bitwise identical results.
+ * workspace: at least scc_gated_backward_workspace_bytes(...) bytes, as above (dg and du among them: 2*Cout planes).
+ * Errors: as scc_gated_forward; SCC_ERR_SHAPE also where the 2*Cout planes are too large to index.
+ */
+size_t scc_gated_backward_workspace_bytes(int N, int Cin, int Cout, int H, int W, int cg, double co, scc_dtype dtype, scc_dtype grad);
+int scc_gated_backward(const void* x, const void* w, const void* dy, void* dx, void* dw, int N, int Cin, int Cout, int H, int W, int cg,
+                       double co, scc_activation act, scc_dtype dtype, scc_dtype grad, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * Orthogonalised momentum update of a list of weight matrices.  For every matrix of rows[i] x cols[i], dense and row-major:
+ *     m <- momentum * m + g;   u = g + momentum * m (nesterov != 0), or m
+ *     w <- (1 - lr * weight_decay) * w - lr * sqrt(max(1, rows / cols)) * O(u)
+ * O(u), which scc_orthogonalise alone computes (u = g there), brings the singular values of u near 1 and leaves its singular vectors: with
+ * x = u / (||u||_F + eps), or the transpose of that where rows > cols, `steps` times
+ *     p = x x^T,   x <- a * x + (b * p + c * p p) x.
+ * O(0) = 0; a matrix with a NaN or an infinity comes out as NaN and leaves the others alone.  All products are to binary32 accuracy (split
+ * factors, as in scc_forward), sums binary32, the norm's binary64, in a fixed order: two calls give bitwise identical results.
+ * g, w and o have the type `dtype`, m is binary32.  The arrays of pointers and sizes are HOST arrays, read before the call
+ * returns; the matrices are device memory, and no two of one list may overlap.  scc_orthogonalise may write o over g.
+ * workspace: at least scc_orthogonal_workspace_bytes(...) bytes (about 36 bytes an element), 256-byte aligned, owned by the caller, contents
+ * undefined before and after.
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count, rows or cols < 1, or a matrix of over 2^31/40 elements), SCC_ERR_DTYPE, SCC_ERR_OPTION
+ * (steps outside 1 .. 100, a value that is not finite, eps < 0), SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH.
+ */
+typedef struct {
+    float lr, momentum, weight_decay;   /* scc_orthogonalise reads none of these three ... */
+    int nesterov;                       /* ... nor this */
+    int steps;
+    float a, b, c, eps;
+} scc_orthogonal_options;
+size_t scc_orthogonal_workspace_bytes(int count, const int* rows, const int* cols);
+int scc_orthogonalise(int count, const void* const* g, void* const* o, const int* rows, const int* cols,
+                      const scc_orthogonal_options* options, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+int scc_orthogonal_step(int count, void* const* w, const void* const* g, float* const* m, const int* rows, const int* cols,
+                        const scc_orthogonal_options* options, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static, human-readable name of a status code (never NULL). */
 const char* scc_status_string(int status);

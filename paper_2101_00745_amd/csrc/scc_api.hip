@@ -1,7 +1,6 @@
 // C ABI of the SCC library: argument validation, window arithmetic, kernel selection.
 // Every check except the launch status happens on the host before any HIP call.
-#include "scc.h"
-#include "scc_common.h"
+#include "scc_entry.h"
 
 #include <algorithm>
 #include <cmath>
@@ -13,9 +12,9 @@
 // handle for hipGetSymbolAddress; the device address it resolves to is what the kernels get.
 static __device__ __align__(256) unsigned char scratch[SCC_STATIC_SCRATCH_BYTES];
 
-namespace {
+using namespace scc;
 
-using scc::Problem;
+namespace {
 
 long long gcd_ll(long long a, long long b)
 {
@@ -27,8 +26,9 @@ long long gcd_ll(long long a, long long b)
     return a;
 }
 
-// Algorithm 1 in closed form.  Returns SCC_OK or the status that rejects the arguments.
-int make_problem(int N, int Cin, int Cout, int H, int W, int cg, double co, Problem* out)
+}  // namespace
+
+int scc::make_problem(int N, int Cin, int Cout, int H, int W, int cg, double co, Problem* out)
 {
     if (N <= 0 || Cin <= 0 || Cout <= 0 || H <= 0 || W <= 0 || cg < 1) return SCC_ERR_SHAPE;
     if (Cin % cg != 0) return SCC_ERR_SHAPE;
@@ -54,14 +54,7 @@ int make_problem(int N, int Cin, int Cout, int H, int W, int cg, double co, Prob
     return SCC_OK;
 }
 
-bool dtype_ok(scc_dtype d) { return d == SCC_F32 || d == SCC_BF16; }
-
-int launch_status(hipError_t e) { return e == hipSuccess ? SCC_OK : SCC_ERR_LAUNCH; }
-
-// The launchers report hipGetLastError(), which also returns (and clears) an error an EARLIER, unrelated call of
-// the process left behind.  Every entry point that launches drops such a leftover first, so that SCC_ERR_LAUNCH
-// always speaks of this call's own kernels.
-void drop_stale_error() { (void)hipGetLastError(); }
+namespace {
 
 // Device address of `scratch` on the current device, resolved once per device (each GPU holds its own copy
 // of the array at its own address).
@@ -81,13 +74,6 @@ int scratch_of_current_device(void** out)
     }
     *out = g_scratch_ptr[dev];
     return SCC_OK;
-}
-
-// f(T()) with T the storage type of `dtype`
-template <typename F>
-int with_type(scc_dtype dtype, F&& f)
-{
-    return dtype == SCC_F32 ? f(float()) : f(scc::bf16_t());
 }
 
 // SCC_FORWARD_*, or SCC_ERR_WORKSPACE.  bf16 layers that gain from it keep their weights in registers and leave a workspace they are
@@ -128,14 +114,6 @@ int run_backward_input(const T* dy, const T* w, T* dx, const Problem& p, void* w
     return launch_status(scc::launch_backward_input_generic(dy, w, dx, p, st));
 }
 
-int size_of(scc_dtype dtype) { return dtype == SCC_F32 ? 4 : 2; }
-
-// Whether a call may use `need` bytes of its workspace.
-bool holds(size_t need, const void* workspace, size_t workspace_bytes)
-{
-    return need == 0 || (workspace && workspace_bytes >= need && ((uintptr_t)workspace & 255u) == 0);
-}
-
 // Grad-weight: the kernel that shares its operands between filter tiles on the layers that gain from it (`shared`) where
 // the workspace holds its partial sums, else the one with a tile per wavefront, else the one for any shape.  A workspace of
 // weight_least bytes is what a call cannot do without.
@@ -172,8 +150,6 @@ int run_weight(const void* x, const void* dy, void* dw, const Problem& p, scc_dt
         return launch_status(scc::launch_backward_weight_generic((In)x, (In)dy, (float*)dw, p, st));
     });
 }
-
-size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -693,6 +669,7 @@ const char* scc_status_string(int status)
         case SCC_ERR_LAUNCH: return "SCC_ERR_LAUNCH: the HIP runtime refused the kernel launch";
         case SCC_ERR_SCRATCH:
             return "SCC_ERR_SCRATCH: the problem needs more scratch than the library's static buffer holds";
+        case SCC_ERR_OPTION: return "SCC_ERR_OPTION: an activation, a number of steps or a coefficient out of its range";
         default: return "unknown scc status";
     }
 }

@@ -1,0 +1,140 @@
+// Gated sliding-channel layer, the opening of a gated feed-forward block: two sliding-channel convolutions of the same input and
+// windows, the first through an activation, multiplied:
+//   g[n,k,p] = sum_j w[0][k,j] x[n,(s_k+j) mod Cin,p],   u[n,k,p] the same with w[1],   y = act(g) u.
+// Declarations shared by its kernels and entry points.
+#pragma once
+#include "scc_band.h"
+#include "scc_common.h"
+
+namespace scc {
+namespace gated {
+
+enum { kSilu = 0, kGelu = 1 };
+
+constexpr int kRows = 32;               // filters of a tile: one operand of v_mfma_f32_32x32x16_bf16
+constexpr int kWaves = 4;               // wavefronts of a workgroup, a tile each at a time
+constexpr int kLds = 160 << 10;         // bytes of LDS of a CU
+
+// How the filters are cut into tiles.  Rows are filters in the order of their windows' starts (scc_band.h), so a tile's 32 windows
+// lie in one short stretch of the channel circle; the circle is held in chunks of 8 channels, the last one filled up with zeros.
+// A layer with far fewer filters than windows has its rows in the order of the filters, each tile on the whole circle.
+struct Plan {
+    Band b;
+    int whole;          // rows are filters in their own order
+    int rows;           // rows with a filter, or with a hole that a gradient has to be zero in
+    int tiles;          // of 32 rows
+    int chunks;         // of 8 channels
+    int steps;          // K steps of 16 channels of the longest tile
+    uint32_t a_at;      // byte offset of the packed weights in the workspace, behind the table of filters
+    size_t bytes;       // of both
+};
+
+// Filters, rounded up so that a second set of as many behind the first starts on the first window again.
+inline long long padded_filters(const Problem& p) { return (long long)(p.Cout + p.period - 1) / p.period * p.period; }
+
+__host__ __device__ inline void walk_of(const Problem& p, const Plan& t, int tile, int& q0, int& count)
+{
+    q0 = 0;
+    count = t.chunks;
+    if (t.whole) return;
+    const int r1 = tile * kRows + kRows - 1;
+    const int m0 = tile * kRows / t.b.F, m1 = (r1 < t.rows ? r1 : t.rows - 1) / t.b.F;
+    const long long span = p.L + (long long)t.b.g * (m1 - m0);
+    if (span >= p.Cin) return;
+    const int first = t.b.g * m0, end = first + (int)span;     // first < Cin
+    q0 = first / 8;
+    const int n = end <= p.Cin ? (end + 7) / 8 - q0 : t.chunks - q0 + (end - p.Cin + 7) / 8;
+    count = n < t.chunks ? n : t.chunks;
+}
+
+inline Plan make_plan(const Problem& p, int es, bool grad)
+{
+    Plan t;
+    t.b = make_band(p);
+    const long long grid = padded_filters(p);      // P * F
+    t.chunks = (p.Cin + 7) / 8;
+    // K steps of either order; a tile of the window order spans L + g * (windows - 1) channels
+    const long long span = p.L + (long long)t.b.g * ((kRows + t.b.F - 1) / t.b.F);
+    const long long by_window = (grid + kRows - 1) / kRows * (span < p.Cin ? span : p.Cin);
+    const long long own = grad ? grid : p.Cout;
+    t.whole = (own + kRows - 1) / kRows * p.Cin < by_window;
+    t.rows = (int)(t.whole ? own : grid);
+    t.tiles = (t.rows + kRows - 1) / kRows;
+    t.steps = 0;
+    for (int i = 0; i < t.tiles; ++i) {
+        int q0, count;
+        walk_of(p, t, i, q0, count);
+        const int s = (count + 1) / 2;
+        t.steps = s > t.steps ? s : t.steps;
+    }
+    t.a_at = (uint32_t)((t.tiles * kRows * 4 + 255) / 256 * 256);
+    t.bytes = t.a_at + (size_t)t.tiles * t.steps * 2 * (es == 2 ? 1 : 3) * 1024;
+    return t;
+}
+
+// What a launch of the product does with a tile of columns.
+struct Shape {
+    int ct;             // columns are 32 * ct
+    bool columns;       // single columns; else groups of ct pixels of a plane
+    bool raw;           // binary32 stays whole in LDS and is cut when it is read
+    int lds;
+    unsigned gx, gy;    // column tiles, shares of the filter tiles
+};
+
+// false: the layer's channels do not fit LDS
+bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape* s);
+
+// The gradient's first stage: for dy, the two projections are computed again and dh = (dy u act'(g), dy act(g)) is written as the
+// output gradient of one layer of 2 * padded filters, h * n_stride + filter * k_stride + pixel.
+struct GradOut {
+    long long n_stride, k_stride;
+    int padded;         // filters of either half
+    long long columns;  // columns to write, those past the input's as zeros (HW == 1 only)
+};
+
+template <typename T>
+hipError_t launch_pack(const T* w, char* ws, const Problem& p, const Plan& t, hipStream_t st);
+template <typename T>
+hipError_t launch_product(const T* x, const char* ws, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st);
+template <typename T>
+hipError_t launch_product_grad(const T* x, const char* ws, const T* dy, T* dh, const GradOut& o, const Problem& p, const Plan& t,
+                               const Shape& s, int act, hipStream_t st);
+
+// any shape (scc_gated_any.hip); dy null: y alone is written to out
+template <typename T>
+hipError_t launch_any(const T* x, const T* w, const T* dy, T* out, const GradOut& o, const Problem& p, int act, hipStream_t st);
+// few columns (scc_gated_any.hip)
+bool few_preferred(const Problem& p);
+template <typename T>
+hipError_t launch_few(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st);
+
+// out[c][r] = in[r][c], r < rows; columns of out from rows to width are zeros
+template <typename T>
+hipError_t launch_transpose(const T* in, T* out, long long rows, int cols, long long in_pitch, long long out_pitch, long long width,
+                            hipStream_t st);
+// The padded filters' weights behind one another, and their gradients back; a null source or target is passed over.
+template <typename T>
+hipError_t launch_spread(const T* w, T* wide, const Problem& p, int padded, hipStream_t st);
+template <typename T>
+hipError_t launch_gather(const float* wide, T* dw, const Problem& p, int padded, hipStream_t st);
+
+// three arrays at once, and one back
+hipError_t launch_widen(const bf16_t* const (&from)[3], float* const (&to)[3], const int (&count)[3], hipStream_t st);
+hipError_t launch_narrow(const float* from, bf16_t* to, int count, hipStream_t st);
+
+// act(g) and act'(g), binary32.  exp2 and the reciprocal are the hardware's (1 ulp).
+__device__ __forceinline__ void activate(int act, float g, float& a, float& slope)
+{
+    if (act == kSilu) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+        a = g * s;
+        slope = fmaf(a, 1.f - s, s);        // s (1 + g (1 - s))
+    } else {
+        const float phi = 0.5f * erfcf(g * -0.70710678f);
+        a = g * phi;
+        slope = fmaf(g * 0.39894228f, __builtin_amdgcn_exp2f(g * g * -0.72134752f), phi);
+    }
+}
+
+}  // namespace gated
+}  // namespace scc

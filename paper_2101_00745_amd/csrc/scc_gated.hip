@@ -1,0 +1,436 @@
+// The gated layer on the matrix cores (see scc_gated.h): packed weights, a tile of columns on chip for all channels.
+//
+// pack_gated (first launch) writes, for every tile of 32 filters and K step of 16 channels, the weights of both projections in
+// the operand layout of v_mfma_f32_32x32x16_bf16 (64 lanes x 8 values, binary32 weights cut into their three bf16 pieces), zero where a channel is outside
+// a filter's window, and the table of the rows' filters.
+// gated_product (second launch): a workgroup reads its 32*CT columns of x for ALL channels once, into LDS, in the layout of the
+// other operand: chunks of 8 channels of a column, 16 bytes.  After one barrier its wavefronts go their own ways: each takes a tile of filters at a
+// time, walks the tile's stretch of the channel circle with the weights coming from L2 straight into registers, and keeps g and u
+// of the same filters and columns in the same lanes, so that the activation and the product are register arithmetic and only y is written.
+// x crosses the memory bus once and neither projection ever does.
+#include "scc_gated.h"
+
+namespace scc {
+namespace gated {
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> constexpr int pieces = sizeof(T) == 2 ? 1 : 3;
+
+// 8 values as one operand piece (bf16) or three (binary32, cut)
+template <typename T>
+__device__ __forceinline__ void cut8(const T (&v)[8], u32x4 (&o)[pieces<T>])
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[0][e] = (uint32_t)v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
+    } else {
+        uint32_t hi[4], mid[4], lo[4];
+        split3<8>([&](int e) { return v[e]; }, hi, mid, lo);
+        o[0] = u32x4{hi[0], hi[1], hi[2], hi[3]};
+        o[1] = u32x4{mid[0], mid[1], mid[2], mid[3]};
+        o[2] = u32x4{lo[0], lo[1], lo[2], lo[3]};
+    }
+}
+
+__device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, f32x16 c)
+{
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// c += a * b: bf16 one product, binary32 six of the nine partial products of the cut factors (what is dropped is below 2^-21)
+template <int NP>
+__device__ __forceinline__ f32x16 product(const u32x4 (&a)[NP], const u32x4 (&b)[NP], f32x16 c)
+{
+    if constexpr (NP == 3) {
+        c = mfma(a[2], b[0], c);
+        c = mfma(a[0], b[2], c);
+        c = mfma(a[1], b[1], c);
+        c = mfma(a[1], b[0], c);
+        c = mfma(a[0], b[1], c);
+    }
+    return mfma(a[0], b[0], c);
+}
+
+// filter of a row: -1 past the rows; from Cout on it is a hole
+__device__ __forceinline__ int filter_of(const Plan& t, int row)
+{
+    if (row >= t.rows) return -1;
+    if (t.whole) return row;
+    const int m = row / t.b.F, i = row - m * t.b.F;
+    return (int)(((uint32_t)m * (uint32_t)t.b.inv) % (uint32_t)t.b.P) + t.b.P * i;
+}
+
+// One wavefront per (tile, K step, projection).
+template <typename T>
+__global__ __launch_bounds__(256) void pack_gated(const T* __restrict__ w, char* __restrict__ ws, Problem P, Plan t)
+{
+    const int unit = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (unit >= t.tiles * t.steps * 2) return;
+    const int half = unit & 1, step = unit / 2 % t.steps, tile = unit / 2 / t.steps;
+    const int lane = threadIdx.x & 63, f = lane & 31, h = lane >> 5;
+    int q0, count;
+    walk_of(P, t, tile, q0, count);
+    const int k = filter_of(t, tile * kRows + f);
+    if (step == 0 && half == 0 && h == 0) ((int*)ws)[tile * kRows + f] = k;
+
+    const int e = 2 * step + h;
+    int q = q0 + e;
+    q -= q >= t.chunks ? t.chunks : 0;
+    const bool real = (e < count) & (k >= 0) & (k < P.Cout);
+    const int s = real ? (int)((long long)k * P.stride % P.Cin) : 0;
+    const T* const row = w + (size_t)half * P.Cout * P.L + (size_t)(real ? k : 0) * P.L;
+    T v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = 8 * q + i;
+        int j = c - s;
+        j += j < 0 ? P.Cin : 0;
+        const bool in = real & (c < P.Cin) & (j < P.L);
+        const T x = row[in ? j : 0];
+        v[i] = in ? x : T(0);
+    }
+    u32x4 o[pieces<T>];
+    cut8(v, o);
+    char* const to = ws + t.a_at + (size_t)((tile * t.steps + step) * 2 + half) * pieces<T> * 1024 + lane * 16;
+#pragma unroll
+    for (int i = 0; i < pieces<T>; ++i) *(u32x4*)(to + i * 1024) = o[i];
+}
+
+template <typename T>
+struct Args {
+    const T* x;
+    const char* ws;
+    const T* dy;    // gradient only
+    T* out;         // y, or dh
+    Problem p;
+    Plan t;
+    Groups q;       // groups of pixels
+    GradOut o;
+    int act;
+};
+
+// LDS: [piece][chunk][column + 1 unused][8 bf16], or with RAW [chunk][half][column + 1][4 binary32].  The unused column shifts the
+// chunks against each other, so that lanes that fill consecutive chunks of a column do not meet on the same banks.
+template <typename T, int CT, bool COLUMNS, bool RAW, bool GRAD>
+__global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
+{
+    typedef T vec __attribute__((ext_vector_type(CT), aligned(sizeof(T))));
+    constexpr int NP = pieces<T>;
+    constexpr int kCols = 32 * CT, kPitch = (kCols + 1) * 16;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Problem& P = A.p;
+    const Plan& t = A.t;
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid & 63, f = lane & 31, h = lane >> 5;
+    const int piece = t.chunks * kPitch;
+
+    auto park = [&](int chunk, int column, const T (&v)[8]) {
+        if constexpr (RAW) {
+            float* const to = (float*)(lds + (size_t)chunk * 2 * kPitch + column * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                to[e] = v[e];
+                to[kPitch / 4 + e] = v[4 + e];
+            }
+        } else {
+            u32x4 o[NP];
+            cut8(v, o);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) *(u32x4*)(lds + i * piece + chunk * kPitch + column * 16) = o[i];
+        }
+    };
+
+    // where this lane's columns are: one group of CT pixels, or CT single columns 32 apart
+    uint32_t n[COLUMNS ? CT : 1], px[COLUMNS ? CT : 1];
+    bool live[COLUMNS ? CT : 1], real[COLUMNS ? CT : 1];
+    if constexpr (COLUMNS) {
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+            const long long c = (long long)blockIdx.x * kCols + 32 * j + f;
+            real[j] = c < P.NQ;
+            live[j] = GRAD ? c < A.o.columns : real[j];
+            const uint32_t u = (uint32_t)(real[j] ? c : P.NQ - 1);
+            n[j] = P.HW == 1 ? (uint32_t)c : u / (uint32_t)P.HW;      // tokens past the last are written, not read
+            px[j] = P.HW == 1 ? 0u : u - n[j] * (uint32_t)P.HW;
+        }
+        // 8 consecutive chunks of a column, then the next column: a row of tokens is read in whole cache lines
+        const int blocks = (t.chunks + 7) / 8;
+        const bool whole = P.HW == 1 && P.Cin % 8 == 0 && ((uintptr_t)A.x & 15u) == 0;
+        for (int unit = tid; unit < blocks * 8 * kCols; unit += 256) {
+            const int chunk = unit / (8 * kCols) * 8 + (unit & 7), column = unit % (8 * kCols) >> 3;
+            if (chunk >= t.chunks) continue;
+            const long long c = (long long)blockIdx.x * kCols + column;
+            const uint32_t u = (uint32_t)(c < P.NQ ? c : P.NQ - 1);
+            const uint32_t sample = u / (uint32_t)P.HW, pixel = u - sample * (uint32_t)P.HW;
+            const T* const from = A.x + (size_t)sample * P.Cin * P.HW + pixel;
+            T v[8];
+            if (whole) {
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                    *(u32x4*)((char*)v + 16 * i) = *(const u32x4*)((const char*)(from + 8 * chunk) + 16 * i);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int ch = 8 * chunk + e;
+                    const T a = from[(size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW];
+                    v[e] = ch < P.Cin ? a : T(0);
+                }
+            }
+            park(chunk, column, v);
+        }
+    } else {
+        const long long u = (long long)blockIdx.x * 32 + f;
+        live[0] = real[0] = u < A.q.count;
+        column_of_group((uint32_t)(live[0] ? u : A.q.count - 1), A.q, n[0], px[0]);
+        const T* const from = A.x + (size_t)n[0] * P.Cin * P.HW + px[0];
+#pragma unroll 2
+        for (int chunk = tid >> 5; chunk < t.chunks; chunk += 8) {
+            vec r[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int ch = 8 * chunk + e;
+                r[e] = *(const vec*)(from + (size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW);
+            }
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+                T v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 8 * chunk + e < P.Cin ? r[e][j] : T(0);
+                park(chunk, 32 * j + f, v);
+            }
+        }
+    }
+    __syncthreads();
+
+    for (int tile = (int)blockIdx.y * kWaves + wave; tile < t.tiles; tile += (int)gridDim.y * kWaves) {
+        int q0, count;
+        walk_of(P, t, tile, q0, count);
+        const int steps = (count + 1) / 2;
+        const char* a_at = A.ws + t.a_at + (size_t)tile * t.steps * 2 * NP * 1024 + lane * 16;
+        f32x16 acc[2][CT];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) acc[i][j] = f32x16{};
+
+        constexpr int D = NP == 1 ? 4 : 2;      // K steps whose weights are in flight
+        u32x4 a[D][2][NP];
+        auto fetch = [&](int slot, int step) {
+            const char* const from = a_at + (size_t)(step < steps ? step : steps - 1) * 2 * NP * 1024;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < NP; ++k) a[slot][i][k] = *(const u32x4*)(from + (i * NP + k) * 1024);
+        };
+#pragma unroll
+        for (int d = 0; d < D; ++d) fetch(d, d);
+        for (int s0 = 0; s0 < steps; s0 += D) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                if (s0 + d < steps) {
+                    int q = q0 + 2 * (s0 + d) + h;
+                    q -= q >= t.chunks ? t.chunks : 0;
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        u32x4 b[NP];
+                        if constexpr (RAW) {
+                            const float* const from = (const float*)(lds + (size_t)q * 2 * kPitch + (32 * j + f) * 16);
+                            T v[8];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                v[e] = from[e];
+                                v[4 + e] = from[kPitch / 4 + e];
+                            }
+                            cut8(v, b);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < NP; ++i) b[i] = *(const u32x4*)(lds + i * piece + q * kPitch + (32 * j + f) * 16);
+                        }
+                        acc[0][j] = product<NP>(a[d][0], b, acc[0][j]);
+                        acc[1][j] = product<NP>(a[d][1], b, acc[1][j]);
+                    }
+                    fetch(d, s0 + d + D);
+                }
+            }
+        }
+
+        // acc[.][j][r]: row (r & 3) + 8 * (r >> 2) + 4 * h of the tile, column 32 * j + f
+        const int* const table = (const int*)A.ws + tile * kRows + 4 * h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i32x4 filters = *(const i32x4*)(table + 8 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int k = filters[e], r = 4 * i + e;
+                if constexpr (!GRAD) {
+                    if (k < 0 || k >= P.Cout) continue;
+                    float y[CT];
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        float v, slope;
+                        activate(A.act, acc[0][j][r], v, slope);
+                        y[j] = v * acc[1][j][r];
+                    }
+                    if constexpr (COLUMNS) {
+#pragma unroll
+                        for (int j = 0; j < CT; ++j)
+                            if (live[j]) A.out[((size_t)n[j] * P.Cout + k) * P.HW + px[j]] = from_f32<T>(y[j]);
+                    } else {
+                        vec o;
+#pragma unroll
+                        for (int j = 0; j < CT; ++j) o[j] = from_f32<T>(y[j]);
+                        if (live[0]) *(vec*)(A.out + ((size_t)n[0] * P.Cout + k) * P.HW + px[0]) = o;
+                    }
+                } else {
+                    if (k < 0) continue;
+                    const bool there = k < P.Cout;      // a hole's gradients are zeros
+                    float up[CT];
+                    if constexpr (COLUMNS) {
+#pragma unroll
+                        for (int j = 0; j < CT; ++j)
+                            up[j] = there && real[j] ? to_f32(A.dy[((size_t)n[j] * P.Cout + k) * P.HW + px[j]]) : 0.f;
+                    } else {
+                        vec v;
+                        if (there) v = *(const vec*)(A.dy + ((size_t)n[0] * P.Cout + k) * P.HW + px[0]);
+#pragma unroll
+                        for (int j = 0; j < CT; ++j) up[j] = there ? to_f32((T)v[j]) : 0.f;
+                    }
+                    float dg[CT], du[CT];
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        float v, slope;
+                        activate(A.act, acc[0][j][r], v, slope);
+                        const bool zero = !there || (COLUMNS && !real[COLUMNS ? j : 0]);
+                        dg[j] = zero ? 0.f : up[j] * acc[1][j][r] * slope;
+                        du[j] = zero ? 0.f : up[j] * v;
+                    }
+                    T* const at = A.out + (size_t)k * A.o.k_stride;
+                    const size_t second = (size_t)A.o.padded * A.o.k_stride;
+                    if constexpr (COLUMNS) {
+#pragma unroll
+                        for (int j = 0; j < CT; ++j) {
+                            if (!live[j]) continue;
+                            T* const to = at + (size_t)n[j] * A.o.n_stride + px[j];
+                            to[0] = from_f32<T>(dg[j]);
+                            to[second] = from_f32<T>(du[j]);
+                        }
+                    } else {
+                        vec o0, o1;
+#pragma unroll
+                        for (int j = 0; j < CT; ++j) {
+                            o0[j] = from_f32<T>(dg[j]);
+                            o1[j] = from_f32<T>(du[j]);
+                        }
+                        T* const to = at + (size_t)n[0] * A.o.n_stride + px[0];
+                        if (live[0]) {
+                            *(vec*)to = o0;
+                            *(vec*)(to + second) = o1;
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int CT, bool COLUMNS, bool RAW, bool GRAD>
+hipError_t start(const Args<T>& a, const Shape& s, hipStream_t st)
+{
+    auto* const kernel = gated_product<T, CT, COLUMNS, RAW, GRAD>;
+    static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (allowed != hipSuccess) return allowed;
+    kernel<<<dim3(s.gx, s.gy), dim3(256), s.lds, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, bool GRAD>
+hipError_t start_as(const Args<T>& a, const Shape& s, hipStream_t st)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (s.columns) {
+            if (s.ct == 4) return start<T, 4, true, false, GRAD>(a, s, st);
+            if (s.ct == 2) return start<T, 2, true, false, GRAD>(a, s, st);
+            return start<T, 1, true, false, GRAD>(a, s, st);
+        }
+        if (s.ct == 4) return start<T, 4, false, false, GRAD>(a, s, st);
+        if (s.ct == 2) return start<T, 2, false, false, GRAD>(a, s, st);
+        return start<T, 1, false, false, GRAD>(a, s, st);
+    } else {
+        if (s.raw) {
+            if (s.columns) return start<T, 1, true, true, GRAD>(a, s, st);
+            return start<T, 1, false, true, GRAD>(a, s, st);
+        }
+        if (s.columns) {
+            if (s.ct == 2) return start<T, 2, true, false, GRAD>(a, s, st);
+            return start<T, 1, true, false, GRAD>(a, s, st);
+        }
+        if (s.ct == 2) return start<T, 2, false, false, GRAD>(a, s, st);
+        return start<T, 1, false, false, GRAD>(a, s, st);
+    }
+}
+
+int lds_of(const Plan& t, int es, int ct, bool raw) { return t.chunks * (32 * ct + 1) * 16 * (es == 2 ? 1 : raw ? 2 : 3); }
+
+}  // namespace
+
+bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape* s)
+{
+    s->columns = p.HW < 4;
+    s->raw = false;
+    int ct = es == 2 ? 4 : 2;
+    auto tiles = [&](int c) { return s->columns ? (stored + 32 * c - 1) / (32 * c) : (column_groups(p, c).count + 31) / 32; };
+    while (ct > 1 && (lds_of(t, es, ct, false) > kLds / 2 || tiles(ct) < 256)) ct /= 2;
+    if (lds_of(t, es, ct, false) > kLds) {
+        s->raw = true;
+        if (es == 2 || lds_of(t, es, 1, true) > kLds) return false;
+    }
+    s->ct = ct;
+    s->lds = lds_of(t, es, ct, s->raw);
+    const long long gx = tiles(ct);
+    const long long shares = (t.tiles + kWaves - 1) / kWaves;
+    const long long gy = gx >= 512 ? 1 : 512 / gx < shares ? 512 / gx : shares;
+    s->gx = (unsigned)gx;
+    s->gy = (unsigned)gy;
+    return true;
+}
+
+template <typename T>
+hipError_t launch_pack(const T* w, char* ws, const Problem& p, const Plan& t, hipStream_t st)
+{
+    const int units = t.tiles * t.steps * 2;
+    pack_gated<T><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(w, ws, p, t);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_product(const T* x, const char* ws, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st)
+{
+    const Groups q = s.columns ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.ct);
+    return start_as<T, false>(Args<T>{x, ws, nullptr, y, p, t, q, GradOut{0, 0, 0, 0}, act}, s, st);
+}
+
+template <typename T>
+hipError_t launch_product_grad(const T* x, const char* ws, const T* dy, T* dh, const GradOut& o, const Problem& p, const Plan& t,
+                               const Shape& s, int act, hipStream_t st)
+{
+    const Groups q = s.columns ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.ct);
+    return start_as<T, true>(Args<T>{x, ws, dy, dh, p, t, q, o, act}, s, st);
+}
+
+#define INSTANCES(T)                                                                                                          \
+    template hipError_t launch_pack(const T*, char*, const Problem&, const Plan&, hipStream_t);                               \
+    template hipError_t launch_product(const T*, const char*, T*, const Problem&, const Plan&, const Shape&, int, hipStream_t); \
+    template hipError_t launch_product_grad(const T*, const char*, const T*, T*, const GradOut&, const Problem&, const Plan&,  \
+                                            const Shape&, int, hipStream_t);
+INSTANCES(float)
+INSTANCES(bf16_t)
+
+}  // namespace gated
+}  // namespace scc

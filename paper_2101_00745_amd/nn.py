@@ -181,3 +181,62 @@ class DWSCCBlock(torch.nn.Module):
     def extra_repr(self):
         return "%d, %d, cg=%d, co=%g, stride=%d, bias=%s" % (self.in_channels, self.out_channels, self.cg, self.co,
                                                              self.stride, self.bias is not None)
+
+
+class GatedSCCFunction(torch.autograd.Function):
+    """y = act(SCC(x; weight[0])) * SCC(x; weight[1]).  Neither projection is kept between the passes: the forward never writes them, and the
+    backward computes them again."""
+
+    @staticmethod
+    def forward(ctx, x, weight, cg, co, act):
+        x, weight = x.contiguous(), weight.contiguous()
+        ctx.save_for_backward(x, weight)
+        ctx.cg, ctx.co, ctx.act = int(cg), float(co), act
+        return _scc.scc_gated_forward(x, weight, ctx.cg, ctx.co, act=act)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight = ctx.saved_tensors
+        dx, dw = _scc._gated_backward(x, weight, dy.contiguous(), ctx.cg, ctx.co, ctx.act, True)    # dw in the weights' type
+        grads = (dx if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None)
+        return (*_first_order(grads, dy, x, weight), None, None, None)
+
+
+def gated_scc(x, weight, cg, co, act="silu"):
+    """Functional form: y = act(SCC(x; weight[0])) * SCC(x; weight[1]), weight [2, Cout, Cin//cg]."""
+    return GatedSCCFunction.apply(x, weight, cg, co, act)
+
+
+class GatedSCC(torch.nn.Module):
+    """Gated sliding-channel layer from ``in_channels`` to ``out_channels``: two SCCs of the same windows, the first through an activation
+    ("silu" or "gelu"), multiplied."""
+
+    def __init__(self, in_channels, out_channels, cg=2, co=0.5, act="silu", device="cuda", dtype=torch.float32):
+        super().__init__()
+        L, _, _ = _scc.scc_window_params(in_channels, out_channels, cg, co)
+        _scc._activation(act)
+        self.in_channels, self.out_channels, self.cg, self.co, self.act = in_channels, out_channels, int(cg), float(co), act
+        self.weight = torch.nn.Parameter(torch.empty(2, out_channels, L, device=device, dtype=dtype))
+        self.reset_parameters()
+
+    def reset_parameters(self):
+        with torch.no_grad():
+            self.weight.normal_(0.0, math.sqrt(2.0 / self.weight.shape[2]))
+
+    def forward(self, x):
+        return gated_scc(x, self.weight, self.cg, self.co, self.act)
+
+    def extra_repr(self):
+        return "%d, %d, cg=%d, co=%g, act=%s" % (self.in_channels, self.out_channels, self.cg, self.co, self.act)
+
+
+class GatedFeedForward(torch.nn.Module):
+    """A gated feed-forward block on the channels of [N, channels, H, W]: GatedSCC to ``hidden`` channels, SCC back."""
+
+    def __init__(self, channels, hidden, cg=2, co=0.5, act="silu", device="cuda", dtype=torch.float32):
+        super().__init__()
+        self.up = GatedSCC(channels, hidden, cg, co, act, device=device, dtype=dtype)
+        self.down = SCC(hidden, channels, cg, co, device=device, dtype=dtype)
+
+    def forward(self, x):
+        return self.down(self.up(x))

@@ -24,11 +24,18 @@ SYMBOLS = ("scc_window_params", "scc_forward", "scc_forward_workspace_bytes", "s
            "scc_depthwise3x3_backward", "scc_dw_forward_workspace_bytes", "scc_dw_forward_fusable", "scc_dw_forward",
            "scc_dw_forward_scratch", "scc_dw_forward_path", "scc_dw_forward_scratch_path",
            "scc_dw_backward_workspace_bytes", "scc_dw_backward", "scc_dw_backward_as_workspace_bytes", "scc_dw_backward_as",
-           "scc_status_string")
+           "scc_gated_forward_workspace_bytes", "scc_gated_forward_path", "scc_gated_forward", "scc_gated_backward_workspace_bytes",
+           "scc_gated_backward", "scc_orthogonal_workspace_bytes", "scc_orthogonalise", "scc_orthogonal_step", "scc_status_string")
+ACTIVATIONS = {"silu": 0, "gelu": 1}    # scc_activation of include/scc.h
 STATIC_SCRATCH_BYTES = 32 << 20    # SCC_STATIC_SCRATCH_BYTES of include/scc.h
 
 _lib = None
 _native = None      # the module of the plain calls
+
+
+class _OrthogonalOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int),
+                ("steps", ctypes.c_int), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 class SccError(RuntimeError):
@@ -99,6 +106,23 @@ def load():
     lib.scc_dw_backward_as_workspace_bytes.restype = c_sz
     lib.scc_dw_backward_as.argtypes = [c_vp] * 7 + dw_shape + [c_int, c_vp, c_sz, c_vp]
     lib.scc_dw_backward_as.restype = c_int
+    lib.scc_gated_forward_workspace_bytes.argtypes = shape
+    lib.scc_gated_forward_workspace_bytes.restype = c_sz
+    lib.scc_gated_forward_path.argtypes = shape
+    lib.scc_gated_forward_path.restype = c_int
+    lib.scc_gated_forward.argtypes = [c_vp] * 3 + shape[:-1] + [c_int, c_int, c_vp, c_sz, c_vp]     # ... co act dtype
+    lib.scc_gated_forward.restype = c_int
+    lib.scc_gated_backward_workspace_bytes.argtypes = shape + [c_int]
+    lib.scc_gated_backward_workspace_bytes.restype = c_sz
+    lib.scc_gated_backward.argtypes = [c_vp] * 5 + shape[:-1] + [c_int, c_int, c_int, c_vp, c_sz, c_vp]
+    lib.scc_gated_backward.restype = c_int
+    vpp = ctypes.POINTER(c_vp)
+    lib.scc_orthogonal_workspace_bytes.argtypes = [c_int, ip, ip]
+    lib.scc_orthogonal_workspace_bytes.restype = c_sz
+    for name, lists in (("scc_orthogonalise", 2), ("scc_orthogonal_step", 3)):
+        call = getattr(lib, name)
+        call.argtypes = [c_int] + [vpp] * lists + [ip, ip, ctypes.POINTER(_OrthogonalOptions), c_int, c_vp, c_sz, c_vp]
+        call.restype = c_int
     lib.scc_status_string.argtypes = [c_int]
     lib.scc_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -488,3 +512,114 @@ def _dw_backward(x, kdw, w, dy, cg, co, dw_stride, stored):
     _launch(dev, load().scc_dw_backward_as, x.data_ptr(), kdw.data_ptr(), w.data_ptr(), dy.data_ptr(), dx.data_ptr(),
             dk.data_ptr(), dw.data_ptr(), *shape, ws_ptr, ws_len)
     return dx, dk, dw
+
+
+def _activation(act):
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(sorted(ACTIVATIONS)), act))
+    return code
+
+
+def _gated_layer(x, w, cg, co):
+    """(N, Cin, Cout, H, W, cg, co) of a gated layer."""
+    if x.dim() != 4:
+        raise ValueError("x must be [N, Cin, H, W]")
+    N, Cin, H, W = x.shape
+    if w.dtype != x.dtype or w.dim() != 3 or w.shape[0] != 2 or (cg >= 1 and Cin % cg == 0 and w.shape[2] != Cin // cg):
+        raise ValueError("w must be [2, Cout, Cin//cg] with the dtype of x")
+    return N, Cin, w.shape[1], H, W, cg, float(co)
+
+
+def scc_gated_forward_workspace_bytes(N, Cin, Cout, H, W, cg, co, dtype=torch.float32):
+    code = SCC_F32 if dtype == torch.float32 else SCC_BF16
+    return int(load().scc_gated_forward_workspace_bytes(N, Cin, Cout, H, W, cg, float(co), code))
+
+
+def scc_gated_forward(x, w, cg, co, act="silu", out=None, workspace=None):
+    """y = act(SCC(x; w[0])) * SCC(x; w[1]), the layer that a gated feed-forward block opens with: x [N,Cin,H,W], w [2,Cout,Cin//cg]
+    -> y [N,Cout,H,W] (same dtype).  A sequence of S tokens is a map of S x 1, single tokens are N maps of 1 x 1.  act: "silu" or
+    "gelu" (with erf).  A workspace is allocated where the layer needs one and none is given."""
+    code = _activation(act)
+    dev = _dev(x, w)
+    layer = _gated_layer(x, w, cg, co)
+    y = x.new_empty((x.shape[0], w.shape[1], x.shape[2], x.shape[3])) if out is None else out
+    if out is not None:
+        _dev(x, out)
+        if out.shape != (x.shape[0], w.shape[1], x.shape[2], x.shape[3]) or out.dtype != x.dtype:
+            raise ValueError("out must be [N, Cout, H, W] with the dtype of x")
+    dtype = _dtype_code(x)
+    ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_gated_forward_workspace_bytes", *layer, dtype), dev, workspace)
+    _launch(dev, load().scc_gated_forward, x.data_ptr(), w.data_ptr(), y.data_ptr(), *layer, code, dtype, ws_ptr, ws_len)
+    return y
+
+
+def scc_gated_backward(x, w, dy, cg, co, act="silu"):
+    """(dx, dw) of scc_gated_forward: dy [N,Cout,H,W] -> dx like x, dw [2,Cout,Cin//cg] float32."""
+    return _gated_backward(x, w, dy, cg, co, act, False)
+
+
+def _gated_backward(x, w, dy, cg, co, act, stored):
+    """scc_gated_backward; stored: dw in the type of x, rounded from the same sums."""
+    code = _activation(act)
+    dev = _dev(x, w, dy)
+    layer = _gated_layer(x, w, cg, co)
+    if dy.dtype != x.dtype or tuple(dy.shape) != (x.shape[0], w.shape[1], x.shape[2], x.shape[3]):
+        raise ValueError("dy must be [N, Cout, H, W] with the dtype of x")
+    dtype = _dtype_code(x)
+    grad = x.dtype if stored else torch.float32
+    need = _workspace_need("scc_gated_backward_workspace_bytes", *layer, dtype, _CODES[grad])
+    ws, ws_ptr, ws_len = _scratch(need, dev)
+    dx = torch.empty_like(x)
+    dw = torch.empty(w.shape, dtype=grad, device=dev)
+    _launch(dev, load().scc_gated_backward, x.data_ptr(), w.data_ptr(), dy.data_ptr(), dx.data_ptr(), dw.data_ptr(), *layer, code, dtype,
+            _CODES[grad], ws_ptr, ws_len)
+    return dx, dw
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)   # brings singular values between 0.001 and 1 to 0.7 .. 1.2 in five steps
+
+
+def _matrices(*lists):
+    """Lists of equally many matrices, one in each list per weight, of one device; the first and second of one dtype."""
+    first = lists[0]
+    if len(first) == 0 or any(len(l) != len(first) for l in lists):
+        raise ValueError("lists of equally many matrices are wanted, at least one")
+    dev = _dev(*(t for l in lists for t in l))
+    for ts in zip(*lists):
+        if any(t.dim() != 2 or t.shape != ts[0].shape for t in ts):
+            raise ValueError("a weight, its gradient and its momentum are matrices of the same shape")
+        if ts[0].dtype != first[0].dtype or (len(ts) > 1 and ts[1].dtype != first[0].dtype):
+            raise ValueError("weights and gradients of one call share their dtype")
+    return dev, _dtype_code(first[0])
+
+
+def _orthogonal(dev, name, lists, options, dtype):
+    count = len(lists[0])
+    pointers = [(ctypes.c_void_p * count)(*[t.data_ptr() for t in l]) for l in lists]
+    rows = (ctypes.c_int * count)(*[t.shape[0] for t in lists[0]])
+    cols = (ctypes.c_int * count)(*[t.shape[1] for t in lists[0]])
+    lib = load()
+    ws, ws_ptr, ws_len = _scratch(int(lib.scc_orthogonal_workspace_bytes(count, rows, cols)), dev)
+    _launch(dev, getattr(lib, name), count, *pointers, rows, cols, ctypes.byref(options), dtype, ws_ptr, ws_len)
+
+
+def scc_orthogonalise(matrices, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7):
+    """The matrices with their singular values brought near 1 by `steps` Newton-Schulz steps x <- a x + (b x x^T + c (x x^T)^2) x from
+    x / (||x||_F + eps): a list of [rows, cols], float32 or bfloat16 -> a list of the same."""
+    dev, dtype = _matrices(matrices)
+    out = [torch.empty_like(t) for t in matrices]
+    _orthogonal(dev, "scc_orthogonalise", (matrices, out), _OrthogonalOptions(0, 0, 0, 0, steps, *coefficients, eps), dtype)
+    return out
+
+
+def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, coefficients=NEWTON_SCHULZ,
+                        eps=1e-7):
+    """One step of the orthogonalised momentum update on a list of weight matrices, in place:
+    m <- momentum m + g, u = g + momentum m (nesterov) or m, w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows/cols)) O(u), O as
+    scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32."""
+    dev, dtype = _matrices(weights, grads, momenta)
+    if any(m.dtype != torch.float32 for m in momenta):
+        raise ValueError("momenta are float32")
+    options = _OrthogonalOptions(lr, momentum, weight_decay, int(bool(nesterov)), steps, *coefficients, eps)
+    _orthogonal(dev, "scc_orthogonal_step", (weights, grads, momenta), options, dtype)

@@ -1,0 +1,244 @@
+"""The orthogonalised momentum update against its definition in 64 bits (the polynomial applied to the singular values), its refusals, and the
+optimiser over it.
+
+Bars.  The iteration multiplies an error of its first products by up to a^5 = 484 in directions of small singular values, but those errors
+enter relative to singular values below 1/3; products and sums are good to some 2^-24 of their terms: 2-norm 2e-5 in float32 holds
+with a margin of several.  bfloat16 results are rounded once, 2^-9: 2-norm 4e-3."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2101_00745_amd as S
+from paper_2101_00745_amd import scc as B
+
+A, C3, C5 = 3.4445, -4.7750, 2.0315
+BAR = {torch.float32: 2e-5, torch.bfloat16: 4e-3}
+DTYPES = [pytest.param(torch.float32, id="f32"), pytest.param(torch.bfloat16, id="bf16")]
+
+
+def polynomial(u, steps=5, eps=1e-7, coefficients=(A, C3, C5)):
+    a, b, c = coefficients
+    left, s, right = np.linalg.svd(u, full_matrices=False)
+    s = s / (math.sqrt(np.sum(s * s)) + eps)
+    for _ in range(steps):
+        s = a * s + b * s ** 3 + c * s ** 5
+    return (left * s) @ right
+
+
+def matrices(shapes, dtype, seed=0, scale=0.01):
+    rng = np.random.default_rng(5200 + seed)
+    out = []
+    for r, c in shapes:
+        few = rng.standard_normal((r, 2)) @ rng.standard_normal((2, c))
+        out.append(torch.from_numpy(((rng.standard_normal((r, c)) + few) * scale).astype(np.float32)).to(dtype))
+    return out
+
+
+def off(got, ref):
+    got = got.double().cpu().numpy()
+    return float(np.linalg.norm(got - ref) / max(np.linalg.norm(ref), 1e-300))
+
+
+SHAPES = [(64, 64), (1, 1), (1, 300), (257, 1), (31, 33), (32, 96), (96, 32), (33, 200), (200, 33), (256, 64), (100, 100), (129, 257), (512, 160)]
+
+
+def pointers(n, value=0x1000):
+    return (ctypes.c_void_p * n)(*[value] * n)
+
+
+def options(**over):
+    o = dict(lr=0.1, momentum=0.9, weight_decay=0.0, nesterov=1, steps=5, a=A, b=C3, c=C5, eps=1e-7)
+    o.update(over)
+    return ctypes.byref(B._OrthogonalOptions(*[o[k] for k in ("lr", "momentum", "weight_decay", "nesterov", "steps", "a", "b", "c", "eps")]))
+
+
+def test_refusals():
+    lib = S.load()
+    n = 3
+    rows, cols = (ctypes.c_int * n)(4, 5, 6), (ctypes.c_int * n)(7, 8, 9)
+    need = lib.scc_orthogonal_workspace_bytes(n, rows, cols)
+    ws = ctypes.c_void_p(0x1000)
+    assert need > 0
+
+    def step(w=pointers(n), g=pointers(n), m=pointers(n), rows=rows, cols=cols, o=options(), dtype=0, ws=ws, size=need, count=n):
+        return lib.scc_orthogonal_step(count, w, g, m, rows, cols, o, dtype, ws, size, None)
+
+    for hole in ("w", "g", "m"):
+        assert step(**{hole: None}) == -1
+        assert step(**{hole: (ctypes.c_void_p * n)(0x1000, None, 0x1000)}) == -1
+    for hole in ("rows", "cols", "o"):
+        assert step(**{hole: None}) == -1
+    assert step(count=0) == -2 and step(count=-1) == -2
+    assert step(rows=(ctypes.c_int * n)(4, 0, 6)) == -2 and step(cols=(ctypes.c_int * n)(4, 5, -6)) == -2
+    assert step(rows=(ctypes.c_int * n)(1 << 20, 1, 1), cols=(ctypes.c_int * n)(1 << 10, 1, 1)) == -2
+    assert step(dtype=2) == -4
+    for bad in (dict(steps=0), dict(steps=101), dict(lr=math.nan), dict(a=math.inf), dict(eps=-1.0), dict(momentum=-math.inf)):
+        assert step(o=options(**bad)) == -8
+    assert step(ws=None, size=0) == -5 and step(size=need - 1) == -5 and step(ws=ctypes.c_void_p(0x1010)) == -5
+    assert lib.scc_orthogonalise(n, None, pointers(n), rows, cols, options(), 0, ws, need, None) == -1
+    assert lib.scc_orthogonalise(n, pointers(n), pointers(n), rows, cols, options(steps=0), 0, ws, need, None) == -8
+    assert lib.scc_orthogonal_workspace_bytes(0, rows, cols) == 0
+    assert lib.scc_orthogonal_workspace_bytes(n, None, cols) == 0
+
+
+def test_binding_refuses():
+    m = torch.zeros(4, 4)
+    with pytest.raises(ValueError):
+        S.scc_orthogonalise([m])            # no CPU path
+    with pytest.raises(ValueError):
+        S.scc_orthogonalise([])
+    with pytest.raises(ValueError):
+        S.scc_orthogonal_step([m], [m, m], [m], lr=0.1)
+
+
+@pytest.mark.gpu
+def test_binding_refuses_on_the_gpu():
+    m = torch.zeros(4, 6, device="cuda")
+    for lists in (([m], [m.bfloat16()], [m]), ([m], [m], [m.bfloat16()]), ([m], [torch.zeros(6, 4, device="cuda")], [m]),
+                  ([m.t()], [m.t()], [m.t()]), ([m[0]], [m[0]], [m[0]]), ([m, m.bfloat16()], [m, m.bfloat16()], [m, m])):
+        with pytest.raises(ValueError):
+            S.scc_orthogonal_step(*lists, lr=0.1)
+    with pytest.raises(TypeError):
+        S.scc_orthogonalise([m.double()])
+    with pytest.raises(B.SccError):
+        S.scc_orthogonalise([m], steps=0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_orthogonalise(dtype):
+    gs = matrices(SHAPES, dtype)
+    kept = [g.clone() for g in gs]
+    dev = [g.cuda() for g in gs]
+    out = S.scc_orthogonalise(dev)
+    for g, o, d, k in zip(gs, out, dev, kept):
+        assert o.dtype == dtype and torch.equal(d.cpu(), k)
+        assert off(o, polynomial(g.double().numpy())) <= BAR[dtype], tuple(g.shape)
+    again = S.scc_orthogonalise(dev)
+    assert all(torch.equal(a, b) for a, b in zip(out, again))
+    # alone and in the list, a matrix comes out the same
+    assert torch.equal(S.scc_orthogonalise([dev[8]])[0], out[8])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+def test_number_of_steps(steps):
+    gs = matrices([(40, 70), (70, 40)], torch.float32, seed=1)
+    coefficients = (1.5, -0.5, 0.0)         # the cubic iteration, which converges
+    for g, o in zip(gs, S.scc_orthogonalise([g.cuda() for g in gs], steps=steps, coefficients=coefficients)):
+        assert off(o, polynomial(g.double().numpy(), steps=steps, coefficients=coefficients)) <= 2e-5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [1e-25, 1e-12, 1.0, 1e12, 1e25])
+def test_scales(scale):
+    """The norm's squares would leave binary32 at both ends; eps takes over where the norm is far below it."""
+    g, = matrices([(48, 80)], torch.float32, seed=2, scale=1.0)
+    g = g * scale
+    assert off(S.scc_orthogonalise([g.cuda()])[0], polynomial(g.double().numpy())) <= 2e-5
+
+
+@pytest.mark.gpu
+def test_zero_and_non_finite_matrices():
+    gs = matrices([(40, 24), (24, 40), (33, 65), (40, 40)], torch.float32, seed=3)
+    gs[0].zero_()
+    gs[1][3, 5] = math.nan
+    gs[2][7, 11] = math.inf
+    out = S.scc_orthogonalise([g.cuda() for g in gs])
+    assert not out[0].any()
+    assert torch.isnan(out[1]).all() and torch.isnan(out[2]).all()
+    assert off(out[3], polynomial(gs[3].double().numpy())) <= 2e-5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_step(dtype, nesterov):
+    shapes = SHAPES * 4                     # more matrices than a launch takes
+    ws, gs = matrices(shapes, dtype, seed=4, scale=0.2), matrices(shapes, dtype, seed=5)
+    ms = matrices(shapes, torch.float32, seed=6, scale=0.05)
+    wd, gd, md = [[t.cuda() for t in l] for l in (ws, gs, ms)]
+    S.scc_orthogonal_step(wd, gd, md, lr=0.3, momentum=0.9, weight_decay=0.05, nesterov=nesterov)
+    for i, (w, g, m) in enumerate(zip(ws, gs, ms)):
+        w, g, m = (t.double().numpy() for t in (w, g, m))
+        m = 0.9 * m + g
+        o = polynomial(g + 0.9 * m if nesterov else m)
+        want = w * (1 - 0.3 * 0.05) - 0.3 * math.sqrt(max(1.0, w.shape[0] / w.shape[1])) * o
+        assert off(md[i], m) <= 2e-7
+        assert off(wd[i], want) <= BAR[dtype]
+        assert torch.equal(gd[i].cpu(), gs[i])
+
+
+@pytest.mark.gpu
+def test_optimiser_on_a_gated_block():
+    """The optimiser's steps are the operator's, on matrices and on stacks of two; a student block fits its teacher."""
+    from paper_2101_00745_amd.nn import GatedFeedForward
+    from paper_2101_00745_amd.optim import OrthogonalMomentum
+    torch.manual_seed(0)
+    student, teacher = GatedFeedForward(32, 64), GatedFeedForward(32, 64)
+    opt = OrthogonalMomentum(student.parameters(), lr=0.02, momentum=0.9, weight_decay=0.01)
+    x = torch.randn(64, 32, 4, 4, device="cuda")
+    with torch.no_grad():
+        target = teacher(x)
+    losses = []
+    for i in range(80):
+        opt.zero_grad()
+        loss = torch.nn.functional.mse_loss(student(x), target)
+        loss.backward()
+        if i == 0:
+            before, grad = student.up.weight.detach().clone(), student.up.weight.grad.clone()
+        opt.step()
+        if i == 0:
+            for k in range(2):
+                o = polynomial(1.9 * grad[k].double().cpu().numpy())
+                want = before[k].double().cpu().numpy() * (1 - 0.02 * 0.01) - 0.02 * math.sqrt(64 / 16) * o
+                assert off(student.up.weight[k].detach(), want) <= 2e-5
+        losses.append(float(loss.detach()))
+    assert losses[-1] < 0.7 * losses[0], losses[::10]
+    state = opt.state_dict()
+    again = OrthogonalMomentum(student.parameters())
+    again.load_state_dict(state)
+    assert torch.equal(again.state[student.up.weight]["momentum"], opt.state[student.up.weight]["momentum"])
+    with pytest.raises(ValueError):
+        OrthogonalMomentum([torch.nn.Parameter(torch.zeros(3, device="cuda"))])
+    with pytest.raises(ValueError):
+        OrthogonalMomentum(student.parameters(), momentum=1.0)
+
+
+@pytest.mark.gpu
+def test_momenta_stay_float32_through_a_checkpoint():
+    from paper_2101_00745_amd.optim import OrthogonalMomentum
+    p = torch.nn.Parameter(torch.randn(40, 24, device="cuda").bfloat16())
+    opt = OrthogonalMomentum([p], lr=0.1)
+    p.grad = torch.randn_like(p)
+    opt.step()
+    again = OrthogonalMomentum([p], lr=0.1)
+    again.load_state_dict(opt.state_dict())
+    assert again.state[p]["momentum"].dtype == torch.float32
+    assert torch.equal(again.state[p]["momentum"], opt.state[p]["momentum"])
+    again.step()
+
+
+@pytest.mark.gpu
+def test_captured_graph_and_stream():
+    gs = [g.cuda() for g in matrices([(64, 32), (48, 200)], torch.float32, seed=8)]
+    S.scc_orthogonalise(gs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = S.scc_orthogonalise(gs)
+    for i in range(4):
+        for g in gs:
+            g.mul_(0.7).add_(0.001 * i)
+        want = S.scc_orthogonalise(gs)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        other = S.scc_orthogonalise(gs)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, want))
