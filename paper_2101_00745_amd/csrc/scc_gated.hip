@@ -110,30 +110,61 @@ struct Args {
     T* out;         // y, or dh
     Problem p;
     Plan t;
-    Groups q;       // groups of pixels
+    Groups q;       // groups of V pixels
     GradOut o;
+    Deal deal;      // (column tile, share of the filter tiles)
     int act;
 };
 
-// LDS: [piece][chunk][column + 1 unused][8 bf16], or with RAW [chunk][half][column + 1][4 binary32].  The unused column shifts the
-// chunks against each other, so that lanes that fill consecutive chunks of a column do not meet on the same banks.
-template <typename T, int CT, bool COLUMNS, bool RAW, bool GRAD>
-__global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
+// V: pixels of a plane that one load takes, 1: single columns.  LDS: [piece][chunk][column + 1 unused][8 bf16], or with RAW
+// [chunk][half][column + 1][4 binary32]; column c of the tile lies at (c % CT) * 32 + c / CT, so that a lane's CT columns of a result are
+// neighbours.  The unused column shifts the chunks against each other; lanes next to each other fill V/CT chunks, then the next group (of single
+// columns 8 chunks, so that a row of tokens is read in whole cache lines), and so do not meet on the same banks.
+template <typename T, int CT, int V, bool RAW, bool GRAD>
+__global__ __launch_bounds__(512) void gated_product(Args<T> A)
 {
+    constexpr bool COLUMNS = V == 1;
+    typedef T lvec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     typedef T vec __attribute__((ext_vector_type(CT), aligned(sizeof(T))));
     constexpr int NP = pieces<T>;
     constexpr int kCols = 32 * CT, kPitch = (kCols + 1) * 16;
+    constexpr int D = NP == 1 ? 4 : 2;      // K steps whose weights are in flight
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Problem& P = A.p;
     const Plan& t = A.t;
-    const int tid = threadIdx.x;
+    int ct, share;
+    if (!dealt(A.deal, (int)blockIdx.x, ct, share)) return;     // the whole workgroup leaves
+    const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, f = lane & 31, h = lane >> 5;
     const int piece = t.chunks * kPitch;
 
+    int q0, steps;
+    const char* a_at;
+    u32x4 a[D][2][NP];
+    auto fetch = [&](int slot, int step) {
+        const char* const from = a_at + (size_t)(step < steps ? step : steps - 1) * 2 * NP * 1024;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) a[slot][i][k] = *(const u32x4*)(from + (i * NP + k) * 1024);
+    };
+    auto begin = [&](int tile) {            // a tile's walk, and its first weights on their way
+        int count;
+        walk_of(P, t, tile, q0, count);
+        steps = (count + 1) / 2;
+        a_at = A.ws + t.a_at + (size_t)tile * t.steps * 2 * NP * 1024 + lane * 16;
+#pragma unroll
+        for (int d = 0; d < D; ++d) fetch(d, d);
+    };
+    const int shares = A.deal.inner;
+    int tile = share * waves + wave;
+    if (tile < t.tiles) begin(tile);
+
     auto park = [&](int chunk, int column, const T (&v)[8]) {
+        const int slot = column % CT * 32 + column / CT;
         if constexpr (RAW) {
-            float* const to = (float*)(lds + (size_t)chunk * 2 * kPitch + column * 16);
+            float* const to = (float*)(lds + (size_t)chunk * 2 * kPitch + slot * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 to[e] = v[e];
@@ -143,30 +174,29 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
             u32x4 o[NP];
             cut8(v, o);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) *(u32x4*)(lds + i * piece + chunk * kPitch + column * 16) = o[i];
+            for (int i = 0; i < NP; ++i) *(u32x4*)(lds + i * piece + chunk * kPitch + slot * 16) = o[i];
         }
     };
 
-    // where this lane's columns are: one group of CT pixels, or CT single columns 32 apart
+    // where this lane's columns of a result are: CT pixels of a group, or CT single columns
     uint32_t n[COLUMNS ? CT : 1], px[COLUMNS ? CT : 1];
     bool live[COLUMNS ? CT : 1], real[COLUMNS ? CT : 1];
     if constexpr (COLUMNS) {
 #pragma unroll
         for (int j = 0; j < CT; ++j) {
-            const long long c = (long long)blockIdx.x * kCols + 32 * j + f;
+            const long long c = (long long)ct * kCols + CT * f + j;
             real[j] = c < P.NQ;
             live[j] = GRAD ? c < A.o.columns : real[j];
             const uint32_t u = (uint32_t)(real[j] ? c : P.NQ - 1);
             n[j] = P.HW == 1 ? (uint32_t)c : u / (uint32_t)P.HW;      // tokens past the last are written, not read
             px[j] = P.HW == 1 ? 0u : u - n[j] * (uint32_t)P.HW;
         }
-        // 8 consecutive chunks of a column, then the next column: a row of tokens is read in whole cache lines
         const int blocks = (t.chunks + 7) / 8;
         const bool whole = P.HW == 1 && P.Cin % 8 == 0 && ((uintptr_t)A.x & 15u) == 0;
-        for (int unit = tid; unit < blocks * 8 * kCols; unit += 256) {
+        for (int unit = tid; unit < blocks * 8 * kCols; unit += threads) {
             const int chunk = unit / (8 * kCols) * 8 + (unit & 7), column = unit % (8 * kCols) >> 3;
             if (chunk >= t.chunks) continue;
-            const long long c = (long long)blockIdx.x * kCols + column;
+            const long long c = (long long)ct * kCols + column;
             const uint32_t u = (uint32_t)(c < P.NQ ? c : P.NQ - 1);
             const uint32_t sample = u / (uint32_t)P.HW, pixel = u - sample * (uint32_t)P.HW;
             const T* const from = A.x + (size_t)sample * P.Cin * P.HW + pixel;
@@ -179,58 +209,79 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int ch = 8 * chunk + e;
-                    const T a = from[(size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW];
-                    v[e] = ch < P.Cin ? a : T(0);
+                    const T b = from[(size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW];
+                    v[e] = ch < P.Cin ? b : T(0);
                 }
             }
             park(chunk, column, v);
         }
     } else {
-        const long long u = (long long)blockIdx.x * 32 + f;
-        live[0] = real[0] = u < A.q.count;
-        column_of_group((uint32_t)(live[0] ? u : A.q.count - 1), A.q, n[0], px[0]);
-        const T* const from = A.x + (size_t)n[0] * P.Cin * P.HW + px[0];
+        constexpr int kGroups = kCols / V, S = V / CT;
+        const uint32_t base = (uint32_t)ct * kGroups, last = (uint32_t)(A.q.count - 1);
+        {
+            const uint32_t u = base + CT * f / V;
+            live[0] = real[0] = u <= last;
+            column_of_group(live[0] ? u : last, A.q, n[0], px[0]);
+            px[0] += CT * f % V;
+        }
+        const int g = tid / S % kGroups;        // the same in every round: a round's threads are a multiple of S * kGroups
+        uint32_t sample, pixel;
+        column_of_group(base + g < last ? base + g : last, A.q, sample, pixel);
+        const T* const from = A.x + (size_t)sample * P.Cin * P.HW + pixel;
+        const int per = threads / kGroups;      // chunks of a round
 #pragma unroll 2
-        for (int chunk = tid >> 5; chunk < t.chunks; chunk += 8) {
-            vec r[8];
+        for (int chunk = tid / (S * kGroups) * S + tid % S; chunk < t.chunks; chunk += per) {
+            lvec r[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int ch = 8 * chunk + e;
-                r[e] = *(const vec*)(from + (size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW);
+                r[e] = *(const lvec*)(from + (size_t)(ch < P.Cin ? ch : P.Cin - 1) * P.HW);
             }
 #pragma unroll
-            for (int j = 0; j < CT; ++j) {
+            for (int j = 0; j < V; ++j) {
                 T v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = 8 * chunk + e < P.Cin ? r[e][j] : T(0);
-                park(chunk, 32 * j + f, v);
+                park(chunk, g * V + j, v);
             }
         }
     }
     __syncthreads();
 
-    for (int tile = (int)blockIdx.y * kWaves + wave; tile < t.tiles; tile += (int)gridDim.y * kWaves) {
-        int q0, count;
-        walk_of(P, t, tile, q0, count);
-        const int steps = (count + 1) / 2;
-        const char* a_at = A.ws + t.a_at + (size_t)tile * t.steps * 2 * NP * 1024 + lane * 16;
+    // a filter's plane of these columns is k * HW (of dh: k * k_stride) on from here; both fit 32 bits
+    T* out[COLUMNS ? CT : 1];
+    const T* grad[COLUMNS ? CT : 1];
+#pragma unroll
+    for (int j = 0; j < (COLUMNS ? CT : 1); ++j) {
+        grad[j] = GRAD ? A.dy + (size_t)(real[j] ? n[j] : 0) * P.Cout * P.HW + px[j] : nullptr;
+        out[j] = A.out + (GRAD ? (size_t)n[j] * A.o.n_stride : (size_t)n[j] * P.Cout * P.HW) + px[j];
+    }
+    while (tile < t.tiles) {
+        const int now = tile;
         f32x16 acc[2][CT];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < CT; ++j) acc[i][j] = f32x16{};
-
-        constexpr int D = NP == 1 ? 4 : 2;      // K steps whose weights are in flight
-        u32x4 a[D][2][NP];
-        auto fetch = [&](int slot, int step) {
-            const char* const from = a_at + (size_t)(step < steps ? step : steps - 1) * 2 * NP * 1024;
+        const int* const table = (const int*)A.ws + now * kRows + 4 * h;
+        i32x4 filters[4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i) filters[i] = *(const i32x4*)(table + 8 * i);
+        // dy under way while the projections are computed: of rows without a filter, and of columns past the last, the first one's
+        vec up[GRAD ? 16 : 1];
+        if constexpr (GRAD) {
 #pragma unroll
-                for (int k = 0; k < NP; ++k) a[slot][i][k] = *(const u32x4*)(from + (i * NP + k) * 1024);
-        };
+            for (int r = 0; r < 16; ++r) {
+                const int k = filters[r / 4][r % 4];
+                const uint32_t plane = (uint32_t)k < (uint32_t)P.Cout ? (uint32_t)k * (uint32_t)P.HW : 0u;
+                if constexpr (COLUMNS) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) fetch(d, d);
+                    for (int j = 0; j < CT; ++j) up[r][j] = grad[j][plane];
+                } else {
+                    up[r] = *(const vec*)(grad[0] + plane);
+                }
+            }
+        }
         for (int s0 = 0; s0 < steps; s0 += D) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
@@ -256,21 +307,22 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
                         acc[0][j] = product<NP>(a[d][0], b, acc[0][j]);
                         acc[1][j] = product<NP>(a[d][1], b, acc[1][j]);
                     }
-                    fetch(d, s0 + d + D);
+                    if (s0 + d + D < steps) fetch(d, s0 + d + D);
                 }
             }
         }
+        tile += shares * waves;
+        if (tile < t.tiles) begin(tile);
 
-        // acc[.][j][r]: row (r & 3) + 8 * (r >> 2) + 4 * h of the tile, column 32 * j + f
-        const int* const table = (const int*)A.ws + tile * kRows + 4 * h;
+        // acc[.][j][r]: row (r & 3) + 8 * (r >> 2) + 4 * h of the tile, column CT * f + j
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const i32x4 filters = *(const i32x4*)(table + 8 * i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int k = filters[e], r = 4 * i + e;
+                const int k = filters[i][e], r = 4 * i + e;
+                const bool there = (uint32_t)k < (uint32_t)P.Cout;      // else past the rows, or a hole, whose gradients are zeros
+                const uint32_t plane = (uint32_t)k * (uint32_t)P.HW;
                 if constexpr (!GRAD) {
-                    if (k < 0 || k >= P.Cout) continue;
                     float y[CT];
 #pragma unroll
                     for (int j = 0; j < CT; ++j) {
@@ -281,45 +333,31 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
                     if constexpr (COLUMNS) {
 #pragma unroll
                         for (int j = 0; j < CT; ++j)
-                            if (live[j]) A.out[((size_t)n[j] * P.Cout + k) * P.HW + px[j]] = from_f32<T>(y[j]);
+                            if (there & live[j]) out[j][plane] = from_f32<T>(y[j]);
                     } else {
                         vec o;
 #pragma unroll
                         for (int j = 0; j < CT; ++j) o[j] = from_f32<T>(y[j]);
-                        if (live[0]) *(vec*)(A.out + ((size_t)n[0] * P.Cout + k) * P.HW + px[0]) = o;
+                        if (there & live[0]) *(vec*)(out[0] + plane) = o;
                     }
                 } else {
-                    if (k < 0) continue;
-                    const bool there = k < P.Cout;      // a hole's gradients are zeros
-                    float up[CT];
-                    if constexpr (COLUMNS) {
-#pragma unroll
-                        for (int j = 0; j < CT; ++j)
-                            up[j] = there && real[j] ? to_f32(A.dy[((size_t)n[j] * P.Cout + k) * P.HW + px[j]]) : 0.f;
-                    } else {
-                        vec v;
-                        if (there) v = *(const vec*)(A.dy + ((size_t)n[0] * P.Cout + k) * P.HW + px[0]);
-#pragma unroll
-                        for (int j = 0; j < CT; ++j) up[j] = there ? to_f32((T)v[j]) : 0.f;
-                    }
                     float dg[CT], du[CT];
 #pragma unroll
                     for (int j = 0; j < CT; ++j) {
                         float v, slope;
                         activate(A.act, acc[0][j][r], v, slope);
                         const bool zero = !there || (COLUMNS && !real[COLUMNS ? j : 0]);
-                        dg[j] = zero ? 0.f : up[j] * acc[1][j][r] * slope;
-                        du[j] = zero ? 0.f : up[j] * v;
+                        const float d = to_f32((T)up[r][j]);
+                        dg[j] = zero ? 0.f : d * acc[1][j][r] * slope;
+                        du[j] = zero ? 0.f : d * v;
                     }
-                    T* const at = A.out + (size_t)k * A.o.k_stride;
-                    const size_t second = (size_t)A.o.padded * A.o.k_stride;
+                    const size_t to = (uint32_t)k * (uint32_t)A.o.k_stride, second = (uint32_t)A.o.padded * (uint32_t)A.o.k_stride;
                     if constexpr (COLUMNS) {
 #pragma unroll
                         for (int j = 0; j < CT; ++j) {
-                            if (!live[j]) continue;
-                            T* const to = at + (size_t)n[j] * A.o.n_stride + px[j];
-                            to[0] = from_f32<T>(dg[j]);
-                            to[second] = from_f32<T>(du[j]);
+                            if (!((k >= 0) & live[j])) continue;
+                            out[j][to] = from_f32<T>(dg[j]);
+                            out[j][to + second] = from_f32<T>(du[j]);
                         }
                     } else {
                         vec o0, o1;
@@ -328,10 +366,9 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
                             o0[j] = from_f32<T>(dg[j]);
                             o1[j] = from_f32<T>(du[j]);
                         }
-                        T* const to = at + (size_t)n[0] * A.o.n_stride + px[0];
-                        if (live[0]) {
-                            *(vec*)to = o0;
-                            *(vec*)(to + second) = o1;
+                        if ((k >= 0) & live[0]) {
+                            *(vec*)(out[0] + to) = o0;
+                            *(vec*)(out[0] + to + second) = o1;
                         }
                     }
                 }
@@ -340,13 +377,13 @@ __global__ __launch_bounds__(256, 2) void gated_product(Args<T> A)
     }
 }
 
-template <typename T, int CT, bool COLUMNS, bool RAW, bool GRAD>
+template <typename T, int CT, int V, bool RAW, bool GRAD>
 hipError_t start(const Args<T>& a, const Shape& s, hipStream_t st)
 {
-    auto* const kernel = gated_product<T, CT, COLUMNS, RAW, GRAD>;
+    auto* const kernel = gated_product<T, CT, V, RAW, GRAD>;
     static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (allowed != hipSuccess) return allowed;
-    kernel<<<dim3(s.gx, s.gy), dim3(256), s.lds, st>>>(a);
+    kernel<<<dim3(8u * (unsigned)a.deal.chunk), dim3(64 * s.waves), s.lds, st>>>(a);
     return hipGetLastError();
 }
 
@@ -354,25 +391,30 @@ template <typename T, bool GRAD>
 hipError_t start_as(const Args<T>& a, const Shape& s, hipStream_t st)
 {
     if constexpr (sizeof(T) == 2) {
-        if (s.columns) {
-            if (s.ct == 4) return start<T, 4, true, false, GRAD>(a, s, st);
-            if (s.ct == 2) return start<T, 2, true, false, GRAD>(a, s, st);
-            return start<T, 1, true, false, GRAD>(a, s, st);
+        switch (s.v * 8 + s.ct) {
+            case 8 + 1: return start<T, 1, 1, false, GRAD>(a, s, st);
+            case 8 + 2: return start<T, 2, 1, false, GRAD>(a, s, st);
+            case 8 + 4: return start<T, 4, 1, false, GRAD>(a, s, st);
+            case 32 + 1: return start<T, 1, 4, false, GRAD>(a, s, st);
+            case 32 + 2: return start<T, 2, 4, false, GRAD>(a, s, st);
+            case 32 + 4: return start<T, 4, 4, false, GRAD>(a, s, st);
+            case 64 + 1: return start<T, 1, 8, false, GRAD>(a, s, st);
+            case 64 + 2: return start<T, 2, 8, false, GRAD>(a, s, st);
+            case 64 + 4: return start<T, 4, 8, false, GRAD>(a, s, st);
+            default: return hipErrorInvalidValue;
         }
-        if (s.ct == 4) return start<T, 4, false, false, GRAD>(a, s, st);
-        if (s.ct == 2) return start<T, 2, false, false, GRAD>(a, s, st);
-        return start<T, 1, false, false, GRAD>(a, s, st);
     } else {
-        if (s.raw) {
-            if (s.columns) return start<T, 1, true, true, GRAD>(a, s, st);
-            return start<T, 1, false, true, GRAD>(a, s, st);
+        switch (s.v * 8 + s.ct * 2 + (s.raw ? 1 : 0)) {
+            case 8 + 2: return start<T, 1, 1, false, GRAD>(a, s, st);
+            case 8 + 4: return start<T, 2, 1, false, GRAD>(a, s, st);
+            case 8 + 3: return start<T, 1, 1, true, GRAD>(a, s, st);
+            case 8 + 5: return start<T, 2, 1, true, GRAD>(a, s, st);
+            case 32 + 2: return start<T, 1, 4, false, GRAD>(a, s, st);
+            case 32 + 4: return start<T, 2, 4, false, GRAD>(a, s, st);
+            case 32 + 3: return start<T, 1, 4, true, GRAD>(a, s, st);
+            case 32 + 5: return start<T, 2, 4, true, GRAD>(a, s, st);
+            default: return hipErrorInvalidValue;
         }
-        if (s.columns) {
-            if (s.ct == 2) return start<T, 2, true, false, GRAD>(a, s, st);
-            return start<T, 1, true, false, GRAD>(a, s, st);
-        }
-        if (s.ct == 2) return start<T, 2, false, false, GRAD>(a, s, st);
-        return start<T, 1, false, false, GRAD>(a, s, st);
     }
 }
 
@@ -382,22 +424,23 @@ int lds_of(const Plan& t, int es, int ct, bool raw) { return t.chunks * (32 * ct
 
 bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape* s)
 {
-    s->columns = p.HW < 4;
-    s->raw = false;
+    s->v = p.HW < 4 ? 1 : es == 2 && p.HW % 8 == 0 ? 8 : 4;
+    s->waves = 8;
+    if (lds_of(t, es, 1, true) > kLds) return false;
+    auto tiles = [&](int c) {
+        const long long units = s->v == 1 ? stored : column_groups(p, s->v).count;
+        return (units + 32 * c / s->v - 1) / (32 * c / s->v);
+    };
+    const int most = (t.tiles + s->waves - 1) / s->waves;
     int ct = es == 2 ? 4 : 2;
-    auto tiles = [&](int c) { return s->columns ? (stored + 32 * c - 1) / (32 * c) : (column_groups(p, c).count + 31) / 32; };
-    while (ct > 1 && (lds_of(t, es, ct, false) > kLds / 2 || tiles(ct) < 256)) ct /= 2;
-    if (lds_of(t, es, ct, false) > kLds) {
-        s->raw = true;
-        if (es == 2 || lds_of(t, es, 1, true) > kLds) return false;
-    }
+    while (ct > 1 && (lds_of(t, es, ct, true) > kLds || tiles(ct) * most < 192)) ct /= 2;
     s->ct = ct;
-    s->lds = lds_of(t, es, ct, s->raw);
-    const long long gx = tiles(ct);
-    const long long shares = (t.tiles + kWaves - 1) / kWaves;
-    const long long gy = gx >= 512 ? 1 : 512 / gx < shares ? 512 / gx : shares;
-    s->gx = (unsigned)gx;
-    s->gy = (unsigned)gy;
+    s->raw = es == 4 && lds_of(t, es, s->ct, false) > kLds / 2;
+    s->lds = lds_of(t, es, s->ct, s->raw);
+    const long long gx = tiles(s->ct);
+    const long long gy = gx >= 192 ? 1 : (256 + gx / 2) / gx < most ? (256 + gx / 2) / gx : most;
+    if (gx * gy > 1 << 22) return false;
+    s->deal = make_deal(gx, (int)gy);
     return true;
 }
 
@@ -412,16 +455,16 @@ hipError_t launch_pack(const T* w, char* ws, const Problem& p, const Plan& t, hi
 template <typename T>
 hipError_t launch_product(const T* x, const char* ws, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st)
 {
-    const Groups q = s.columns ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.ct);
-    return start_as<T, false>(Args<T>{x, ws, nullptr, y, p, t, q, GradOut{0, 0, 0, 0}, act}, s, st);
+    const Groups q = s.v == 1 ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.v);
+    return start_as<T, false>(Args<T>{x, ws, nullptr, y, p, t, q, GradOut{0, 0, 0, 0}, s.deal, act}, s, st);
 }
 
 template <typename T>
 hipError_t launch_product_grad(const T* x, const char* ws, const T* dy, T* dh, const GradOut& o, const Problem& p, const Plan& t,
                                const Shape& s, int act, hipStream_t st)
 {
-    const Groups q = s.columns ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.ct);
-    return start_as<T, true>(Args<T>{x, ws, dy, dh, p, t, q, o, act}, s, st);
+    const Groups q = s.v == 1 ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.v);
+    return start_as<T, true>(Args<T>{x, ws, dy, dh, p, t, q, o, s.deal, act}, s, st);
 }
 
 #define INSTANCES(T)                                                                                                          \
