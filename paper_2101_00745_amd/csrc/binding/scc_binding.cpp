@@ -334,11 +334,294 @@ PyObject* dw_block(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// x [N,Cin,H,W], w [2,Cout,Cin/cg], cg, co and the activation's code of a gated layer's call, dy behind w where there is one
+bool gated(PyObject* const* args, int tensors, Args* a, int* act, Layer* l)
+{
+    if (!PyLong_CheckExact(args[tensors + 2]) || !parse(args, tensors + 2, tensors, false, a)) return false;
+    *act = (int)PyLong_AsLong(args[tensors + 2]);
+    const at::Tensor &x = *a->t[0], &w = *a->t[1];
+    return w.dim() == 3 && w.size(0) == 2 && w.is_contiguous() && layer(*a, x, w.select(0, 0), l);
+}
+
+template <typename F>
+at::Tensor gated_forward_of(const at::Tensor& x, const at::Tensor& w, const Args& a, int act, const Layer& l, F&& run)
+{
+    at::Tensor y = at::empty({l.N, l.Cout, l.H, l.W}, x.options());
+    const size_t need = scc_gated_forward_workspace_bytes(l.N, l.Cin, l.Cout, l.H, l.W, a.cg, a.co, l.dtype);
+    const at::Tensor ws = scratch(need, x);
+    const int rc = run([&](void* st) {
+        return scc_gated_forward(x.data_ptr(), w.data_ptr(), y.data_ptr(), l.N, l.Cin, l.Cout, l.H, l.W, a.cg, a.co,
+                                 (scc_activation)act, l.dtype, address(ws), need, st);
+    });
+    return rc == SCC_OK ? y : at::Tensor();
+}
+
+// dx, dw; none where the call failed
+template <typename F>
+std::vector<at::Tensor> gated_backward_of(const at::Tensor& x, const at::Tensor& w, const at::Tensor& dy, const Args& a, int act,
+                                          const Layer& l, scc_dtype grad, F&& run)
+{
+    at::Tensor dx = at::empty_like(x);
+    at::Tensor dw = at::empty(w.sizes(), x.options().dtype(grad == SCC_F32 ? at::kFloat : at::kBFloat16));
+    const size_t need = scc_gated_backward_workspace_bytes(l.N, l.Cin, l.Cout, l.H, l.W, a.cg, a.co, l.dtype, grad);
+    const at::Tensor ws = scratch(need, x);
+    const int rc = run([&](void* st) {
+        return scc_gated_backward(x.data_ptr(), w.data_ptr(), dy.data_ptr(), dx.data_ptr(), dw.data_ptr(), l.N, l.Cin, l.Cout, l.H,
+                                  l.W, a.cg, a.co, (scc_activation)act, l.dtype, grad, address(ws), need, st);
+    });
+    if (rc != SCC_OK) return {};
+    return {dx, dw};
+}
+
+PyObject* gated_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args a;
+    Layer l;
+    int act;
+    if (n != 5 || !gated(args, 2, &a, &act, &l)) Py_RETURN_NONE;
+    const at::Tensor &x = *a.t[0], &w = *a.t[1];
+    at::Tensor y = gated_forward_of(x, w, a, act, l, [&](auto&& f) { return launch(x, f); });
+    if (!y.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* gated_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args a;
+    Layer l;
+    int act;
+    if (n != 7 || !PyBool_Check(args[6]) || !gated(args, 3, &a, &act, &l)) Py_RETURN_NONE;
+    const at::Tensor &x = *a.t[0], &w = *a.t[1], &dy = *a.t[2];
+    if (!outputs(dy, x, l)) Py_RETURN_NONE;
+    const std::vector<at::Tensor> g = gated_backward_of(x, w, dy, a, act, l, args[6] == Py_True ? l.dtype : SCC_F32,
+                                                        [&](auto&& f) { return launch(x, f); });
+    if (g.empty()) Py_RETURN_NONE;
+    return tuple_of({g[0], g[1]});
+    END_HANDLE_TH_ERRORS
+}
+
+struct FirstOrderPair : torch::autograd::Function<FirstOrderPair> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext*, const at::Tensor& dx, const at::Tensor& dw,
+                                                  const at::Tensor&, const at::Tensor&, const at::Tensor&)
+    {
+        return {dx.detach(), dw.detach()};
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, torch::autograd::variable_list)
+    {
+        TORCH_CHECK(false, "sliding-channel convolution has no second derivative");
+    }
+};
+
+// nn.GatedSCCFunction for a plain call whose two tensors want gradients, as Block is nn.DWSCCFunction
+struct Gated : torch::autograd::Function<Gated> {
+    struct Refused {};
+
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, int64_t cg, double co,
+                              int64_t act)
+    {
+        const Args a = {{&x, &w, nullptr, nullptr}, (int)cg, 1, co};
+        Layer l;
+        at::Tensor y;
+        if (layer(a, x, w.select(0, 0), &l)) y = gated_forward_of(x, w, a, (int)act, l, [&](auto&& f) { return launch(x, f); });
+        if (!y.defined()) throw Refused();
+        ctx->save_for_backward({x, w});
+        ctx->saved_data["cg"] = cg;
+        ctx->saved_data["co"] = co;
+        ctx->saved_data["act"] = act;
+        return y;
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const torch::autograd::variable_list saved = ctx->get_saved_variables();
+        const at::Tensor &x = saved[0], &w = saved[1];
+        const at::Tensor dy = grads[0].contiguous();
+        const Args a = {{&x, &w, &dy, nullptr}, (int)ctx->saved_data["cg"].toInt(), 1, ctx->saved_data["co"].toDouble()};
+        const int act = (int)ctx->saved_data["act"].toInt();
+        Layer l;
+        std::vector<at::Tensor> g;
+        if (w.dim() == 3 && w.is_contiguous() && layer(a, x, w.select(0, 0), &l) && outputs(dy, x, l))
+            g = gated_backward_of(x, w, dy, a, act, l, l.dtype, [&](auto&& f) { return f(stream_of(x)); });
+        if (g.empty()) g = general(a, act);
+        if (at::GradMode::is_enabled()) g = FirstOrderPair::apply(g[0], g[1], x, w, dy);
+        return {g[0], g[1], at::Tensor(), at::Tensor(), at::Tensor()};
+    }
+
+    static std::vector<at::Tensor> general(const Args& a, int act)
+    {
+        struct Locked {
+            PyGILState_STATE s = PyGILState_Ensure();
+            ~Locked() { PyGILState_Release(s); }
+        } locked;
+        std::vector<at::Tensor> g;
+        PyObject* m = PyImport_ImportModule("paper_2101_00745_amd.scc");
+        PyObject* t[3] = {};
+        for (int i = 0; i < 3; ++i) t[i] = THPVariable_Wrap(*a.t[i]);
+        PyObject* r = m ? PyObject_CallMethod(m, "_gated_backward", "OOOidiO", t[0], t[1], t[2], a.cg, a.co, act, Py_True) : nullptr;
+        for (int i = 0; r && i < 2; ++i) g.push_back(THPVariable_Unpack(PyTuple_GetItem(r, i)));
+        for (int i = 0; i < 3; ++i) Py_XDECREF(t[i]);
+        Py_XDECREF(r);
+        Py_XDECREF(m);
+        if (!r) {
+            python_error e;
+            e.persist();
+            throw e;
+        }
+        return g;
+    }
+};
+
+PyObject* gated_block(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    Args a;
+    Layer l;
+    int act;
+    if (n != 5 || !at::GradMode::is_enabled() || !gated(args, 2, &a, &act, &l)) Py_RETURN_NONE;
+    const at::Tensor &x = *a.t[0], &w = *a.t[1];
+    for (int i = 0; i < 2; ++i)
+        if (!a.t[i]->requires_grad() || a.t[i]->is_inference() || a.t[i]->_fw_grad(0).defined()) Py_RETURN_NONE;
+    try {
+        return THPVariable_Wrap(Gated::apply(x, w, (int64_t)a.cg, a.co, (int64_t)act));
+    } catch (const Gated::Refused&) {
+        Py_RETURN_NONE;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// A list of plain matrices of one type.
+bool matrices(PyObject* o, Py_ssize_t count, at::ScalarType type, std::vector<const at::Tensor*>* out)
+{
+    if (!PyList_CheckExact(o) || PyList_GET_SIZE(o) != count) return false;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject* e = PyList_GET_ITEM(o, i);
+        if (!THPVariable_CheckExact(e)) return false;
+        const at::Tensor& t = THPVariable_Unpack(e);
+        if (!plain(t) || t.dim() != 2 || t.scalar_type() != type || !fits(t)) return false;
+        out->push_back(&t);
+    }
+    return true;
+}
+
+// A list's addresses and sizes, as the library takes them
+struct List {
+    std::vector<void*> address;
+    std::vector<int> rows, cols;
+    size_t need;
+    at::Tensor ws;
+};
+
+bool begin_list(PyObject* first, std::vector<const at::Tensor*>* ts, List* l)
+{
+    if (c10::impl::TorchDispatchModeTLS::any_modes_set() || at::impl::PythonTorchFunctionTLS::stack_len() > 0) return false;
+    if (!PyList_CheckExact(first) || PyList_GET_SIZE(first) < 1 || PyList_GET_SIZE(first) > INT_MAX) return false;
+    PyObject* e = PyList_GET_ITEM(first, 0);
+    if (!THPVariable_CheckExact(e)) return false;
+    if (!matrices(first, PyList_GET_SIZE(first), THPVariable_Unpack(e).scalar_type(), ts)) return false;
+    for (const at::Tensor* t : *ts) {
+        l->address.push_back(t->data_ptr());
+        l->rows.push_back((int)t->size(0));
+        l->cols.push_back((int)t->size(1));
+    }
+    l->need = scc_orthogonal_workspace_bytes((int)ts->size(), l->rows.data(), l->cols.data());
+    if (l->need) l->ws = scratch(l->need, *(*ts)[0]);
+    return l->need != 0;
+}
+
+bool numbers(PyObject* const* a, int n, double* out)
+{
+    for (int i = 0; i < n; ++i) {
+        out[i] = PyFloat_AsDouble(a[i]);
+        if (out[i] == -1.0 && PyErr_Occurred()) {
+            PyErr_Clear();
+            return false;
+        }
+    }
+    return true;
+}
+
+bool same_shapes(const std::vector<const at::Tensor*>& a, const std::vector<const at::Tensor*>& b)
+{
+    for (size_t i = 0; i < a.size(); ++i)
+        if (a[i]->sizes() != b[i]->sizes()) return false;
+    return true;
+}
+
+// (matrices, steps, a, b, c, eps) -> list of their orthogonalised forms, or None
+PyObject* orthogonalise(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    std::vector<const at::Tensor*> g;
+    List l;
+    double v[4];
+    int steps;
+    if (n != 6 || !integer(args[1], &steps) || !numbers(args + 2, 4, v) || !begin_list(args[0], &g, &l)) Py_RETURN_NONE;
+    std::vector<at::Tensor> out;
+    std::vector<void*> to;
+    for (const at::Tensor* t : g) {
+        out.push_back(at::empty_like(*t));
+        to.push_back(out.back().data_ptr());
+    }
+    const scc_orthogonal_options o = {0.f, 0.f, 0.f, 0, steps, (float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+    const scc_dtype dtype = g[0]->scalar_type() == at::kFloat ? SCC_F32 : SCC_BF16;
+    const int rc = launch(l.ws, [&](void* st) {
+        return scc_orthogonalise((int)g.size(), l.address.data(), to.data(), l.rows.data(), l.cols.data(), &o, dtype, l.ws.data_ptr(),
+                                 l.need, st);
+    });
+    if (rc != SCC_OK) Py_RETURN_NONE;
+    PyObject* r = PyList_New((Py_ssize_t)out.size());
+    for (size_t i = 0; r && i < out.size(); ++i) PyList_SET_ITEM(r, (Py_ssize_t)i, THPVariable_Wrap(out[i]));
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// (weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> True, or None
+PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    std::vector<const at::Tensor*> w, g, m;
+    List l;
+    double v[3], e[4];
+    int steps;
+    if (n != 12 || !numbers(args + 3, 3, v) || !PyBool_Check(args[6]) || !integer(args[7], &steps) || !numbers(args + 8, 4, e) ||
+        !begin_list(args[0], &w, &l))
+        Py_RETURN_NONE;
+    const Py_ssize_t count = (Py_ssize_t)w.size();
+    if (!matrices(args[1], count, w[0]->scalar_type(), &g) || !matrices(args[2], count, at::kFloat, &m) || !same_shapes(w, g) ||
+        !same_shapes(w, m))
+        Py_RETURN_NONE;
+    std::vector<void*> from;
+    std::vector<float*> momenta;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        from.push_back(g[i]->data_ptr());
+        momenta.push_back((float*)m[i]->data_ptr());
+    }
+    const scc_orthogonal_options o = {(float)v[0], (float)v[1], (float)v[2], args[6] == Py_True, steps,
+                                      (float)e[0], (float)e[1], (float)e[2], (float)e[3]};
+    const scc_dtype dtype = w[0]->scalar_type() == at::kFloat ? SCC_F32 : SCC_BF16;
+    const int rc = launch(l.ws, [&](void* st) {
+        return scc_orthogonal_step((int)count, l.address.data(), from.data(), momenta.data(), l.rows.data(), l.cols.data(), &o, dtype,
+                                   l.ws.data_ptr(), l.need, st);
+    });
+    if (rc != SCC_OK) Py_RETURN_NONE;
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 #define METHOD(name, doc) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, doc}
 PyMethodDef methods[] = {METHOD(forward, "(x, w, cg, co) -> y or None"), METHOD(backward, "(x, dy, w, cg, co) -> (dx, dw) or None"),
                          METHOD(dw_forward, "(x, kdw, w, cg, co, stride) -> y or None"),
                          METHOD(dw_block, "(x, kdw, w, cg, co, stride) -> y under autograd, or None"),
                          METHOD(dw_backward, "(x, kdw, w, dy, cg, co, stride, stored) -> (dx, dkdw, dw) or None"),
+                         METHOD(gated_forward, "(x, w, cg, co, act) -> y or None"),
+                         METHOD(gated_backward, "(x, w, dy, cg, co, act, stored) -> (dx, dw) or None"),
+                         METHOD(gated_block, "(x, w, cg, co, act) -> y under autograd, or None"),
+                         METHOD(orthogonalise, "(matrices, steps, a, b, c, eps) -> list or None"),
+                         METHOD(orthogonal_step, "(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> True or None"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -188,40 +188,90 @@ __global__ __launch_bounds__(256) void ns_normalise(Batch B, Starts S, Options o
 
 enum { kGram, kPoly, kApply, kLast };
 
-// One tile of p = x x^T (kGram) or q = b p + c p p (kPoly), on and above the diagonal and mirrored; or of a x + q x, into the other two panels
-// (kApply) or the weights (kLast).
+// Which panels a stage multiplies: rows of `left` by rows of `right`, over k_tiles
+struct Factors {
+    const char *left, *right;
+    int k_tiles;
+};
+
+template <int STAGE>
+__device__ __forceinline__ Factors factors_of(const Matrix& m, const Parts& parts, const char* base, int from)
+{
+    if constexpr (STAGE == kGram) return {base + parts.x[from], base + parts.x[from], m.l};
+    else if constexpr (STAGE == kPoly) return {base + parts.p, base + parts.p, m.s};
+    else return {base + parts.q, base + parts.xt[from], m.s};
+}
+
+// block-th pair (i, j), i <= j, of the upper triangle: column j holds j + 1 of them
+__device__ __forceinline__ void triangle(int block, int& i, int& j)
+{
+    j = (int)((sqrtf(8.f * (float)block + 1.f) - 1.f) * 0.5f);
+    while (j * (j + 1) / 2 > block) --j;
+    while ((j + 1) * (j + 2) / 2 <= block) ++j;
+    i = block - j * (j + 1) / 2;
+}
+
+// Four sums of a tile's column f, rows 8 * q + 4 * h + e, to what the stage makes of them: into the panel that has columns as rows (or the
+// weights); v is then what was stored.
 template <typename T, int STAGE>
-__global__ __launch_bounds__(256) void ns_product(Batch B, Starts S, Options o, int from, int update, char* ws)
+__device__ __forceinline__ void finish_quad(const Matrix& m, const Parts& parts, char* base, const Options& o, int from, int update, int ti,
+                                            int tj, int q, int f, int h, float (&v)[4])
+{
+    const size_t at = quad_at(tj, m.s, ti, q, f, h);
+    if constexpr (STAGE != kGram) {
+        float x[4];
+        load_quad(base + (STAGE == kPoly ? parts.p : parts.xt[from]) + at, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = STAGE == kPoly ? fmaf(o.b, x[e], o.c * v[e]) : fmaf(o.a, x[e], v[e]);
+    }
+    if constexpr (STAGE == kLast) {
+        const float scale = update ? o.lr * sqrtf(fmaxf(1.f, (float)m.rows / (float)m.cols)) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = ti * kTile + 8 * q + 4 * h + e, j = tj * kTile + f;
+            if (!inside(m, i, j)) continue;
+            T* const w = (T*)m.w + place(m, i, j);
+            *w = from_f32<T>(update ? to_f32(*w) * (1.f - o.lr * o.decay) - scale * v[e] : v[e]);
+        }
+    } else {
+        store_quad(base + (STAGE == kGram ? parts.p : STAGE == kPoly ? parts.q : parts.xt[from ^ 1]) + at, v);
+    }
+}
+
+// the panel that has a stage's rows as rows: the mirrored half of a symmetric result, or the other panel of x
+template <int STAGE>
+__device__ __forceinline__ char* rows_of(const Parts& parts, char* base, int from)
+{
+    return base + (STAGE == kGram ? parts.p : STAGE == kPoly ? parts.q : parts.x[from ^ 1]);
+}
+
+// One 32 x 32 tile of p = x x^T (kGram) or q = b p + c p p (kPoly), on and above the diagonal and mirrored; or of a x + q x, into the other two
+// panels (kApply) or the weights (kLast).  The wavefronts take the K steps in turn, four steps' loads in flight each.
+constexpr int kSplit = 8;
+
+template <typename T, int STAGE>
+__global__ __launch_bounds__(64 * kSplit) void ns_product(Batch B, Starts S, Options o, int from, int update, char* ws)
 {
     int block = (int)blockIdx.x;
     const Matrix& m = B.mat[matrix_of(S, B.count, block)];
     const Parts parts = parts_of(m.s, m.l);
     char* const base = ws + m.at;
-    int ti, tj, k_tiles;
-    const char *left, *right;
+    int ti, tj;
     if constexpr (STAGE == kGram || STAGE == kPoly) {
-        // column tj of the upper triangle holds tj + 1 tiles
-        tj = (int)((sqrtf(8.f * (float)block + 1.f) - 1.f) * 0.5f);
-        while (tj * (tj + 1) / 2 > block) --tj;
-        while ((tj + 1) * (tj + 2) / 2 <= block) ++tj;
-        ti = block - tj * (tj + 1) / 2;
-        k_tiles = STAGE == kGram ? m.l : m.s;
-        left = right = base + (STAGE == kGram ? parts.x[from] : parts.p);
+        triangle(block, ti, tj);
     } else {
         ti = block / m.l;
         tj = block - ti * m.l;
-        k_tiles = m.s;
-        left = base + parts.q;
-        right = base + parts.xt[from];
     }
+    const Factors F = factors_of<STAGE>(m, parts, base, from);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, f = lane & 31, h = lane >> 5;
-    const int steps = 2 * k_tiles;
+    const int steps = 2 * F.k_tiles;
     f32x16 acc = {};
-    const char* const a0 = step_of(left, ti, k_tiles, 0) + lane * 16;
-    const char* const b0 = step_of(right, tj, k_tiles, 0) + lane * 16;
-#pragma unroll 2
-    for (int k = wave; k < steps; k += 4) {
+    const char* const a0 = step_of(F.left, ti, F.k_tiles, 0) + lane * 16;
+    const char* const b0 = step_of(F.right, tj, F.k_tiles, 0) + lane * 16;
+#pragma unroll 4
+    for (int k = wave; k < steps; k += kSplit) {
         u32x4 a[3], b[3];
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
@@ -230,45 +280,133 @@ __global__ __launch_bounds__(256) void ns_product(Batch B, Starts S, Options o, 
         }
         acc = product(a, b, acc);
     }
-    __shared__ float partial[4][kTile * kPitch];
+    __shared__ float partial[kSplit][kTile * kPitch];
 #pragma unroll
     for (int r = 0; r < 16; ++r) partial[wave][((r & 3) + 8 * (r >> 2) + 4 * h) * kPitch + f] = acc[r];
     __syncthreads();
-    // rows 8 * wave + 4 * h + e, column f, are this lane's from here
+    // the first four wavefronts' lanes: rows 8 * wave + 4 * h + e, column f
     float v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int at = (8 * wave + 4 * h + e) * kPitch + f;
-        v[e] = (partial[0][at] + partial[1][at]) + (partial[2][at] + partial[3][at]);
-    }
-    if constexpr (STAGE == kLast) {
-        float x[4];
-        load_quad(base + parts.xt[from] + quad_at(tj, m.s, ti, wave, f, h), x);
-        const float scale = update ? o.lr * sqrtf(fmaxf(1.f, (float)m.rows / (float)m.cols)) : 0.f;
+    if (wave < 4) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int i = ti * kTile + 8 * wave + 4 * h + e, j = tj * kTile + f;
-            if (!inside(m, i, j)) continue;
-            T* const w = (T*)m.w + place(m, i, j);
-            const float r = fmaf(o.a, x[e], v[e]);
-            *w = from_f32<T>(update ? to_f32(*w) * (1.f - o.lr * o.decay) - scale * r : r);
+            const int at = (8 * wave + 4 * h + e) * kPitch + f;
+            v[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSplit; ++i) v[e] += partial[i][at];
         }
-        return;
+        finish_quad<T, STAGE>(m, parts, base, o, from, update, ti, tj, wave, f, h, v);
     }
-    if constexpr (STAGE == kPoly || STAGE == kApply) {
-        float x[4];
-        load_quad(base + (STAGE == kPoly ? parts.p : parts.xt[from]) + quad_at(tj, m.s, ti, wave, f, h), x);
+    if (STAGE == kLast || (STAGE != kApply && ti == tj)) return;
+    __syncthreads();
+    if (wave < 4) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = STAGE == kPoly ? fmaf(o.b, x[e], o.c * v[e]) : fmaf(o.a, x[e], v[e]);
+        for (int e = 0; e < 4; ++e) partial[0][(8 * wave + 4 * h + e) * kPitch + f] = v[e];
     }
-    char* const to = base + (STAGE == kGram ? parts.p : STAGE == kPoly ? parts.q : parts.xt[from ^ 1]);
-    store_quad(to + quad_at(tj, m.s, ti, wave, f, h), v);          // column f as a row
-    if (STAGE != kApply && ti == tj) return;
     __syncthreads();
+    store_rows(rows_of<STAGE>(parts, base, from), ti, STAGE == kApply ? m.l : m.s, tj, partial[0], tid);
+}
+
+// The same in blocks of 4 x 4 tiles, for lists with enough of them: four wavefronts of 2 x 2 tiles share a K step's 24 KB through LDS, two
+// buffers, one barrier a step; the loads of the step after the next are in flight meanwhile.
+constexpr int kBlock = 4;
+
+template <typename T, int STAGE>
+__global__ __launch_bounds__(256, 2) void ns_product_wide(Batch B, Starts S, Options o, int from, int update, char* ws)
+{
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * kBlock * 3072];
+    int block = (int)blockIdx.x;
+    const Matrix& m = B.mat[matrix_of(S, B.count, block)];
+    const Parts parts = parts_of(m.s, m.l);
+    char* const base = ws + m.at;
+    int bi, bj;
+    if constexpr (STAGE == kGram || STAGE == kPoly) {
+        triangle(block, bi, bj);
+    } else {
+        const int across = (m.l + kBlock - 1) / kBlock;
+        bi = block / across;
+        bj = block - bi * across;
+    }
+    const Factors F = factors_of<STAGE>(m, parts, base, from);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid & 63, f = lane & 31, h = lane >> 5;
+    const int steps = 2 * F.k_tiles;
+    const int rows_l = m.s, rows_r = STAGE == kGram || STAGE == kPoly ? m.s : m.l;      // tiles of either factor
+
+    // a wavefront fetches two of the eight tiles' steps; tiles past the edge are the last one's again, and not stored
+    const char* src[2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) partial[0][(8 * wave + 4 * h + e) * kPitch + f] = v[e];
+    for (int i = 0; i < 2; ++i) {
+        const int which = 2 * wave + i, r = (which < kBlock ? bi * kBlock + which : bj * kBlock + which - kBlock);
+        src[i] = which < kBlock ? step_of(F.left, r < rows_l ? r : rows_l - 1, F.k_tiles, 0) : step_of(F.right, r < rows_r ? r : rows_r - 1, F.k_tiles, 0);
+        src[i] += lane * 16;
+    }
+    u32x4 next[2][6];
+    auto fetch = [&](int set, int k) {
+        k = k < steps ? k : steps - 1;
+#pragma unroll
+        for (int i = 0; i < 6; ++i) next[set][i] = *(const u32x4*)(src[i / 3] + (size_t)k * 3072 + i % 3 * 1024);
+    };
+    auto park = [&](int set, int buffer) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) *(u32x4*)(lds[buffer] + (2 * wave + i / 3) * 3072 + i % 3 * 1024 + lane * 16) = next[set][i];
+    };
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] = f32x16{};
+    const int wi = wave >> 1, wj = wave & 1;
+    auto multiply = [&](int buffer) {
+        u32x4 a[2][3], b[2][3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                a[i][p] = *(const u32x4*)(lds[buffer] + (2 * wi + i) * 3072 + p * 1024 + lane * 16);
+                b[i][p] = *(const u32x4*)(lds[buffer] + (kBlock + 2 * wj + i) * 3072 + p * 1024 + lane * 16);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = product(a[i], b[j], acc[i][j]);
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    park(0, 0);
+    for (int k = 0; k < steps; k += 2) {        // steps is even
+        __syncthreads();
+        fetch(0, k + 2);
+        multiply(0);
+        park(1, 1);
+        __syncthreads();
+        fetch(1, k + 3);
+        multiply(1);
+        park(0, 0);
+    }
     __syncthreads();
-    store_rows(STAGE == kApply ? base + parts.x[from ^ 1] : to, ti, STAGE == kApply ? m.l : m.s, tj, partial[0], tid);
+    float* const tile = (float*)lds + wave * kTile * kPitch;       // a wavefront's own
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int ti = bi * kBlock + 2 * wi + i, tj = bj * kBlock + 2 * wj + j;
+            if (ti >= rows_l || tj >= rows_r || ((STAGE == kGram || STAGE == kPoly) && ti > tj)) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+                finish_quad<T, STAGE>(m, parts, base, o, from, update, ti, tj, q, f, h, v);
+                if constexpr (STAGE != kLast) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) tile[(8 * q + 4 * h + e) * kPitch + f] = v[e];
+                }
+            }
+            if (STAGE == kLast || (STAGE != kApply && ti == tj)) continue;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            char* const to = rows_of<STAGE>(parts, base, from);
+            store_rows(to, ti, STAGE == kApply ? m.l : m.s, tj, tile, lane);
+            store_rows(to, ti, STAGE == kApply ? m.l : m.s, tj, tile, lane + 64);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
 }
 
 template <typename F>
@@ -288,16 +426,30 @@ int starts_of(const Batch& b, Starts* s, F&& tiles)
 template <typename T>
 hipError_t launch_orthogonal(const Batch& batch, const Options& o, bool update, char* ws, hipStream_t st)
 {
-    Starts all, half;
+    Starts all, half, wide_all, wide_half;
     const int n = starts_of(batch, &all, [](const Matrix& m) { return m.s * m.l; });
     const int nh = starts_of(batch, &half, [](const Matrix& m) { return m.s * (m.s + 1) / 2; });
+    auto blocks = [](int tiles) { return (tiles + kBlock - 1) / kBlock; };
+    const int nw = starts_of(batch, &wide_all, [&](const Matrix& m) { return blocks(m.s) * blocks(m.l); });
+    const int nwh = starts_of(batch, &wide_half, [&](const Matrix& m) { return blocks(m.s) * (blocks(m.s) + 1) / 2; });
+    const bool wide = nwh >= 96;
     ns_momentum<T><<<dim3(n), dim3(256), 0, st>>>(batch, all, o, ws);
     ns_normalise<T><<<dim3(n), dim3(256), 0, st>>>(batch, all, o, ws);
     for (int i = 0; i < o.steps; ++i) {
-        ns_product<T, kGram><<<dim3(nh), dim3(256), 0, st>>>(batch, half, o, i & 1, 0, ws);
-        ns_product<T, kPoly><<<dim3(nh), dim3(256), 0, st>>>(batch, half, o, i & 1, 0, ws);
-        if (i + 1 < o.steps) ns_product<T, kApply><<<dim3(n), dim3(256), 0, st>>>(batch, all, o, i & 1, 0, ws);
-        else ns_product<T, kLast><<<dim3(n), dim3(256), 0, st>>>(batch, all, o, i & 1, update ? 1 : 0, ws);
+        const bool last = i + 1 == o.steps;
+        const int from = i & 1, up = update ? 1 : 0;
+        if (wide) {
+            ns_product_wide<T, kGram><<<dim3(nwh), dim3(256), 0, st>>>(batch, wide_half, o, from, 0, ws);
+            ns_product_wide<T, kPoly><<<dim3(nwh), dim3(256), 0, st>>>(batch, wide_half, o, from, 0, ws);
+            if (last) ns_product_wide<T, kLast><<<dim3(nw), dim3(256), 0, st>>>(batch, wide_all, o, from, up, ws);
+            else ns_product_wide<T, kApply><<<dim3(nw), dim3(256), 0, st>>>(batch, wide_all, o, from, 0, ws);
+        } else {
+            constexpr int threads = 64 * kSplit;
+            ns_product<T, kGram><<<dim3(nh), dim3(threads), 0, st>>>(batch, half, o, from, 0, ws);
+            ns_product<T, kPoly><<<dim3(nh), dim3(threads), 0, st>>>(batch, half, o, from, 0, ws);
+            if (last) ns_product<T, kLast><<<dim3(n), dim3(threads), 0, st>>>(batch, all, o, from, up, ws);
+            else ns_product<T, kApply><<<dim3(n), dim3(threads), 0, st>>>(batch, all, o, from, 0, ws);
+        }
     }
     return hipGetLastError();
 }

@@ -203,7 +203,12 @@ class GatedSCCFunction(torch.autograd.Function):
 
 
 def gated_scc(x, weight, cg, co, act="silu"):
-    """Functional form: y = act(SCC(x; weight[0])) * SCC(x; weight[1]), weight [2, Cout, Cin//cg]."""
+    """Functional form: y = act(SCC(x; weight[0])) * SCC(x; weight[1]), weight [2, Cout, Cin//cg].  Plain training calls run in native code, as
+    dw_scc's do."""
+    if not (torch.compiler.is_compiling() or _transforms_active() or _tracing_state() is not None):
+        y = (_scc._native or _scc._load_native()).gated_block(x, weight, cg, co, _scc._activation(act))
+        if y is not None:
+            return y
     return GatedSCCFunction.apply(x, weight, cg, co, act)
 
 

@@ -136,7 +136,7 @@ class _NoNative:
     def forward(*args):
         return None
 
-    backward = dw_forward = dw_backward = dw_block = forward
+    backward = dw_forward = dw_backward = dw_block = gated_forward = gated_backward = gated_block = orthogonalise = orthogonal_step = forward
 
 
 def _load_native():
@@ -515,7 +515,8 @@ def _dw_backward(x, kdw, w, dy, cg, co, dw_stride, stored):
 
 
 def _activation(act):
-    code = ACTIVATIONS.get(act)
+    """The library's code of an activation's name; a code stays what it is."""
+    code = ACTIVATIONS.get(act, act if act in ACTIVATIONS.values() else None)
     if code is None:
         raise ValueError("act must be one of %s, got %r" % (", ".join(sorted(ACTIVATIONS)), act))
     return code
@@ -541,6 +542,10 @@ def scc_gated_forward(x, w, cg, co, act="silu", out=None, workspace=None):
     -> y [N,Cout,H,W] (same dtype).  A sequence of S tokens is a map of S x 1, single tokens are N maps of 1 x 1.  act: "silu" or
     "gelu" (with erf).  A workspace is allocated where the layer needs one and none is given."""
     code = _activation(act)
+    if out is None and workspace is None:
+        y = (_native or _load_native()).gated_forward(x, w, cg, co, code)
+        if y is not None:
+            return y
     dev = _dev(x, w)
     layer = _gated_layer(x, w, cg, co)
     y = x.new_empty((x.shape[0], w.shape[1], x.shape[2], x.shape[3])) if out is None else out
@@ -562,6 +567,9 @@ def scc_gated_backward(x, w, dy, cg, co, act="silu"):
 def _gated_backward(x, w, dy, cg, co, act, stored):
     """scc_gated_backward; stored: dw in the type of x, rounded from the same sums."""
     code = _activation(act)
+    grads = (_native or _load_native()).gated_backward(x, w, dy, cg, co, code, stored)
+    if grads is not None:
+        return grads
     dev = _dev(x, w, dy)
     layer = _gated_layer(x, w, cg, co)
     if dy.dtype != x.dtype or tuple(dy.shape) != (x.shape[0], w.shape[1], x.shape[2], x.shape[3]):
@@ -607,6 +615,9 @@ def _orthogonal(dev, name, lists, options, dtype):
 def scc_orthogonalise(matrices, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7):
     """The matrices with their singular values brought near 1 by `steps` Newton-Schulz steps x <- a x + (b x x^T + c (x x^T)^2) x from
     x / (||x||_F + eps): a list of [rows, cols], float32 or bfloat16 -> a list of the same."""
+    out = (_native or _load_native()).orthogonalise(matrices, steps, *coefficients, eps)
+    if out is not None:
+        return out
     dev, dtype = _matrices(matrices)
     out = [torch.empty_like(t) for t in matrices]
     _orthogonal(dev, "scc_orthogonalise", (matrices, out), _OrthogonalOptions(0, 0, 0, 0, steps, *coefficients, eps), dtype)
@@ -618,6 +629,9 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
     """One step of the orthogonalised momentum update on a list of weight matrices, in place:
     m <- momentum m + g, u = g + momentum m (nesterov) or m, w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows/cols)) O(u), O as
     scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32."""
+    native = _native or _load_native()
+    if native.orthogonal_step(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, *coefficients, eps):
+        return
     dev, dtype = _matrices(weights, grads, momenta)
     if any(m.dtype != torch.float32 for m in momenta):
         raise ValueError("momenta are float32")
