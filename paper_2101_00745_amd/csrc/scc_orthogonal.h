@@ -50,12 +50,35 @@ struct Batch {
     int count;
 };
 
+// What a workgroup of a product needs to know, one load from the workspace: the first launch writes these for the others.
+struct Block {
+    uint32_t at;            // of the matrix in the workspace, in units of 256 bytes
+    int s, l;               // tiles of the matrix
+    int bi, bj;             // the block
+    int matrix;             // in the list
+    int unused[2];
+};
+
+// A batch's workspace: the matrices' descriptions, the blocks of both kinds of products (at most a tile each), then the matrices' parts.
+struct Layout {
+    size_t half, whole, matrices;
+};
+
+inline Layout layout_of(size_t half_tiles, size_t tiles)
+{
+    Layout o;
+    o.half = (kBatch * sizeof(Matrix) + 255) / 256 * 256;
+    o.whole = o.half + (half_tiles * sizeof(Block) + 255) / 256 * 256;
+    o.matrices = o.whole + (tiles * sizeof(Block) + 255) / 256 * 256;
+    return o;
+}
+
 struct Options {
     float lr, momentum, decay, a, b, c, eps;
     int nesterov, steps;
 };
 
-// update: w is read and moved; else O(u) is written over it
+// update: w is read and moved; else O(u) is written over it.  The workspace begins with the batch's layout_of.
 template <typename T>
 hipError_t launch_orthogonal(const Batch& batch, const Options& o, bool update, char* workspace, hipStream_t st);
 

@@ -30,14 +30,29 @@ void tiles_of(int rows, int cols, int* s, int* l)
     *l = a < b ? b : a;
 }
 
-size_t workspace_of(int count, const int* rows, const int* cols)
+Layout list_layout(int count, const int* rows, const int* cols)
 {
-    size_t most = 0, now = 0;
+    size_t half = 0, tiles = 0;
     for (int i = 0; i < count; ++i) {
-        if (i % kBatch == 0) now = 0;       // batches run one after the other in the same workspace
         int s, l;
         tiles_of(rows[i], cols[i], &s, &l);
-        now += parts_of(s, l).bytes;
+        half += (size_t)s * (s + 1) / 2;
+        tiles += (size_t)s * l;
+    }
+    return layout_of(half, tiles);
+}
+
+size_t workspace_of(int count, const int* rows, const int* cols)
+{
+    size_t most = 0;
+    for (int at = 0; at < count; at += kBatch) {        // batches run one after the other in the same workspace
+        const int n = count - at < kBatch ? count - at : kBatch;
+        size_t now = list_layout(n, rows + at, cols + at).matrices;
+        for (int i = at; i < at + n; ++i) {
+            int s, l;
+            tiles_of(rows[i], cols[i], &s, &l);
+            now += parts_of(s, l).bytes;
+        }
         most = now > most ? now : most;
     }
     return most;
@@ -71,7 +86,7 @@ int run(int count, void* const* w, const void* const* g, float* const* m, const 
     for (int at = 0; at < count; at += kBatch) {
         Batch b;
         b.count = count - at < kBatch ? count - at : kBatch;
-        size_t bytes = 0;
+        size_t bytes = list_layout(b.count, rows + at, cols + at).matrices;
         for (int i = 0; i < b.count; ++i) {
             Matrix& t = b.mat[i];
             t = {g[at + i], update ? m[at + i] : nullptr, w[at + i], rows[at + i], cols[at + i], 0, 0, bytes};
