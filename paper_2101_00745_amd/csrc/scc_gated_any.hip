@@ -104,18 +104,50 @@ __global__ __launch_bounds__(256) void gated_few(const T* __restrict__ x, const 
     }
 }
 
-template <typename T>
+// 64 x 64 values through LDS, four of a row with one access where rows begin on whole groups of four.
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void transpose(const T* __restrict__ in, T* __restrict__ out, long long rows, int cols,
                                                  long long in_pitch, long long out_pitch, long long width)
 {
-    __shared__ T tile[64][65];
+    typedef T vec __attribute__((ext_vector_type(4)));
+    __shared__ T tile[64][68];
     const unsigned across = (unsigned)((cols + 63) / 64);
     const long long r0 = (long long)(blockIdx.x / across) * 64;
-    const int c0 = (int)(blockIdx.x % across) * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    for (int i = y; i < 64; i += 4) tile[i][x] = r0 + i < rows && c0 + x < cols ? in[(r0 + i) * in_pitch + c0 + x] : T(0);
+    const int c0 = (int)(blockIdx.x % across) * 64, x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
+    vec v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const long long r = r0 + y + 16 * k;
+        v[k] = vec{};
+        if (r < rows) {
+            const T* const from = in + r * in_pitch + c0 + x;
+            if (WHOLE) {
+                if (c0 + x < cols) v[k] = *(const vec*)from;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c0 + x + e < cols) v[k][e] = from[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tile[x + e][y + 16 * k] = v[k][e];
     __syncthreads();
-    for (int i = y; i < 64; i += 4)
-        if (c0 + i < cols && r0 + x < width) out[(long long)(c0 + i) * out_pitch + r0 + x] = tile[x][i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = y + 16 * k;
+        if (c0 + c >= cols) continue;
+        T* const to = out + (long long)(c0 + c) * out_pitch + r0 + x;
+        if (WHOLE) {
+            if (r0 + x < width) *(vec*)to = *(const vec*)&tile[c][x];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r0 + x + e < width) to[e] = tile[c][x + e];
+        }
+    }
 }
 
 template <typename T>
@@ -188,7 +220,11 @@ template <typename T>
 hipError_t launch_transpose(const T* in, T* out, long long rows, int cols, long long in_pitch, long long out_pitch, long long width,
                             hipStream_t st)
 {
-    transpose<T><<<dim3(blocks_of(width, 64) * blocks_of(cols, 64)), dim3(256), 0, st>>>(in, out, rows, cols, in_pitch, out_pitch, width);
+    const bool whole = cols % 4 == 0 && in_pitch % 4 == 0 && out_pitch % 4 == 0 && width % 4 == 0 &&
+                       (((uintptr_t)in | (uintptr_t)out) & (4 * sizeof(T) - 1)) == 0;
+    const dim3 grid(blocks_of(width, 64) * blocks_of(cols, 64));
+    if (whole) transpose<T, true><<<grid, dim3(256), 0, st>>>(in, out, rows, cols, in_pitch, out_pitch, width);
+    else transpose<T, false><<<grid, dim3(256), 0, st>>>(in, out, rows, cols, in_pitch, out_pitch, width);
     return hipGetLastError();
 }
 

@@ -284,11 +284,16 @@ __device__ __forceinline__ char* rows_of(const Parts& parts, char* base, int fro
     return base + (STAGE == kGram ? parts.p : STAGE == kPoly ? parts.q : parts.x[from ^ 1]);
 }
 
-// This workgroup's block: an eighth of the list in a row for each XCD, as matrix_of.
-__device__ __forceinline__ bool take_block(const Block* blocks, int count, Block& b)
+// The blocks of each XCD, in a row as matrix_of deals them, but of equal work: a block's is its K steps and a fixed part.
+struct Shares {
+    int begin[9], most;
+};
+
+// This workgroup's block; most * 8 of them are launched.
+__device__ __forceinline__ bool take_block(const Block* blocks, const Shares& shares, Block& b)
 {
-    const int each = ((int)gridDim.x + 7) / 8, i = ((int)blockIdx.x & 7) * each + ((int)blockIdx.x >> 3);
-    if (i >= count) return false;
+    const int xcd = (int)blockIdx.x & 7, i = shares.begin[xcd] + ((int)blockIdx.x >> 3);
+    if (i >= shares.begin[xcd + 1]) return false;
     b = blocks[i];
     return true;
 }
@@ -302,17 +307,17 @@ __device__ __forceinline__ bool wanted(const Block& m, int ti, int tj)
 }
 
 // One block of R x R tiles of p = x x^T (kGram) or q = b p + c p p (kPoly), on and above the diagonal and mirrored; or of a x + q x, into the other two
-// panels (kApply) or the weights (kLast).  The eight wavefronts take the K steps in turn, loads of several steps in flight each, straight
+// panels (kApply) or the weights (kLast).  The wavefronts (eight for a tile alone, four for 2 x 2) take the K steps in turn, loads of several steps in flight each, straight
 // from the panels into registers, and add up through LDS.
-constexpr int kSplit = 8;
+template <int R> constexpr int split_of = R == 1 ? 8 : 4;
 
 template <typename T, int STAGE, int R>
-__global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, int count, Options o, int from, int update, char* ws)
+__global__ __launch_bounds__(64 * split_of<R>, 2) void ns_product(const Block* blocks, Shares shares, Options o, int from, int update, char* ws)
 {
-    constexpr int kArea = kTile * kPitch, kParts = R == 1 ? kSplit : kSplit / 2;
+    constexpr int kSplit = split_of<R>, kArea = kTile * kPitch, kParts = R == 1 ? kSplit : kSplit / 2;
     __shared__ float partial[kParts][R * R][kArea];
     Block m;
-    if (!take_block(blocks, count, m)) return;      // the whole workgroup
+    if (!take_block(blocks, shares, m)) return;      // the whole workgroup
     const Parts parts = parts_of(m.s, m.l);
     char* const base = ws + (size_t)m.at * 256;
     const int bi = m.bi, bj = m.bj;
@@ -321,7 +326,7 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
     const int lane = tid & 63, f = lane & 31, h = lane >> 5;
     const int steps = 2 * F.k_tiles;
     const int rows_r = STAGE == kGram || STAGE == kPoly ? m.s : m.l;
-    f32x16 acc[R][R], low[R][R];    // the products of the pieces below the first on their own: two chains of dependent instructions
+    f32x16 acc[R][R], low[R][R];    // every other partial product on its own: two chains of dependent instructions
     const char *a0[R], *b0[R];      // tiles past the edge are the last one's again, and not stored
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -346,7 +351,7 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
 #pragma unroll
     for (int d = 0; d < kAhead; ++d)
         if (wave + d * kSplit < steps) fetch(d, wave + d * kSplit);
-    // each wavefront finishes a quad of rows of a tile (R == 2: two): rows 8 * q + 4 * h + e, column f; what they are added to is under way
+    // each wavefront finishes quads of rows of a tile: rows 8 * q + 4 * h + e, column f; what they are added to is under way
     constexpr int kQuads = R * R * 4, kRounds = (kQuads + kSplit - 1) / kSplit;
     float old[kRounds][4] = {};
 #pragma unroll
@@ -361,13 +366,13 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
             const int k = k0 + d * kSplit;
             if (k >= steps) break;
 #pragma unroll
-            for (int p = 0; p < 5; ++p)
+            for (int p = 0; p < 6; ++p)
 #pragma unroll
                 for (int i = 0; i < R; ++i)
 #pragma unroll
                     for (int j = 0; j < R; ++j) {
-                        if (p < 3) low[i][j] = mfma(a[d][i][kLeft[p]], b[d][j][kRight[p]], low[i][j]);
-                        if (p > 1) acc[i][j] = mfma(a[d][i][kLeft[p + 1]], b[d][j][kRight[p + 1]], acc[i][j]);
+                        f32x16& to = p % 2 == 0 ? low[i][j] : acc[i][j];
+                        to = mfma(a[d][i][kLeft[p]], b[d][j][kRight[p]], to);
                     }
             if (k + kAhead * kSplit < steps) fetch(d, k + kAhead * kSplit);
         }
@@ -382,7 +387,7 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
     };
     if constexpr (R == 1) {
         give(wave);
-    } else {        // wavefront w + 4 gives its sums to w
+    } else {        // the upper half of the wavefronts give their sums to the lower
         if (wave >= kParts) give(wave - kParts);
         __syncthreads();
         if (wave < kParts) {
@@ -403,9 +408,13 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int at = (8 * q + 4 * h + e) * kPitch + f;
-            v[e] = 0.f;
-#pragma unroll
-            for (int w = 0; w < kParts; ++w) v[e] += partial[w][t][at];
+            // K steps w and w + 2 first, in either shape, so that short products come out the same in both
+            if constexpr (R == 1) {
+                v[e] = ((partial[0][t][at] + partial[2][t][at]) + (partial[1][t][at] + partial[3][t][at])) +
+                       ((partial[4][t][at] + partial[6][t][at]) + (partial[5][t][at] + partial[7][t][at]));
+            } else {
+                v[e] = partial[0][t][at] + partial[1][t][at];
+            }
         }
         finish_quad<T, STAGE>(m, (const Matrix*)ws, parts, base, o, from, update, ti, tj, q, f, h, old[i], v);
         if constexpr (STAGE != kLast) {
@@ -415,10 +424,11 @@ __global__ __launch_bounds__(64 * kSplit) void ns_product(const Block* blocks, i
     }
     if constexpr (STAGE != kLast) {
         __syncthreads();
-        const int t = tid / 128;        // 128 threads a tile
-        const int ti = bi * R + t / R, tj = bj * R + t % R;
-        if (t < R * R && wanted<STAGE>(m, ti, tj) && (STAGE == kApply || ti != tj))
-            store_rows(rows_of<STAGE>(parts, base, from), ti, STAGE == kApply ? m.l : m.s, tj, partial[0][t], tid % 128);
+        for (int t = tid / 128; t < R * R; t += kSplit / 2) {       // 128 threads a tile
+            const int ti = bi * R + t / R, tj = bj * R + t % R;
+            if (wanted<STAGE>(m, ti, tj) && (STAGE == kApply || ti != tj))
+                store_rows(rows_of<STAGE>(parts, base, from), ti, STAGE == kApply ? m.l : m.s, tj, partial[0][t], tid % 128);
+        }
     }
 }
 
@@ -438,13 +448,15 @@ __device__ __forceinline__ void interleave()
 // one barrier a step; the global loads of the step behind it are in flight.
 constexpr int kBlock = 4;
 
-template <typename T, int STAGE>
-__global__ __launch_bounds__(256, 2) void ns_product_wide(const Block* blocks, int count, Options o, int from, int update, char* ws)
+// AHEAD: steps whose loads are in flight, two where two workgroups share a CU's registers, four where a launch has one for each CU at
+// most (p of six matrices of 1000 x 1024: 56 us with two, 47 with four; x, 384 workgroups: 93 and 105).
+template <typename T, int STAGE, int AHEAD>
+__global__ __launch_bounds__(256, AHEAD == 2 ? 2 : 1) void ns_product_wide(const Block* blocks, Shares shares, Options o, int from, int update, char* ws)
 {
     constexpr int kBuffer = 2 * kBlock * 3072;
     __shared__ __attribute__((aligned(16))) char lds[3 * kBuffer];
     Block m;
-    if (!take_block(blocks, count, m)) return;      // the whole workgroup
+    if (!take_block(blocks, shares, m)) return;      // the whole workgroup
     const Parts parts = parts_of(m.s, m.l);
     char* const base = ws + (size_t)m.at * 256;
     const int bi = m.bi, bj = m.bj;
@@ -462,8 +474,7 @@ __global__ __launch_bounds__(256, 2) void ns_product_wide(const Block* blocks, i
         src[i] = tile < kBlock ? step_of(F.left, r < m.s ? r : m.s - 1, F.k_tiles, 0) : step_of(F.right, r < rows_r ? r : rows_r - 1, F.k_tiles, 0);
         src[i] += lane * 16;
     }
-    constexpr int kAhead = 2;       // steps whose loads are in flight
-    u32x4 next[kAhead][6];
+    u32x4 next[AHEAD][6];
     auto fetch = [&](int set, int k) {
         k = k < steps ? k : steps - 1;
 #pragma unroll
@@ -496,22 +507,22 @@ __global__ __launch_bounds__(256, 2) void ns_product_wide(const Block* blocks, i
                 for (int j = 0; j < 2; ++j) acc[i][j] = mfma(a[set][i][kLeft[p]], b[set][j][kRight[p]], acc[i][j]);
     };
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) fetch(d, d);
+    for (int d = 0; d < AHEAD; ++d) fetch(d, d);
     park(0, 0);
-    fetch(0, kAhead);
+    fetch(0, AHEAD);
     park(1, kBuffer);
     __syncthreads();
     take(0, 0);
     int now = kBuffer;              // the buffer of the step after this one
-    for (int k0 = 0; k0 < steps; k0 += kAhead) {
+    for (int k0 = 0; k0 < steps; k0 += AHEAD) {
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) {
+        for (int d = 0; d < AHEAD; ++d) {
             const int k = k0 + d, after = now == 2 * kBuffer ? 0 : now + kBuffer;
             if (k >= steps) break;
-            fetch((d + 1) % kAhead, k + 1 + kAhead);
+            fetch((d + 1) % AHEAD, k + 1 + AHEAD);
             take(1 - d % 2, now);       // step k + 1
             multiply(d % 2);
-            park((d + 2) % kAhead, after);         // step k + 2: its buffer was last read before the last barrier
+            park((d + 2) % AHEAD, after);         // step k + 2: its buffer was last read before the last barrier
             now = after;
             // One wavefront per SIMD issues in order: 24 memory instructions in a row would hold up the matrix pipe for as long as it works.
             interleave<12, 0x100>();    // LDS reads
@@ -768,21 +779,44 @@ hipError_t launch_orthogonal(const Batch& batch, const Options& o, bool update, 
     auto choose = [&](bool half, int* side, Starts* s) {
         for (*side = kBlock;; *side /= 2) {
             const int count = starts_of(batch, s, [&](const Matrix& m) { return blocks_of(m, *side, half); });
-            if (*side == 1 || count >= (*side == kBlock ? 192 : half ? 160 : 64)) return count;
+            if (*side == 1 || count >= (*side == kBlock ? 192 : half ? 160 : 64)) return;
         }
     };
-    const int half = choose(true, &plan.half_side, &plan.half), whole = choose(false, &plan.whole_side, &plan.whole);
+    choose(true, &plan.half_side, &plan.half);
+    choose(false, &plan.whole_side, &plan.whole);
+    // work in K steps; a block's other launches' worth of latency counts as four
+    auto share = [&](const Starts& s, bool gram) {
+        auto each = [&](int i) { return (long long)(gram ? batch.mat[i].l : batch.mat[i].s) + 4; };
+        long long total = 0, done = 0;
+        for (int i = 0; i < batch.count; ++i) total += each(i) * (s.at[i + 1] - s.at[i]);
+        Shares r;
+        r.most = 0;
+        int i = 0;
+        for (int x = 0; x < 9; ++x) {
+            const long long goal = (total * x + 7) / 8;
+            while (i < batch.count && done + each(i) * (s.at[i + 1] - s.at[i]) <= goal) {
+                done += each(i) * (s.at[i + 1] - s.at[i]);
+                ++i;
+            }
+            r.begin[x] = i == batch.count ? s.at[i] : s.at[i] + (int)((goal - done + each(i) - 1) / each(i));
+            if (x > 0 && r.begin[x] - r.begin[x - 1] > r.most) r.most = r.begin[x] - r.begin[x - 1];
+        }
+        return r;
+    };
+    const Shares gram = share(plan.half, true), poly = share(plan.half, false), apply = share(plan.whole, false);
     ns_momentum<T><<<grid_of(n), dim3(256), 0, st>>>(batch, all, plan, o, ws);
     ns_normalise<T><<<grid_of(n), dim3(256), 0, st>>>(batch, all, o, ws);
     auto run = [&](auto stage, int from) {
         constexpr int STAGE = decltype(stage)::value;
         constexpr bool kHalf = STAGE == kGram || STAGE == kPoly;
-        const int up = update ? 1 : 0, side = kHalf ? plan.half_side : plan.whole_side, count = kHalf ? half : whole;
+        const int up = update ? 1 : 0, side = kHalf ? plan.half_side : plan.whole_side;
         const Block* const blocks = (const Block*)(ws + (kHalf ? plan.at.half : plan.at.whole));
-        const dim3 grid = grid_of(count);
-        if (side == kBlock) ns_product_wide<T, STAGE><<<grid, dim3(256), 0, st>>>(blocks, count, o, from, up, ws);
-        else if (side == 2) ns_product<T, STAGE, 2><<<grid, dim3(64 * kSplit), 0, st>>>(blocks, count, o, from, up, ws);
-        else ns_product<T, STAGE, 1><<<grid, dim3(64 * kSplit), 0, st>>>(blocks, count, o, from, up, ws);
+        const Shares& sh = STAGE == kGram ? gram : STAGE == kPoly ? poly : apply;
+        const dim3 grid(8u * (unsigned)sh.most);
+        if (side == kBlock && grid.x <= 256) ns_product_wide<T, STAGE, 4><<<grid, dim3(256), 0, st>>>(blocks, sh, o, from, up, ws);
+        else if (side == kBlock) ns_product_wide<T, STAGE, 2><<<grid, dim3(256), 0, st>>>(blocks, sh, o, from, up, ws);
+        else if (side == 2) ns_product<T, STAGE, 2><<<grid, dim3(64 * split_of<2>), 0, st>>>(blocks, sh, o, from, up, ws);
+        else ns_product<T, STAGE, 1><<<grid, dim3(64 * split_of<1>), 0, st>>>(blocks, sh, o, from, up, ws);
     };
     for (int i = 0; i < o.steps; ++i) {
         run(std::integral_constant<int, kGram>(), i & 1);
