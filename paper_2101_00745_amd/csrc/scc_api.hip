@@ -312,6 +312,15 @@ size_t scc_backward_workspace_bytes(int N, int Cin, int Cout, int H, int W, int 
 int scc_backward(const void* x, const void* dy, const void* w, void* dx, void* dw, int N, int Cin, int Cout, int H,
                  int W, int cg, double co, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream)
 {
+    return scc::backward(x, dy, w, dx, dw, N, Cin, Cout, H, W, cg, co, dtype, workspace, workspace_bytes, stream, nullptr);
+}
+
+}  // extern "C"
+
+int scc::backward(const void* x, const void* dy, const void* w, void* dx, void* dw, int N, int Cin, int Cout, int H, int W, int cg,
+                  double co, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream, SliceSum* later)
+{
+    if (later) *later = {(const float*)dw, Cout * (cg > 0 ? Cin / cg : 0), 1};
     if (!x || !dy || !w || !dx || !dw) return SCC_ERR_NULL;
     Problem p;
     const int rc = make_problem(N, Cin, Cout, H, W, cg, co, &p);
@@ -324,21 +333,23 @@ int scc_backward(const void* x, const void* dy, const void* w, void* dx, void* d
     const hipStream_t st = (hipStream_t)stream;
     if (path == SCC_BACKWARD_FUSED)
         return launch_status(scc::launch_backward_fused((const float*)x, (const float*)dy, (const float*)w, (float*)dx,
-                                                        (float*)dw, (float*)workspace, p, st));
+                                                        (float*)dw, (float*)workspace, p, st, later));
     if (path == SCC_BACKWARD_SHARED || path == SCC_BACKWARD_MERGED)
         return with_type(dtype, [&](auto t) {
             typedef decltype(t) T;
             return launch_status(path == SCC_BACKWARD_SHARED
                                      ? scc::launch_backward_shared((const T*)x, (const T*)dy, (const T*)w, (T*)dx, (float*)dw,
-                                                                   workspace, p, st)
+                                                                   workspace, p, st, later)
                                      : scc::launch_backward_merged((const T*)x, (const T*)dy, (const T*)w, (T*)dx, (float*)dw,
-                                                                   (float*)workspace, p, st));
+                                                                   (float*)workspace, p, st, later));
         });
     // every other layer: the two passes one after the other
     const int r1 = scc_backward_input(dy, w, dx, N, Cin, Cout, H, W, cg, co, dtype, stream);
     if (r1 != SCC_OK) return r1;
     return scc_backward_weight(x, dy, dw, N, Cin, Cout, H, W, cg, co, dtype, workspace, workspace_bytes, stream);
 }
+
+extern "C" {
 
 // Geometry of the depthwise stage; SCC_ERR_SHAPE for a stride below 1 or maps too large for 32-bit pixel indices.
 static int make_dw_geom(int C, int H, int W, int dw_stride, scc::DwGeom* g)

@@ -8,6 +8,10 @@ namespace scc {
 // Algorithm 1 in closed form (scc_api.hip).  Returns SCC_OK or the status that rejects the arguments.
 int make_problem(int N, int Cin, int Cout, int H, int W, int cg, double co, Problem* out);
 
+// scc_backward (scc_api.hip); with `later`, a sum over slices of the batch is left to the caller: *later says of what, dw itself where there is one.
+int backward(const void* x, const void* dy, const void* w, void* dx, void* dw, int N, int Cin, int Cout, int H, int W, int cg, double co,
+             scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream, SliceSum* later);
+
 inline bool dtype_ok(scc_dtype d) { return d == SCC_F32 || d == SCC_BF16; }
 
 inline int launch_status(hipError_t e) { return e == hipSuccess ? SCC_OK : SCC_ERR_LAUNCH; }

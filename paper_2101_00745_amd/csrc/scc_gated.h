@@ -21,7 +21,7 @@ constexpr int kLds = 160 << 10;         // bytes of LDS of a CU
 struct Plan {
     Band b;
     int whole;          // rows are filters in their own order
-    int rows;           // rows with a filter, or with a hole that a gradient has to be zero in
+    int rows;           // rows with a filter, or with a hole, where a gradient has to be zero
     int tiles;          // of 32 rows
     int chunks;         // of 8 channels
     int steps;          // K steps of 16 channels of the longest tile
@@ -82,45 +82,76 @@ struct Shape {
 };
 
 // false: the layer's channels do not fit LDS
-bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape* s);
+bool make_shape(const Problem& p, const Plan& t, int es, Shape* s);
 
-// The gradient's first stage: for dy, the two projections are computed again and dh = (dy u act'(g), dy act(g)) is written as the
-// output gradient of one layer of 2 * padded filters, h * n_stride + filter * k_stride + pixel.
-struct GradOut {
-    long long n_stride, k_stride;
-    int padded;         // filters of either half
-    long long columns;  // columns to write, those past the input's as zeros (HW == 1 only)
+// What comes before the product: the weights in operand layout, the table of the rows' filters and, for a gradient, what the
+// layer of both projections' filters is given (scc_gated_prepare.hip).  A sample of few pixels is a row of channels: the gradient takes
+// such layers, and those of few columns, as planes of one sample of all columns, zeros up to `width`.  One launch, from the type of the
+// tensors to that of the kernels (binary32 for bfloat16 of few columns).
+struct Planes {
+    const void* from;       // null: not wanted
+    void* to;
+    int channels;
 };
+struct Prepare {
+    const void* w;
+    char* packed;           // null: no product follows
+    void* wide;             // null, or both halves of the weights, each with rows of zeros up to `padded`
+    int padded;
+    Planes planes[2];       // x and dy
+    long long width;
+};
+template <typename From, typename To>
+hipError_t launch_prepare(const Prepare& a, const Problem& p, const Plan& t, hipStream_t st);
 
+// And what comes after: dx from planes (null: it is there), dw from partial sums over slices of the batch, without the padding's rows.
+struct Finish {
+    Planes dx;
+    long long width;
+    SliceSum sum;
+    void* dw;               // null: it is there
+    int padded;
+};
+template <typename From, typename To, typename Grad>
+hipError_t launch_finish(const Finish& a, const Problem& p, hipStream_t st);
+
+// The gradient's first stage: for dy, the two projections are computed again and dh = (dy u act'(g), dy act(g)) is written as the output gradient of
+// one layer of 2 * padded filters.
 template <typename T>
-hipError_t launch_pack(const T* w, char* ws, const Problem& p, const Plan& t, hipStream_t st);
+hipError_t launch_product(const T* x, const char* packed, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st);
 template <typename T>
-hipError_t launch_product(const T* x, const char* ws, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st);
-template <typename T>
-hipError_t launch_product_grad(const T* x, const char* ws, const T* dy, T* dh, const GradOut& o, const Problem& p, const Plan& t,
+hipError_t launch_product_grad(const T* x, const char* packed, const T* dy, T* dh, int padded, const Problem& p, const Plan& t,
                                const Shape& s, int act, hipStream_t st);
 
-// any shape (scc_gated_any.hip); dy null: y alone is written to out
+// any shape (scc_gated_any.hip); dy null: y alone is written to out; the second half of w begins w_rows filters behind the first
 template <typename T>
-hipError_t launch_any(const T* x, const T* w, const T* dy, T* out, const GradOut& o, const Problem& p, int act, hipStream_t st);
+hipError_t launch_any(const T* x, const T* w, int w_rows, const T* dy, T* out, int padded, const Problem& p, int act, hipStream_t st);
 // few columns (scc_gated_any.hip)
 bool few_preferred(const Problem& p);
 template <typename T>
 hipError_t launch_few(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st);
 
-// out[c][r] = in[r][c], r < rows; columns of out from rows to width are zeros
-template <typename T>
-hipError_t launch_transpose(const T* in, T* out, long long rows, int cols, long long in_pitch, long long out_pitch, long long width,
-                            hipStream_t st);
-// The padded filters' weights behind one another, and their gradients back; a null source or target is passed over.
-template <typename T>
-hipError_t launch_spread(const T* w, T* wide, const Problem& p, int padded, hipStream_t st);
-template <typename T>
-hipError_t launch_gather(const float* wide, T* dw, const Problem& p, int padded, hipStream_t st);
+// ---- device code that more than one kernel needs ----
 
-// three arrays at once, and one back
-hipError_t launch_widen(const bf16_t* const (&from)[3], float* const (&to)[3], const int (&count)[3], hipStream_t st);
-hipError_t launch_narrow(const float* from, bf16_t* to, int count, hipStream_t st);
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> constexpr int pieces = sizeof(T) == 2 ? 1 : 3;
+
+// 8 values as one operand piece (bfloat16) or three (binary32, cut)
+template <typename T>
+__device__ __forceinline__ void cut8(const T (&v)[8], u32x4 (&o)[pieces<T>])
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[0][e] = (uint32_t)v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
+    } else {
+        uint32_t hi[4], mid[4], lo[4];
+        split3<8>([&](int e) { return v[e]; }, hi, mid, lo);
+        o[0] = u32x4{hi[0], hi[1], hi[2], hi[3]};
+        o[1] = u32x4{mid[0], mid[1], mid[2], mid[3]};
+        o[2] = u32x4{lo[0], lo[1], lo[2], lo[3]};
+    }
+}
 
 // act(g) and act'(g), binary32; exp2 and the reciprocal are the hardware's (1 ulp).  GELU takes erfc from one exponential that its slope
 // needs anyway: erfc(x) = exp(-x^2) q(t), t = 1 / (1 + 0.47 x), x >= 0, the form of Hastings' approximations, with a polynomial q of

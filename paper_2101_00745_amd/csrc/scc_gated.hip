@@ -1,9 +1,6 @@
 // The gated layer on the matrix cores (see scc_gated.h): packed weights, a tile of columns on chip for all channels.
 //
-// pack_gated (first launch) writes, for every tile of 32 filters and K step of 16 channels, the weights of both projections in
-// the operand layout of v_mfma_f32_32x32x16_bf16 (64 lanes x 8 values, binary32 weights cut into their three bf16 pieces), zero where a channel is outside
-// a filter's window, and the table of the rows' filters.
-// gated_product (second launch): a workgroup reads its 32*CT columns of x for ALL channels once, into LDS, in the layout of the
+// A workgroup reads its 32*CT columns of x for ALL channels once, into LDS, in the layout of the
 // other operand: chunks of 8 channels of a column, 16 bytes.  After one barrier its wavefronts go their own ways: each takes a tile of filters at a
 // time, walks the tile's stretch of the channel circle with the weights coming from L2 straight into registers, and keeps g and u
 // of the same filters and columns in the same lanes, so that the activation and the product are register arithmetic and only y is written.
@@ -16,26 +13,7 @@ namespace gated {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-template <typename T> constexpr int pieces = sizeof(T) == 2 ? 1 : 3;
-
-// 8 values as one operand piece (bf16) or three (binary32, cut)
-template <typename T>
-__device__ __forceinline__ void cut8(const T (&v)[8], u32x4 (&o)[pieces<T>])
-{
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[0][e] = (uint32_t)v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
-    } else {
-        uint32_t hi[4], mid[4], lo[4];
-        split3<8>([&](int e) { return v[e]; }, hi, mid, lo);
-        o[0] = u32x4{hi[0], hi[1], hi[2], hi[3]};
-        o[1] = u32x4{mid[0], mid[1], mid[2], mid[3]};
-        o[2] = u32x4{lo[0], lo[1], lo[2], lo[3]};
-    }
-}
 
 __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, f32x16 c)
 {
@@ -57,51 +35,6 @@ __device__ __forceinline__ f32x16 product(const u32x4 (&a)[NP], const u32x4 (&b)
     return mfma(a[0], b[0], c);
 }
 
-// filter of a row: -1 past the rows; from Cout on it is a hole
-__device__ __forceinline__ int filter_of(const Plan& t, int row)
-{
-    if (row >= t.rows) return -1;
-    if (t.whole) return row;
-    const int m = row / t.b.F, i = row - m * t.b.F;
-    return (int)(((uint32_t)m * (uint32_t)t.b.inv) % (uint32_t)t.b.P) + t.b.P * i;
-}
-
-// One wavefront per (tile, K step, projection).
-template <typename T>
-__global__ __launch_bounds__(256) void pack_gated(const T* __restrict__ w, char* __restrict__ ws, Problem P, Plan t)
-{
-    const int unit = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    if (unit >= t.tiles * t.steps * 2) return;
-    const int half = unit & 1, step = unit / 2 % t.steps, tile = unit / 2 / t.steps;
-    const int lane = threadIdx.x & 63, f = lane & 31, h = lane >> 5;
-    int q0, count;
-    walk_of(P, t, tile, q0, count);
-    const int k = filter_of(t, tile * kRows + f);
-    if (step == 0 && half == 0 && h == 0) ((int*)ws)[tile * kRows + f] = k;
-
-    const int e = 2 * step + h;
-    int q = q0 + e;
-    q -= q >= t.chunks ? t.chunks : 0;
-    const bool real = (e < count) & (k >= 0) & (k < P.Cout);
-    const int s = real ? (int)((long long)k * P.stride % P.Cin) : 0;
-    const T* const row = w + (size_t)half * P.Cout * P.L + (size_t)(real ? k : 0) * P.L;
-    T v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = 8 * q + i;
-        int j = c - s;
-        j += j < 0 ? P.Cin : 0;
-        const bool in = real & (c < P.Cin) & (j < P.L);
-        const T x = row[in ? j : 0];
-        v[i] = in ? x : T(0);
-    }
-    u32x4 o[pieces<T>];
-    cut8(v, o);
-    char* const to = ws + t.a_at + (size_t)((tile * t.steps + step) * 2 + half) * pieces<T> * 1024 + lane * 16;
-#pragma unroll
-    for (int i = 0; i < pieces<T>; ++i) *(u32x4*)(to + i * 1024) = o[i];
-}
-
 template <typename T>
 struct Args {
     const T* x;
@@ -111,7 +44,7 @@ struct Args {
     Problem p;
     Plan t;
     Groups q;       // groups of V pixels
-    GradOut o;
+    int padded;     // gradient only: filters of either half of dh
     Deal deal;      // (column tile, share of the filter tiles)
     int act;
 };
@@ -124,6 +57,7 @@ template <typename T, int CT, int V, bool RAW, bool GRAD>
 __global__ __launch_bounds__(512) void gated_product(Args<T> A)
 {
     constexpr bool COLUMNS = V == 1;
+    static_assert(!(COLUMNS && GRAD), "the gradient has its columns in planes");
     typedef T lvec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     typedef T vec __attribute__((ext_vector_type(CT), aligned(sizeof(T))));
     constexpr int NP = pieces<T>;
@@ -180,16 +114,15 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
 
     // where this lane's columns of a result are: CT pixels of a group, or CT single columns
     uint32_t n[COLUMNS ? CT : 1], px[COLUMNS ? CT : 1];
-    bool live[COLUMNS ? CT : 1], real[COLUMNS ? CT : 1];
+    bool live[COLUMNS ? CT : 1];
     if constexpr (COLUMNS) {
 #pragma unroll
         for (int j = 0; j < CT; ++j) {
             const long long c = (long long)ct * kCols + CT * f + j;
-            real[j] = c < P.NQ;
-            live[j] = GRAD ? c < A.o.columns : real[j];
-            const uint32_t u = (uint32_t)(real[j] ? c : P.NQ - 1);
-            n[j] = P.HW == 1 ? (uint32_t)c : u / (uint32_t)P.HW;      // tokens past the last are written, not read
-            px[j] = P.HW == 1 ? 0u : u - n[j] * (uint32_t)P.HW;
+            live[j] = c < P.NQ;
+            const uint32_t u = (uint32_t)(live[j] ? c : P.NQ - 1);
+            n[j] = u / (uint32_t)P.HW;
+            px[j] = u - n[j] * (uint32_t)P.HW;
         }
         const int blocks = (t.chunks + 7) / 8;
         const bool whole = P.HW == 1 && P.Cin % 8 == 0 && ((uintptr_t)A.x & 15u) == 0;
@@ -220,7 +153,7 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
         const uint32_t base = (uint32_t)ct * kGroups, last = (uint32_t)(A.q.count - 1);
         {
             const uint32_t u = base + CT * f / V;
-            live[0] = real[0] = u <= last;
+            live[0] = u <= last;
             column_of_group(live[0] ? u : last, A.q, n[0], px[0]);
             px[0] += CT * f % V;
         }
@@ -248,14 +181,12 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
     }
     __syncthreads();
 
-    // a filter's plane of these columns is k * HW (of dh: k * k_stride) on from here; both fit 32 bits
+    // a filter's plane of these columns is k * HW on from here, which fits 32 bits
     T* out[COLUMNS ? CT : 1];
-    const T* grad[COLUMNS ? CT : 1];
+    const T* grad = nullptr;
 #pragma unroll
-    for (int j = 0; j < (COLUMNS ? CT : 1); ++j) {
-        grad[j] = GRAD ? A.dy + (size_t)(real[j] ? n[j] : 0) * P.Cout * P.HW + px[j] : nullptr;
-        out[j] = A.out + (GRAD ? (size_t)n[j] * A.o.n_stride : (size_t)n[j] * P.Cout * P.HW) + px[j];
-    }
+    for (int j = 0; j < (COLUMNS ? CT : 1); ++j) out[j] = A.out + (size_t)n[j] * (GRAD ? 2 * (size_t)A.padded : (size_t)P.Cout) * P.HW + px[j];
+    if constexpr (GRAD) grad = A.dy + (size_t)n[0] * P.Cout * P.HW + px[0];
     while (tile < t.tiles) {
         const int now = tile;
         f32x16 acc[2][CT];
@@ -274,12 +205,7 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
             for (int r = 0; r < 16; ++r) {
                 const int k = filters[r / 4][r % 4];
                 const uint32_t plane = (uint32_t)k < (uint32_t)P.Cout ? (uint32_t)k * (uint32_t)P.HW : 0u;
-                if constexpr (COLUMNS) {
-#pragma unroll
-                    for (int j = 0; j < CT; ++j) up[r][j] = grad[j][plane];
-                } else {
-                    up[r] = *(const vec*)(grad[0] + plane);
-                }
+                up[r] = *(const vec*)(grad + plane);
             }
         }
         for (int s0 = 0; s0 < steps; s0 += D) {
@@ -341,35 +267,18 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
                         if (there & live[0]) *(vec*)(out[0] + plane) = o;
                     }
                 } else {
-                    float dg[CT], du[CT];
+                    vec dg, du;
 #pragma unroll
                     for (int j = 0; j < CT; ++j) {
                         float v, slope;
                         activate(A.act, acc[0][j][r], v, slope);
-                        const bool zero = !there || (COLUMNS && !real[COLUMNS ? j : 0]);
                         const float d = to_f32((T)up[r][j]);
-                        dg[j] = zero ? 0.f : d * acc[1][j][r] * slope;
-                        du[j] = zero ? 0.f : d * v;
+                        dg[j] = from_f32<T>(there ? d * acc[1][j][r] * slope : 0.f);
+                        du[j] = from_f32<T>(there ? d * v : 0.f);
                     }
-                    const size_t to = (uint32_t)k * (uint32_t)A.o.k_stride, second = (uint32_t)A.o.padded * (uint32_t)A.o.k_stride;
-                    if constexpr (COLUMNS) {
-#pragma unroll
-                        for (int j = 0; j < CT; ++j) {
-                            if (!((k >= 0) & live[j])) continue;
-                            out[j][to] = from_f32<T>(dg[j]);
-                            out[j][to + second] = from_f32<T>(du[j]);
-                        }
-                    } else {
-                        vec o0, o1;
-#pragma unroll
-                        for (int j = 0; j < CT; ++j) {
-                            o0[j] = from_f32<T>(dg[j]);
-                            o1[j] = from_f32<T>(du[j]);
-                        }
-                        if ((k >= 0) & live[0]) {
-                            *(vec*)(out[0] + to) = o0;
-                            *(vec*)(out[0] + to + second) = o1;
-                        }
+                    if ((k >= 0) & live[0]) {
+                        *(vec*)(out[0] + plane) = dg;
+                        *(vec*)(out[0] + (size_t)A.padded * P.HW + plane) = du;
                     }
                 }
             }
@@ -390,11 +299,15 @@ hipError_t start(const Args<T>& a, const Shape& s, hipStream_t st)
 template <typename T, bool GRAD>
 hipError_t start_as(const Args<T>& a, const Shape& s, hipStream_t st)
 {
+    if constexpr (!GRAD) {
+        if (s.v == 1) {
+            if (s.ct == 1) return s.raw ? start<T, 1, 1, sizeof(T) == 4, false>(a, s, st) : start<T, 1, 1, false, false>(a, s, st);
+            if (s.ct == 2) return s.raw ? start<T, 2, 1, sizeof(T) == 4, false>(a, s, st) : start<T, 2, 1, false, false>(a, s, st);
+            if constexpr (sizeof(T) == 2) return start<T, 4, 1, false, false>(a, s, st);
+        }
+    }
     if constexpr (sizeof(T) == 2) {
         switch (s.v * 8 + s.ct) {
-            case 8 + 1: return start<T, 1, 1, false, GRAD>(a, s, st);
-            case 8 + 2: return start<T, 2, 1, false, GRAD>(a, s, st);
-            case 8 + 4: return start<T, 4, 1, false, GRAD>(a, s, st);
             case 32 + 1: return start<T, 1, 4, false, GRAD>(a, s, st);
             case 32 + 2: return start<T, 2, 4, false, GRAD>(a, s, st);
             case 32 + 4: return start<T, 4, 4, false, GRAD>(a, s, st);
@@ -405,10 +318,6 @@ hipError_t start_as(const Args<T>& a, const Shape& s, hipStream_t st)
         }
     } else {
         switch (s.v * 8 + s.ct * 2 + (s.raw ? 1 : 0)) {
-            case 8 + 2: return start<T, 1, 1, false, GRAD>(a, s, st);
-            case 8 + 4: return start<T, 2, 1, false, GRAD>(a, s, st);
-            case 8 + 3: return start<T, 1, 1, true, GRAD>(a, s, st);
-            case 8 + 5: return start<T, 2, 1, true, GRAD>(a, s, st);
             case 32 + 2: return start<T, 1, 4, false, GRAD>(a, s, st);
             case 32 + 4: return start<T, 2, 4, false, GRAD>(a, s, st);
             case 32 + 3: return start<T, 1, 4, true, GRAD>(a, s, st);
@@ -422,13 +331,13 @@ int lds_of(const Plan& t, int es, int ct, bool raw) { return t.chunks * (32 * ct
 
 }  // namespace
 
-bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape* s)
+bool make_shape(const Problem& p, const Plan& t, int es, Shape* s)
 {
     s->v = p.HW < 4 ? 1 : es == 2 && p.HW % 8 == 0 ? 8 : 4;
     s->waves = 8;
     if (lds_of(t, es, 1, true) > kLds) return false;
     auto tiles = [&](int c) {
-        const long long units = s->v == 1 ? stored : column_groups(p, s->v).count;
+        const long long units = s->v == 1 ? p.NQ : column_groups(p, s->v).count;
         return (units + 32 * c / s->v - 1) / (32 * c / s->v);
     };
     const int most = (t.tiles + s->waves - 1) / s->waves;
@@ -445,33 +354,24 @@ bool make_shape(const Problem& p, const Plan& t, int es, long long stored, Shape
 }
 
 template <typename T>
-hipError_t launch_pack(const T* w, char* ws, const Problem& p, const Plan& t, hipStream_t st)
-{
-    const int units = t.tiles * t.steps * 2;
-    pack_gated<T><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(w, ws, p, t);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t launch_product(const T* x, const char* ws, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st)
+hipError_t launch_product(const T* x, const char* packed, T* y, const Problem& p, const Plan& t, const Shape& s, int act, hipStream_t st)
 {
     const Groups q = s.v == 1 ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.v);
-    return start_as<T, false>(Args<T>{x, ws, nullptr, y, p, t, q, GradOut{0, 0, 0, 0}, s.deal, act}, s, st);
+    return start_as<T, false>(Args<T>{x, packed, nullptr, y, p, t, q, 0, s.deal, act}, s, st);
 }
 
 template <typename T>
-hipError_t launch_product_grad(const T* x, const char* ws, const T* dy, T* dh, const GradOut& o, const Problem& p, const Plan& t,
+hipError_t launch_product_grad(const T* x, const char* packed, const T* dy, T* dh, int padded, const Problem& p, const Plan& t,
                                const Shape& s, int act, hipStream_t st)
 {
     const Groups q = s.v == 1 ? Groups{1, 0, 1, p.NQ} : column_groups(p, s.v);
-    return start_as<T, true>(Args<T>{x, ws, dy, dh, p, t, q, o, s.deal, act}, s, st);
+    return start_as<T, true>(Args<T>{x, packed, dy, dh, p, t, q, padded, s.deal, act}, s, st);
 }
 
 #define INSTANCES(T)                                                                                                          \
-    template hipError_t launch_pack(const T*, char*, const Problem&, const Plan&, hipStream_t);                               \
     template hipError_t launch_product(const T*, const char*, T*, const Problem&, const Plan&, const Shape&, int, hipStream_t); \
-    template hipError_t launch_product_grad(const T*, const char*, const T*, T*, const GradOut&, const Problem&, const Plan&,  \
-                                            const Shape&, int, hipStream_t);
+    template hipError_t launch_product_grad(const T*, const char*, const T*, T*, int, const Problem&, const Plan&, const Shape&, \
+                                            int, hipStream_t);
 INSTANCES(float)
 INSTANCES(bf16_t)
 

@@ -18,79 +18,109 @@ int forward_path(const Problem& p, int es, Plan* plan, Shape* shape)
 {
     if (few_preferred(p)) return SCC_GATED_FEW;
     *plan = make_plan(p, es, false);
-    return make_shape(p, *plan, es, p.NQ, shape) ? SCC_GATED_PRODUCT : SCC_GATED_ANY;
+    return make_shape(p, *plan, es, shape) ? SCC_GATED_PRODUCT : SCC_GATED_ANY;
 }
 
-// The parts of the gradient's workspace.  dh, the gradient of both projections, is the output gradient of one sliding-channel layer
-// of 2 * padded filters (the second half starts on the first window again), whose gradients scc_backward takes.  Rows of single
-// tokens (HW == 1) are turned into planes of one sample for it, its kernels' layout, and dx turned back.
+// A gradient as it is computed.  dh, the gradient of both projections, is the output gradient of one sliding-channel layer of 2 * padded filters (the
+// second half starts on the first window again), whose gradients the framework's other kernels take.  They want planes of some
+// pixels and 64 columns at least: layers of less are turned into planes of one sample, filled up with zeros, and dx turned back.
+// bfloat16 layers of fewer columns than that are widened to binary32 on the way.  dg and du are then not rounded between the stages: rounded,
+// they leave 2^-9 of every product in dw, and with few columns that shows where products cancel; and such a call's time is its
+// launches', not its bytes'.
+constexpr int kFewColumns = 64;
+
 struct Parts {
+    Problem p;          // the layer in planes
+    scc_dtype type;     // of the kernels
+    bool planes, widened, product, spread, gathered;
     Plan plan;
     Shape shape;
-    bool product;       // the two projections run on the matrix cores
     int padded;
-    bool tokens, spread, gathered;
-    int N, HW;          // of the wide layer
-    size_t packed, dh, wide_w, wide_dw, planes, dplanes, rest, rest_bytes, bytes;
+    size_t packed, dh, wide_w, wide_dw, x, dy, dx, rest, rest_bytes, bytes;
 };
 
 int make_parts(const Problem& p, int cg, double co, scc_dtype dtype, scc_dtype grad, Parts* out)
 {
     Parts t;
-    const size_t es = size_of(dtype);
     const long long padded = padded_filters(p), most = std::numeric_limits<int>::max();
-    t.tokens = p.HW == 1;
-    const long long HW = t.tokens ? (p.NQ + 7) / 8 * 8 : p.HW;
-    if (2 * padded * HW > most || 2 * padded * p.L > most || HW * p.Cin > most) return SCC_ERR_SHAPE;
+    t.planes = p.HW < 4 || p.NQ < kFewColumns;
+    t.widened = dtype == SCC_BF16 && p.NQ < kFewColumns;
+    t.type = t.widened ? SCC_F32 : dtype;
+    t.p = p;
+    if (t.planes) {
+        const long long width = p.NQ < kFewColumns ? kFewColumns : (p.NQ + 7) / 8 * 8;
+        if (width > most) return SCC_ERR_SHAPE;
+        t.p.N = 1;
+        t.p.HW = (int)width;
+        t.p.NQ = width;
+    }
+    if (2 * padded * t.p.HW > most || 2 * padded * p.L > most || (long long)t.p.HW * p.Cin > most) return SCC_ERR_SHAPE;
     t.padded = (int)padded;
-    t.N = t.tokens ? 1 : p.N;
-    t.HW = (int)HW;
-    t.plan = make_plan(p, (int)es, true);
-    t.product = make_shape(p, t.plan, (int)es, t.tokens ? HW : p.NQ, &t.shape);
-    t.spread = padded != p.Cout;
-    t.gathered = t.spread || grad == SCC_BF16;
+    const size_t es = size_of(t.type), columns = (size_t)t.p.NQ;
+    t.plan = make_plan(t.p, (int)es, true);
+    t.product = make_shape(t.p, t.plan, (int)es, &t.shape);
+    t.spread = padded != p.Cout || t.widened;
+    t.gathered = padded != p.Cout || grad == SCC_BF16;
     size_t at = 0;
     auto part = [&](bool used, size_t bytes) {
         const size_t here = at;
         at += used ? align256(bytes) : 0;
         return here;
     };
-    const size_t columns = (size_t)t.N * t.HW;
     t.packed = part(t.product, t.plan.bytes);
     t.dh = part(true, columns * 2 * padded * es);
     t.wide_w = part(t.spread, (size_t)2 * padded * p.L * es);
     t.wide_dw = part(t.gathered, (size_t)2 * padded * p.L * 4);
-    t.planes = part(t.tokens, columns * p.Cin * es);
-    t.dplanes = part(t.tokens, columns * p.Cin * es);
-    t.rest_bytes = scc_backward_workspace_bytes(t.N, p.Cin, 2 * t.padded, t.HW, 1, cg, co, dtype);
+    t.x = part(t.planes, columns * p.Cin * es);
+    t.dy = part(t.planes, columns * p.Cout * es);
+    t.dx = part(t.planes, columns * p.Cin * es);
+    t.rest_bytes = scc_backward_workspace_bytes(t.p.N, p.Cin, 2 * t.padded, t.p.HW, 1, cg, co, t.type);
     t.rest = part(true, t.rest_bytes);
     t.bytes = at;
     *out = t;
     return SCC_OK;
 }
 
-// bfloat16 layers of fewer columns are widened, and their gradients are those of binary32: dg and du are then not rounded between the
-// stages.  Rounded, they leave 2^-9 of every product in dw, and with few columns that shows where products cancel.  Such a
-// call's time is its launches' (two more), not its bytes'.
-constexpr int kWidened = 64;
-
-bool widened(const Problem& p, scc_dtype dtype) { return dtype == SCC_BF16 && p.NQ < kWidened; }
-
-// The widened call's workspace: x, w, dy and dx in binary32, then what the binary32 call takes.
-struct Wide {
-    size_t w, dy, dx, rest, rest_bytes, bytes;
-};
-
-Wide wide_of(const Problem& p, size_t rest_bytes)
+// From: the tensors' type; T: the kernels'
+template <typename From, typename T>
+int run_backward(const From* x, const From* w, const From* dy, From* dx, void* dw, const Problem& p, const Parts& t, int cg, double co,
+                 int act, scc_dtype grad, char* ws, hipStream_t st)
 {
-    Wide t;
-    t.w = align256((size_t)p.NQ * p.Cin * 4);
-    t.dy = t.w + align256((size_t)2 * p.Cout * p.L * 4);
-    t.dx = t.dy + align256((size_t)p.NQ * p.Cout * 4);
-    t.rest = t.dx + t.w;
-    t.rest_bytes = rest_bytes;
-    t.bytes = t.rest + rest_bytes;
-    return t;
+    Prepare before = {};
+    before.w = w;
+    before.packed = t.product ? ws + t.packed : nullptr;
+    before.wide = t.spread ? ws + t.wide_w : nullptr;
+    before.padded = t.padded;
+    before.width = t.p.HW;
+    if (t.planes) {
+        before.planes[0] = {x, ws + t.x, p.Cin};
+        before.planes[1] = {dy, ws + t.dy, p.Cout};
+    }
+    hipError_t e = launch_prepare<From, T>(before, p, t.plan, st);
+    if (e != hipSuccess) return SCC_ERR_LAUNCH;
+    const T* const px = t.planes ? (const T*)(ws + t.x) : (const T*)x;
+    const T* const py = t.planes ? (const T*)(ws + t.dy) : (const T*)dy;
+    const T* const pw = t.spread ? (const T*)(ws + t.wide_w) : (const T*)w;
+    T* const pdx = t.planes ? (T*)(ws + t.dx) : (T*)dx;
+    T* const dh = (T*)(ws + t.dh);
+    if (t.product) {
+        e = launch_product_grad(px, ws + t.packed, py, dh, t.padded, t.p, t.plan, t.shape, act, st);
+    } else {
+        e = launch_any(px, pw, t.spread ? t.padded : p.Cout, py, dh, t.padded, t.p, act, st);
+    }
+    if (e != hipSuccess) return SCC_ERR_LAUNCH;
+    SliceSum sum;
+    float* const wide_dw = t.gathered ? (float*)(ws + t.wide_dw) : (float*)dw;
+    const int r = scc::backward(px, dh, pw, pdx, wide_dw, t.p.N, p.Cin, 2 * t.padded, t.p.HW, 1, cg, co, t.type, ws + t.rest, t.rest_bytes,
+                                st, &sum);
+    if (r != SCC_OK) return r;
+    Finish after = {};
+    after.width = t.p.HW;
+    if (t.planes) after.dx = {pdx, dx, p.Cin};
+    after.sum = sum;
+    after.dw = t.gathered || sum.slices > 1 ? dw : nullptr;
+    after.padded = t.padded;
+    return launch_status(grad == SCC_F32 ? launch_finish<T, From, float>(after, p, st) : launch_finish<T, From, bf16_t>(after, p, st));
 }
 
 }  // namespace
@@ -137,8 +167,11 @@ int scc_gated_forward(const void* x, const void* w, void* y, int N, int Cin, int
         typedef decltype(t) T;
         const T *tx = (const T*)x, *tw = (const T*)w;
         if (path == SCC_GATED_FEW) return launch_status(launch_few(tx, tw, (T*)y, p, act_of(act), st));
-        if (path == SCC_GATED_ANY) return launch_status(launch_any(tx, tw, (const T*)nullptr, (T*)y, GradOut{0, 0, 0, 0}, p, act_of(act), st));
-        const int e = launch_status(launch_pack(tw, (char*)workspace, p, plan, st));
+        if (path == SCC_GATED_ANY) return launch_status(launch_any(tx, tw, p.Cout, (const T*)nullptr, (T*)y, 0, p, act_of(act), st));
+        Prepare before = {};
+        before.w = w;
+        before.packed = (char*)workspace;
+        const int e = launch_status(launch_prepare<T, T>(before, p, plan, st));
         return e != SCC_OK ? e : launch_status(launch_product(tx, (const char*)workspace, (T*)y, p, plan, shape, act_of(act), st));
     });
 }
@@ -148,8 +181,7 @@ size_t scc_gated_backward_workspace_bytes(int N, int Cin, int Cout, int H, int W
     Problem p;
     Parts t;
     if (make_problem(N, Cin, Cout, H, W, cg, co, &p) != SCC_OK || !dtype_ok(dtype) || !dtype_ok(grad)) return 0;
-    if (make_parts(p, cg, co, widened(p, dtype) ? SCC_F32 : dtype, grad, &t) != SCC_OK) return 0;
-    return widened(p, dtype) ? wide_of(p, t.bytes).bytes : t.bytes;
+    return make_parts(p, cg, co, dtype, grad, &t) == SCC_OK ? t.bytes : 0;
 }
 
 int scc_gated_backward(const void* x, const void* w, const void* dy, void* dx, void* dw, int N, int Cin, int Cout, int H, int W, int cg,
@@ -163,59 +195,19 @@ int scc_gated_backward(const void* x, const void* w, const void* dy, void* dx, v
     if (!dtype_ok(dtype) || !dtype_ok(grad)) return SCC_ERR_DTYPE;
     if (!act_ok(act)) return SCC_ERR_OPTION;
     Parts t;
-    rc = make_parts(p, cg, co, widened(p, dtype) ? SCC_F32 : dtype, grad, &t);
+    rc = make_parts(p, cg, co, dtype, grad, &t);
     if (rc != SCC_OK) return rc;
-    const hipStream_t st = (hipStream_t)stream;
-    char* const ws = (char*)workspace;
-    if (widened(p, dtype)) {
-        const Wide v = wide_of(p, t.bytes);
-        if (!holds(v.bytes, workspace, workspace_bytes)) return SCC_ERR_WORKSPACE;
-        drop_stale_error();
-        const bf16_t* const from[3] = {(const bf16_t*)x, (const bf16_t*)w, (const bf16_t*)dy};
-        float* const to[3] = {(float*)ws, (float*)(ws + v.w), (float*)(ws + v.dy)};
-        const int counts[3] = {(int)p.NQ * p.Cin, 2 * p.Cout * p.L, (int)p.NQ * p.Cout};
-        const int r = launch_status(launch_widen(from, to, counts, st));
-        if (r != SCC_OK) return r;
-        rc = scc_gated_backward(to[0], to[1], to[2], ws + v.dx, dw, N, Cin, Cout, H, W, cg, co, act, SCC_F32, grad, ws + v.rest,
-                                v.rest_bytes, stream);
-        return rc != SCC_OK ? rc : launch_status(launch_narrow((const float*)(ws + v.dx), (bf16_t*)dx, counts[0], st));
-    }
     if (!holds(t.bytes, workspace, workspace_bytes)) return SCC_ERR_WORKSPACE;
     drop_stale_error();
-    return with_type(dtype, [&](auto v) {
-        typedef decltype(v) T;
-        const T *tx = (const T*)x, *tw = (const T*)w, *ty = (const T*)dy;
-        const long long plane = t.HW;
-        const GradOut o = {t.tokens ? 1 : 2ll * t.padded * plane, plane, t.padded, t.tokens ? plane : p.NQ};
-        hipError_t e = hipSuccess;
-        if (t.product) {
-            e = launch_pack(tw, ws + t.packed, p, t.plan, st);
-            if (e == hipSuccess)
-                e = launch_product_grad(tx, ws + t.packed, ty, (T*)(ws + t.dh), o, p, t.plan, t.shape, act_of(act), st);
-        } else {
-            e = launch_any(tx, tw, ty, (T*)(ws + t.dh), o, p, act_of(act), st);
-        }
-        const void *wide_w = w, *wide_x = x;
-        if (e == hipSuccess && t.spread) {
-            wide_w = ws + t.wide_w;
-            e = launch_spread(tw, (T*)(ws + t.wide_w), p, t.padded, st);
-        }
-        if (e == hipSuccess && t.tokens) {
-            wide_x = ws + t.planes;
-            e = launch_transpose(tx, (T*)(ws + t.planes), p.NQ, p.Cin, p.Cin, plane, plane, st);
-        }
-        if (e != hipSuccess) return (int)SCC_ERR_LAUNCH;
-        void* const wide_dx = t.tokens ? (void*)(ws + t.dplanes) : dx;
-        void* const wide_dw = t.gathered ? (void*)(ws + t.wide_dw) : dw;
-        const int r = scc_backward(wide_x, ws + t.dh, wide_w, wide_dx, wide_dw, t.N, Cin, 2 * t.padded, t.HW, 1, cg, co, dtype,
-                                   ws + t.rest, t.rest_bytes, stream);
-        if (r != SCC_OK) return r;
-        if (t.tokens) e = launch_transpose((const T*)(ws + t.dplanes), (T*)dx, p.Cin, (int)p.NQ, plane, p.Cin, p.Cin, st);
-        if (e == hipSuccess && t.gathered)
-            e = grad == SCC_F32 ? launch_gather((const float*)(ws + t.wide_dw), (float*)dw, p, t.padded, st)
-                                : launch_gather((const float*)(ws + t.wide_dw), (bf16_t*)dw, p, t.padded, st);
-        return launch_status(e);
-    });
+    const hipStream_t st = (hipStream_t)stream;
+    char* const ws = (char*)workspace;
+    auto run = [&](auto from, auto to) {
+        typedef decltype(from) From;
+        return run_backward<From, decltype(to)>((const From*)x, (const From*)w, (const From*)dy, (From*)dx, dw, p, t, cg, co, act_of(act), grad,
+                                                ws, st);
+    };
+    if (t.widened) return run(bf16_t(), float());
+    return dtype == SCC_F32 ? run(float(), float()) : run(bf16_t(), bf16_t());
 }
 
 }  // extern "C"
