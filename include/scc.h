@@ -357,17 +357,18 @@ int scc_backward_weight_static(const void* x, const void* dy, void* dw,
  * channels rotated by s_k, unless co is 0 or 1).  A sequence of S tokens is a map of S x 1 pixels, single tokens are N maps of 1 x 1.
  * x: in, N*Cin*H*W.  w: in, 2*Cout*L: the gate's weights, then the other's.  y: out, N*Cout*H*W.  g and u are binary32
  * sums (products as in scc_forward) and never reach memory; y is rounded once.  Non-finite inputs as for scc_forward.
- * Three paths (scc_gated_forward_path): up to 4 columns N*H*W a kernel that is a reading of the weights; else a product on the
- * matrix cores with the weights packed into the workspace, for layers whose channels fit on chip for 32 columns (2528 in bf16, 1240 in
- * fp32); else a plain kernel for any shape.  workspace: at least scc_gated_forward_workspace_bytes(...) bytes, 256-byte aligned,
+ * Four paths (scc_gated_forward_path): one column N*H*W is a reading of the weights; layers of up to some hundred million products take their operands
+ * straight into the matrix cores; larger ones whose channels fit on chip for 32 columns (2528 in bf16, 1240 in fp32) take weights packed
+ * into the workspace; the rest a plain kernel for any shape.  workspace: at least scc_gated_forward_workspace_bytes(...) bytes, 256-byte aligned,
  * owned by the caller, contents undefined before and after; NULL where the query returns 0 (as it does for invalid arguments).
  * Errors: as scc_forward (2*Cout*L is limited as Cout*L is there), SCC_ERR_WORKSPACE, and SCC_ERR_OPTION for an unknown activation.
  */
 typedef enum { SCC_SILU = 0, SCC_GELU = 1 } scc_activation;
 typedef enum {
     SCC_GATED_ANY = 0,      /* the kernel for any shape */
-    SCC_GATED_FEW = 1,      /* few columns */
-    SCC_GATED_PRODUCT = 2   /* matrix cores */
+    SCC_GATED_ONE = 1,      /* one column */
+    SCC_GATED_PRODUCT = 2,  /* matrix cores, packed weights */
+    SCC_GATED_DIRECT = 3    /* matrix cores, operands straight from the tensors */
 } scc_gated_paths;
 size_t scc_gated_forward_workspace_bytes(int N, int Cin, int Cout, int H, int W, int cg, double co, scc_dtype dtype);
 int scc_gated_forward_path(int N, int Cin, int Cout, int H, int W, int cg, double co, scc_dtype dtype);

@@ -12,7 +12,6 @@ namespace gated {
 enum { kSilu = 0, kGelu = 1 };
 
 constexpr int kRows = 32;               // filters of a tile: one operand of v_mfma_f32_32x32x16_bf16
-constexpr int kWaves = 4;               // wavefronts of a workgroup, a tile each at a time
 constexpr int kLds = 160 << 10;         // bytes of LDS of a CU
 
 // How the filters are cut into tiles.  Rows are filters in the order of their windows' starts (scc_band.h), so a tile's 32 windows
@@ -126,10 +125,18 @@ hipError_t launch_product_grad(const T* x, const char* packed, const T* dy, T* d
 // any shape (scc_gated_any.hip); dy null: y alone is written to out; the second half of w begins w_rows filters behind the first
 template <typename T>
 hipError_t launch_any(const T* x, const T* w, int w_rows, const T* dy, T* out, int padded, const Problem& p, int act, hipStream_t st);
-// few columns (scc_gated_any.hip)
-bool few_preferred(const Problem& p);
+// one column (scc_gated_any.hip)
+bool one_preferred(const Problem& p);
 template <typename T>
-hipError_t launch_few(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st);
+hipError_t launch_one(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st);
+
+// a batch of single tokens and the like (scc_gated_direct.hip)
+bool direct_preferred(const Problem& p, int es, bool grad);
+template <typename T>
+hipError_t launch_direct(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st);
+// width: of dh's planes, 0 where it is N samples as y is
+template <typename T, typename To>
+hipError_t launch_direct_grad(const T* x, const T* w, const T* dy, To* dh, int padded, long long width, const Problem& p, int act, hipStream_t st);
 
 // ---- device code that more than one kernel needs ----
 

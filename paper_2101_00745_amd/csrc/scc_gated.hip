@@ -62,7 +62,7 @@ __global__ __launch_bounds__(512) void gated_product(Args<T> A)
     typedef T vec __attribute__((ext_vector_type(CT), aligned(sizeof(T))));
     constexpr int NP = pieces<T>;
     constexpr int kCols = 32 * CT, kPitch = (kCols + 1) * 16;
-    constexpr int D = NP == 1 ? 4 : 2;      // K steps whose weights are in flight
+    constexpr int D = NP == 1 && !(GRAD && CT == 4) ? 4 : 2;       // K steps whose weights are in flight (four: 24 registers too many)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Problem& P = A.p;
     const Plan& t = A.t;

@@ -1,4 +1,4 @@
-// The gated layer beside the matrix cores' product: any shape, and few columns.
+// The gated layer beside the matrix cores' product: any shape, and one column.
 #include "scc_gated.h"
 
 namespace scc {
@@ -48,57 +48,37 @@ __global__ __launch_bounds__(256) void gated_any(const T* __restrict__ x, const 
     }
 }
 
-// Few columns: the weights are what has to be read.  Half a wavefront per projection of a filter, lanes along the window; the
-// columns' channels lie in LDS as binary32, the circle continued by a window so that no index wraps.
-constexpr int kFew = 4;      // columns at most
-
-template <typename T, int Q>
-__global__ __launch_bounds__(256) void gated_few(const T* __restrict__ x, const T* __restrict__ w, T* __restrict__ y, Problem P, int act)
+// One column, a single token: the weights are what has to be read.  Half a wavefront per projection of a filter, lanes along the window; the
+// column's channels lie in LDS as binary32, the circle continued by a window so that no index wraps.  512 -> 1024, cg 2, bf16, a megabyte of
+// weights: 3.2 us, of which a launch alone is 2.3; 1024 -> 1024 dense, f32 4.8 (the matrix cores' kernel for few columns 8.7).
+template <typename T>
+__global__ __launch_bounds__(256) void gated_one(const T* __restrict__ x, const T* __restrict__ w, T* __restrict__ y, Problem P, int act)
 {
-    extern __shared__ __attribute__((aligned(16))) float circle[];     // [column][Cin + L]
+    extern __shared__ __attribute__((aligned(16))) float circle[];     // Cin + L
     const int lane = threadIdx.x & 63, f = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int k = (int)blockIdx.x * 4 + wave;
-    const int width = P.Cin + P.L;
-    for (int i = threadIdx.x; i < Q * width; i += 256) {
-        const int q = i / width, e = i - q * width;
-        const int c = e >= P.Cin ? e - P.Cin : e;
-        const int n = q / P.HW, p = q - n * P.HW;
-        circle[i] = to_f32(x[((size_t)n * P.Cin + c) * P.HW + p]);
-    }
+    for (int e = threadIdx.x; e < P.Cin + P.L; e += 256) circle[e] = to_f32(x[e >= P.Cin ? e - P.Cin : e]);
     __syncthreads();
     if (k >= P.Cout) return;
     const int s = (int)((long long)k * P.stride % P.Cin);
     const T* const row = w + ((size_t)h * P.Cout + k) * P.L;
-    float sum[Q];
-#pragma unroll
-    for (int q = 0; q < Q; ++q) sum[q] = 0.f;
+    const float* const window = circle + s;
+    float sum = 0.f;
     typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     const int full = P.L & ~7;
     for (int j = 8 * f; j < full; j += 256) {
         const vec v = *(const vec*)(row + j);
 #pragma unroll
-        for (int q = 0; q < Q; ++q)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[q] = fmaf(to_f32((T)v[e]), circle[q * width + s + j + e], sum[q]);
+        for (int e = 0; e < 8; ++e) sum = fmaf(to_f32((T)v[e]), window[j + e], sum);
     }
-    if (full + f < P.L) {
-        const float v = to_f32(row[full + f]);
+    if (full + f < P.L) sum = fmaf(to_f32(row[full + f]), window[full + f], sum);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) sum[q] = fmaf(v, circle[q * width + s + full + f], sum[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum[q] += __shfl_xor(sum[q], off, 64);
-        const float u = __shfl_xor(sum[q], 32, 64);
-        float a, slope;
-        activate(act, sum[q], a, slope);
-        if (lane == 0) {
-            const int n = q / P.HW, p = q - n * P.HW;
-            y[((size_t)n * P.Cout + k) * P.HW + p] = from_f32<T>(a * u);
-        }
-    }
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    const float u = __shfl_xor(sum, 32, 64);
+    float a, slope;
+    activate(act, sum, a, slope);
+    if (lane == 0) y[k] = from_f32<T>(a * u);
 }
 
 unsigned blocks_of(long long n, int each) { return (unsigned)((n + each - 1) / each); }
@@ -115,25 +95,18 @@ hipError_t launch_any(const T* x, const T* w, int w_rows, const T* dy, T* out, i
     return hipGetLastError();
 }
 
-bool few_preferred(const Problem& p) { return p.NQ <= kFew && p.NQ * (long long)(p.Cin + p.L) * 4 <= 64 << 10; }
+bool one_preferred(const Problem& p) { return p.NQ == 1 && (p.Cin + p.L) * 4ll <= 64 << 10; }
 
 template <typename T>
-hipError_t launch_few(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st)
+hipError_t launch_one(const T* x, const T* w, T* y, const Problem& p, int act, hipStream_t st)
 {
-    const dim3 grid(blocks_of(p.Cout, 4));
-    const int lds = (int)p.NQ * (p.Cin + p.L) * 4;
-    switch (p.NQ) {
-        case 1: gated_few<T, 1><<<grid, dim3(256), lds, st>>>(x, w, y, p, act); break;
-        case 2: gated_few<T, 2><<<grid, dim3(256), lds, st>>>(x, w, y, p, act); break;
-        case 3: gated_few<T, 3><<<grid, dim3(256), lds, st>>>(x, w, y, p, act); break;
-        default: gated_few<T, 4><<<grid, dim3(256), lds, st>>>(x, w, y, p, act); break;
-    }
+    gated_one<T><<<dim3(blocks_of(p.Cout, 4)), dim3(256), (p.Cin + p.L) * 4, st>>>(x, w, y, p, act);
     return hipGetLastError();
 }
 
 #define INSTANCES(T)                                                                                        \
     template hipError_t launch_any(const T*, const T*, int, const T*, T*, int, const Problem&, int, hipStream_t); \
-    template hipError_t launch_few(const T*, const T*, T*, const Problem&, int, hipStream_t);
+    template hipError_t launch_one(const T*, const T*, T*, const Problem&, int, hipStream_t);
 INSTANCES(float)
 INSTANCES(bf16_t)
 

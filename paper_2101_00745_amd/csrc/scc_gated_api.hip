@@ -16,7 +16,8 @@ int act_of(scc_activation act) { return act == SCC_SILU ? kSilu : kGelu; }
 // SCC_GATED_*, and for the product what its launch does
 int forward_path(const Problem& p, int es, Plan* plan, Shape* shape)
 {
-    if (few_preferred(p)) return SCC_GATED_FEW;
+    if (one_preferred(p)) return SCC_GATED_ONE;
+    if (direct_preferred(p, es, false)) return SCC_GATED_DIRECT;
     *plan = make_plan(p, es, false);
     return make_shape(p, *plan, es, shape) ? SCC_GATED_PRODUCT : SCC_GATED_ANY;
 }
@@ -32,7 +33,7 @@ constexpr int kFewColumns = 64;
 struct Parts {
     Problem p;          // the layer in planes
     scc_dtype type;     // of the kernels
-    bool planes, widened, product, spread, gathered;
+    bool planes, widened, direct, product, spread, gathered;
     Plan plan;
     Shape shape;
     int padded;
@@ -58,7 +59,8 @@ int make_parts(const Problem& p, int cg, double co, scc_dtype dtype, scc_dtype g
     t.padded = (int)padded;
     const size_t es = size_of(t.type), columns = (size_t)t.p.NQ;
     t.plan = make_plan(t.p, (int)es, true);
-    t.product = make_shape(t.p, t.plan, (int)es, &t.shape);
+    t.direct = direct_preferred(p, (int)size_of(dtype), true);
+    t.product = !t.direct && make_shape(t.p, t.plan, (int)es, &t.shape);
     t.spread = padded != p.Cout || t.widened;
     t.gathered = padded != p.Cout || grad == SCC_BF16;
     size_t at = 0;
@@ -72,7 +74,7 @@ int make_parts(const Problem& p, int cg, double co, scc_dtype dtype, scc_dtype g
     t.wide_w = part(t.spread, (size_t)2 * padded * p.L * es);
     t.wide_dw = part(t.gathered, (size_t)2 * padded * p.L * 4);
     t.x = part(t.planes, columns * p.Cin * es);
-    t.dy = part(t.planes, columns * p.Cout * es);
+    t.dy = part(t.planes && !t.direct, columns * p.Cout * es);
     t.dx = part(t.planes, columns * p.Cin * es);
     t.rest_bytes = scc_backward_workspace_bytes(t.p.N, p.Cin, 2 * t.padded, t.p.HW, 1, cg, co, t.type);
     t.rest = part(true, t.rest_bytes);
@@ -92,10 +94,8 @@ int run_backward(const From* x, const From* w, const From* dy, From* dx, void* d
     before.wide = t.spread ? ws + t.wide_w : nullptr;
     before.padded = t.padded;
     before.width = t.p.HW;
-    if (t.planes) {
-        before.planes[0] = {x, ws + t.x, p.Cin};
-        before.planes[1] = {dy, ws + t.dy, p.Cout};
-    }
+    if (t.planes) before.planes[0] = {x, ws + t.x, p.Cin};
+    if (t.planes && !t.direct) before.planes[1] = {dy, ws + t.dy, p.Cout};
     hipError_t e = launch_prepare<From, T>(before, p, t.plan, st);
     if (e != hipSuccess) return SCC_ERR_LAUNCH;
     const T* const px = t.planes ? (const T*)(ws + t.x) : (const T*)x;
@@ -103,7 +103,9 @@ int run_backward(const From* x, const From* w, const From* dy, From* dx, void* d
     const T* const pw = t.spread ? (const T*)(ws + t.wide_w) : (const T*)w;
     T* const pdx = t.planes ? (T*)(ws + t.dx) : (T*)dx;
     T* const dh = (T*)(ws + t.dh);
-    if (t.product) {
+    if (t.direct) {
+        e = launch_direct_grad(x, w, dy, dh, t.padded, t.planes ? (long long)t.p.HW : 0ll, p, act, st);
+    } else if (t.product) {
         e = launch_product_grad(px, ws + t.packed, py, dh, t.padded, t.p, t.plan, t.shape, act, st);
     } else {
         e = launch_any(px, pw, t.spread ? t.padded : p.Cout, py, dh, t.padded, t.p, act, st);
@@ -166,7 +168,8 @@ int scc_gated_forward(const void* x, const void* w, void* y, int N, int Cin, int
     return with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
         const T *tx = (const T*)x, *tw = (const T*)w;
-        if (path == SCC_GATED_FEW) return launch_status(launch_few(tx, tw, (T*)y, p, act_of(act), st));
+        if (path == SCC_GATED_ONE) return launch_status(launch_one(tx, tw, (T*)y, p, act_of(act), st));
+        if (path == SCC_GATED_DIRECT) return launch_status(launch_direct(tx, tw, (T*)y, p, act_of(act), st));
         if (path == SCC_GATED_ANY) return launch_status(launch_any(tx, tw, p.Cout, (const T*)nullptr, (T*)y, 0, p, act_of(act), st));
         Prepare before = {};
         before.w = w;

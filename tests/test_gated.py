@@ -16,7 +16,7 @@ from paper_2101_00745_amd import scc as B
 
 TOL = {torch.float32: 2e-5, torch.bfloat16: 1e-2}
 DTYPES = [pytest.param(torch.float32, id="f32"), pytest.param(torch.bfloat16, id="bf16")]
-ANY, FEW, PRODUCT = 0, 1, 2
+ANY, ONE, PRODUCT, DIRECT = 0, 1, 2, 3
 
 erf = np.vectorize(math.erf)
 
@@ -60,27 +60,38 @@ def off(got, ref):
 
 # (N, Cin, Cout, H, W, cg, co), path in float32, path in bfloat16
 SHAPES = [
-    ((1, 32, 32, 8, 8, 2, 0.5), PRODUCT, PRODUCT),
-    ((3, 64, 96, 9, 7, 4, 0.5), PRODUCT, PRODUCT),          # odd planes
-    ((2, 128, 100, 7, 7, 2, 0.33), PRODUCT, PRODUCT),       # fewer filters than windows: holes
-    ((4, 30, 61, 5, 5, 2, 0.5), PRODUCT, PRODUCT),          # channels off the chunks of 8
-    ((33, 20, 13, 1, 3, 2, 0.33), PRODUCT, PRODUCT),        # three pixels: single columns
-    ((7, 24, 40, 2, 1, 1, 0.5), PRODUCT, PRODUCT),          # dense, rotated
-    ((130, 64, 96, 1, 1, 4, 0.5), PRODUCT, PRODUCT),        # tokens as rows
-    ((45, 36, 50, 1, 1, 3, 0.4), PRODUCT, PRODUCT),         # tokens of an odd width
-    ((1, 512, 64, 2, 2, 8, 0.5), FEW, FEW),                 # four columns
-    ((1, 96, 40, 3, 1, 1, 0.0), FEW, FEW),
-    ((2, 200, 70, 1, 1, 2, 0.5), FEW, FEW),
-    ((1, 7, 3, 1, 1, 7, 0.0), FEW, FEW),                    # windows of one channel
-    ((1, 1, 1, 1, 1, 1, 1.0), FEW, FEW),
-    ((9, 1, 2, 1, 1, 1, 0.0), PRODUCT, PRODUCT),
-    ((2, 768, 20, 3, 3, 2, 0.33), PRODUCT, PRODUCT),        # far fewer filters than windows
-    ((2, 16, 5, 300, 1, 1, 1.0), PRODUCT, PRODUCT),         # a sequence, every filter on the same window
-    ((40, 1024, 48, 1, 1, 2, 0.5), PRODUCT, PRODUCT),       # binary32 cut when it is read
-    ((2, 1000, 33, 5, 1, 4, 0.25), PRODUCT, PRODUCT),
-    ((2, 1304, 24, 5, 1, 4, 0.5), ANY, PRODUCT),            # channels that do not fit
-    ((6, 2592, 9, 1, 1, 8, 0.5), ANY, ANY),
-    ((64, 64, 300, 16, 16, 4, 0.5), PRODUCT, PRODUCT),      # wider tiles of columns
+    ((1, 32, 32, 8, 8, 2, 0.5), DIRECT, DIRECT),
+    ((3, 64, 96, 9, 7, 4, 0.5), DIRECT, DIRECT),            # odd planes
+    ((2, 128, 100, 7, 7, 2, 0.33), DIRECT, DIRECT),         # fewer filters than windows: holes
+    ((4, 30, 61, 5, 5, 2, 0.5), DIRECT, DIRECT),            # channels off the chunks of 8
+    ((33, 20, 13, 1, 3, 2, 0.33), DIRECT, DIRECT),          # three pixels
+    ((7, 24, 40, 2, 1, 1, 0.5), DIRECT, DIRECT),            # dense, rotated
+    ((130, 64, 96, 1, 1, 4, 0.5), DIRECT, DIRECT),          # tokens as rows
+    ((45, 36, 50, 1, 1, 3, 0.4), DIRECT, DIRECT),           # tokens of an odd width
+    ((1, 512, 64, 2, 2, 8, 0.5), DIRECT, DIRECT),           # four columns
+    ((1, 96, 40, 3, 1, 1, 0.0), DIRECT, DIRECT),
+    ((2, 200, 70, 1, 1, 2, 0.5), DIRECT, DIRECT),
+    ((1, 7, 3, 1, 1, 7, 0.0), ONE, ONE),                    # windows of one channel
+    ((1, 1, 1, 1, 1, 1, 1.0), ONE, ONE),
+    ((1, 510, 77, 1, 1, 2, 0.33), ONE, ONE),                # a token of an odd width
+    ((1, 16000, 9, 1, 1, 2, 0.5), DIRECT, DIRECT),          # ... whose channels do not fit that kernel's LDS
+    ((9, 1, 2, 1, 1, 1, 0.0), DIRECT, DIRECT),
+    ((5, 6, 17, 2, 2, 2, 0.5), DIRECT, DIRECT),             # fewer channels than a load takes
+    ((2, 768, 20, 3, 3, 2, 0.33), DIRECT, DIRECT),          # far fewer filters than windows
+    ((2, 16, 5, 300, 1, 1, 1.0), DIRECT, DIRECT),           # a sequence, every filter on the same window
+    ((40, 1024, 48, 1, 1, 2, 0.5), DIRECT, DIRECT),
+    ((2, 1000, 33, 5, 1, 4, 0.25), DIRECT, DIRECT),
+    ((6, 2592, 9, 1, 1, 8, 0.5), DIRECT, DIRECT),
+    ((64, 64, 300, 16, 16, 1, 0.5), PRODUCT, PRODUCT),
+    ((200, 128, 200, 9, 9, 2, 0.33), PRODUCT, PRODUCT),     # windows anywhere, odd planes, holes
+    ((90, 250, 141, 10, 9, 2, 0.5), PRODUCT, PRODUCT),      # channels off the chunks of 8, fewer filters than windows
+    ((120, 512, 300, 8, 5, 4, 0.5), PRODUCT, PRODUCT),       # binary32 cut when it is read
+    ((1000, 200, 400, 1, 3, 1, 0.33), PRODUCT, PRODUCT),    # three pixels: single columns
+    ((4300, 264, 264, 1, 1, 1, 0.33), DIRECT, PRODUCT),
+    ((4300, 513, 300, 1, 1, 1, 0.33), DIRECT, PRODUCT),     # tokens of an odd width
+    ((4099, 512, 520, 1, 1, 1, 0.5), PRODUCT, PRODUCT),     # tokens as rows
+    ((80, 1304, 200, 5, 5, 4, 0.5), ANY, PRODUCT),          # channels that do not fit
+    ((40, 2592, 70, 5, 5, 1, 0.5), ANY, ANY),
 ]
 IDS = ["x".join(str(v) for v in s[0]) for s in SHAPES]
 
@@ -133,7 +144,7 @@ def test_invalid_arguments_are_rejected_on_the_host(over, code):
 
 def test_null_pointers_and_workspaces_are_rejected():
     lib = S.load()
-    shape = (2, 8, 6, 3, 3, 2, 0.5)
+    shape = (200, 128, 200, 9, 9, 2, 0.33)
     need, back = lib.scc_gated_forward_workspace_bytes(*shape, 0), lib.scc_gated_backward_workspace_bytes(*shape, 0, 1)
     for i in range(3):
         ptrs = [FAKE] * 3
