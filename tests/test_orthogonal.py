@@ -242,3 +242,51 @@ def test_captured_graph_and_stream():
         other = S.scc_orthogonalise(gs)
     stream.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(other, want))
+
+
+# Lists with enough blocks of 4 x 4 tiles for a workgroup each, sides off a tile and off a block, both ways round; the second has enough
+# in its rectangular products alone.
+LARGE = [[(1000, 1024), (1024, 1000)] * 3, [(500, 520), (520, 500)] * 7]
+
+
+def iterate(g, dtype, eps=1e-7):
+    x = g.to(dtype)
+    x = x.t().contiguous() if g.shape[0] > g.shape[1] else x
+    x = x / (x.norm() + eps)
+    for _ in range(5):
+        p = x @ x.t()
+        x = A * x + (C3 * p + C5 * (p @ p)) @ x
+    return (x.t() if g.shape[0] > g.shape[1] else x).cpu()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shapes", LARGE, ids=["all", "rectangular"])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_lists(shapes, dtype):
+    """Results are rounded once from float32, whose error may not exceed that of the same iteration in plain float32 products (half as
+    much again for another order of the sums): the bar above does not tell the one from a few times as much."""
+    dev = [g.cuda() for g in matrices(shapes, dtype, seed=6)]
+    out = S.scc_orthogonalise(dev)
+    for g, o in zip(dev, out):
+        ref = iterate(g, torch.float64).numpy()
+        bar = 1.5 * off(iterate(g, torch.float32), ref) if dtype == torch.float32 else BAR[dtype]
+        assert off(o, ref) <= bar, tuple(g.shape)
+    assert all(torch.equal(a, b) for a, b in zip(out, S.scc_orthogonalise(dev)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_step_of_a_large_list(dtype):
+    gs = matrices(LARGE[0], dtype, seed=7)
+    ws = [w.cuda() for w in matrices(LARGE[0], dtype, seed=8, scale=0.05)]
+    ms = [m.cuda() for m in matrices(LARGE[0], torch.float32, seed=9)]
+    w0, m0 = [w.double() for w in ws], [m.double() for m in ms]
+    dev = [g.cuda() for g in gs]
+    S.scc_orthogonal_step(ws, dev, ms, lr=0.1, momentum=0.9, weight_decay=0.1)
+    for g, w, m, wo, mo in zip(dev, ws, ms, w0, m0):
+        momentum = 0.9 * mo + g.double()
+        assert off(m, momentum.cpu().numpy()) <= 1e-6
+        o = iterate(g.double() + 0.9 * momentum, torch.float64).cuda()
+        r, c = g.shape
+        ref = (1 - 0.1 * 0.1) * wo - 0.1 * math.sqrt(max(1.0, r / c)) * o
+        assert off(w, ref.cpu().numpy()) <= BAR[dtype]
