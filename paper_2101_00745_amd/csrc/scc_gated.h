@@ -164,7 +164,7 @@ __device__ __forceinline__ void cut8(const T (&v)[8], u32x4 (&o)[pieces<T>])
 // needs anyway: erfc(x) = exp(-x^2) q(t), t = 1 / (1 + 0.47 x), x >= 0, the form of Hastings' approximations, with a polynomial q of
 // degree 7 fitted here (least absolute error of erfc: 1.2e-8; evaluated in binary32 g Phi(g) is off by 4e-7 at most, half an ulp
 // of the larger values).  The library's erfcf is two branches of some 40 instructions, which a wavefront takes both: the dense
-// layer of 16000 columns, bf16, 60 us of which 20 were that.
+// layer of 16000 columns, bf16, 60 us of which 10 were that.
 __device__ __forceinline__ void activate(int act, float g, float& a, float& slope)
 {
     if (act == kSilu) {

@@ -5,6 +5,12 @@
 // time, walks the tile's stretch of the channel circle with the weights coming from L2 straight into registers, and keeps g and u
 // of the same filters and columns in the same lanes, so that the activation and the product are register arithmetic and only y is written.
 // x crosses the memory bus once and neither projection ever does.
+//
+// What bounds it: the memory of a large map (f32 128 x 128 -> 512 on 32x32, cg 2: 160 us, where a copy of its 335 MB takes 68 and its
+// products, six matrix instructions each, 79), the products of a dense layer (bf16 8 x 2000 tokens 512 -> 1024: 42 us after the weights, 33.5 GFLOP, 0.8 PFLOP/s of the
+// 1.3 that a large library product reaches), and in between the filling of LDS, which nothing in the workgroup overlaps
+// (f32 128 x 256 -> 256 on 16x16, cg 4: 25 us for 67 MB).  Operands straight from the tensors, with no LDS between, took 29 in place of 32 us there
+// and 182 in place of 165 on 32x32, and were not kept.
 #include "scc_gated.h"
 
 namespace scc {
@@ -331,6 +337,14 @@ int lds_of(const Plan& t, int es, int ct, bool raw) { return t.chunks * (32 * ct
 
 }  // namespace
 
+// Columns of a tile: as many as LDS holds and as leave 192 of the CUs a workgroup, if the filters are shared out too.  us forward with 32, 64 and 128:
+// f32 128 x 256 -> 256 on 16x16, cg 4 (512 tiles of 64) 35, 32, -; 128 x 128 -> 512 on 32x32, cg 2 200, 160, -; 16 x 256 -> 256 on 16x16, cg 2 (64 of 64,
+// one share) 16.2, 19.2, -; bf16 8 x 2000 tokens 512 -> 1024 dense 63, 52, 45; 32 x 512 -> 512 on 14x14, cg 8 (49 tiles of 128, two shares) 15.0, 12.3,
+// 14.7; 64 x 512 -> 1000 on 7x7, cg 2 20, 17, 21.
+// Shares of the filters among workgroups with the same columns: about one workgroup a CU.  With 1, 2, 4, 8: f32 16x16 above (one) 32, 43, 77, 93; 7x7 (four) 93,
+// 54, 36, 40; bf16 14x14 (two) 15.2, 12.4, 17.3, 21; 2000 tokens (two) 66, 46, 51, 61.
+// Binary32 stays whole where its three pieces would take more than half of LDS, a workgroup a CU: cut and whole 16x16 31.3 and 32.1, 32x32 163 and
+// 173; 7x7 (512 channels: 196 KB cut, so with 32 columns) 255 and 36.
 bool make_shape(const Problem& p, const Plan& t, int es, Shape* s)
 {
     s->v = p.HW < 4 ? 1 : es == 2 && p.HW % 8 == 0 ? 8 : 4;

@@ -1,11 +1,15 @@
 // Orthogonalised momentum update: Newton-Schulz products of a list of matrices (see scc_orthogonal.h).
 //
-// Every launch runs one stage of all matrices of the list, a workgroup per 32 x 32 tile of a result.  Products are binary32 products by the
+// Every launch runs one stage of all matrices of the list, a workgroup per block of 1, 2 x 2 or 4 x 4 tiles of 32 x 32 of a result.  Products are binary32 products by the
 // exact three-way cut of both factors (six of nine partial products on v_mfma_f32_32x32x16_bf16, see split3): rounded to bfloat16, the usual
 // form of this iteration, an error of the first steps is multiplied by up to a^steps = 484 in the directions of small singular
 // values.  All factors lie in the workspace cut and in operand layout, so that a product's loop is 1 KB loads straight into
-// registers and matrix instructions: panel [row tile][K step of 16][piece][lane][8 bf16], row tiles of 32, padding zero.  The tile's
-// four wavefronts take the K steps in turn and add up through LDS in a fixed order.
+// registers (blocks of 4 x 4 tiles: through LDS) and matrix instructions: panel [row tile][K step of 16][piece][lane][8 bf16], row tiles of 32, padding zero.
+// Wavefronts of small blocks take the K steps in turn and add up through LDS in a fixed order.
+//
+// What bounds it: three dependent launches a step and, of small lists, their latencies (256 x 64: 16 launches and 72 us; the thirteen layers
+// 64x16 to 1024x512: 243 us, p 15, q 9, x 22 us a step against 8 us of matrix work); of large ones the matrix pipes (six of 1000 x 1024:
+// 0.97 ms, 126 TFLOP/s of binary32 products where six matrix instructions each allow 218).
 #include "scc_orthogonal.h"
 
 #include <type_traits>
@@ -449,7 +453,7 @@ __device__ __forceinline__ void interleave()
 constexpr int kBlock = 4;
 
 // AHEAD: steps whose loads are in flight, two where two workgroups share a CU's registers, four where a launch has one for each CU at
-// most (p of six matrices of 1000 x 1024: 56 us with two, 47 with four; x, 384 workgroups: 93 and 105).
+// most (p of six matrices of 1000 x 1024: 56 us with two, 46 with four; x, 384 workgroups: 93 and 100).
 template <typename T, int STAGE, int AHEAD>
 __global__ __launch_bounds__(256, AHEAD == 2 ? 2 : 1) void ns_product_wide(const Block* blocks, Shares shares, Options o, int from, int update, char* ws)
 {
@@ -498,18 +502,38 @@ __global__ __launch_bounds__(256, AHEAD == 2 ? 2 : 1) void ns_product_wide(const
                 b[set][i][p] = *(const u32x4*)(lds + buffer + (kBlock + 2 * wj + i) * 3072 + p * 1024 + lane * 16);
             }
     };
-    // A step's six products add up from zero, and their sum goes to the steps' before in one rounding to nearest.  In one chain of 6 * steps matrix
-    // instructions the result of five steps was off by 5.1e-6 of its norm (six of 1000 x 1024), so 7.5e-7; plain binary32 products: 2.6e-6.
-    auto multiply = [&](int set) {
+    // One chain of 6 * steps matrix instructions loses too much: five steps of six matrices of 1000 x 1024 were off by 5.1e-6 of the result's norm,
+    // where plain binary32 products are off by 2.6e-6.  So the products below the first pieces' have sums of their own where there are registers for
+    // them (8.4e-7); else a step's six add up from zero, and their sum goes to the steps' before on the vector unit (7.5e-7), which
+    // another workgroup's matrix instructions hide (p: 46 us with the former in a workgroup a CU, 59 with the latter).
+    constexpr bool kTwo = AHEAD == 4;
+    f32x16 low[2][2];
+    if constexpr (kTwo) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            f32x16 sum[2] = {};
+        for (int i = 0; i < 4; ++i) low[i >> 1][i & 1] = f32x16{};
+    }
+    auto multiply = [&](int set) {
+        if constexpr (kTwo) {
 #pragma unroll
             for (int p = 0; p < 6; ++p)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) sum[j] = mfma(a[set][i][kLeft[p]], b[set][j][kRight[p]], sum[j]);
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] += sum[j];
+                    for (int j = 0; j < 2; ++j) {
+                        f32x16& to = p < 5 ? low[i][j] : acc[i][j];
+                        to = mfma(a[set][i][kLeft[p]], b[set][j][kRight[p]], to);
+                    }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f32x16 sum[2] = {};
+#pragma unroll
+                for (int p = 0; p < 6; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) sum[j] = mfma(a[set][i][kLeft[p]], b[set][j][kRight[p]], sum[j]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] += sum[j];
+            }
         }
     };
 #pragma unroll
@@ -536,6 +560,10 @@ __global__ __launch_bounds__(256, AHEAD == 2 ? 2 : 1) void ns_product_wide(const
             interleave<6, 0x200>();     // LDS writes
             __syncthreads();
         }
+    }
+    if constexpr (kTwo) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] += low[i >> 1][i & 1];
     }
     float* const tile = (float*)lds + wave * kTile * kPitch;       // a wavefront's own
 #pragma unroll
@@ -781,11 +809,15 @@ hipError_t launch_orthogonal(const Batch& batch, const Options& o, bool update, 
     size_t half_tiles = 0;
     for (int i = 0; i < batch.count; ++i) half_tiles += blocks_of(batch.mat[i], 1, true);
     plan.at = layout_of(half_tiles, n);
-    // tiles of a block's side
+    // Tiles of a block's side: the widest that gives enough of the CUs a workgroup, 192 of 4 x 4 tiles (they share a K step's operands among
+    // four wavefronts) or more than 128 of 2 x 2.  us of a whole update.  x, sides 1 and 2: 512 x 512 (64 blocks of side 2) 117 and 146, twice (128) 175 and
+    // 179, 704 x 768 (132) 188 and 168, 1000 x 1024 (256) 437 and 339, the thirteen layers (385) 284 and 242; sides 2 and 4: two of 1000 x 1024 (128 of
+    // side 4) 521 and 588, three (192) equal, six (384) 1028 and 994.  p and q, sides 1 and 2: the thirteen layers (106) 242 and 260, 960 x 1024 (120)
+    // equal, 1000 x 1024 (136) 340 and 287, six of 512 x 512 (216) 308 and 255; sides 2 and 4: three of 1000 x 1024 (108) 616 and 718, six (216) 1070 and 992.
     auto choose = [&](bool half, int* side, Starts* s) {
         for (*side = kBlock;; *side /= 2) {
             const int count = starts_of(batch, s, [&](const Matrix& m) { return blocks_of(m, *side, half); });
-            if (*side == 1 || count >= (*side == kBlock ? 192 : half ? 160 : 64)) return;
+            if (*side == 1 || (*side == kBlock ? count >= 192 : count > 128)) return;
         }
     };
     choose(true, &plan.half_side, &plan.half);
