@@ -50,7 +50,7 @@ struct Order {
     int whole, rows;
 };
 
-// filter of a row (from Cout on it is a hole) and its window's start; false: past the rows
+// filter of a row (from Cout on it is a hole) and its window's start; false: past the rows.  Of at most 65536 windows (direct_preferred).
 __device__ __forceinline__ bool filter_of(const Order& o, const Problem& P, int row, int& k, int& start)
 {
     if (o.whole) {
@@ -242,6 +242,7 @@ bool direct_preferred(const Problem& p, int es, bool grad)
     const double products = (double)p.NQ * ((o.rows + kFilters - 1) / kFilters * kFilters) * channels_of(p, o.b, o.whole);
     const bool whole = p.Cin % 8 == 0 && p.L % 8 == 0 && o.b.g % 8 == 0;    // loads of 8 channels
     if (p.NQ > 1 << 20) return false;                                       // grid.y
+    if (!o.whole && o.b.P > 65536) return false;                            // filter_of: m * inv is below P^2, and has 32 bits
     const double token = grad ? (es == 4 ? 2e8 : whole ? 1.5e8 : 5e7) : es == 4 ? 1e9 : whole ? 5e8 : 2.5e8;
     const double map = grad || es == 2 ? 1e8 : 2e8;
     return products <= (p.HW > 1 ? map : token);
