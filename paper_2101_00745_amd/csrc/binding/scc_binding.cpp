@@ -579,6 +579,13 @@ PyObject* orthogonalise(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// Tells autograd that a tensor has other values now, so that a graph which saved it is not run on them.
+void moved(const std::vector<const at::Tensor*>& ts)
+{
+    for (const at::Tensor* t : ts)
+        if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // (weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> True, or None
 PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -608,6 +615,8 @@ PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
                                    l.ws.data_ptr(), l.need, st);
     });
     if (rc != SCC_OK) Py_RETURN_NONE;
+    moved(w);
+    moved(m);
     Py_RETURN_TRUE;
     END_HANDLE_TH_ERRORS
 }

@@ -225,6 +225,11 @@ def _workspace_need(query, *shape):
     return int(getattr(load(), query)(*shape))
 
 
+def _moved(*tensors):
+    """Tells autograd that tensors of the caller's have other values now, so that a graph which saved one is not run on them."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _scratch(need, dev, workspace=None):
     """(tensor to keep alive until the call has been enqueued, its address, its size); nothing where nothing is needed."""
     if workspace is None:
@@ -628,7 +633,8 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
                         eps=1e-7):
     """One step of the orthogonalised momentum update on a list of weight matrices, in place:
     m <- momentum m + g, u = g + momentum m (nesterov) or m, w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows/cols)) O(u), O as
-    scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32."""
+    scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32.  A graph that saved a weight cannot be
+    run backward afterwards, as after any change in place."""
     native = _native or _load_native()
     if native.orthogonal_step(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, *coefficients, eps):
         return
@@ -637,3 +643,4 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
         raise ValueError("momenta are float32")
     options = _OrthogonalOptions(lr, momentum, weight_decay, int(bool(nesterov)), steps, *coefficients, eps)
     _orthogonal(dev, "scc_orthogonal_step", (weights, grads, momenta), options, dtype)
+    _moved(*weights, *momenta)
