@@ -226,8 +226,11 @@ def _workspace_need(query, *shape):
 
 
 def _moved(*tensors):
-    """Tells autograd that tensors of the caller's have other values now, so that a graph which saved one is not run on them."""
-    torch.autograd.graph.increment_version(tensors)
+    """Tells autograd that tensors of the caller's (None: none given) have other values now, so that a graph which saved one is not run on
+    them."""
+    tensors = [t for t in tensors if t is not None]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
 
 
 def _scratch(need, dev, workspace=None):
@@ -265,6 +268,7 @@ def scc_forward(x, w, cg, co, out=None, workspace=None):
     need = _workspace_need("scc_forward_workspace_bytes", *shape) if workspace is None and out is None else 0
     ws, ws_ptr, ws_len = _scratch(need, dev, workspace)
     _launch(dev, load().scc_forward_ws, x.data_ptr(), w.data_ptr(), y.data_ptr(), *shape, ws_ptr, ws_len)
+    _moved(out)
     return y
 
 
@@ -288,6 +292,7 @@ def scc_backward_input(dy, w, Cin, cg, co, out=None, workspace=None):
     need = _workspace_need("scc_backward_input_workspace_bytes", *shape) if workspace is None and out is None else 0
     ws, ws_ptr, ws_len = _scratch(need, dev, workspace)
     _launch(dev, load().scc_backward_input_ws, dy.data_ptr(), w.data_ptr(), dx.data_ptr(), *shape, ws_ptr, ws_len)
+    _moved(out)
     return dx
 
 
@@ -315,6 +320,7 @@ def scc_backward_weight(x, dy, cg, co, out=None, workspace=None):
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _launch(dev, load().scc_backward_weight, x.data_ptr(), dy.data_ptr(), dw.data_ptr(), *shape, ws_ptr, ws_len)
+    _moved(out)
     return dw
 
 
@@ -331,6 +337,7 @@ def scc_backward_weight_static(x, dy, cg, co, out):
         raise ValueError("out must be float32 [Cout, Cin//cg]")
     _launch(dev, load().scc_backward_weight_static, x.data_ptr(), dy.data_ptr(), out.data_ptr(), N, Cin, Cout, H, W, cg,
             float(co), _dtype_code(x))
+    _moved(out)
     return out
 
 
@@ -368,6 +375,7 @@ def scc_backward(x, dy, w, cg, co, out_dx=None, out_dw=None, workspace=None):
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _launch(dev, load().scc_backward, x.data_ptr(), dy.data_ptr(), w.data_ptr(), dx.data_ptr(), dw.data_ptr(), *shape,
             ws_ptr, ws_len)
+    _moved(out_dx, out_dw)
     return dx, dw
 
 
@@ -397,6 +405,7 @@ def scc_depthwise3x3_forward(x, kdw, dw_stride=1, out=None):
         assert out.shape == (N, C, Ho, Wo) and out.dtype == x.dtype
     _launch(dev, load().scc_depthwise3x3_forward, x.data_ptr(), kdw.data_ptr(), z.data_ptr(), N, C, H, W, dw_stride,
             _dtype_code(x))
+    _moved(out)
     return z
 
 
@@ -429,6 +438,7 @@ def scc_depthwise3x3_backward(x, kdw, dz, dw_stride=1, need_dx=True, need_dk=Tru
     _launch(dev, load().scc_depthwise3x3_backward, x.data_ptr(), kdw.data_ptr(), dz.data_ptr(),
             dx.data_ptr() if dx is not None else None, dk.data_ptr() if dk is not None else None, N, C, H, W, dw_stride,
             code, ws_ptr, ws_len)
+    _moved(out_dx if need_dx else None, out_dk if need_dk else None)
     return dx, dk
 
 
@@ -483,6 +493,7 @@ def scc_dw_forward(x, kdw, w, cg, co, dw_stride=1, out=None, workspace=None, fus
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _launch(dev, call, x.data_ptr(), kdw.data_ptr(), w.data_ptr(), y.data_ptr(), *shape, ws_ptr, ws_len)
+    _moved(out)
     return y
 
 
@@ -561,6 +572,7 @@ def scc_gated_forward(x, w, cg, co, act="silu", out=None, workspace=None):
     dtype = _dtype_code(x)
     ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_gated_forward_workspace_bytes", *layer, dtype), dev, workspace)
     _launch(dev, load().scc_gated_forward, x.data_ptr(), w.data_ptr(), y.data_ptr(), *layer, code, dtype, ws_ptr, ws_len)
+    _moved(out)
     return y
 
 
