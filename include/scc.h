@@ -404,7 +404,8 @@ int scc_gated_backward(const void* x, const void* w, const void* dy, void* dx, v
  * workspace: at least scc_orthogonal_workspace_bytes(...) bytes (about 36 bytes an element), 256-byte aligned, owned by the caller, contents
  * undefined before and after.
  * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count, rows or cols < 1, or a matrix of over 2^31/40 elements), SCC_ERR_DTYPE, SCC_ERR_OPTION
- * (steps outside 1 .. 100, a value that is not finite, eps < 0), SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH.
+ * (steps outside 1 .. 100, a value that is not finite, eps < 0), SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH (some of the list's weights and momenta
+ * may have moved, so the call is not to be made again; every other error leaves them as they were).
  */
 typedef struct {
     float lr, momentum, weight_decay;   /* scc_orthogonalise reads none of these three ... */

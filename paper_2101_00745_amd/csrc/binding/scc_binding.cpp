@@ -5,8 +5,8 @@
 // batch 128 925 -> 709 (then bound by its kernels), its forward at batch 16 145 -> 114, one 8x8 image forward and backward 18.6 -> 11.6.
 // Each function here serves the call that a program makes all day (dense,
 // contiguous tensors of the right shapes on the current device, no `out`, no workspace, no modes) and returns None for
-// everything else, errors included: scc.py then goes its general way, which raises what there is to raise.  Nothing is kept
-// from one call to the next.
+// everything else, errors included: scc.py then goes its general way, which raises what there is to raise (orthogonal_step, which moves
+// its arguments, answers a failed call's status instead).  Nothing is kept from one call to the next.
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
@@ -586,7 +586,9 @@ void moved(const std::vector<const at::Tensor*>& ts)
         if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
 }
 
-// (weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> True, or None
+// (weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> the library's status, or None where the call is not
+// plain.  It moves the caller's tensors, some of a list's even where a later launch fails, so a call that was made is not for scc.py to
+// make again.
 PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
@@ -614,10 +616,11 @@ PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         return scc_orthogonal_step((int)count, l.address.data(), from.data(), momenta.data(), l.rows.data(), l.cols.data(), &o, dtype,
                                    l.ws.data_ptr(), l.need, st);
     });
-    if (rc != SCC_OK) Py_RETURN_NONE;
-    moved(w);
-    moved(m);
-    Py_RETURN_TRUE;
+    if (rc == SCC_OK || rc == SCC_ERR_LAUNCH) {
+        moved(w);
+        moved(m);
+    }
+    return PyLong_FromLong(rc);
     END_HANDLE_TH_ERRORS
 }
 
@@ -630,7 +633,7 @@ PyMethodDef methods[] = {METHOD(forward, "(x, w, cg, co) -> y or None"), METHOD(
                          METHOD(gated_backward, "(x, w, dy, cg, co, act, stored) -> (dx, dw) or None"),
                          METHOD(gated_block, "(x, w, cg, co, act) -> y under autograd, or None"),
                          METHOD(orthogonalise, "(matrices, steps, a, b, c, eps) -> list or None"),
-                         METHOD(orthogonal_step, "(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> True or None"),
+                         METHOD(orthogonal_step, "(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> status or None"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

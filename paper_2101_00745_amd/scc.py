@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libscc_hip.so")
 
 SCC_F32, SCC_BF16 = 0, 1
+SCC_ERR_LAUNCH = -6
 SYMBOLS = ("scc_window_params", "scc_forward", "scc_forward_workspace_bytes", "scc_forward_ws", "scc_backward_input",
            "scc_backward_input_workspace_bytes", "scc_backward_input_ws",
            "scc_backward_weight_workspace_bytes", "scc_backward_weight", "scc_backward_weight_static",
@@ -140,7 +141,8 @@ class _NoNative:
 
 
 def _load_native():
-    """The plain calls: each answers None where a call is not plain (or fails), and the general way below it then goes on.  Where
+    """The plain calls: each answers None where a call is not plain (or fails, if it only reads its arguments), and the general way below
+    it then goes on.  Where
     the module is not built, or not for this torch, every call takes that way: the same kernels, some microseconds more of host time."""
     global _native
     load()
@@ -648,11 +650,17 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
     scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32.  A graph that saved a weight cannot be
     run backward afterwards, as after any change in place."""
     native = _native or _load_native()
-    if native.orthogonal_step(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, *coefficients, eps):
-        return
+    status = native.orthogonal_step(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, *coefficients, eps)
+    if status is not None:                      # made, if it failed too: once more would move a part of the list twice
+        return _check(status)
     dev, dtype = _matrices(weights, grads, momenta)
     if any(m.dtype != torch.float32 for m in momenta):
         raise ValueError("momenta are float32")
     options = _OrthogonalOptions(lr, momentum, weight_decay, int(bool(nesterov)), steps, *coefficients, eps)
-    _orthogonal(dev, "scc_orthogonal_step", (weights, grads, momenta), options, dtype)
+    try:
+        _orthogonal(dev, "scc_orthogonal_step", (weights, grads, momenta), options, dtype)
+    except SccError as e:
+        if e.status == SCC_ERR_LAUNCH:          # in the middle of a list, perhaps
+            _moved(*weights, *momenta)
+        raise
     _moved(*weights, *momenta)

@@ -1,4 +1,4 @@
-"""Calls that write tensors of the caller's tell autograd so."""
+"""Calls that write tensors of the caller's tell autograd so, and one that fails is not made again."""
 
 import pytest
 import torch
@@ -83,3 +83,63 @@ def test_an_out_tensor_is_written_in_place():
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             kept.backward()
     assert [t._version for t in (x, dy, w, kdw, gated)] == read
+
+
+class Recorder:
+    """In the native module's place: one call answers what it is told to."""
+
+    def __init__(self, answer):
+        self.answer, self.calls = answer, 0
+
+    def orthogonal_step(self, *args):
+        self.calls += 1
+        return self.answer
+
+
+def test_a_step_that_failed_is_not_made_again(monkeypatch):
+    """A list of more matrices than a launch takes may have moved in part; the general way would move that part once more."""
+    def again(*args):
+        raise AssertionError("the call was made a second time")
+
+    monkeypatch.setattr(B, "_orthogonal", again)
+    m = torch.zeros(4, 4)
+    for status in (-6, -8):
+        native = Recorder(status)
+        monkeypatch.setattr(B, "_native", native)
+        with pytest.raises(B.SccError) as e:
+            S.scc_orthogonal_step([m], [m], [m], lr=0.1)
+        assert e.value.status == status and native.calls == 1
+    monkeypatch.setattr(B, "_native", Recorder(0))
+    S.scc_orthogonal_step([m], [m], [m], lr=0.1)
+
+
+@pytest.mark.gpu
+def test_the_native_step_answers_its_status(monkeypatch):
+    def again(*args):
+        raise AssertionError("the call was made a second time")
+
+    w, g, m = (torch.ones(4, 6, device="cuda") for _ in range(3))
+    with monkeypatch.context() as patch:
+        patch.setattr(B, "_orthogonal", again)
+        with pytest.raises(B.SccError) as e:
+            S.scc_orthogonal_step([w], [g], [m], lr=0.1, steps=101)
+        assert e.value.status == -8
+        S.scc_orthogonal_step([w], [g], [m], lr=0.1)
+    with pytest.raises(ValueError):             # not a plain call: the general way says what is wrong with it
+        S.scc_orthogonal_step([w.t()], [g.t()], [m.t()], lr=0.1)
+
+
+@pytest.mark.gpu
+def test_the_general_way_raises_versions_where_something_may_have_moved(monkeypatch):
+    monkeypatch.setattr(B, "_native", B._NoNative)
+    w, g, m = (torch.ones(4, 6, device="cuda") for _ in range(3))
+    for status, raised in ((-6, 1), (-8, 0)):
+        def fail(*args):
+            raise B.SccError(status, "")
+
+        with monkeypatch.context() as patch:
+            patch.setattr(B, "_orthogonal", fail)
+            before = [t._version for t in (w, g, m)]
+            with pytest.raises(B.SccError):
+                S.scc_orthogonal_step([w], [g], [m], lr=0.1)
+        assert [t._version - b for t, b in zip((w, g, m), before)] == [raised, 0, raised]
