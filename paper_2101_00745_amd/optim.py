@@ -7,17 +7,22 @@ from . import scc as _scc
 class OrthogonalMomentum(torch.optim.Optimizer):
     """m <- momentum m + g; w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows/cols)) O(g + momentum m), O five Newton-Schulz steps, which bring
     the singular values near 1 (``scc_orthogonal_step``).  Takes weights of two dimensions, or of three as a stack of matrices (the
-    gate's and the other's of a ``GatedSCC``); everything else (biases, depthwise filters) belongs to another optimiser.  All matrices
+    gate's and the other's of a ``GatedSCC``); everything else (biases, depthwise filters) is refused and belongs to another optimiser.  All matrices
     of a group and dtype are updated by one call; the momenta are float32."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5):
         if lr < 0.0 or not 0.0 <= momentum < 1.0 or weight_decay < 0.0 or steps < 1:
             raise ValueError("lr and weight_decay must not be negative, momentum must lie in [0, 1), steps must be at least 1")
         super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, steps=steps))
-        for group in self.param_groups:
-            for p in group["params"]:
-                if p.dim() not in (2, 3):
-                    raise ValueError("weights must be matrices or stacks of matrices, got %s" % (tuple(p.shape),))
+
+    def add_param_group(self, param_group):
+        """Groups of the constructor come through here as well.  A stack of 3 x 3 matrices has the shape of depthwise filters, [C, 3, 3], and is
+        taken for those."""
+        super().add_param_group(param_group)
+        for p in self.param_groups[-1]["params"]:
+            if p.dim() not in (2, 3) or (p.dim() == 3 and tuple(p.shape[1:]) == (3, 3)):
+                self.param_groups.pop()
+                raise ValueError("weights must be matrices or stacks of matrices, and no depthwise filters [C, 3, 3]; got %s" % (tuple(p.shape),))
 
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
