@@ -190,6 +190,9 @@ __global__ __launch_bounds__(256) void ns_momentum(Batch B, Starts S, Plan plan,
     if (threadIdx.x == 0) ((double*)(ws + m.at + parts_of(m.s, m.l).sums))[block] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// u / (||u|| + eps), 0 where that is 0 / 0 (only u = 0 has a norm of 0; a NaN stays one)
+__device__ __forceinline__ float normalised(float u, float norm) { return norm == 0.f ? 0.f : u / norm; }
+
 // x = u / (||u|| + eps) into both panels
 template <typename T>
 __global__ __launch_bounds__(256) void ns_normalise(Batch B, Starts S, Options o, char* ws)
@@ -218,7 +221,7 @@ __global__ __launch_bounds__(256) void ns_normalise(Batch B, Starts S, Options o
         float v = 0.f;
         if (inside(m, i, j)) {
             const size_t at = place(m, i, j);
-            v = update_of<T>(m, o, at, m.m ? m.m[at] : 0.f) / norm;
+            v = normalised(update_of<T>(m, o, at, m.m ? m.m[at] : 0.f), norm);
         }
         tile[ii * kPitch + jj] = v;
     }
@@ -726,7 +729,7 @@ __global__ __launch_bounds__(64 * kAlone) void ns_alone(Batch B, Options o, int 
     const float norm = (float)sqrt(sum) + o.eps;
     for (int e = tid; e < s * kTile * l * kTile; e += 64 * kAlone) {
         const int i = e / (l * kTile), j = e - i * (l * kTile);
-        x[i * xp + j] /= norm;
+        x[i * xp + j] = normalised(x[i * xp + j], norm);
     }
     __syncthreads();
 
