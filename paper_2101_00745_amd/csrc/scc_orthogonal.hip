@@ -190,8 +190,21 @@ __global__ __launch_bounds__(256) void ns_momentum(Batch B, Starts S, Plan plan,
     if (threadIdx.x == 0) ((double*)(ws + m.at + parts_of(m.s, m.l).sums))[block] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// ||u|| + eps in binary32, times a power of two that u is to be multiplied by as well: binary32 values have norms that it does not hold, or holds
+// with a few bits only.
+struct Norm {
+    float by, value;
+};
+
+__device__ __forceinline__ Norm norm_of(double squares, float eps)
+{
+    const double root = sqrt(squares);
+    const float by = root > 0x1p120 ? 0x1p-64f : root < 0x1p-100 ? 0x1p64f : 1.f;
+    return {by, (float)(root * by) + eps * by};
+}
+
 // u / (||u|| + eps), 0 where that is 0 / 0 (only u = 0 has a norm of 0; a NaN stays one)
-__device__ __forceinline__ float normalised(float u, float norm) { return norm == 0.f ? 0.f : u / norm; }
+__device__ __forceinline__ float normalised(float u, const Norm& n) { return n.value == 0.f ? 0.f : u * n.by / n.value; }
 
 // x = u / (||u|| + eps) into both panels
 template <typename T>
@@ -211,7 +224,7 @@ __global__ __launch_bounds__(256) void ns_normalise(Batch B, Starts S, Options o
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
     if ((tid & 63) == 0) part[tid >> 6] = sum;
     __syncthreads();
-    const float norm = (float)sqrt((part[0] + part[1]) + (part[2] + part[3])) + o.eps;
+    const Norm norm = norm_of((part[0] + part[1]) + (part[2] + part[3]), o.eps);
     const int ti = block / m.l, tj = block - ti * m.l;
     const bool flip = m.rows > m.cols;
     const int x = tid & 31, y = tid >> 5;
@@ -726,7 +739,7 @@ __global__ __launch_bounds__(64 * kAlone) void ns_alone(Batch B, Options o, int 
     __syncthreads();
     sum = 0;
     for (int i = 0; i < kAlone; ++i) sum += sums[i];
-    const float norm = (float)sqrt(sum) + o.eps;
+    const Norm norm = norm_of(sum, o.eps);
     for (int e = tid; e < s * kTile * l * kTile; e += 64 * kAlone) {
         const int i = e / (l * kTile), j = e - i * (l * kTile);
         x[i * xp + j] = normalised(x[i * xp + j], norm);

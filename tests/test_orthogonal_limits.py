@@ -26,3 +26,15 @@ def test_zero_matrices_without_eps(shapes, dtype):
     ms = [torch.zeros(s, device="cuda") for s in shapes]
     S.scc_orthogonal_step(ws, [g.cuda() for g in gs], ms, lr=0.5, eps=0.0)
     assert torch.equal(ws[0], before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", ["least", 1e-38, 1e36, 1e37])
+@pytest.mark.parametrize("shapes", [SMALL, STAGED], ids=["small", "staged"])
+def test_norms_outside_float32(shapes, scale, dtype):
+    """Every value is a number of the type; the norm is beyond its largest, or so small that too few bits of it are left."""
+    scale = {torch.float32: 3e-43, torch.bfloat16: 3e-39}[dtype] if scale == "least" else scale       # multiples of the least value
+    gs = [torch.from_numpy(g.double().numpy() * scale).to(dtype) for g in matrices(shapes, torch.float32, seed=22, scale=1.0)]
+    for g, o in zip(gs, S.scc_orthogonalise([g.cuda() for g in gs], eps=0.0)):
+        assert torch.isfinite(g).all() and off(o, polynomial(g.double().numpy(), eps=0.0)) <= BAR[dtype], tuple(g.shape)
