@@ -358,7 +358,7 @@ int scc_backward_weight_static(const void* x, const void* dy, void* dw,
  * x: in, N*Cin*H*W.  w: in, 2*Cout*L: the gate's weights, then the other's.  y: out, N*Cout*H*W.  g and u are binary32
  * sums (products as in scc_forward) and never reach memory; y is rounded once.  Non-finite inputs as for scc_forward.
  * Four paths (scc_gated_forward_path): one column N*H*W is a reading of the weights; layers of up to some hundred million products take their operands
- * straight into the matrix cores; larger ones whose channels fit on chip for 32 columns (2528 in bf16, 1240 in fp32) take weights packed
+ * straight into the matrix cores; larger ones whose channels fit on chip for 32 columns (2480 in bf16, 1240 in fp32) take weights packed
  * into the workspace; the rest a plain kernel for any shape.  workspace: at least scc_gated_forward_workspace_bytes(...) bytes, 256-byte aligned,
  * owned by the caller, contents undefined before and after; NULL where the query returns 0 (as it does for invalid arguments).
  * Errors: as scc_forward (2*Cout*L is limited as Cout*L is there), SCC_ERR_WORKSPACE, and SCC_ERR_OPTION for an unknown activation.

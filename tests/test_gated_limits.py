@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2101_00745_amd as S
-from tests.test_gated import ANY, DIRECT, DTYPES, TOL, inputs, off, reference
+from tests.test_gated import ANY, DIRECT, DTYPES, PRODUCT, TOL, inputs, off, reference
 
 # (N, Cin, Cout, H, W, cg, co) with Cin / gcd(stride, Cin) windows, more than 65536: index times inverse leaves 32 bits
 MANY_WINDOWS = [(1, 90000, 64, 1, 1, 2000, 0.5), (3, 90000, 70, 1, 1, 2000, 0.5), (2, 131074, 40, 2, 1, 65537, 0.5), (5, 70000, 33, 1, 1, 7000, 0.1)]
@@ -58,3 +58,26 @@ def test_layers_of_many_windows(shape, dtype):
     assert off(S.scc_gated_forward(x.cuda(), w.cuda(), cg, co), y) <= TOL[dtype]
     got = S.scc_gated_backward(x.cuda(), w.cuda(), dy.cuda(), cg, co)
     assert off(got[0], dx) <= TOL[dtype] and off(got[1], dw) <= TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype,most", [(0, 1240), (1, 2480)])
+def test_most_channels_of_the_packed_product(dtype, most):
+    """32 columns of all channels in 160 KB: chunks of 8 channels, 33 columns of 16 bytes each, binary32 whole as two."""
+    assert most == 8 * ((160 << 10) // (33 * (32, 16)[dtype]))
+    lib = S.load()
+    for channels, path in ((most, PRODUCT), (most + 8, ANY)):
+        assert lib.scc_gated_forward_path(200, channels, 512, 8, 8, 1, 0.5, dtype) == path
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,most", [pytest.param(torch.float32, 1240, id="f32"), pytest.param(torch.bfloat16, 2480, id="bf16")])
+def test_layers_on_both_sides_of_the_packed_product(dtype, most):
+    for channels in (most, most + 8):
+        shape = (120, channels, 100, 5, 5, 1, 0.5)
+        path = S.load().scc_gated_forward_path(*shape, int(dtype == torch.bfloat16))
+        assert path == (PRODUCT if channels == most else ANY)
+        (x, w, dy), wide = inputs(shape, dtype, seed=12)
+        y, dx, dw = reference(wide[0], wide[1], 1, 0.5, "gelu", wide[2])
+        assert off(S.scc_gated_forward(x.cuda(), w.cuda(), 1, 0.5, act="gelu"), y) <= TOL[dtype]
+        got = S.scc_gated_backward(x.cuda(), w.cuda(), dy.cuda(), 1, 0.5, act="gelu")
+        assert off(got[0], dx) <= TOL[dtype] and off(got[1], dw) <= TOL[dtype]
