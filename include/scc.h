@@ -400,7 +400,8 @@ int scc_gated_backward(const void* x, const void* w, const void* dy, void* dx, v
  * O(0) = 0; a matrix with a NaN or an infinity comes out as NaN and leaves the others alone.  All products are to binary32 accuracy (split
  * factors, as in scc_forward), sums binary32, the norm's binary64, in a fixed order: two calls give bitwise identical results.
  * g, w and o have the type `dtype`, m is binary32.  The arrays of pointers and sizes are HOST arrays, read before the call
- * returns; the matrices are device memory, and no two of one list may overlap.  scc_orthogonalise may write o over g.
+ * returns; the matrices are device memory.  No w, m or o may overlap another matrix of the call, which is not checked here; only an o may be
+ * its own g.
  * workspace: at least scc_orthogonal_workspace_bytes(...) bytes (about 36 bytes an element), 256-byte aligned, owned by the caller, contents
  * undefined before and after.
  * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count, rows or cols < 1, or a matrix of over 2^31/40 elements), SCC_ERR_DTYPE, SCC_ERR_OPTION

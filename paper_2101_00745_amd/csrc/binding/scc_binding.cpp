@@ -20,6 +20,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <climits>
 
 #include "scc.h"
@@ -579,6 +580,29 @@ PyObject* orthogonalise(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// Whether memory of a weight or a momentum belongs to another tensor of a step as well: its workgroups would write it at the same time.
+bool overlap(std::initializer_list<const std::vector<const at::Tensor*>*> written, const std::vector<const at::Tensor*>& read)
+{
+    struct Span {
+        uintptr_t first, last;
+        bool written;
+    };
+    std::vector<Span> spans;
+    auto add = [&](const std::vector<const at::Tensor*>& ts, bool w) {
+        for (const at::Tensor* t : ts) spans.push_back({(uintptr_t)t->data_ptr(), (uintptr_t)t->data_ptr() + t->nbytes(), w});
+    };
+    for (const auto* ts : written) add(*ts, true);
+    add(read, false);
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.first < b.first; });
+    uintptr_t end = 0, end_written = 0;
+    for (const Span& s : spans) {
+        if (s.first < (s.written ? end : end_written)) return true;
+        end = std::max(end, s.last);
+        if (s.written) end_written = std::max(end_written, s.last);
+    }
+    return false;
+}
+
 // Tells autograd that a tensor has other values now, so that a graph which saved it is not run on them.
 void moved(const std::vector<const at::Tensor*>& ts)
 {
@@ -601,7 +625,7 @@ PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
         Py_RETURN_NONE;
     const Py_ssize_t count = (Py_ssize_t)w.size();
     if (!matrices(args[1], count, w[0]->scalar_type(), &g) || !matrices(args[2], count, at::kFloat, &m) || !same_shapes(w, g) ||
-        !same_shapes(w, m))
+        !same_shapes(w, m) || overlap({&w, &m}, g))
         Py_RETURN_NONE;
     std::vector<void*> from;
     std::vector<float*> momenta;

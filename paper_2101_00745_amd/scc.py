@@ -621,6 +621,18 @@ def _matrices(*lists):
     return dev, _dtype_code(first[0])
 
 
+def _overlap(written, read):
+    """Whether memory of one of the written tensors belongs to another tensor of either list as well."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w) for ts, w in ((written, True), (read, False)) for t in ts)
+    end = end_written = 0
+    for first, last, w in spans:
+        if first < (end if w else end_written):
+            return True
+        end = max(end, last)
+        end_written = max(end_written, last) if w else end_written
+    return False
+
+
 def _orthogonal(dev, name, lists, options, dtype):
     count = len(lists[0])
     pointers = [(ctypes.c_void_p * count)(*[t.data_ptr() for t in l]) for l in lists]
@@ -647,7 +659,8 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
                         eps=1e-7):
     """One step of the orthogonalised momentum update on a list of weight matrices, in place:
     m <- momentum m + g, u = g + momentum m (nesterov) or m, w <- (1 - lr weight_decay) w - lr sqrt(max(1, rows/cols)) O(u), O as
-    scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32.  A graph that saved a weight cannot be
+    scc_orthogonalise.  weights and grads: float32 or bfloat16, one dtype for all; momenta: float32; no weight or momentum may overlap another tensor
+    of the call.  A graph that saved a weight cannot be
     run backward afterwards, as after any change in place."""
     native = _native or _load_native()
     status = native.orthogonal_step(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, *coefficients, eps)
@@ -656,6 +669,8 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
     dev, dtype = _matrices(weights, grads, momenta)
     if any(m.dtype != torch.float32 for m in momenta):
         raise ValueError("momenta are float32")
+    if _overlap((*weights, *momenta), grads):
+        raise ValueError("weights and momenta may not share memory with each other or with a gradient")
     options = _OrthogonalOptions(lr, momentum, weight_decay, int(bool(nesterov)), steps, *coefficients, eps)
     try:
         _orthogonal(dev, "scc_orthogonal_step", (weights, grads, momenta), options, dtype)

@@ -1,4 +1,4 @@
-"""Calls that write tensors of the caller's tell autograd so, and one that fails is not made again."""
+"""Calls that write tensors of the caller's tell autograd so, one that fails is not made again, and one that would write memory twice not at all."""
 
 import pytest
 import torch
@@ -143,3 +143,32 @@ def test_the_general_way_raises_versions_where_something_may_have_moved(monkeypa
             with pytest.raises(B.SccError):
                 S.scc_orthogonal_step([w], [g], [m], lr=0.1)
         assert [t._version - b for t, b in zip((w, g, m), before)] == [raised, 0, raised]
+
+
+def test_memory_that_would_be_written_twice():
+    """The matrices of a list are moved at the same time, by different workgroups."""
+    a, b, c, d = (torch.zeros(6, 8) for _ in range(4))
+    stack = torch.zeros(3, 6, 8)
+    assert not B._overlap([a, b], [c, d]) and not B._overlap([a], [c, c]) and not B._overlap([], [c, c])
+    assert not B._overlap([stack[0], stack[2]], [stack[1]])             # neighbours
+    for written, read in (([a, a], []), ([a], [a]), ([a, stack.flatten()[40:100]], [stack[1]]), ([stack[1]], [a, stack]), ([stack], [stack[2, 5:]]),
+                          ([stack[0], b, stack.flatten()[47:60]], [])):
+        assert B._overlap(written, read)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ROUTES)
+def test_shared_memory_is_refused(name, monkeypatch):
+    from paper_2101_00745_amd.optim import OrthogonalMomentum
+    route(name, monkeypatch)
+    w, v, g, m, n = (torch.ones(4, 6, device="cuda") for _ in range(5))
+    for lists in (([w, w], [g, g], [m, n]), ([w, v], [g, g], [m, m]), ([w], [w], [m]), ([w], [g], [g]), ([w], [g], [w])):
+        with pytest.raises(ValueError, match="share memory"):
+            S.scc_orthogonal_step(*lists, lr=0.1)
+    S.scc_orthogonal_step([w, v], [g, g], [m, n], lr=0.1)               # one gradient, read twice
+    p = torch.nn.Parameter(torch.ones(4, 6, device="cuda"))
+    p.grad = g
+    with pytest.warns(UserWarning, match="duplicate"):
+        opt = OrthogonalMomentum([p, p])
+    with pytest.raises(ValueError, match="share memory"):
+        opt.step()
