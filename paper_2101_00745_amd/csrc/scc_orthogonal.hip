@@ -9,7 +9,7 @@
 //
 // What bounds it: three dependent launches a step and, of small lists, their latencies (256 x 64: 17 launches and 72 us; the thirteen layers
 // 64x16 to 1024x512: 243 us, p 15, q 9, x 22 us a step against 8 us of matrix work); of large ones the matrix pipes (six of 1000 x 1024:
-// 0.96 ms, 126 TFLOP/s of binary32 products where six matrix instructions each allow 218).
+// 0.98 ms, 124 TFLOP/s of binary32 products where six matrix instructions each allow 218).
 #include "scc_orthogonal.h"
 
 #include <type_traits>
