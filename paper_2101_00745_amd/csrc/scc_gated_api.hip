@@ -25,14 +25,17 @@ int forward_path(const Problem& p, int es, Plan* plan, Shape* shape)
 // A gradient as it is computed.  dh, the gradient of both projections, is the output gradient of one sliding-channel layer of 2 * padded filters (the
 // second half starts on the first window again), whose gradients the framework's other kernels take.  They want planes of some
 // pixels and 64 columns at least: layers of less are turned into planes of one sample, filled up with zeros, and dx turned back.
-// bfloat16 layers of fewer columns than that are widened to binary32 on the way.  dg and du are then not rounded between the stages: rounded,
-// they leave 2^-9 of every product in dw, and with few columns that shows where products cancel; and such a call's time is its
-// launches', not its bytes'.
-// bfloat16 layers of more columns do hand dg and du on in bfloat16, as the gradient that one layer hands the next.  dx and dw are then off by 0.0023
-// of their norm where one rounding at the end leaves 0.0017.  A second bfloat16 part of both would bring that back for twice the filters in the products behind:
+// bfloat16 layers of fewer columns than that, or of few weights, are widened to binary32 on the way.  dg and du are then not rounded between the
+// stages: rounded, they leave 2^-9 of every product in dw, which shows where products cancel, with few columns or where no weight of few has a
+// sum much larger than its terms'.  Of 2255 random layers of 64 columns or more the rounding left dw of the 122 with fewer than 16 weights up to 18 times as far
+// off as one rounding at the end (0.010 of its norm; inputs were found with 0.1 of the largest value), of the 412 up to 128 weights 4.7 times, of the 1721 with more
+// 2.6 times (0.004 of the norm), half of all 1.4 times.  Widened, those of up to 128 weights take 1.1 times as long, 7 us more, in the middle; 3.7 times at most, with
+// a hundred thousand columns.
+// The others hand dg and du on in bfloat16, as the gradient that one layer hands the next.  A second bfloat16 part of both would make them exact for
+// twice the filters in the products behind:
 // us of these, without and with it, 64 x 512 -> 512 on 14x14, cg 8 25 and 36 (of a step's 66), 4096 tokens 256 -> 512, cg 2 14 and 27 (68), 65536 of them
 // 66 and 122, 64 x 512 -> 1024 on 7x7, cg 2 44 and 109, 8 x 2000 tokens 512 -> 1024 dense 109 and 574.
-constexpr int kFewColumns = 64;
+constexpr int kFewColumns = 64, kFewWeights = 128;
 
 struct Parts {
     Problem p;          // the layer in planes
@@ -48,8 +51,10 @@ int make_parts(const Problem& p, int cg, double co, scc_dtype dtype, scc_dtype g
 {
     Parts t;
     const long long padded = padded_filters(p), most = std::numeric_limits<int>::max();
-    t.planes = p.HW < 4 || p.NQ < kFewColumns;
-    t.widened = dtype == SCC_BF16 && p.NQ < kFewColumns;
+    // one sample of all columns has to fit an index, which the layer's own samples may where it does not
+    const bool few = 2ll * p.Cout * p.L <= kFewWeights && 2 * padded * (p.NQ + 7) <= most && p.Cin * (p.NQ + 7) <= most;
+    t.widened = dtype == SCC_BF16 && (p.NQ < kFewColumns || few);
+    t.planes = p.HW < 4 || p.NQ < kFewColumns || t.widened;
     t.type = t.widened ? SCC_F32 : dtype;
     t.p = p;
     if (t.planes) {

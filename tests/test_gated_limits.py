@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2101_00745_amd as S
+from paper_2101_00745_amd import scc as B
 from tests.test_gated import ANY, DIRECT, DTYPES, PRODUCT, TOL, inputs, off, reference
 
 # (N, Cin, Cout, H, W, cg, co) with Cin / gcd(stride, Cin) windows, more than 65536: index times inverse leaves 32 bits
@@ -109,3 +110,21 @@ def test_frozen_weights_and_inputs(shape, dtype):
     dw, = torch.autograd.grad(gated_scc(data, w, cg, co), w, dy)
     assert torch.equal(dx, both[0]) and torch.equal(dw, both[1])
     assert not gated_scc(data, frozen, cg, co).requires_grad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,seed", [((2, 5, 1, 7, 7, 5, 0.5), 100), ((9, 8, 2, 4, 4, 8, 0.0), 31), ((300, 14, 1, 1, 1, 7, 0.0), 1), ((40, 6, 1, 6, 8, 3, 0.0), 271),
+                                        ((100, 7, 2, 2, 2, 7, 0.5), 218), ((2, 5, 1, 7, 7, 5, 0.5), 30)])
+def test_few_weights_whose_products_cancel(shape, seed):
+    """Inputs for which the gradients between the stages, rounded to bfloat16, put dw off by 0.024 to 0.11 of its largest value."""
+    cg, co = shape[5:]
+    (x, w, dy), wide = inputs(shape, torch.bfloat16, seed=seed)
+    _, dx, dw = reference(wide[0], wide[1], cg, co, "silu", wide[2])
+    got = B._gated_backward(x.cuda(), w.cuda(), dy.cuda(), cg, co, "silu", False)
+    assert off(got[0], dx) <= TOL[torch.bfloat16] and off(got[1], dw) <= TOL[torch.bfloat16]
+
+
+def test_few_weights_of_more_columns_than_one_sample_indexes_are_not_refused():
+    lib = S.load()
+    for shape in ((1 << 20, 1, 1, 32, 32, 1, 0.5), (1 << 20, 4, 2, 16, 16, 2, 0.5), (1 << 13, 16, 1, 256, 256, 16, 0.5)):
+        assert lib.scc_gated_backward_workspace_bytes(*shape, 1, 0) > 0
