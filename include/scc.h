@@ -59,6 +59,7 @@
 #define SCC_H
 
 #include <stddef.h>
+#include <stdint.h>
 
 #ifdef __cplusplus
 extern "C" {
@@ -75,7 +76,7 @@ typedef enum {
     SCC_ERR_WORKSPACE = -5, /* workspace missing, misaligned or smaller than the call needs */
     SCC_ERR_LAUNCH = -6,    /* the HIP runtime refused a launch (hipGetLastError != hipSuccess) */
     SCC_ERR_SCRATCH = -7,   /* scc_backward_weight_static: the problem needs more than SCC_STATIC_SCRATCH_BYTES */
-    SCC_ERR_OPTION = -8     /* an activation, a number of steps or a coefficient out of its range */
+    SCC_ERR_OPTION = -8     /* an activation, a reduction, a number of steps or a coefficient out of its range */
 } scc_status;
 
 /* Size of the device buffer the library itself holds, per GPU, for scc_backward_weight_static. */
@@ -422,6 +423,91 @@ int scc_orthogonalise(int count, const void* const* g, void* const* o, const int
                       const scc_orthogonal_options* options, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
 int scc_orthogonal_step(int count, void* const* w, const void* const* g, float* const* m, const int* rows, const int* cols,
                         const scc_orthogonal_options* options, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Residual norm, which stands in front of a feed-forward block: the residual's addition and a root-mean-square norm over the channels,
+ *     h = x + residual,   y = h / sqrt(mean_c h^2 + eps) * w
+ * for every pixel of every sample (a sequence of S tokens is a map of S x 1, single tokens are N maps of 1 x 1).
+ * x, residual, h, y: N*C*H*W.  w: C values of the same type.  residual may be NULL (h = x, and h has to be NULL too); h may be NULL where the sum
+ * is not wanted.  Sums are binary32; h and y are each rounded once, from the unrounded sum.  Values whose squares leave binary32
+ * are scaled first.  A NaN or an infinity makes its own pixel's y NaN (0 for the other channels beside an infinity) and no other's.
+ * scc_norm_quantised writes y in 8 bits: q[n][c][h][w] * scale[n][h][w], q e4m3 (of the OCP's 8-bit formats the one without infinities), rounded to
+ * nearest even, scale the smallest power of two that brings the pixel's largest |y| to 448 or less (between 2^-120 and 2^120; 1 for a pixel of zeros).
+ * Outputs must not alias inputs or each other.
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W >= 2^31), SCC_ERR_DTYPE, SCC_ERR_OPTION (eps not positive and finite), SCC_ERR_LAUNCH.
+ */
+int scc_norm_forward(const void* x, const void* residual, const void* w, void* h, void* y, int N, int C, int H, int W, float eps,
+                     scc_dtype dtype, void* stream);
+int scc_norm_quantised(const void* x, const void* residual, const void* w, void* h, uint8_t* q, float* scale, int N, int C, int H, int W,
+                       float eps, scc_dtype dtype, void* stream);
+
+/*
+ * Gradients of the residual norm, h = x + residual added up again, with r = 1 / sqrt(mean_c h^2 + eps), a = dy w:
+ *     dx = dh + r (a - h r mean_c(a h r)),   dw[c] = sum over samples and pixels of dy h r
+ * dx is the gradient of x and of the residual.  residual may be NULL: the stored h in the place of x is enough in binary32; in bf16 its rounding would
+ * put dw off by half a step for each token, against half a step at the end.  dh: the gradient that reaches h by itself, or NULL.  dw: of the type `grad` (SCC_F32, or SCC_BF16 for
+ * bf16 tensors).  Sums are binary32, in a fixed order: two calls give bitwise identical results.
+ * workspace: at least scc_norm_backward_workspace_bytes(...) bytes, 256-byte aligned, owned by the caller, contents undefined before and
+ * after.  Errors: as above, and SCC_ERR_WORKSPACE.
+ */
+size_t scc_norm_backward_workspace_bytes(int N, int C, int H, int W, scc_dtype dtype);
+int scc_norm_backward(const void* x, const void* residual, const void* w, const void* dy, const void* dh, void* dx, void* dw, int N, int C, int H, int W,
+                      float eps, scc_dtype dtype, scc_dtype grad, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cross entropy over a vocabulary, without its logits in memory: for every pixel t (token) of x, with y_t = target[t],
+ *     l_tv = sum_c x_tc w_vc,   lse_t = log sum_v exp(l_tv),   loss_t = lse_t - l_{t,y_t}, or 0 where y_t is `ignored`
+ * x: N*C*H*W.  w: V*C, one row for each element of the vocabulary, the type of x.  target: N*H*W.  lse: out, N*H*W (0 where ignored).  loss: out, N*H*W
+ * values (SCC_NONE), or one: their sum (SCC_SUM) or that divided by the number of tokens that are not ignored (SCC_MEAN; 0 if there are
+ * none).  A target that is neither `ignored` nor in 0 .. V-1 gives a NaN for its token; nothing is read there.  Logits are binary32 sums (products as in
+ * scc_forward).  Non-finite inputs as for scc_forward.
+ */
+typedef enum { SCC_NONE = 0, SCC_SUM = 1, SCC_MEAN = 2 } scc_reduction;
+size_t scc_vocabulary_loss_workspace_bytes(int N, int C, int H, int W, int V, scc_reduction reduction, scc_dtype dtype);
+int scc_vocabulary_loss(const void* x, const void* w, const long long* target, float* loss, float* lse, int N, int C, int H, int W, int V,
+                        long long ignored, scc_reduction reduction, scc_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients, the logits computed again in pieces of the vocabulary: with p_tv = exp(l_tv - lse_t) - [v = y_t] and d_t the gradient of token t's
+ * loss (dloss[t], or dloss[0], or dloss[0] / count; 0 where ignored),
+ *     dx_tc = d_t sum_v p_tv w_vc,   dw_vc = sum_t d_t p_tv x_tc
+ * lse: as scc_vocabulary_loss wrote it, from the same x, w, target and `ignored`.  dx: out, as x.  dw: out, V*C values of the type `grad` (SCC_F32, or
+ * SCC_BF16 for bf16 tensors).  Sums are binary32, in a fixed order: two calls give bitwise identical results.  In bf16 p is rounded to 11
+ * bits between the products, and so is d_t x_tc; of a channel's values those below 2^-31 of its largest lose bits.
+ * workspace, for both: at least the query's bytes, 256-byte aligned, owned by the caller, contents undefined before and after (0 for invalid
+ * arguments).  It holds a copy of w (three bf16 pieces for each value of binary32) and, for the gradients, one piece's p.
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W or V over 2^26, C over 2^20), SCC_ERR_DTYPE, SCC_ERR_OPTION (reduction),
+ * SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH.
+ */
+size_t scc_vocabulary_gradients_workspace_bytes(int N, int C, int H, int W, int V, scc_dtype dtype);
+int scc_vocabulary_gradients(const void* x, const void* w, const long long* target, const float* lse, const float* dloss, void* dx, void* dw,
+                             int N, int C, int H, int W, int V, long long ignored, scc_reduction reduction, scc_dtype dtype, scc_dtype grad,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A step of AdamW on a list of weights, those that the orthogonalised update does not take (vectors, filters, embeddings), in place.  For element j
+ * of weight i, with t the step's number, from 1:
+ *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2
+ *     w <- (1 - lr weight_decay) w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * w, g: of the type `dtype`, sizes[i] elements; w is rounded to nearest.  States, with first_scales and second_scales NULL: first[i] (m) and second[i] (v)
+ * are binary32.  With both not NULL the states are in 8 bits: first[i] and second[i] are bytes of e4m3, and the scales, ceil(sizes[i] / 256) binary32
+ * powers of two, one for each 256 consecutive elements: m = first * scale, v = (second * scale)^2.  They are rounded up or down at random so that
+ * the expectation of what is stored is m (v); a v above 0 stays above 0; what is not finite is stored as NaN.  The random numbers are a hash of seed, t,
+ * i and j: the same call gives the same bits.  States of zeros (with any scales) are the beginning.
+ * step: t; or device_step, not NULL: its address in device memory, read when the call runs, so that a captured call can be replayed (it is not
+ * changed; values below 1 are not refused there).
+ * The arrays of pointers and sizes are HOST arrays, read before the call returns; the tensors are device memory.  No tensor that is written may
+ * overlap another tensor of the call, which is not checked here.
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count < 1, a size < 1 or over 2^40), SCC_ERR_DTYPE, SCC_ERR_OPTION (a beta outside [0, 1), eps < 0, a value
+ * that is not finite, step < 1), SCC_ERR_LAUNCH (some of the list may have moved, so the call is not to be made again).
+ */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    uint64_t seed;
+} scc_adamw_options;
+int scc_adamw_step(int count, void* const* w, const void* const* g, void* const* first, void* const* second, float* const* first_scales,
+                   float* const* second_scales, const long long* sizes, const scc_adamw_options* options, long long step,
+                   const long long* device_step, scc_dtype dtype, void* stream);
 
 /* Static, human-readable name of a status code (never NULL). */
 const char* scc_status_string(int status);

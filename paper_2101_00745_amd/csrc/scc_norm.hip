@@ -1,0 +1,711 @@
+// Root-mean-square norm over the channels with the residual's addition, its 8-bit output and its gradients.
+//
+// All of it is bound by memory: forward reads x and r and writes h and y, backward reads x, r, dy and dh and writes dx, each
+// element once.  So a
+// token's channels stay in registers between the sum over them and their second use, as they were loaded (bf16 pairs are not widened
+// before they are used).  Two layouts: tokens as rows (H*W = 1: the channels of a token are consecutive; a group of 16 to 1024 lanes per token)
+// and tokens as columns (a workgroup has some consecutive columns and all their channels: lanes along the pixels, so that a channel's load
+// is one piece of 64 or 128 bytes, wavefronts along the channels).  Vectors are 16 bytes; where their width does not divide a row the last one overlaps
+// the one before it: both store the same bits, sums count the shared elements once.
+#include "scc_norm.h"
+
+namespace scc {
+namespace norm {
+namespace {
+
+template <typename T, int V> struct VecOf { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+template <typename T> struct VecOf<T, 1> { typedef T type; };
+
+template <typename T, int V>
+struct Vec {
+    typename VecOf<T, V>::type v;
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (V == 1) return to_f32(v);
+        else return to_f32((T)v[e]);
+    }
+    __device__ __forceinline__ void set(int e, float f)
+    {
+        if constexpr (V == 1) v = from_f32<T>(f);
+        else v[e] = from_f32<T>(f);
+    }
+    __device__ __forceinline__ void load(const T* p) { v = *(const typename VecOf<T, V>::type*)p; }
+    __device__ __forceinline__ void store(T* p) const { *(typename VecOf<T, V>::type*)p = v; }
+    __device__ __forceinline__ void clear()
+    {
+        if constexpr (V == 1) v = 0;
+        else
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = 0;
+    }
+};
+
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// Squares of values beyond 2^60 leave binary32: sums that come out above this are taken again of scaled values.
+constexpr float kLargeSum = 1e37f;
+constexpr float kShrink = 8.077935669463161e-28f;    // 2^-90: the square of the largest value times 2^31 channels fits
+
+__device__ __forceinline__ float inverse_rms(float sum, float shrink, const Shape& s)
+{
+    // shrink is 1, or kShrink with the sum of the shrunk squares
+    return shrink / sqrtf(sum / (float)s.C + s.eps * shrink * shrink);
+}
+
+// The smallest power of two that brings `most` to 448, e4m3's largest value, or less; 1 for 0.  A NaN among y makes no difference here.
+__device__ __forceinline__ float scale_of(float most)
+{
+    const uint32_t b = __float_as_uint(most);
+    int k = (int)(b >> 23) - 127 - ((b & 0x7fffffu) <= 0x600000u ? 8 : 7);
+    k = k < -120 ? -120 : k > 120 ? 120 : k;
+    return most > 0.f ? __uint_as_float((uint32_t)(k + 127) << 23) : 1.f;
+}
+
+// e4m3 of v, to nearest even; what is not finite becomes NaN
+__device__ __forceinline__ uint32_t e4m3(float v)
+{
+    const uint32_t q = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xffu;
+    return fabsf(v) <= 448.f ? q : 0x7fu;
+}
+
+template <int V>
+__device__ __forceinline__ void store_bytes(uint8_t* to, const uint32_t (&q)[V])
+{
+    if constexpr (V == 1) {
+        *to = (uint8_t)q[0];
+    } else {
+        typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(1)));
+        words o;
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const uint32_t packed = q[4 * i] | q[4 * i + 1] << 8 | q[4 * i + 2] << 16 | q[4 * i + 3] << 24;
+            if constexpr (V == 4) { o = packed; } else { o[i] = packed; }
+        }
+        *(words*)to = o;
+    }
+}
+
+// ---- tokens as rows ----
+
+template <int TPT, typename F>
+__device__ __forceinline__ float over_group(float v, float* lds, F&& op)
+{
+#pragma unroll
+    for (int m = 1; m < (TPT < 64 ? TPT : 64); m *= 2) v = op(v, __shfl_xor(v, m));
+    if constexpr (TPT > 64) {
+        constexpr int W = TPT / 64;
+        __syncthreads();                        // the sums of the one before have been read
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        const int first = (threadIdx.x >> 6) / W * W;
+        v = lds[first];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v = op(v, lds[first + i]);
+    }
+    return v;
+}
+
+template <int TPT> constexpr int kRowThreads = TPT < 256 ? 256 : TPT;
+
+// NV vectors of V channels per lane; NV = 0: any number, read again instead of kept
+template <typename T, int V, int TPT, int NV, bool BYTES>
+__global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ w,
+                                                                 T* __restrict__ h, void* __restrict__ y, float* __restrict__ scale,
+                                                                 Shape s)
+{
+    __shared__ float lds[TPT > 64 ? kRowThreads<TPT> / 64 : 1];
+    const int lane = threadIdx.x % TPT;
+    const size_t token = (size_t)blockIdx.x * (kRowThreads<TPT> / TPT) + threadIdx.x / TPT;
+    const bool there = token < (size_t)s.N;
+    const size_t base = (there ? token : (size_t)s.N - 1) * s.C;
+    const int count = NV ? NV : (s.C + V * TPT - 1) / (V * TPT);
+    Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1];
+    auto place = [&](int j) { return (lane + j * TPT) * V; };
+    auto start = [&](int at) { return at < s.C - V ? at : s.C - V; };
+    auto fetch = [&](int j, int k) {
+        const int at = place(j);
+        xs[k].clear();
+        rs[k].clear();
+        if (at < s.C) {
+            xs[k].load(x + base + start(at));
+            if (r) rs[k].load(r + base + start(at));
+        }
+    };
+    if constexpr (NV > 0)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) fetch(j, j);
+    auto squares = [&](float shrink) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0;
+            if constexpr (NV == 0) fetch(j, 0);
+            const int at = place(j);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float v = (xs[k].get(e) + rs[k].get(e)) * shrink;
+                if (start(at) + e >= at) sum = fmaf(v, v, sum);
+            }
+        }
+        return over_group<TPT>(sum, lds, add);
+    };
+    float shrink = 1.f, sum = squares(1.f);
+    if (!(sum < kLargeSum)) {
+        if constexpr (TPT > 64) __syncthreads();
+        shrink = kShrink;
+        sum = squares(kShrink);
+    }
+    const float rstd = inverse_rms(sum, shrink, s);
+    auto value = [&](int k, int e, const Vec<T, V>& g) { return (xs[k].get(e) + rs[k].get(e)) * rstd * g.get(e); };
+    float unit = 1.f, inverse = 1.f;
+    if constexpr (BYTES) {
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0, at = place(j);
+            if constexpr (NV == 0) fetch(j, 0);
+            if (at >= s.C) continue;
+            Vec<T, V> g;
+            g.load(w + start(at));
+#pragma unroll
+            for (int e = 0; e < V; ++e) most = fmaxf(most, fabsf(value(k, e, g)));
+        }
+        unit = scale_of(over_group<TPT>(most, lds, fmaxf));
+        inverse = 1.f / unit;
+        if (there && lane == 0) scale[token] = unit;
+    }
+    if (!there) return;
+#pragma unroll
+    for (int j = 0; j < count; ++j) {
+        const int k = NV ? j : 0, at = place(j);
+        if constexpr (NV == 0) fetch(j, 0);
+        if (at >= s.C) continue;
+        const size_t to = base + start(at);
+        Vec<T, V> g, o;
+        g.load(w + start(at));
+        if constexpr (BYTES) {
+            uint32_t q[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e, g) * inverse);
+            store_bytes<V>((uint8_t*)y + to, q);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.set(e, value(k, e, g));
+            o.store((T*)y + to);
+        }
+        if (h) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.set(e, xs[k].get(e) + rs[k].get(e));
+            o.store(h + to);
+        }
+    }
+}
+
+// One row of dw's sums for each group of lanes, which takes every gridDim.x * groups'th token.
+template <typename T, int V, int TPT, int NV>
+__global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ w,
+                                                                  const T* __restrict__ dy, const T* __restrict__ dh, T* __restrict__ dx, float* __restrict__ part,
+                                                                  Shape s)
+{
+    constexpr int kGroups = kRowThreads<TPT> / TPT;
+    __shared__ float lds[TPT > 64 ? kRowThreads<TPT> / 64 : 1];
+    const int lane = threadIdx.x % TPT;
+    const size_t group = (size_t)blockIdx.x * kGroups + threadIdx.x / TPT, groups = (size_t)gridDim.x * kGroups;
+    auto place = [&](int j) { return (lane + j * TPT) * V; };
+    auto start = [&](int at) { return at < s.C - V ? at : s.C - V; };
+    float sums[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[j][e] = 0.f;
+    // every group of a workgroup makes as many rounds, the last perhaps on a token that is none
+    for (size_t first = (size_t)blockIdx.x * kGroups; first < (size_t)s.N; first += groups) {
+        const size_t token = first + threadIdx.x / TPT;
+        const bool there = token < (size_t)s.N;
+        const size_t base = (there ? token : (size_t)s.N - 1) * s.C;
+        Vec<T, V> xs[NV], rs[NV], ds[NV], gs[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int at = place(j);
+            xs[j].clear();
+            rs[j].clear();
+            ds[j].clear();
+            gs[j].clear();
+            if (at < s.C) {
+                xs[j].load(x + base + start(at));
+                if (r) rs[j].load(r + base + start(at));
+                ds[j].load(dy + base + start(at));
+                gs[j].load(w + start(at));
+            }
+        }
+        auto both = [&](float shrink, float& sum, float& dot) {
+            sum = dot = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int at = place(j);
+                    if (start(at) + e < at) continue;
+                    const float v = (xs[j].get(e) + rs[j].get(e)) * shrink;
+                    sum = fmaf(v, v, sum);
+                    dot = fmaf(ds[j].get(e) * gs[j].get(e), v, dot);
+                }
+            sum = over_group<TPT>(sum, lds, add);
+            dot = over_group<TPT>(dot, lds, add);
+        };
+        float shrink = 1.f, sum, dot;
+        both(1.f, sum, dot);
+        if (!(sum < kLargeSum)) {
+            shrink = kShrink;
+            both(kShrink, sum, dot);
+        }
+        const float rstd = inverse_rms(sum, shrink, s);
+        const float inner = dot * (rstd / shrink) / (float)s.C;      // mean_c(a h s)
+        if (!there) continue;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int at = place(j);
+            if (at >= s.C) continue;
+            Vec<T, V> extra, o;
+            extra.clear();
+            if (dh) extra.load(dh + base + start(at));
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float hat = (xs[j].get(e) + rs[j].get(e)) * rstd, d = ds[j].get(e);
+                o.set(e, fmaf(d * gs[j].get(e) - hat * inner, rstd, extra.get(e)));
+                sums[j][e] = fmaf(d, hat, sums[j][e]);
+            }
+            o.store(dx + base + start(at));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int at = place(j);
+            if (at < s.C && start(at) + e >= at) part[group * s.C + start(at) + e] = sums[j][e];
+        }
+}
+
+// ---- tokens as columns ----
+
+// LANES groups of V columns, THREADS / LANES channels at a time, NV times that in registers (0: any number, read again)
+template <int V, int LANES, int THREADS>
+struct Columns {
+    static constexpr int kRows = THREADS / LANES, kWaves = THREADS / 64;
+    float lds[kWaves][LANES * V];
+
+    // sums over all channels of each of the thread's columns
+    template <typename F>
+    __device__ __forceinline__ void reduce(float (&v)[V], F&& op)
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+#pragma unroll
+            for (int m = LANES; m < 64; m *= 2) v[e] = op(v[e], __shfl_xor(v[e], m));
+        __syncthreads();
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        if (lane < LANES)
+#pragma unroll
+            for (int e = 0; e < V; ++e) lds[wave][lane * V + e] = v[e];
+        __syncthreads();
+        if (threadIdx.x < LANES * V) {
+            float total = lds[0][threadIdx.x];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) total = op(total, lds[i][threadIdx.x]);
+            lds[0][threadIdx.x] = total;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = lds[0][(threadIdx.x % LANES) * V + e];
+    }
+};
+
+template <int V>
+__device__ __forceinline__ bool any_large(const float (&sum)[V])
+{
+    bool large = false;
+#pragma unroll
+    for (int e = 0; e < V; ++e) large |= !(sum[e] < kLargeSum);
+    return __syncthreads_or(large);
+}
+
+template <typename T, int V, int LANES, int THREADS, int NV, bool BYTES>
+__global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ w,
+                                                           T* __restrict__ h, void* __restrict__ y, float* __restrict__ scale, Shape s,
+                                                           Groups groups)
+{
+    typedef Columns<V, LANES, THREADS> Cols;
+    __shared__ Cols cols;
+    const uint32_t group = blockIdx.x * LANES + threadIdx.x % LANES;
+    const bool there = group < (uint32_t)groups.count;
+    uint32_t n, p;
+    column_of_group(there ? group : (uint32_t)groups.count - 1, groups, n, p);
+    const size_t base = (size_t)n * s.C * s.HW + p;
+    const int row = threadIdx.x / LANES;
+    const int count = NV ? NV : (s.C + Cols::kRows - 1) / Cols::kRows;
+    Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1];
+    auto fetch = [&](int j, int k) {
+        const int c = row + j * Cols::kRows;
+        xs[k].clear();
+        rs[k].clear();
+        if (c < s.C) {
+            xs[k].load(x + base + (size_t)c * s.HW);
+            if (r) rs[k].load(r + base + (size_t)c * s.HW);
+        }
+    };
+    if constexpr (NV > 0)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) fetch(j, j);
+    float sum[V], rstd[V];
+    auto squares = [&](float shrink) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0;
+            if constexpr (NV == 0) fetch(j, 0);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float v = (xs[k].get(e) + rs[k].get(e)) * shrink;
+                sum[e] = fmaf(v, v, sum[e]);
+            }
+        }
+        cols.reduce(sum, add);
+    };
+    squares(1.f);
+#pragma unroll
+    for (int e = 0; e < V; ++e) rstd[e] = inverse_rms(sum[e], 1.f, s);
+    if (any_large(sum)) {
+        bool large[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) large[e] = !(sum[e] < kLargeSum);
+        squares(kShrink);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (large[e]) rstd[e] = inverse_rms(sum[e], kShrink, s);
+    }
+    auto value = [&](int k, int e, float g) { return (xs[k].get(e) + rs[k].get(e)) * rstd[e] * g; };
+    float inverse[V];
+    if constexpr (BYTES) {
+        float most[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) most[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0, c = row + j * Cols::kRows;
+            if constexpr (NV == 0) fetch(j, 0);
+            if (c >= s.C) continue;
+            const float g = to_f32(w[c]);
+#pragma unroll
+            for (int e = 0; e < V; ++e) most[e] = fmaxf(most[e], fabsf(value(k, e, g)));
+        }
+        cols.reduce(most, fmaxf);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float unit = scale_of(most[e]);
+            inverse[e] = 1.f / unit;
+            if (there && row == 0) scale[(size_t)n * s.HW + p + e] = unit;
+        }
+    }
+    if (!there) return;
+#pragma unroll
+    for (int j = 0; j < count; ++j) {
+        const int k = NV ? j : 0, c = row + j * Cols::kRows;
+        if constexpr (NV == 0) fetch(j, 0);
+        if (c >= s.C) continue;
+        const size_t to = base + (size_t)c * s.HW;
+        const float g = to_f32(w[c]);
+        Vec<T, V> o;
+        if constexpr (BYTES) {
+            uint32_t q[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e, g) * inverse[e]);
+            store_bytes<V>((uint8_t*)y + to, q);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.set(e, value(k, e, g));
+            o.store((T*)y + to);
+        }
+        if (h) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.set(e, xs[k].get(e) + rs[k].get(e));
+            o.store(h + to);
+        }
+    }
+}
+
+// A workgroup takes every gridDim.x'th tile and keeps its sums of dw in registers; with NV = 0, where it may have any number of channels, in its row of
+// the workspace, which only it writes.
+template <typename T, int V, int LANES, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ w,
+                                                            const T* __restrict__ dy, const T* __restrict__ dh, T* __restrict__ dx,
+                                                            float* __restrict__ part, Shape s,
+                                                            Groups groups)
+{
+    typedef Columns<V, LANES, THREADS> Cols;
+    __shared__ Cols cols;
+    const int row = threadIdx.x / LANES;
+    const int count = NV ? NV : (s.C + Cols::kRows - 1) / Cols::kRows;
+    const uint32_t tiles = ((uint32_t)groups.count + LANES - 1) / LANES;
+    float sums[NV ? NV : 1];
+#pragma unroll
+    for (int j = 0; j < (NV ? NV : 1); ++j) sums[j] = 0.f;
+    auto over_lanes = [&](float v) {
+#pragma unroll
+        for (int m = 1; m < LANES; m *= 2) v += __shfl_xor(v, m);
+        return v;
+    };
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t group = tile * LANES + threadIdx.x % LANES;
+        const bool there = group < (uint32_t)groups.count;
+        const uint32_t u = there ? group : (uint32_t)groups.count - 1;
+        uint32_t n, p;
+        column_of_group(u, groups, n, p);
+        const uint32_t own = (u - n * (uint32_t)groups.per) * V - p;    // columns of this group that the one before it has
+        const size_t base = (size_t)n * s.C * s.HW + p;
+        Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1], ds[NV ? NV : 1];
+        auto fetch = [&](int j, int k) {
+            const int c = row + j * Cols::kRows;
+            xs[k].clear();
+            rs[k].clear();
+            ds[k].clear();
+            if (c < s.C) {
+                xs[k].load(x + base + (size_t)c * s.HW);
+                if (r) rs[k].load(r + base + (size_t)c * s.HW);
+                ds[k].load(dy + base + (size_t)c * s.HW);
+            }
+        };
+        if constexpr (NV > 0)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) fetch(j, j);
+        float sum[V], dot[V], rstd[V], inner[V];
+        auto both = [&](float shrink) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] = dot[e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < count; ++j) {
+                const int k = NV ? j : 0, c = row + j * Cols::kRows;
+                if constexpr (NV == 0) fetch(j, 0);
+                const float g = c < s.C ? to_f32(w[c]) : 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float v = (xs[k].get(e) + rs[k].get(e)) * shrink;
+                    sum[e] = fmaf(v, v, sum[e]);
+                    dot[e] = fmaf(ds[k].get(e) * g, v, dot[e]);
+                }
+            }
+            cols.reduce(sum, add);
+            cols.reduce(dot, add);
+        };
+        auto finish = [&](int e, float shrink) {
+            rstd[e] = inverse_rms(sum[e], shrink, s);
+            inner[e] = dot[e] * (rstd[e] / shrink) / (float)s.C;
+        };
+        both(1.f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) finish(e, 1.f);
+        if (any_large(sum)) {
+            bool large[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) large[e] = !(sum[e] < kLargeSum);
+            both(kShrink);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (large[e]) finish(e, kShrink);
+        }
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0, c = row + j * Cols::kRows;
+            if constexpr (NV == 0) fetch(j, 0);
+            float mine = 0.f;
+            if (c < s.C && there) {
+                const size_t at = base + (size_t)c * s.HW;
+                const float g = to_f32(w[c]);
+                Vec<T, V> extra, o;
+                extra.clear();
+                if (dh) extra.load(dh + at);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float hat = (xs[k].get(e) + rs[k].get(e)) * rstd[e], d = ds[k].get(e);
+                    o.set(e, fmaf(d * g - hat * inner[e], rstd[e], extra.get(e)));
+                    if ((uint32_t)e >= own) mine = fmaf(d, hat, mine);
+                }
+                o.store(dx + at);
+            }
+            if constexpr (NV > 0) {
+                sums[j] += mine;
+            } else {
+                mine = over_lanes(mine);
+                if (threadIdx.x % LANES == 0 && c < s.C) {
+                    float* to = part + (size_t)blockIdx.x * s.C + c;
+                    *to = tile == blockIdx.x ? mine : *to + mine;
+                }
+            }
+        }
+    }
+    if constexpr (NV > 0)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = row + j * Cols::kRows;
+            const float v = over_lanes(sums[j]);
+            if (threadIdx.x % LANES == 0 && c < s.C) part[(size_t)blockIdx.x * s.C + c] = v;
+        }
+}
+
+// dw[c] = sum over rows of part[row][c], in a fixed order: 16 wavefronts take the rows in turn, 64 channels a workgroup
+template <typename D>
+__global__ __launch_bounds__(1024) void weight_sums(const float* __restrict__ part, D* __restrict__ dw, int rows, int C)
+{
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    if (c < C)
+        for (int i = wave; i < rows; i += 16) sum += part[(size_t)i * C + c];
+    lds[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < C) {
+        for (int i = 1; i < 16; ++i) sum += lds[i][lane];
+        dw[c] = from_f32<D>(sum);
+    }
+}
+
+// ---- which form a shape takes ----
+
+// Vectors that a token's channels (or a plane's pixels) are read in: 16 bytes where there are as many.
+template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
+
+constexpr int kKept = 4;            // vectors of a lane that stay in registers
+
+// f(V, TPT, NV) as constants for tokens as rows
+template <typename T, typename F>
+hipError_t with_rows(int C, F&& f)
+{
+    auto width = [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        if (C <= V * 16 * 2) return f(v, std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+        if (C <= V * 64 * kKept) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, kKept>());
+        if (C <= V * 256 * kKept) return f(v, std::integral_constant<int, 256>(), std::integral_constant<int, kKept>());
+        if (C <= V * 1024 * kKept) return f(v, std::integral_constant<int, 1024>(), std::integral_constant<int, kKept>());
+        return f(v, std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
+    };
+    if (C >= kWide<T>) return width(std::integral_constant<int, kWide<T>>());
+    return width(std::integral_constant<int, 1>());
+}
+
+// f(V, LANES, THREADS, NV) as constants for tokens as columns
+template <typename T, typename F>
+hipError_t with_columns(int C, int HW, F&& f)
+{
+    auto width = [&](auto v, auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        if (C <= 256 / L * kKept) return f(v, lanes, std::integral_constant<int, 256>(), std::integral_constant<int, kKept>());
+        if (C <= 1024 / L * kKept) return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, kKept>());
+        if (C <= 1024 / L * 8) return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+        return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
+    };
+    if (HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>());
+    return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
+}
+
+Groups groups_of(const Shape& s, int V)
+{
+    Problem p = {};
+    p.N = s.N;
+    p.HW = s.HW;
+    return column_groups(p, V);
+}
+
+constexpr int kSumRows = 1024;      // most rows of dw's sums, one for each group of lanes
+
+// Workgroups of the backward pass and the rows of sums that they leave
+struct Grid {
+    int blocks, rows;
+};
+
+template <typename T>
+Grid backward_grid(const Shape& s)
+{
+    Grid g = {1, 1};
+    // tokens as rows, of too many channels for registers: as planes of one pixel
+    const bool rows = s.HW == 1 && s.C <= kWide<T> * 1024 * kKept && s.C >= kWide<T>;
+    if (rows) {
+        (void)with_rows<T>(s.C, [&](auto, auto tpt, auto) {
+            constexpr int TPT = decltype(tpt)::value, G = kRowThreads<TPT> / TPT;
+            const int most = (s.N + G - 1) / G, wanted = kSumRows / G;
+            g.blocks = most < wanted ? most : wanted;
+            g.rows = g.blocks * G;
+            return hipSuccess;
+        });
+    } else {
+        (void)with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto) {
+            const long long tiles = (groups_of(s, decltype(v)::value).count + decltype(lanes)::value - 1) / decltype(lanes)::value;
+            const int wanted = decltype(threads)::value == 256 ? kSumRows : 512;
+            g.blocks = g.rows = (int)(tiles < wanted ? tiles : wanted);
+            return hipSuccess;
+        });
+    }
+    return g;
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, float* scale, const Shape& s, hipStream_t st)
+{
+    if (s.HW == 1)
+        return with_rows<T>(s.C, [&](auto v, auto tpt, auto nv) {
+            constexpr int V = decltype(v)::value, TPT = decltype(tpt)::value, NV = decltype(nv)::value, G = kRowThreads<TPT> / TPT;
+            const int blocks = (s.N + G - 1) / G;
+            if (scale) forward_rows<T, V, TPT, NV, true><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
+            else forward_rows<T, V, TPT, NV, false><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
+            return hipGetLastError();
+        });
+    return with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto nv) {
+        constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
+        const Groups g = groups_of(s, V);
+        const int blocks = (int)((g.count + L - 1) / L);
+        if (scale) forward_columns<T, V, L, TH, NV, true><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
+        else forward_columns<T, V, L, TH, NV, false><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
+        return hipGetLastError();
+    });
+}
+
+size_t backward_workspace(const Shape& s, int es)
+{
+    const Grid g = es == 4 ? backward_grid<float>(s) : backward_grid<bf16_t>(s);
+    return (size_t)g.rows * s.C * sizeof(float);
+}
+
+template <typename T, typename D>
+hipError_t launch_backward(const T* x, const T* r, const T* w, const T* dy, const T* dh, T* dx, D* dw, float* part, const Shape& s, hipStream_t st)
+{
+    const Grid g = backward_grid<T>(s);
+    hipError_t e;
+    if (s.HW == 1 && s.C <= kWide<T> * 1024 * kKept && s.C >= kWide<T>)
+        e = with_rows<T>(s.C, [&](auto v, auto tpt, auto nv) {
+            constexpr int V = decltype(v)::value, TPT = decltype(tpt)::value, NV = decltype(nv)::value;
+            if constexpr (NV > 0 && V > 1)
+                backward_rows<T, V, TPT, NV><<<g.blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, dy, dh, dx, part, s);
+            return hipGetLastError();
+        });
+    else
+        e = with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto nv) {
+            constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
+            backward_columns<T, V, L, TH, NV><<<g.blocks, TH, 0, st>>>(x, r, w, dy, dh, dx, part, s, groups_of(s, V));
+            return hipGetLastError();
+        });
+    if (e != hipSuccess) return e;
+    weight_sums<D><<<(s.C + 63) / 64, 1024, 0, st>>>(part, dw, g.rows, s.C);
+    return hipGetLastError();
+}
+
+#define INSTANCE(T)                                                                                                                        \
+    template hipError_t launch_forward<T>(const T*, const T*, const T*, T*, void*, float*, const Shape&, hipStream_t);                     \
+    template hipError_t launch_backward<T, float>(const T*, const T*, const T*, const T*, const T*, T*, float*, float*, const Shape&, hipStream_t);
+INSTANCE(float)
+INSTANCE(bf16_t)
+template hipError_t launch_backward<bf16_t, bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*, const bf16_t*, const bf16_t*, bf16_t*, bf16_t*, float*, const Shape&, hipStream_t);
+
+}  // namespace norm
+}  // namespace scc

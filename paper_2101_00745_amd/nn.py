@@ -245,3 +245,103 @@ class GatedFeedForward(torch.nn.Module):
 
     def forward(self, x):
         return self.down(self.up(x))
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    """y = norm(x + residual) * weight and h = x + residual.  The backward pass keeps h in float32, x and the residual in bfloat16, where h is rounded."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        x, weight = x.contiguous(), weight.contiguous()
+        residual = None if residual is None else residual.contiguous()
+        y, h = _scc.scc_norm_forward(x, weight, residual, eps)
+        if residual is None:
+            ctx.save_for_backward(x, None, weight)
+        elif x.dtype == torch.float32:
+            ctx.save_for_backward(h, None, weight)
+        else:
+            ctx.save_for_backward(x, residual, weight)
+        ctx.eps = eps
+        ctx.set_materialize_grads(False)
+        return (y, h) if residual is not None else y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        x, residual, weight = ctx.saved_tensors
+        if dy is None and dh is None:
+            return None, None, None, None
+        dh = None if dh is None else dh.contiguous()
+        dy = torch.zeros_like(x) if dy is None else dy.contiguous()
+        dx, dw = _scc._norm_backward(x, weight, dy, residual, dh, ctx.eps, True)
+        need_x, need_r, need_w = ctx.needs_input_grad[:3]
+        used = [t for t in (dy, dh, x, residual, weight) if t is not None]
+        dx, dw = _first_order((dx if need_x or need_r else None, dw if need_w else None), *used)
+        return dx if need_x else None, dx if need_r else None, dw, None
+
+
+def residual_norm(x, weight, residual=None, eps=1e-6):
+    """Functional form: (y, h) with h = x + residual and y = h / sqrt(mean over the channels of h^2 + eps) * weight; without a residual h is x."""
+    if residual is None:
+        return ResidualNormFunction.apply(x, None, weight, float(eps)), x
+    return ResidualNormFunction.apply(x, residual, weight, float(eps))
+
+
+class ResidualNorm(torch.nn.Module):
+    """The norm in front of a feed-forward block, with the addition of the branch before it to the residual stream: (y, h) from (x, residual)."""
+
+    def __init__(self, channels, eps=1e-6, device="cuda", dtype=torch.float32):
+        super().__init__()
+        self.channels, self.eps = channels, float(eps)
+        self.weight = torch.nn.Parameter(torch.ones(channels, device=device, dtype=dtype))
+
+    def forward(self, x, residual=None):
+        return residual_norm(x, self.weight, residual, self.eps)
+
+    def extra_repr(self):
+        return "%d, eps=%g" % (self.channels, self.eps)
+
+
+class VocabularyLossFunction(torch.autograd.Function):
+    """Cross entropy of the logits x weight^T, which neither pass keeps: the backward pass computes them again, in pieces."""
+
+    @staticmethod
+    def forward(ctx, x, weight, target, code, ignore_index):
+        x, weight, target = x.contiguous(), weight.contiguous(), target.contiguous()
+        loss, lse = _scc.scc_vocabulary_loss(x, weight, target, code, ignore_index)
+        ctx.save_for_backward(x, weight, target, lse)
+        ctx.code, ctx.ignored = code, ignore_index
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x, weight, target, lse = ctx.saved_tensors
+        dx, dw = _scc._vocabulary_gradients(x, weight, target, lse, dloss.contiguous(), _scc._reduction(ctx.code), ctx.ignored, True)
+        grads = (dx if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None)
+        return (*_first_order(grads, dloss, x, weight), None, None, None)
+
+
+def vocabulary_loss(x, weight, target, reduction="mean", ignore_index=-100):
+    """Functional form: cross entropy over the vocabulary of logits[n,v,h,w] = sum_c x[n,c,h,w] weight[v,c] at target [N,H,W], float32.
+    reduction: "none", "sum" or "mean" (over the targets that are not ignore_index; 0 if there are none)."""
+    return VocabularyLossFunction.apply(x, weight, target, reduction, int(ignore_index))
+
+
+class VocabularyLoss(torch.nn.Module):
+    """What a model of such blocks ends with in training: the projection of ``channels`` to a vocabulary and the cross entropy, as one."""
+
+    def __init__(self, channels, vocabulary, reduction="mean", ignore_index=-100, device="cuda", dtype=torch.float32):
+        super().__init__()
+        _scc._reduction(reduction)
+        self.channels, self.vocabulary, self.reduction, self.ignore_index = channels, vocabulary, reduction, int(ignore_index)
+        self.weight = torch.nn.Parameter(torch.empty(vocabulary, channels, device=device, dtype=dtype))
+        self.reset_parameters()
+
+    def reset_parameters(self):
+        with torch.no_grad():
+            self.weight.normal_(0.0, 1.0 / math.sqrt(self.channels))
+
+    def forward(self, x, target):
+        return vocabulary_loss(x, self.weight, target, self.reduction, self.ignore_index)
+
+    def extra_repr(self):
+        return "%d, %d, reduction=%s, ignore_index=%d" % (self.channels, self.vocabulary, self.reduction, self.ignore_index)

@@ -1,4 +1,5 @@
-"""Optimiser over scc_orthogonal_step: momentum whose update is orthogonalised, for the weight matrices of SCC layers."""
+"""Optimisers: momentum whose update is orthogonalised, for the weight matrices of SCC layers (over scc_orthogonal_step), and AdamW for all other
+weights (over scc_adamw_step)."""
 import torch
 
 from . import scc as _scc
@@ -54,4 +55,92 @@ class OrthogonalMomentum(torch.optim.Optimizer):
             for ws, gs, ms in lists.values():
                 _scc.scc_orthogonal_step(ws, gs, ms, group["lr"], momentum=group["momentum"], weight_decay=group["weight_decay"],
                                          nesterov=group["nesterov"], steps=group["steps"])
+        return loss
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW for the weights that ``OrthogonalMomentum`` does not take, or for all (``scc_adamw_step``): one call, in launches of 60 weights, for all weights of
+    a group, dtype and age.  state_bits: 32, or 8 for states of e4m3 with a scale for each 256 elements, rounded at random (a hash of ``seed``, the
+    step and the place, so that a run repeats).  capturable: the step's number is kept on the GPU, so that a captured step can be replayed; make one
+    step before the capture, which allocates the states."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, seed=0, capturable=False):
+        if lr < 0.0 or not all(0.0 <= b < 1.0 for b in betas) or eps < 0.0 or weight_decay < 0.0:
+            raise ValueError("lr, eps and weight_decay must not be negative, betas must lie in [0, 1)")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32, got %r" % (state_bits,))
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits, seed=int(seed),
+                                      capturable=bool(capturable)))
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # torch brings a state to its parameter's type; these stay what they were
+        indices = [i for group in state_dict["param_groups"] for i in group["params"]]
+        params = [p for group in self.param_groups for p in group["params"]]
+        for i, p in zip(indices, params):
+            for name, value in state_dict["state"].get(i, {}).items():
+                if isinstance(value, torch.Tensor):
+                    self.state[p][name] = value.to(device=p.device, copy=True)
+        for group in self.param_groups:
+            for p in group["params"]:
+                step = self.state[p].get("step") if p in self.state else None
+                if isinstance(step, torch.Tensor):
+                    self.state[p]["step"] = self._shared_step(group, p.device, int(step), step)
+
+    def _shared_step(self, group, device, age, step):
+        """The weights of a group that are equally old share their step's number, where it is on the GPU: one call takes them all."""
+        for p in group["params"]:
+            other = self.state[p].get("step") if p in self.state else None
+            if isinstance(other, torch.Tensor) and other is not step and other.device == device and int(other) == age:
+                return other
+        return step
+
+    def _begin(self, p, group, begun):
+        """The weight's state; begun: the numbers on the GPU of the weights that begin in this step."""
+        state = self.state[p]
+        if not state:
+            if group["capturable"]:
+                if p.device not in begun:
+                    begun[p.device] = torch.zeros((), dtype=torch.int64, device=p.device)
+                state["step"] = begun[p.device]
+            else:
+                state["step"] = 0
+            if group["state_bits"] == 8:
+                blocks = -(-p.numel() // _scc.STATE_BLOCK)
+                for name in ("first", "second"):
+                    state[name] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+                    state[name + "_scales"] = torch.ones(blocks, dtype=torch.float32, device=p.device)
+            else:
+                for name in ("first", "second"):
+                    state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+        return state
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            lists, begun, raised = {}, {}, set()
+            for p in group["params"]:
+                if p.grad is None or p.numel() == 0:
+                    continue
+                state = self._begin(p, group, begun)
+                small = "first_scales" in state
+                if isinstance(state["step"], torch.Tensor):
+                    age = state["step"].data_ptr()
+                    if age not in raised:
+                        state["step"].add_(1)
+                        raised.add(age)
+                else:
+                    state["step"] += 1
+                    age = state["step"]
+                own = lists.setdefault((p.device, p.dtype, small, age), (state["step"], [], [], [], [], [], []))
+                for to, t in zip(own[1:], (p, p.grad.contiguous(), state["first"], state["second"], state.get("first_scales"), state.get("second_scales"))):
+                    to.append(t)
+            for (_, _, small, _), (step, ws, gs, ms, vs, mss, vss) in lists.items():
+                _scc.scc_adamw_step(ws, gs, ms, vs, group["lr"], step, betas=group["betas"], eps=group["eps"],
+                                    weight_decay=group["weight_decay"], first_scales=mss if small else None,
+                                    second_scales=vss if small else None, seed=group["seed"])
         return loss

@@ -26,8 +26,13 @@ SYMBOLS = ("scc_window_params", "scc_forward", "scc_forward_workspace_bytes", "s
            "scc_dw_forward_scratch", "scc_dw_forward_path", "scc_dw_forward_scratch_path",
            "scc_dw_backward_workspace_bytes", "scc_dw_backward", "scc_dw_backward_as_workspace_bytes", "scc_dw_backward_as",
            "scc_gated_forward_workspace_bytes", "scc_gated_forward_path", "scc_gated_forward", "scc_gated_backward_workspace_bytes",
-           "scc_gated_backward", "scc_orthogonal_workspace_bytes", "scc_orthogonalise", "scc_orthogonal_step", "scc_status_string")
+           "scc_gated_backward", "scc_orthogonal_workspace_bytes", "scc_orthogonalise", "scc_orthogonal_step",
+           "scc_norm_forward", "scc_norm_quantised", "scc_norm_backward_workspace_bytes", "scc_norm_backward",
+           "scc_vocabulary_loss_workspace_bytes", "scc_vocabulary_loss", "scc_vocabulary_gradients_workspace_bytes",
+           "scc_vocabulary_gradients", "scc_adamw_step", "scc_status_string")
 ACTIVATIONS = {"silu": 0, "gelu": 1}    # scc_activation of include/scc.h
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}    # scc_reduction of include/scc.h
+STATE_BLOCK = 256                       # elements of a scale of AdamW's states in 8 bits
 STATIC_SCRATCH_BYTES = 32 << 20    # SCC_STATIC_SCRATCH_BYTES of include/scc.h
 
 _lib = None
@@ -37,6 +42,10 @@ _native = None      # the module of the plain calls
 class _OrthogonalOptions(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int),
                 ("steps", ctypes.c_int), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _AdamwOptions(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [("seed", ctypes.c_uint64)]
 
 
 class SccError(RuntimeError):
@@ -124,6 +133,22 @@ def load():
         call = getattr(lib, name)
         call.argtypes = [c_int] + [vpp] * lists + [ip, ip, ctypes.POINTER(_OrthogonalOptions), c_int, c_vp, c_sz, c_vp]
         call.restype = c_int
+    c_float, c_ll = ctypes.c_float, ctypes.c_longlong
+    maps = [c_int] * 4                  # N C H W
+    lib.scc_norm_forward.argtypes = [c_vp] * 5 + maps + [c_float, c_int, c_vp]
+    lib.scc_norm_quantised.argtypes = [c_vp] * 6 + maps + [c_float, c_int, c_vp]
+    lib.scc_norm_backward_workspace_bytes.argtypes = maps + [c_int]
+    lib.scc_norm_backward_workspace_bytes.restype = c_sz
+    lib.scc_norm_backward.argtypes = [c_vp] * 7 + maps + [c_float, c_int, c_int, c_vp, c_sz, c_vp]
+    lib.scc_vocabulary_loss_workspace_bytes.argtypes = maps + [c_int] * 3
+    lib.scc_vocabulary_loss_workspace_bytes.restype = c_sz
+    lib.scc_vocabulary_loss.argtypes = [c_vp] * 5 + maps + [c_int, c_ll, c_int, c_int, c_vp, c_sz, c_vp]
+    lib.scc_vocabulary_gradients_workspace_bytes.argtypes = maps + [c_int] * 2
+    lib.scc_vocabulary_gradients_workspace_bytes.restype = c_sz
+    lib.scc_vocabulary_gradients.argtypes = [c_vp] * 7 + maps + [c_int, c_ll, c_int, c_int, c_int, c_vp, c_sz, c_vp]
+    lib.scc_adamw_step.argtypes = [c_int] + [vpp] * 6 + [ctypes.POINTER(c_ll), ctypes.POINTER(_AdamwOptions), c_ll, c_vp, c_int, c_vp]
+    for name in ("scc_norm_forward", "scc_norm_quantised", "scc_norm_backward", "scc_vocabulary_loss", "scc_vocabulary_gradients", "scc_adamw_step"):
+        getattr(lib, name).restype = c_int
     lib.scc_status_string.argtypes = [c_int]
     lib.scc_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -680,3 +705,173 @@ def scc_orthogonal_step(weights, grads, momenta, lr, momentum=0.95, weight_decay
             _moved(*weights, *momenta)
         raise
     _moved(*weights, *momenta)
+
+
+def _norm_map(x, w, residual):
+    """(device, (N, C, H, W)) of a residual norm's call."""
+    dev = _dev(x, w) if residual is None else _dev(x, w, residual)
+    if x.dim() != 4:
+        raise ValueError("x must be [N, C, H, W]")
+    if w.dtype != x.dtype or tuple(w.shape) != (x.shape[1],):
+        raise ValueError("w must be [C] with the dtype of x")
+    if residual is not None and (residual.dtype != x.dtype or residual.shape != x.shape):
+        raise ValueError("residual must have the shape and dtype of x")
+    return dev, tuple(x.shape)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def scc_norm_forward(x, w, residual=None, eps=1e-6):
+    """(y, h) of the residual norm in front of a feed-forward block: h = x + residual, y = h / sqrt(mean_c h^2 + eps) * w, over the channels of
+    [N,C,H,W]; w [C].  Without a residual h is x itself."""
+    dev, shape = _norm_map(x, w, residual)
+    y = torch.empty_like(x)
+    h = None if residual is None else torch.empty_like(x)
+    _launch(dev, load().scc_norm_forward, x.data_ptr(), _address(residual), w.data_ptr(), _address(h), y.data_ptr(), *shape, float(eps),
+            _dtype_code(x))
+    return y, x if h is None else h
+
+
+def scc_norm_quantised(x, w, residual=None, eps=1e-6):
+    """(q, scale, h): the residual norm's y in 8 bits, q (float8_e4m3fn, the shape of x) * scale (float32 [N,H,W], a power of two for each pixel)."""
+    dev, shape = _norm_map(x, w, residual)
+    q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=dev)
+    scale = torch.empty((shape[0], *shape[2:]), dtype=torch.float32, device=dev)
+    h = None if residual is None else torch.empty_like(x)
+    _launch(dev, load().scc_norm_quantised, x.data_ptr(), _address(residual), w.data_ptr(), _address(h), q.data_ptr(), scale.data_ptr(), *shape,
+            float(eps), _dtype_code(x))
+    return q, scale, x if h is None else h
+
+
+def scc_norm_backward(x, w, dy, residual=None, dh=None, eps=1e-6):
+    """(dx, dw) of scc_norm_forward: dx like x, the gradient of x and of the residual, dw [C] float32.  dh: the gradient that reaches h by itself.  In
+    float32 the h that the forward returned can stand for x and the residual."""
+    return _norm_backward(x, w, dy, residual, dh, eps, False)
+
+
+def _norm_backward(x, w, dy, residual, dh, eps, stored):
+    """scc_norm_backward; stored: dw in the type of x, rounded from the same sums."""
+    dev, shape = _norm_map(x, w, residual)
+    for t in (dy,) if dh is None else (dy, dh):
+        _dev(x, t)
+        if t.dtype != x.dtype or t.shape != x.shape:
+            raise ValueError("dy and dh must have the shape and dtype of x")
+    code = _dtype_code(x)
+    ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_norm_backward_workspace_bytes", *shape, code), dev)
+    dx = torch.empty_like(x)
+    dw = torch.empty(shape[1], dtype=x.dtype if stored else torch.float32, device=dev)
+    _launch(dev, load().scc_norm_backward, x.data_ptr(), _address(residual), w.data_ptr(), dy.data_ptr(), _address(dh), dx.data_ptr(), dw.data_ptr(),
+            *shape, float(eps), code, _CODES[dw.dtype], ws_ptr, ws_len)
+    return dx, dw
+
+
+def _reduction(reduction):
+    """The library's code of a reduction's name."""
+    if reduction not in REDUCTIONS:
+        raise ValueError("reduction must be one of %s, got %r" % (", ".join(sorted(REDUCTIONS)), reduction))
+    return REDUCTIONS[reduction]
+
+
+def _vocabulary(x, w, target, ignore_index):
+    """(device, (N, C, H, W), V, ignore_index) of a vocabulary loss's call."""
+    dev = _dev(x, w, target)
+    if x.dim() != 4:
+        raise ValueError("x must be [N, C, H, W]")
+    if w.dtype != x.dtype or w.dim() != 2 or w.shape[1] != x.shape[1]:
+        raise ValueError("w must be [V, C] with the dtype of x")
+    if target.dtype != torch.int64 or tuple(target.shape) != (x.shape[0], *x.shape[2:]):
+        raise ValueError("target must be int64 [N, H, W]")
+    return dev, tuple(x.shape), w.shape[0], int(ignore_index)
+
+
+def scc_vocabulary_loss(x, w, target, reduction="mean", ignore_index=-100):
+    """(loss, lse): -log softmax over v of sum_c x[n,c,h,w] w[v,c], at v = target[n,h,w], without the logits in memory; x [N,C,H,W], w [V,C],
+    target int64 [N,H,W].  loss: float32, [N,H,W] for "none", else one value; "mean" over the tokens whose target is not ignore_index, 0 if there
+    are none.  lse: float32 [N,H,W], for scc_vocabulary_gradients."""
+    code = _reduction(reduction)
+    dev, shape, V, ignored = _vocabulary(x, w, target, ignore_index)
+    dtype = _dtype_code(x)
+    ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_vocabulary_loss_workspace_bytes", *shape, V, code, dtype), dev)
+    lse = torch.empty(target.shape, dtype=torch.float32, device=dev)
+    loss = torch.empty(target.shape if code == 0 else (), dtype=torch.float32, device=dev)
+    _launch(dev, load().scc_vocabulary_loss, x.data_ptr(), w.data_ptr(), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), *shape, V, ignored,
+            code, dtype, ws_ptr, ws_len)
+    return loss, lse
+
+
+def scc_vocabulary_gradients(x, w, target, lse, dloss, reduction="mean", ignore_index=-100):
+    """(dx, dw) of scc_vocabulary_loss from the lse that it returned: dx like x, dw [V,C] float32; dloss: the loss's gradient, float32 of its shape."""
+    return _vocabulary_gradients(x, w, target, lse, dloss, _reduction(reduction), ignore_index, False)
+
+
+def _vocabulary_gradients(x, w, target, lse, dloss, code, ignore_index, stored):
+    """scc_vocabulary_gradients; stored: dw in the type of x, rounded from the same sums."""
+    dev, shape, V, ignored = _vocabulary(x, w, target, ignore_index)
+    _dev(x, lse, dloss)
+    if lse.dtype != torch.float32 or lse.shape != target.shape:
+        raise ValueError("lse must be float32 [N, H, W]")
+    if dloss.dtype != torch.float32 or tuple(dloss.shape) != (tuple(target.shape) if code == 0 else ()):
+        raise ValueError("dloss must be float32 with the shape of the loss")
+    dtype = _dtype_code(x)
+    ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_vocabulary_gradients_workspace_bytes", *shape, V, dtype), dev)
+    dx = torch.empty_like(x)
+    dw = torch.empty(w.shape, dtype=x.dtype if stored else torch.float32, device=dev)
+    _launch(dev, load().scc_vocabulary_gradients, x.data_ptr(), w.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), dx.data_ptr(),
+            dw.data_ptr(), *shape, V, ignored, code, dtype, _CODES[dw.dtype], ws_ptr, ws_len)
+    return dx, dw
+
+
+def _check_adamw(weights, grads, first, second, first_scales, second_scales):
+    """The device and dtype of an AdamW call whose lists fit together."""
+    if (first_scales is None) != (second_scales is None):
+        raise ValueError("first_scales and second_scales go together")
+    lists = [weights, grads, first, second] + ([first_scales, second_scales] if first_scales is not None else [])
+    if len(weights) == 0 or any(len(l) != len(weights) for l in lists):
+        raise ValueError("lists of equally many tensors are wanted, at least one")
+    dev = _dev(*(t for l in lists for t in l))
+    state = torch.float32 if first_scales is None else torch.float8_e4m3fn
+    for w, g, m, v in zip(weights, grads, first, second):
+        if g.shape != w.shape or m.shape != w.shape or v.shape != w.shape:
+            raise ValueError("a weight, its gradient and its states have the same shape")
+        if w.dtype != weights[0].dtype or g.dtype != w.dtype:
+            raise ValueError("weights and gradients of one call share their dtype")
+        if m.dtype != state or v.dtype != state:
+            raise ValueError("states are float32, or float8_e4m3fn with scales")
+    if first_scales is not None:
+        for w, ms, vs in zip(weights, first_scales, second_scales):
+            if any(s.dtype != torch.float32 or s.numel() != -(-w.numel() // STATE_BLOCK) for s in (ms, vs)):
+                raise ValueError("scales are float32, one for each %d elements of a weight" % STATE_BLOCK)
+    if _overlap([t for l in (lists[0], *lists[2:]) for t in l], grads):
+        raise ValueError("weights and states may not share memory with each other or with a gradient")
+    return dev, _dtype_code(weights[0])
+
+
+def scc_adamw_step(weights, grads, first, second, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, first_scales=None,
+                   second_scales=None, seed=0):
+    """A step of AdamW on a list of weights of any shapes, in place: m <- b1 m + (1 - b1) g, v <- b2 v + (1 - b2) g^2, w <- (1 - lr weight_decay) w -
+    lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps).  weights and grads: float32 or bfloat16, one dtype for all.  States: float32, or with
+    first_scales and second_scales (float32, one for each 256 elements of a weight) float8_e4m3fn, m = first * scale, v = (second * scale)^2,
+    rounded at random with the stored values' expectation kept: a hash of seed, step and place.  step: from 1; or an int64 tensor of one element on
+    the GPU, read when the call runs, for calls that are captured and replayed.  No weight or state may overlap another tensor of the call.  A graph that
+    saved a weight cannot be run backward afterwards, as after any change in place."""
+    dev, dtype = _check_adamw(weights, grads, first, second, first_scales, second_scales)
+    device_step = None
+    if isinstance(step, torch.Tensor):
+        if step.dtype != torch.int64 or step.numel() != 1 or step.device != dev:
+            raise ValueError("step must be a number, or an int64 tensor of one element on the weights' device")
+        device_step, step = step.data_ptr(), 1
+    count = len(weights)
+    lists = [weights, grads, first, second, first_scales, second_scales]
+    pointers = [None if l is None else (ctypes.c_void_p * count)(*[t.data_ptr() for t in l]) for l in lists]
+    sizes = (ctypes.c_longlong * count)(*[w.numel() for w in weights])
+    options = _AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, int(seed) & (2 ** 64 - 1))
+    moved = [t for l in (weights, first, second, first_scales or (), second_scales or ()) for t in l]
+    try:
+        _launch(dev, load().scc_adamw_step, count, *pointers, sizes, ctypes.byref(options), int(step), device_step, dtype)
+    except SccError as e:
+        if e.status == SCC_ERR_LAUNCH:          # in the middle of a list, perhaps
+            _moved(*moved)
+        raise
+    _moved(*moved)

@@ -1,0 +1,360 @@
+"""AdamW on lists of weights, states in 32 bits and in 8: refusals, and the kernel against 64 bits.
+
+Bars, element by element.  32 bits: a moment adds two products, three roundings of the magnitudes, 4 * 2^-24; the update is of two moments (the root
+halves an error), a root, a reciprocal, their corrections and three products at 2^-23 or less each, 16 * 2^-24 of itself, then two roundings of the
+weight.  bfloat16 weights: half a step, 2^-8 of the value, on top.  8 bits: what a step stores is compared bit by bit with the definition in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2101_00745_amd as S
+from paper_2101_00745_amd import optim
+from paper_2101_00745_amd import scc as B
+
+DTYPES = [pytest.param(torch.float32, id="f32"), pytest.param(torch.bfloat16, id="bf16")]
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+ULP = 2.0 ** -24
+LR, BETAS, EPS, DECAY = 1e-2, (0.9, 0.99), 1e-8, 0.1
+SHAPES = [(64,), (1,), (5, 3), (256,), (257,), (33, 70), (2, 40, 24), (2048,), (3000,), (100, 3, 3), (1, 4099)]
+
+
+def step64(w, g, m, v, step, lr=LR, betas=BETAS, eps=EPS, decay=DECAY):
+    """The definition in 64 bits."""
+    b1, b2 = betas
+    m, v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    update = (m / (1 - b1 ** step)) / ((v / (1 - b2 ** step)).sqrt() + eps)
+    return w * (1 - lr * decay) - lr * update, m, v, update
+
+
+def lists(shapes, dtype, seed=0, begun=True):
+    gen = torch.Generator().manual_seed(70 + seed)
+    w = [torch.randn(s, generator=gen).to(dtype) for s in shapes]
+    g = [(torch.randn(s, generator=gen) * 0.1).to(dtype) for s in shapes]
+    m = [torch.randn(s, generator=gen) * (0.05 * begun) for s in shapes]
+    v = [torch.rand(s, generator=gen) * (0.02 * begun) for s in shapes]
+    return w, g, m, v
+
+
+def on_gpu(l):
+    return [t.cuda() for t in l]
+
+
+def check_step(w, g, m, v, before, step, dtype, **options):
+    for w1, g1, m1, v1, (w0, m0, v0) in zip(w, g, m, v, before):
+        want_w, want_m, want_v, update = step64(w0.double(), g1.double().cpu(), m0.double(), v0.double(), step, **options)
+        b1, b2 = options.get("betas", BETAS)
+        size_m = b1 * m0.double().abs() + (1 - b1) * g1.double().cpu().abs()
+        assert ((m1.double().cpu() - want_m).abs() <= 4 * ULP * size_m + 1e-44).all()
+        assert ((v1.double().cpu() - want_v).abs() <= 4 * ULP * want_v + 1e-44).all()
+        lr = options.get("lr", LR)
+        # the moment's own error over the root, which may be larger than the update's where m nearly cancels
+        size = lr * (16 * ULP * update.abs() + 4 * ULP * update.abs() * (size_m / want_m.abs().clamp(min=1e-300)).clamp(max=1e6))
+        assert ((w1.double().cpu() - want_w).abs() <= size + 3 * ULP * (w0.double().abs() + lr * update.abs()) + HALF[dtype] * want_w.abs()).all()
+
+
+def test_refusals():
+    lib = S.load()
+    import ctypes
+    one = 1 << 20                               # an address that no refused call reads
+    ptr = (ctypes.c_void_p * 1)(one)
+    none = (ctypes.c_void_p * 1)(None)
+    size = (ctypes.c_longlong * 1)(5)
+
+    def call(count=1, w=ptr, g=ptr, m=ptr, v=ptr, ms=None, vs=None, sizes=size, step=1, dtype=0, options=True, **o):
+        values = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) | o
+        opts = B._AdamwOptions(*values.values(), 0)
+        return lib.scc_adamw_step(count, w, g, m, v, ms, vs, sizes, ctypes.byref(opts) if options else None, step, None, dtype, None)
+
+    for name in ("w", "g", "m", "v", "sizes"):
+        assert call(**{name: None}) == -1
+    for name in ("w", "g", "m", "v"):
+        assert call(**{name: none}) == -1
+    assert call(options=False) == -1 and call(ms=ptr) == -1 and call(vs=ptr) == -1 and call(ms=ptr, vs=none) == -1 and call(ms=none, vs=ptr) == -1
+    assert call(count=0) == -2 and call(sizes=(ctypes.c_longlong * 1)(0)) == -2 and call(sizes=(ctypes.c_longlong * 1)((1 << 40) + 1)) == -2
+    assert call(dtype=2) == -4 and call(step=0) == -8
+    for o in (dict(lr=math.nan), dict(eps=-1.0), dict(eps=math.inf), dict(beta1=1.0), dict(beta2=-0.1), dict(beta2=math.nan), dict(weight_decay=math.inf)):
+        assert call(**o) == -8
+    for bad in (dict(lr=-1.0), dict(betas=(1.0, 0.9)), dict(eps=-1.0), dict(weight_decay=-1.0), dict(state_bits=16)):
+        with pytest.raises(ValueError):
+            optim.AdamW([torch.nn.Parameter(torch.zeros(2))], **bad)
+    with pytest.raises(ValueError):
+        S.scc_adamw_step(*[[torch.zeros(2)]] * 4, 1e-3, 1)
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    w, g, m, v = [on_gpu(l) for l in lists([(30,), (300,)], torch.float32)]
+    bytes_ = [[torch.zeros(s, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for s in (30, 300)] for _ in range(2)]
+    scales = [[torch.ones(n, device="cuda") for n in (1, 2)] for _ in range(2)]
+    before = [t.clone() for l in (w, m, v) for t in l]
+    for args, more in (((w, g, m, v[:1]), {}), (([], [], [], []), {}), ((w, g[::-1], m, v), {}), ((w, [t.bfloat16() for t in g], m, v), {}),
+                       ((w, g, [t.bfloat16() for t in m], v), {}), ((w, g, m, v), dict(first_scales=scales[0])), ((w, g, m, v), dict(first_scales=scales[0], second_scales=scales[1])),
+                       ((w, g, *bytes_), {}), ((w, g, *bytes_), dict(first_scales=scales[0], second_scales=scales[1][::-1])), ((w, w, m, v), {}), ((w, g, m, m), {}),
+                       ((w, g, [w[0], m[1]], v), {}), ((w, g, m, v), dict(step=torch.ones((), device="cuda"))), ((w, g, m, v), dict(step=torch.ones((), dtype=torch.int64))),
+                       (([w[0][::2]], [g[0][::2]], [m[0][::2]], [v[0][::2]]), {})):
+        with pytest.raises((ValueError, TypeError)):
+            S.scc_adamw_step(*args, LR, **({"step": 1} | more))
+    with pytest.raises(S.SccError):
+        S.scc_adamw_step(w, g, m, v, LR, 0)
+    assert all(torch.equal(a, b) for a, b in zip(before, [t for l in (w, m, v) for t in l]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_steps_in_32_bits(dtype):
+    shapes = SHAPES * 13                        # more than two launches' worth
+    w, g, m, v = [on_gpu(l) for l in lists(shapes, dtype)]
+    for step in (1, 2, 1000):
+        before = [(a.cpu(), b.cpu(), c.cpu()) for a, b, c in zip(w, m, v)]
+        versions = [t._version for t in (*w, *m, *v)]
+        S.scc_adamw_step(w, g, m, v, LR, step, betas=BETAS, eps=EPS, weight_decay=DECAY)
+        assert all(t._version > n for t, n in zip((*w, *m, *v), versions))
+        check_step(w, g, m, v, before, step, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_options(dtype):
+    for options in (dict(betas=(0.0, 0.0)), dict(eps=1e-2), dict(lr=0.0), dict(decay=0.0), dict(lr=1.0, decay=1.0), dict(betas=(0.99, 0.99999))):
+        w, g, m, v = [on_gpu(l) for l in lists([(300,), (40, 7)], dtype, begun=False)]
+        before = [(a.cpu(), b.cpu(), c.cpu()) for a, b, c in zip(w, m, v)]
+        merged = dict(lr=LR, betas=BETAS, eps=EPS, decay=DECAY) | options
+        S.scc_adamw_step(w, g, m, v, merged["lr"], 1, betas=merged["betas"], eps=merged["eps"], weight_decay=merged["decay"])
+        check_step(w, g, m, v, before, 1, dtype, **merged)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_unaligned_weights(dtype):
+    w, g, m, v = [on_gpu(l) for l in lists([(1000,)], dtype)]
+    at = []
+    for l in (w, g, m, v):
+        room = torch.zeros(1003, dtype=l[0].dtype, device="cuda")
+        room[1:1001] = l[0]
+        at.append(room)
+    S.scc_adamw_step(*[[r[1:1001]] for r in at], LR, 3)
+    S.scc_adamw_step(w, g, m, v, LR, 3)
+    for l, r in zip((w, m, v), (at[0], at[2], at[3])):
+        assert torch.equal(l[0], r[1:1001]) and (r[[0, 1001, 1002]] == 0).all()
+
+
+# ---- states in 8 bits ----
+
+def mix(x):
+    x = x.astype(np.uint32)
+    x = (x ^ (x >> np.uint32(16))) * np.uint32(0x6A09E667)
+    x = (x ^ (x >> np.uint32(15))) * np.uint32(0xBB67AE85)
+    return x ^ (x >> np.uint32(16))
+
+
+def word(v):
+    return np.array([v & 0xffffffff], dtype=np.uint64).astype(np.uint32)
+
+
+def hashed(n, seed, step, index):
+    first = mix(word((seed & 0xffffffff) + (seed >> 32) * 0x85157AF5 + step * 0x9E3779B1))
+    key = mix(word(int(first[0]) + index * 0x9E3779B1))
+    return mix((np.arange(n, dtype=np.uint64) + np.uint64(key[0])).astype(np.uint32)).astype(np.int64)
+
+
+GRID = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float().double().numpy()       # 0 .. 448
+
+
+def stored(t, second, random):
+    """(codes' values, scales) of new moments t (float32, flat), by the definition."""
+    n = t.size
+    blocks = np.pad(t.astype(np.float64), (0, -n % 256)).reshape(-1, 256)
+    most = np.abs(blocks).max(1)
+    e = np.frexp(most)[1] - 1
+    k = np.where(most > 0, np.clip((e >> 1 if second else e) - 7, -100, 120), -100)
+    scales = np.exp2(k.astype(np.float64))
+    a = np.abs(blocks / scales[:, None] ** (2 if second else 1)).reshape(-1)[:n]
+    values = GRID * GRID if second else GRID
+    low = np.searchsorted(values, a, side="right") - 1
+    span = values[low + 1] - values[low]
+    if second:
+        up = (random >> 8) * 2.0 ** -24 * span < a - values[low]
+        up |= (low == 0) & (a > 0)
+    else:
+        up = (((random & 0xffff) << 4 | 8) + np.floor((a - values[low]) / span * 2.0 ** 20).astype(np.int64)) >> 20 > 0
+    return GRID[low + up] * np.where(t < 0, -1.0, 1.0), scales
+
+
+def moments32(g, m, v, betas):
+    """The new moments in binary32, rounded operation by operation."""
+    f = np.float32
+    m = m * f(betas[0]) + g * f(1.0 - betas[0])
+    return m, v * f(betas[1]) + (g * g) * f(1.0 - betas[1])
+
+
+def bytes_of(shapes):
+    first, second = [[torch.zeros(s, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for s in shapes] for _ in range(2)]
+    scales = [[torch.ones(-(-math.prod(s) // 256), device="cuda") for s in shapes] for _ in range(2)]
+    return first, second, scales
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_steps_in_8_bits(dtype):
+    """Three steps of all shapes, a wide range of gradients in some of them: codes, scales and weights."""
+    shapes, seed = SHAPES * 6, 12345678901234
+    w, g, _, _ = [on_gpu(l) for l in lists(shapes, dtype, seed=1)]
+    for i in range(0, len(g), 2):
+        g[i].mul_(torch.exp2(torch.randint(-30, 8, g[i].shape, device="cuda").float()).to(dtype))
+    first, second, (fs, ss) = bytes_of(shapes)
+    for step in (1, 2, 3):
+        before = [(a.double().cpu(), b.float().cpu().numpy(), c.float().cpu().numpy(), d.cpu().numpy(), e.cpu().numpy())
+                  for a, b, c, d, e in zip(w, first, second, fs, ss)]
+        S.scc_adamw_step(w, g, first, second, LR, step, betas=BETAS, eps=EPS, weight_decay=DECAY, first_scales=fs, second_scales=ss, seed=seed)
+        for i, (w0, m0, v0, ms, vs) in enumerate(before):
+            n = m0.size
+            at = np.arange(n) // 256
+            g32 = g[i].float().cpu().numpy().reshape(-1)
+            m32, v32 = moments32(g32, m0.reshape(-1) * ms[at], (v0.reshape(-1) * vs[at]) ** 2, BETAS)
+            random = hashed(n, seed, step, i)
+            for got, got_scales, t, square in ((first[i], fs[i], m32, False), (second[i], ss[i], v32, True)):
+                values, scales = stored(t, square, random)
+                assert np.array_equal(got_scales.cpu().numpy().astype(np.float64), scales)
+                assert np.array_equal(got.float().cpu().numpy().reshape(-1).astype(np.float64), values)
+            want, _, _, update = step64(w0.reshape(-1), torch.from_numpy(g32).double(), torch.from_numpy(m0.reshape(-1) * ms[at]).double(),
+                                        torch.from_numpy((v0.reshape(-1) * vs[at]) ** 2).double(), step)
+            size_m = torch.from_numpy(np.abs(m0.reshape(-1) * ms[at]) + np.abs(g32)).double()
+            bar = LR * (24 * ULP * update.abs() + 8 * ULP * size_m / torch.from_numpy(np.sqrt(v32 / (1 - BETAS[1] ** step)) + EPS).double())
+            got = w[i].double().cpu().reshape(-1)
+            assert ((got - want).abs() <= bar + 3 * ULP * (w0.reshape(-1).abs() + LR * update.abs()) + HALF[dtype] * want.abs()).all()
+
+
+@pytest.mark.gpu
+def test_what_is_stored_in_8_bits_has_the_right_expectation():
+    """Without a gradient the states decay by b a step; of 2^20 equal ones, whose steps of e4m3 are coarse, the mean has to follow.  A mean of n
+    roundings of spread s is off by s / sqrt(n): six of those, with s an eighth of the value (a quarter for v) after each step."""
+    n, m0, v0 = 1 << 20, 0.37, 0.0123
+    betas, steps = (0.97, 0.999), 40
+    w, g = [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")]
+    first, second, (fs, ss) = bytes_of([(n,)])
+    fs[0].fill_(2.0 ** -8)
+    ss[0].fill_(2.0 ** -9)
+    code = torch.tensor([m0 * 2 ** 8, math.sqrt(v0) * 2 ** 9]).to(torch.float8_e4m3fn)
+    first[0].copy_(code[0].expand(n))
+    second[0].copy_(code[1].expand(n))
+    start = [float(code[0].float()) * 2.0 ** -8, (float(code[1].float()) * 2.0 ** -9) ** 2]
+    # one large element a block keeps its scale where it is
+    first[0].view(torch.uint8)[::256] = 0x70
+    second[0].view(torch.uint8)[::256] = 0x70
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[::256] = False
+    for step in range(1, steps + 1):
+        S.scc_adamw_step(w, g, first, second, 0.0, step, betas=betas, first_scales=fs, second_scales=ss, seed=9)
+    blocks = torch.arange(n, device="cuda") // 256
+    m = (first[0].float() * fs[0][blocks]).double()[rest]
+    v = (second[0].float() * ss[0][blocks]).double().square()[rest]
+    for got, begin, beta, spread in ((m, start[0], betas[0], 0.125), (v, start[1], betas[1], 0.25)):
+        want = begin * beta ** steps
+        assert abs(float(got.mean()) - want) <= 6 * spread * begin * math.sqrt(steps / n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_values_that_are_not_finite_stay_with_their_element(dtype):
+    shape = (600,)
+    for small in (False, True):
+        w, g, m, v = [on_gpu(l) for l in lists([shape], dtype, seed=3)]
+        w2, g2, m2, v2 = [[t.clone() for t in l] for l in (w, g, m, v)]
+        g2[0][5], g2[0][300] = math.nan, math.inf
+        more = [{}, {}]
+        if small:
+            sides = [bytes_of([shape]) for _ in range(2)]
+            (m, v, s), (m2, v2, s2) = sides
+            more = [dict(first_scales=x[0], second_scales=x[1]) for x in (s, s2)]
+        S.scc_adamw_step(w, g, m, v, LR, 2, **more[0])
+        S.scc_adamw_step(w2, g2, m2, v2, LR, 2, **more[1])
+        fine = torch.ones(600, dtype=torch.bool, device="cuda")
+        fine[[5, 300]] = False
+        assert torch.isnan(w2[0][~fine]).all() and torch.equal(w2[0][fine], w[0][fine])
+        assert not torch.isfinite(m2[0].float()[~fine]).any()
+        if not small:
+            assert torch.equal(m2[0][fine], m[0][fine]) and torch.equal(v2[0][fine], v[0][fine])
+        else:
+            assert torch.isfinite(m2[0].float()[fine]).all() and torch.isfinite(s2[0][0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_optimiser(dtype, bits):
+    """The class against calls by hand, with a weight that gets its first gradient late; saved and loaded in between."""
+    shapes = [(40, 24), (7,), (12, 3, 3), (300,)]
+    params = [torch.nn.Parameter(torch.randn(s, device="cuda").to(dtype)) for s in shapes]
+    by_hand = [p.detach().clone() for p in params]
+    opt = optim.AdamW(params, lr=LR, betas=BETAS, weight_decay=DECAY, state_bits=bits, seed=4)
+    states = []
+    for s in shapes:
+        first, second, scales = bytes_of([s])
+        states.append((first[0], second[0], scales[0][0], scales[1][0]) if bits == 8 else (torch.zeros(s, device="cuda"), torch.zeros(s, device="cuda")))
+    ages = [0] * 4
+    for step in range(5):
+        grads = [torch.randn(s, device="cuda").to(dtype) for s in shapes]
+        if step == 3:
+            saved = opt.state_dict()
+            opt = optim.AdamW(params, lr=1.0)
+            opt.load_state_dict(saved)
+        cohorts = {}
+        for i, (p, grad) in enumerate(zip(params, grads)):
+            p.grad = None if i == 1 and step < 2 else grad
+            if p.grad is not None:
+                ages[i] += 1
+                cohorts.setdefault(ages[i], []).append(i)
+        opt.step()
+        for age, members in cohorts.items():
+            pick = lambda k: [states[i][k] for i in members]  # noqa: E731
+            more = dict(first_scales=pick(2), second_scales=pick(3)) if bits == 8 else {}
+            S.scc_adamw_step([by_hand[i] for i in members], [grads[i] for i in members], pick(0), pick(1), LR, age, betas=BETAS, weight_decay=DECAY, seed=4, **more)
+        for p, h in zip(params, by_hand):
+            assert torch.equal(p.detach(), h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_captured(bits):
+    """A captured step counts on; a replay is the step that an eager call makes."""
+    shapes = [(500,), (33, 20)]
+    a, b = ([torch.nn.Parameter(torch.ones(s, device="cuda")) for s in shapes] for _ in range(2))
+    captured, eager = (optim.AdamW(l, lr=LR, state_bits=bits, seed=2, capturable=c) for l, c in ((a, True), (b, False)))
+    grads = [torch.randn(s, device="cuda") for s in shapes]
+    for l in (a, b):
+        for p, g in zip(l, grads):
+            p.grad = g.clone()
+    captured.step()
+    eager.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.step()
+    for i in range(4):
+        for p, q in zip(a, b):
+            fresh = torch.randn_like(p)
+            p.grad.copy_(fresh)
+            q.grad.copy_(fresh)
+        graph.replay()
+        eager.step()
+        torch.cuda.synchronize()
+        for p, q in zip(a, b):
+            # the corrections come from the host's functions here and from the device's there: two roundings of the update
+            assert ((p - q).abs() <= (i + 2) * 4 * LR * 4 * ULP + 4 * ULP * q.abs()).all()
+    assert int(captured.state[a[0]]["step"]) == 5 and captured.state[a[0]]["step"] is captured.state[a[1]]["step"]
+    saved = captured.state_dict()
+    other = optim.AdamW(a, lr=1.0, capturable=True)
+    other.load_state_dict(saved)
+    assert other.state[a[0]]["step"] is other.state[a[1]]["step"] and int(other.state[a[0]]["step"]) == 5
+
+
+@pytest.mark.gpu
+def test_a_graph_over_moved_weights_is_an_error():
+    w = torch.nn.Parameter(torch.randn(8, device="cuda"))
+    opt = optim.AdamW([w], lr=LR)
+    loss = w.square().sum()
+    loss.backward(retain_graph=True)
+    opt.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()

@@ -1,0 +1,269 @@
+"""The residual norm h = x + r, y = h / sqrt(mean_c h^2 + eps) * w: the formula of its gradient on the CPU (64 bits, against differences), its
+refusals, and the kernels against it.
+
+Bars, element by element.  Binary32: a sum over C channels is a tree below a lane's few dozen terms (at most 128 of them, or C / 1024 where a lane
+has more), so the root is off by at most (128 / 2 + 8) 2^-24 of itself, and four more roundings follow: 80 * 2^-24 of the magnitudes that an
+element adds up.  bfloat16: half a step, 2^-8 of the value, on top.  dw is a sum of T terms at the same bar, with T / 64 + 64 for the 128.  8 bits: half a step
+of e4m3, 2^-4 of the value, or 2^-10 of the scale below its normal range."""
+import math
+
+import pytest
+import torch
+
+import paper_2101_00745_amd as S
+from paper_2101_00745_amd import nn as N
+from paper_2101_00745_amd import scc as B
+
+DTYPES = [pytest.param(torch.float32, id="f32"), pytest.param(torch.bfloat16, id="bf16")]
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+NEAR = 80 * 2.0 ** -24
+EPS = 1e-6
+
+
+def forward(x, r, w, eps=EPS):
+    """(y, h) in 64 bits."""
+    h = x if r is None else x + r
+    return h * w.view(1, -1, 1, 1) / torch.sqrt((h * h).mean(1, keepdim=True) + eps), h
+
+
+def backward(h, w, dy, dh, eps=EPS):
+    """(dx, dw) and the magnitudes that each adds up."""
+    rstd = 1.0 / torch.sqrt((h * h).mean(1, keepdim=True) + eps)
+    a, hat = dy * w.view(1, -1, 1, 1), h * rstd
+    extra = torch.zeros_like(h) if dh is None else dh
+    dx = extra + rstd * (a - hat * (a * hat).mean(1, keepdim=True))
+    dx_size = extra.abs() + rstd * (a.abs() + hat.abs() * (a * hat).abs().mean(1, keepdim=True))
+    return dx, (dy * hat).sum((0, 2, 3)), dx_size, (dy * hat).abs().sum((0, 2, 3))
+
+
+def inputs(shape, dtype, residual=True, seed=0):
+    gen = torch.Generator().manual_seed(100 + seed)
+    N_, C, H, W = shape
+    x, r, dy, dh = (torch.randn(shape, generator=gen).to(dtype) for _ in range(4))
+    w = (1.0 + 0.3 * torch.randn(C, generator=gen)).to(dtype)
+    return x, (r * 2.0 if residual else None), w, dy, (dh if residual else None)
+
+
+def near(got, want, size, dtype, bar=NEAR):
+    got = got.double().cpu()
+    assert got.shape == want.shape
+    off = (got - want).abs() - (bar * size + HALF[dtype] * want.abs())
+    assert not torch.isnan(got).any() and float(off.max()) <= 1e-37, "%g over the bar" % float(off.max())
+
+
+def cuda(*ts):
+    return [None if t is None else t.cuda() for t in ts]
+
+
+def test_gradient_formula_against_differences():
+    gen = torch.Generator().manual_seed(3)
+    x, dy, dh = (torch.randn(2, 7, 3, 2, generator=gen, dtype=torch.float64) for _ in range(3))
+    w = torch.randn(7, generator=gen, dtype=torch.float64)
+    dx, dw, _, _ = backward(x, w, dy, dh, eps=0.1)
+    loss = lambda x, w: float((forward(x, None, w, eps=0.1)[0] * dy).sum() + (x * dh).sum())  # noqa: E731
+    step = 1e-5                                 # error of a central difference: step^2 and 2^-53 / step, some 1e-10 each
+    for t, grad in ((x, dx), (w, dw)):
+        d = torch.randn(t.shape, generator=gen, dtype=torch.float64)
+        ends = [loss(*((t + s * step * d, w) if t is x else (x, t + s * step * d))) for s in (1, -1)]
+        assert abs((ends[0] - ends[1]) / (2 * step) - float((grad * d).sum())) <= 1e-7 * max(1.0, abs(float((grad * d).sum())))
+
+
+def test_refusals():
+    lib = S.load()
+    one = 1 << 20                               # an address that no refused call reads
+    for sizes in ((0, 4, 1, 1), (1, 0, 1, 1), (1, 4, 0, 1), (1, 4, 1, 0), (1 << 16, 1, 1 << 15, 1), (1, 1, 1 << 16, 1 << 16)):
+        assert lib.scc_norm_forward(one, None, one, None, one, *sizes, 1e-6, 0, None) == -2
+        assert lib.scc_norm_backward_workspace_bytes(*sizes, 0) == 0
+    for eps in (0.0, -1.0, math.inf, math.nan):
+        assert lib.scc_norm_forward(one, None, one, None, one, 1, 4, 1, 1, eps, 0, None) == -8
+    assert lib.scc_norm_forward(one, None, one, None, one, 1, 4, 1, 1, 1e-6, 2, None) == -4
+    assert lib.scc_norm_forward(None, None, one, None, one, 1, 4, 1, 1, 1e-6, 0, None) == -1
+    assert lib.scc_norm_forward(one, None, one, one, one, 1, 4, 1, 1, 1e-6, 0, None) == -1       # h without a residual
+    assert lib.scc_norm_quantised(one, None, one, None, one, None, 1, 4, 1, 1, 1e-6, 0, None) == -1
+    assert lib.scc_norm_backward(one, None, one, None, None, one, one, 1, 4, 1, 1, 1e-6, 0, 0, one, 1 << 20, None) == -1
+    assert lib.scc_norm_backward(one, None, one, one, None, one, one, 1, 4, 1, 1, 1e-6, 0, 1, one, 1 << 20, None) == -4
+    need = lib.scc_norm_backward_workspace_bytes(1, 4, 1, 1, 0)
+    assert need > 0
+    for ws, size in ((None, need), (one, need - 1), (one + 8, need)):
+        assert lib.scc_norm_backward(one, None, one, one, None, one, one, 1, 4, 1, 1, 1e-6, 0, 0, ws, size, None) == -5
+    with pytest.raises(ValueError):
+        S.scc_norm_forward(torch.zeros(1, 4, 1, 1), torch.ones(4))          # not on the GPU
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    x, w = torch.zeros(2, 4, 3, 1, device="cuda"), torch.ones(4, device="cuda")
+    for bad in ((x[0], w), (x, w[:3]), (x, w.bfloat16()), (x.permute(0, 2, 1, 3), w), (x, w, x[:1]), (x, w, x.bfloat16())):
+        with pytest.raises((ValueError, TypeError)):
+            S.scc_norm_forward(*bad)
+    with pytest.raises(TypeError):
+        S.scc_norm_forward(x.half(), w.half())
+    with pytest.raises(S.SccError):
+        S.scc_norm_forward(x, w, eps=0.0)
+    with pytest.raises(ValueError):
+        S.scc_norm_backward(x, w, x[:1])
+    with pytest.raises(ValueError):
+        S.scc_norm_backward(x, w, x, dh=x[:1])
+
+
+# (N, C, H, W): rows of every width of group and off the vectors, columns of every width
+SHAPES = [(1, 512, 1, 1), (5, 1, 1, 1), (3, 7, 1, 1), (70, 8, 1, 1), (33, 100, 1, 1), (9, 257, 1, 1), (300, 512, 1, 1), (2, 1030, 1, 1), (17, 2048, 1, 1),
+          (3, 5003, 1, 1), (2, 12000, 1, 1), (1, 40001, 1, 1), (2000, 64, 1, 1), (2, 3, 2, 1), (3, 16, 2, 2), (2, 60, 7, 1), (4, 33, 3, 3), (1, 128, 8, 1),
+          (2, 130, 5, 3), (3, 512, 7, 7), (2, 200, 1, 33), (2, 513, 50, 1), (2, 1000, 9, 2), (1, 1500, 11, 1), (1, 3000, 4, 4), (64, 24, 16, 16), (1, 5, 300, 7),
+          (2, 96, 1000, 1)]
+IDS = ["x".join(map(str, s)) for s in SHAPES]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_forward_and_gradients(shape, dtype):
+    for residual in (True, False):
+        x, r, w, dy, dh = inputs(shape, dtype, residual)
+        y, h = S.scc_norm_forward(*cuda(x, w, r), eps=EPS)
+        want_y, want_h = forward(x.double(), None if r is None else r.double(), w.double())
+        near(y, want_y, want_y.abs(), dtype)
+        near(h, want_h, want_h.abs(), dtype)
+        dx, dw = S.scc_norm_backward(*cuda(x, w, dy, r, dh), eps=EPS)
+        want_dx, want_dw, dx_size, dw_size = backward(want_h, w.double(), dy.double(), None if dh is None else dh.double())
+        near(dx, want_dx, dx_size, dtype)
+        tokens = shape[0] * shape[2] * shape[3]
+        near(dw, want_dw, dw_size, torch.float32, (tokens / 64 + 160) * 2.0 ** -24)
+        assert dw.dtype == torch.float32
+        again = S.scc_norm_backward(*cuda(x, w, dy, r, dh), eps=EPS)
+        assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+        stored = B._norm_backward(*cuda(x, w, dy, r, dh), EPS, True)
+        assert torch.equal(stored[0], dx) and torch.equal(stored[1], dw.to(dtype))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_eight_bits(shape, dtype):
+    x, r, w, _, _ = inputs(shape, dtype, seed=1)
+    q, scale, h = S.scc_norm_quantised(*cuda(x, w, r), eps=EPS)
+    y, _ = forward(x.double(), r.double(), w.double())
+    assert q.dtype == torch.float8_e4m3fn and scale.shape == (shape[0], *shape[2:])
+    scale = scale.double().cpu().unsqueeze(1)
+    most = y.abs().amax(1, keepdim=True)
+    assert torch.equal(torch.exp2(torch.round(torch.log2(scale))), scale)
+    assert ((most * (1 - 2 * NEAR) <= 448 * scale) & (most * (1 + 2 * NEAR) > 224 * scale)).all()
+    got = q.float().double().cpu() * scale
+    assert ((got - y).abs() <= y.abs() * (2.0 ** -4 + 2 * NEAR) + scale * 2.0 ** -10).all()
+    assert torch.equal(h, S.scc_norm_forward(*cuda(x, w, r), eps=EPS)[1])
+    # the values are those of torch's own conversion, but where y is within an error of the middle of two
+    own = (y / scale).float().to(torch.float8_e4m3fn)
+    assert (own.view(torch.uint8) != q.view(torch.uint8).cpu()).double().mean() <= 1e-4 + 2.0 / y.numel()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(6, 40, 1, 1), (2, 40, 3, 1), (3, 700, 1, 1), (2, 300, 9, 1)])
+def test_large_and_empty_tokens(shape, dtype):
+    """Squares that leave binary32, tokens of zeros (a padded batch), and values that are not finite stay with their token."""
+    x, r, w, dy, dh = inputs(shape, dtype, seed=2)
+    big = torch.tensor(2.0 ** 100).to(dtype)
+    x[1] *= big
+    r[1] *= big
+    x[0, :, 0, 0] = 0
+    r[0, :, 0, 0] = 0
+    y, h = S.scc_norm_forward(*cuda(x, w, r), eps=EPS)
+    want, _ = forward(x.double(), r.double(), w.double())
+    near(y, want, want.abs(), dtype)
+    assert (y[0, :, 0, 0] == 0).all()
+    dx, dw = S.scc_norm_backward(*cuda(x, w, dy, r, dh), eps=EPS)
+    want_dx, want_dw, dx_size, dw_size = backward(x.double() + r.double(), w.double(), dy.double(), dh.double())
+    near(dx, want_dx, dx_size, dtype)
+    near(dw, want_dw, dw_size, torch.float32, 200 * 2.0 ** -24)
+    q, scale, _ = S.scc_norm_quantised(*cuda(x, w, r), eps=EPS)
+    assert (q[0, :, 0, 0].float() == 0).all() and float(scale[0, 0, 0]) == 1.0
+    assert torch.isfinite(q.float()).all() and torch.isfinite(scale).all()
+    clean = y.clone()
+    x[1, 3, 0, 0], x[0, 2, -1, 0] = math.nan, math.inf
+    y, _ = S.scc_norm_forward(*cuda(x, w, r), eps=EPS)
+    if shape[2] == 1:
+        assert torch.isnan(y[1]).all() and torch.isnan(y[0, 2]).all()
+        assert torch.equal(y[2:], clean[2:])
+    else:
+        assert torch.isnan(y[1, :, 0]).all() and torch.equal(y[1, :, 1:], clean[1, :, 1:]) and torch.equal(y[0, :, :-1], clean[0, :, :-1])
+    q, _, _ = S.scc_norm_quantised(*cuda(x, w, r), eps=EPS)
+    assert torch.isnan(q[1, :, 0].float()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(50, 96, 1, 1), (3, 96, 20, 1)])
+def test_autograd(shape, dtype):
+    x, r, w, dy, dh = cuda(*inputs(shape, dtype, seed=4))
+    leaves = [t.clone().requires_grad_() for t in (x, r, w)]
+    y, h = N.residual_norm(leaves[0], leaves[2], leaves[1], EPS)
+    torch.autograd.backward((y, h), (dy, dh))
+    kept = (h.detach(), w, dy, None) if dtype == torch.float32 else (x, w, dy, r)
+    dx, dw = B._norm_backward(*kept, dh, EPS, True)
+    assert torch.equal(leaves[0].grad, dx) and torch.equal(leaves[1].grad, dx) and torch.equal(leaves[2].grad, dw)
+    assert leaves[0].grad.data_ptr() != leaves[1].grad.data_ptr()
+    # one of the two outputs alone, no residual, gradients that are not dense
+    y, h = N.residual_norm(leaves[0], leaves[2], leaves[1], EPS)
+    got = torch.autograd.grad(y, leaves, dy, retain_graph=True)
+    assert torch.equal(got[0], S.scc_norm_backward(*kept, eps=EPS)[0])
+    got = torch.autograd.grad(h, leaves, dh.transpose(0, 1).contiguous().transpose(0, 1))
+    assert torch.equal(got[0], dh) and (got[2] == 0).all()
+    y, h = N.residual_norm(leaves[0], leaves[2], eps=EPS)
+    assert h is leaves[0]
+    assert torch.equal(torch.autograd.grad(y, leaves[0], dy)[0], S.scc_norm_backward(x, w, dy, eps=EPS)[0])
+    y, h = N.residual_norm(leaves[0], leaves[2], leaves[1], EPS)
+    grads = torch.autograd.grad((y, h), leaves, (dy, dh), create_graph=True)
+    for g in grads:
+        with pytest.raises(RuntimeError, match="second derivative"):
+            g.sum().backward(retain_graph=True)
+    module = N.ResidualNorm(shape[1], eps=EPS, dtype=dtype)
+    with torch.no_grad():
+        module.weight.copy_(w)
+    assert torch.equal(module(x, r)[0], S.scc_norm_forward(x, w, r, EPS)[0])
+
+
+@pytest.mark.gpu
+def test_unaligned_and_long():
+    """Views that begin anywhere, and a map whose offsets pass 32 bits."""
+    x, r, w, dy, dh = inputs((4, 64, 1, 1), torch.bfloat16, seed=5)
+    flat = torch.zeros(3 * 257, dtype=torch.bfloat16, device="cuda")
+    at = [flat[1:257].view(4, 64, 1, 1), flat[258:514].view(4, 64, 1, 1), flat[515:771].view(4, 64, 1, 1)]
+    for t, v in zip(at, (x, r, dy)):
+        t.copy_(v)
+    y, h = S.scc_norm_forward(at[0], w.cuda(), at[1], EPS)
+    assert torch.equal(y, S.scc_norm_forward(*cuda(x, w, r), eps=EPS)[0])
+    assert torch.equal(S.scc_norm_backward(at[0], w.cuda(), at[2], at[1], eps=EPS)[0], S.scc_norm_backward(*cuda(x, w, dy, r), eps=EPS)[0])
+    big = torch.empty(1, 70000, 1 << 15, 1, dtype=torch.bfloat16, device="cuda")
+    big.fill_(1.0)
+    big[0, 69999, -1] = 5.0
+    y, _ = S.scc_norm_forward(big, torch.ones(70000, dtype=torch.bfloat16, device="cuda"), eps=EPS)
+    del big
+    assert float(y[0, 0, 0, 0]) == 1.0 and abs(float(y[0, 69999, -1, 0]) - 5.0) < 0.05
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(40, 96, 1, 1), (2, 200, 33, 1)])
+def test_captured_and_on_another_stream(shape):
+    x, r, w, dy, dh = cuda(*inputs(shape, torch.bfloat16, seed=6))
+    want_y, want_h = S.scc_norm_forward(x, w, r, EPS)
+    want = S.scc_norm_backward(x, w, dy, r, dh, EPS)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y, h = S.scc_norm_forward(x, w, r, EPS)
+        got = S.scc_norm_backward(x, w, dy, r, dh, EPS)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want_y) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, h = S.scc_norm_forward(x, w, r, EPS)
+        q = S.scc_norm_quantised(x, w, r, EPS)
+        got = S.scc_norm_backward(x, w, dy, r, dh, EPS)
+    for i in range(3):
+        x.copy_(torch.randn_like(x.float()))
+        want_y, want_h = S.scc_norm_forward(x, w, r, EPS)
+        want, want_q = S.scc_norm_backward(x, w, dy, r, dh, EPS), S.scc_norm_quantised(x, w, r, EPS)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want_y) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(q[0].view(torch.uint8), want_q[0].view(torch.uint8)) and torch.equal(q[1], want_q[1])
