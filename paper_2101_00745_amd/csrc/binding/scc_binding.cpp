@@ -13,6 +13,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <ATen/ops/zeros_like.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -648,6 +649,415 @@ PyObject* orthogonal_step(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- residual norm ----
+
+// Gradients of a norm or a vocabulary loss under create_graph, as a function of all that they were computed from (x again for what there is not)
+struct FirstOrderOf : torch::autograd::Function<FirstOrderOf> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext*, const at::Tensor& dx, const at::Tensor& dw,
+                                                  const at::Tensor&, const at::Tensor&, const at::Tensor&, const at::Tensor&, const at::Tensor&)
+    {
+        return {dx.detach(), dw.detach()};
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, torch::autograd::variable_list)
+    {
+        TORCH_CHECK(false, "sliding-channel convolution has no second derivative");
+    }
+};
+
+// f(a, b, c, ...) of scc.py, for what is not plain in a backward pass; the interpreter's lock is not held
+template <typename F>
+std::vector<at::Tensor> from_python(const char* name, F&& arguments)
+{
+    struct Locked {
+        PyGILState_STATE s = PyGILState_Ensure();
+        ~Locked() { PyGILState_Release(s); }
+    } locked;
+    std::vector<at::Tensor> g;
+    PyObject* m = PyImport_ImportModule("paper_2101_00745_amd.scc");
+    PyObject* f = m ? PyObject_GetAttrString(m, name) : nullptr;
+    PyObject* a = f ? arguments() : nullptr;
+    PyObject* r = a ? PyObject_CallObject(f, a) : nullptr;
+    for (int i = 0; r && i < 2; ++i) g.push_back(THPVariable_Unpack(PyTuple_GetItem(r, i)));
+    Py_XDECREF(r);
+    Py_XDECREF(a);
+    Py_XDECREF(f);
+    Py_XDECREF(m);
+    if (g.empty()) {
+        python_error e;
+        e.persist();
+        throw e;
+    }
+    return g;
+}
+
+PyObject* wrapped(const at::Tensor& t)
+{
+    if (t.defined()) return THPVariable_Wrap(t);
+    Py_RETURN_NONE;
+}
+
+bool no_modes() { return !c10::impl::TorchDispatchModeTLS::any_modes_set() && at::impl::PythonTorchFunctionTLS::stack_len() == 0; }
+
+bool wants_gradient(const at::Tensor& t) { return t.requires_grad() && !t.is_inference() && !t._fw_grad(0).defined(); }
+
+struct Map {
+    int N, C, H, W;
+    scc_dtype dtype;
+};
+
+// residual: undefined where there is none
+bool norm_map(const at::Tensor& x, const at::Tensor& w, const at::Tensor& residual, Map* m)
+{
+    if (!plain(x) || !plain(w, x) || x.dim() != 4 || w.dim() != 1 || !fits(x) || w.size(0) != x.size(1)) return false;
+    if (residual.defined() && (!plain(residual, x) || residual.sizes() != x.sizes())) return false;
+    *m = {(int)x.size(0), (int)x.size(1), (int)x.size(2), (int)x.size(3), x.scalar_type() == at::kFloat ? SCC_F32 : SCC_BF16};
+    return true;
+}
+
+struct NormCall {
+    const at::Tensor *x, *w;
+    at::Tensor residual;
+    float eps;
+    Map m;
+};
+
+// (x, w, residual or None, eps)
+bool norm_call(PyObject* const* a, Py_ssize_t n, NormCall* c)
+{
+    if (n != 4 || !no_modes() || !THPVariable_CheckExact(a[0]) || !THPVariable_CheckExact(a[1]) || !PyFloat_CheckExact(a[3])) return false;
+    c->x = &THPVariable_Unpack(a[0]);
+    c->w = &THPVariable_Unpack(a[1]);
+    if (a[2] != Py_None) {
+        if (!THPVariable_CheckExact(a[2])) return false;
+        c->residual = THPVariable_Unpack(a[2]);
+    }
+    c->eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    return norm_map(*c->x, *c->w, c->residual, &c->m);
+}
+
+// y and h (undefined without a residual); none where the call failed
+std::vector<at::Tensor> norm_forward_of(const at::Tensor& x, const at::Tensor& w, const at::Tensor& residual, float eps, const Map& m)
+{
+    at::Tensor y = at::empty(x.sizes(), x.options()), h = residual.defined() ? at::empty(x.sizes(), x.options()) : at::Tensor();
+    const int rc = launch(x, [&](void* st) {
+        return scc_norm_forward(x.data_ptr(), address(residual), w.data_ptr(), address(h), y.data_ptr(), m.N, m.C, m.H, m.W, eps, m.dtype, st);
+    });
+    if (rc != SCC_OK) return {};
+    return {y, h};
+}
+
+PyObject* norm_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    NormCall c;
+    if (!norm_call(args, n, &c)) Py_RETURN_NONE;
+    const std::vector<at::Tensor> o = norm_forward_of(*c.x, *c.w, c.residual, c.eps, c.m);
+    if (o.empty()) Py_RETURN_NONE;
+    return tuple_of({o[0], o[1].defined() ? o[1] : *c.x});
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* norm_quantised(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    NormCall c;
+    if (!norm_call(args, n, &c)) Py_RETURN_NONE;
+    const at::Tensor &x = *c.x, &r = c.residual;
+    at::Tensor q = at::empty(x.sizes(), x.options().dtype(at::kFloat8_e4m3fn));
+    at::Tensor scale = at::empty({c.m.N, c.m.H, c.m.W}, x.options().dtype(at::kFloat));
+    at::Tensor h = r.defined() ? at::empty(x.sizes(), x.options()) : at::Tensor();
+    const int rc = launch(x, [&](void* st) {
+        return scc_norm_quantised(x.data_ptr(), address(r), c.w->data_ptr(), address(h), (uint8_t*)q.data_ptr(), (float*)scale.data_ptr(), c.m.N,
+                                  c.m.C, c.m.H, c.m.W, c.eps, c.m.dtype, st);
+    });
+    if (rc != SCC_OK) Py_RETURN_NONE;
+    return tuple_of({q, scale, h.defined() ? h : x});
+    END_HANDLE_TH_ERRORS
+}
+
+// nn.ResidualNormFunction for a plain call all of whose tensors want gradients
+struct Norm {
+    struct Refused {};
+
+    static std::vector<at::Tensor> gradients(const at::Tensor& x, const at::Tensor& residual, const at::Tensor& w, const at::Tensor& dy_,
+                                             const at::Tensor& dh_, double eps)
+    {
+        const at::Tensor dy = dy_.defined() ? dy_.contiguous() : at::zeros_like(x), dh = dh_.defined() ? dh_.contiguous() : dh_;
+        Map m;
+        std::vector<at::Tensor> g;
+        auto like = [&](const at::Tensor& t) { return plain(t, x) && t.sizes() == x.sizes(); };
+        if (norm_map(x, w, residual, &m) && like(dy) && (!dh.defined() || like(dh))) {
+            at::Tensor dx = at::empty_like(x), dw = at::empty_like(w);
+            const size_t need = scc_norm_backward_workspace_bytes(m.N, m.C, m.H, m.W, m.dtype);
+            const at::Tensor ws = scratch(need, x);
+            const int rc = scc_norm_backward(x.data_ptr(), address(residual), w.data_ptr(), dy.data_ptr(), address(dh), dx.data_ptr(),
+                                             dw.data_ptr(), m.N, m.C, m.H, m.W, (float)eps, m.dtype, m.dtype, address(ws), need, stream_of(x));
+            if (rc == SCC_OK) g = {dx, dw};
+        }
+        if (g.empty())
+            g = from_python("_norm_backward", [&]() {
+                return Py_BuildValue("(NNNNNdO)", wrapped(x), wrapped(w), wrapped(dy), wrapped(residual), wrapped(dh), eps, Py_True);
+            });
+        if (at::GradMode::is_enabled())
+            g = FirstOrderOf::apply(g[0], g[1], x, residual.defined() ? residual : x, w, dy, dh.defined() ? dh : dy);
+        return g;
+    }
+
+    struct Plain : torch::autograd::Function<Plain> {
+        static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, double eps)
+        {
+            Map m;
+            std::vector<at::Tensor> o;
+            if (norm_map(x, w, at::Tensor(), &m)) o = norm_forward_of(x, w, at::Tensor(), (float)eps, m);
+            if (o.empty()) throw Refused();
+            ctx->save_for_backward({x, w});
+            ctx->saved_data["eps"] = eps;
+            ctx->set_materialize_grads(false);
+            return o[0];
+        }
+
+        static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+        {
+            if (!grads[0].defined()) return {at::Tensor(), at::Tensor(), at::Tensor()};
+            const torch::autograd::variable_list s = ctx->get_saved_variables();
+            const std::vector<at::Tensor> g = gradients(s[0], at::Tensor(), s[1], grads[0], at::Tensor(), ctx->saved_data["eps"].toDouble());
+            return {g[0], g[1], at::Tensor()};
+        }
+    };
+
+    struct Residual : torch::autograd::Function<Residual> {
+        static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w,
+                                                      const at::Tensor& residual, double eps)
+        {
+            Map m;
+            std::vector<at::Tensor> o;
+            if (norm_map(x, w, residual, &m)) o = norm_forward_of(x, w, residual, (float)eps, m);
+            if (o.empty()) throw Refused();
+            // in binary32 the sum stands for both; in bf16 it is rounded
+            if (m.dtype == SCC_F32) ctx->save_for_backward({w, o[1]});
+            else ctx->save_for_backward({w, x, residual});
+            ctx->saved_data["eps"] = eps;
+            ctx->set_materialize_grads(false);
+            return {o[0], o[1]};
+        }
+
+        static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+        {
+            if (!grads[0].defined() && !grads[1].defined()) return {at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()};
+            const torch::autograd::variable_list s = ctx->get_saved_variables();
+            const std::vector<at::Tensor> g = gradients(s[1], s.size() > 2 ? s[2] : at::Tensor(), s[0], grads[0], grads[1],
+                                                        ctx->saved_data["eps"].toDouble());
+            return {g[0], g[1], g[0], at::Tensor()};
+        }
+    };
+};
+
+PyObject* norm_block(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    NormCall c;
+    if (!at::GradMode::is_enabled() || !norm_call(args, n, &c) || !wants_gradient(*c.x) || !wants_gradient(*c.w) ||
+        (c.residual.defined() && !wants_gradient(c.residual)))
+        Py_RETURN_NONE;
+    try {
+        if (!c.residual.defined()) return tuple_of({Norm::Plain::apply(*c.x, *c.w, (double)c.eps), *c.x});
+        const torch::autograd::variable_list o = Norm::Residual::apply(*c.x, *c.w, c.residual, (double)c.eps);
+        return tuple_of({o[0], o[1]});
+    } catch (const Norm::Refused&) {
+        Py_RETURN_NONE;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// ---- vocabulary loss ----
+
+struct LossCall {
+    const at::Tensor *x, *w, *target;
+    int code;
+    long long ignored;
+    Map m;
+    int V;
+};
+
+bool loss_map(const at::Tensor& x, const at::Tensor& w, const at::Tensor& target, Map* m, int* V)
+{
+    if (!plain(x) || !plain(w, x) || x.dim() != 4 || w.dim() != 2 || !fits(x) || !fits(w) || w.size(1) != x.size(1)) return false;
+    if (!target.defined() || !target.is_cuda() || target.scalar_type() != at::kLong || !target.is_contiguous() || target.dim() != 3 ||
+        target.get_device() != x.get_device() || target.size(0) != x.size(0) || target.size(1) != x.size(2) || target.size(2) != x.size(3))
+        return false;
+    *m = {(int)x.size(0), (int)x.size(1), (int)x.size(2), (int)x.size(3), x.scalar_type() == at::kFloat ? SCC_F32 : SCC_BF16};
+    *V = (int)w.size(0);
+    return true;
+}
+
+// (x, w, target, code, ignored)
+bool loss_call(PyObject* const* a, Py_ssize_t n, LossCall* c)
+{
+    if (n != 5 || !no_modes() || !PyLong_CheckExact(a[3]) || !PyLong_CheckExact(a[4])) return false;
+    for (int i = 0; i < 3; ++i)
+        if (!THPVariable_CheckExact(a[i])) return false;
+    c->x = &THPVariable_Unpack(a[0]);
+    c->w = &THPVariable_Unpack(a[1]);
+    c->target = &THPVariable_Unpack(a[2]);
+    int overflow = 0, more = 0;
+    c->code = (int)PyLong_AsLongAndOverflow(a[3], &overflow);
+    c->ignored = PyLong_AsLongLongAndOverflow(a[4], &more);
+    return !overflow && !more && loss_map(*c->x, *c->w, *c->target, &c->m, &c->V);
+}
+
+// loss and lse; none where the call failed
+std::vector<at::Tensor> loss_of(const at::Tensor& x, const at::Tensor& w, const at::Tensor& target, int code, long long ignored, const Map& m, int V)
+{
+    const at::TensorOptions f = x.options().dtype(at::kFloat);
+    at::Tensor lse = at::empty(target.sizes(), f), loss = code == SCC_NONE ? at::empty(target.sizes(), f) : at::empty({}, f);
+    const size_t need = scc_vocabulary_loss_workspace_bytes(m.N, m.C, m.H, m.W, V, (scc_reduction)code, m.dtype);
+    const at::Tensor ws = scratch(need, x);
+    const int rc = launch(x, [&](void* st) {
+        return scc_vocabulary_loss(x.data_ptr(), w.data_ptr(), (const long long*)target.data_ptr(), (float*)loss.data_ptr(), (float*)lse.data_ptr(),
+                                   m.N, m.C, m.H, m.W, V, ignored, (scc_reduction)code, m.dtype, address(ws), need, st);
+    });
+    if (rc != SCC_OK) return {};
+    return {loss, lse};
+}
+
+PyObject* vocabulary_loss(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    LossCall c;
+    if (!loss_call(args, n, &c)) Py_RETURN_NONE;
+    const std::vector<at::Tensor> o = loss_of(*c.x, *c.w, *c.target, c.code, c.ignored, c.m, c.V);
+    if (o.empty()) Py_RETURN_NONE;
+    return tuple_of({o[0], o[1]});
+    END_HANDLE_TH_ERRORS
+}
+
+// nn.VocabularyLossFunction for a plain call whose x and weight want gradients
+struct Loss : torch::autograd::Function<Loss> {
+    struct Refused {};
+
+    static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& w, const at::Tensor& target, int64_t code,
+                              int64_t ignored)
+    {
+        Map m;
+        int V;
+        std::vector<at::Tensor> o;
+        if (loss_map(x, w, target, &m, &V)) o = loss_of(x, w, target, (int)code, ignored, m, V);
+        if (o.empty()) throw Refused();
+        ctx->save_for_backward({x, w, target, o[1]});
+        ctx->saved_data["code"] = code;
+        ctx->saved_data["ignored"] = ignored;
+        return o[0];
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads)
+    {
+        const torch::autograd::variable_list s = ctx->get_saved_variables();
+        const at::Tensor &x = s[0], &w = s[1], &target = s[2], &lse = s[3];
+        const at::Tensor d = grads[0].contiguous();
+        const int64_t code = ctx->saved_data["code"].toInt(), ignored = ctx->saved_data["ignored"].toInt();
+        Map m;
+        int V;
+        std::vector<at::Tensor> g;
+        auto like = [&](const at::Tensor& t, const at::Tensor& of) { return plain(t) && t.scalar_type() == at::kFloat && t.sizes() == of.sizes(); };
+        if (loss_map(x, w, target, &m, &V) && like(lse, target) && (code == SCC_NONE ? like(d, target) : plain(d) && d.scalar_type() == at::kFloat && d.dim() == 0)) {
+            at::Tensor dx = at::empty_like(x), dw = at::empty_like(w);
+            const size_t need = scc_vocabulary_gradients_workspace_bytes(m.N, m.C, m.H, m.W, V, m.dtype);
+            const at::Tensor ws = scratch(need, x);
+            const int rc = scc_vocabulary_gradients(x.data_ptr(), w.data_ptr(), (const long long*)target.data_ptr(), (const float*)lse.data_ptr(),
+                                                    (const float*)d.data_ptr(), dx.data_ptr(), dw.data_ptr(), m.N, m.C, m.H, m.W, V, ignored,
+                                                    (scc_reduction)code, m.dtype, m.dtype, address(ws), need, stream_of(x));
+            if (rc == SCC_OK) g = {dx, dw};
+        }
+        if (g.empty())
+            g = from_python("_vocabulary_gradients", [&]() {
+                return Py_BuildValue("(NNNNNLLO)", wrapped(x), wrapped(w), wrapped(target), wrapped(lse), wrapped(d), (long long)code,
+                                     (long long)ignored, Py_True);
+            });
+        if (at::GradMode::is_enabled()) g = FirstOrderOf::apply(g[0], g[1], x, w, d, x, w);
+        return {g[0], g[1], at::Tensor(), at::Tensor(), at::Tensor()};
+    }
+};
+
+PyObject* vocabulary_block(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    LossCall c;
+    if (!at::GradMode::is_enabled() || !loss_call(args, n, &c) || !wants_gradient(*c.x) || !wants_gradient(*c.w)) Py_RETURN_NONE;
+    try {
+        return THPVariable_Wrap(Loss::apply(*c.x, *c.w, *c.target, (int64_t)c.code, (int64_t)c.ignored));
+    } catch (const Loss::Refused&) {
+        Py_RETURN_NONE;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+// ---- AdamW ----
+
+// A list of dense tensors of one type on the current device
+bool tensors(PyObject* o, Py_ssize_t count, at::ScalarType type, std::vector<const at::Tensor*>* out)
+{
+    if (!PyList_CheckExact(o) || PyList_GET_SIZE(o) != count) return false;
+    out->reserve(count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject* e = PyList_GET_ITEM(o, i);
+        if (!THPVariable_CheckExact(e)) return false;
+        const at::Tensor& t = THPVariable_Unpack(e);
+        if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || !t.is_contiguous() || t.scalar_type() != type ||
+            t.numel() < 1 || t.get_device() != c10::hip::current_device())
+            return false;
+        out->push_back(&t);
+    }
+    return true;
+}
+
+// (weights, grads, first, second, first scales or None, second scales or None, lr, step, b1, b2, eps, weight_decay, seed) -> the library's status, or
+// None where the call is not plain; as orthogonal_step
+PyObject* adamw_step(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    double v[5];
+    if (n != 13 || !no_modes() || !PyList_CheckExact(args[0]) || PyList_GET_SIZE(args[0]) < 1 || PyList_GET_SIZE(args[0]) > INT_MAX) Py_RETURN_NONE;
+    if (!PyLong_CheckExact(args[7]) || !PyLong_CheckExact(args[12]) || !numbers(args + 6, 1, v) || !numbers(args + 8, 4, v + 1)) Py_RETURN_NONE;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    PyObject* e = PyList_GET_ITEM(args[0], 0);
+    if (!THPVariable_CheckExact(e)) Py_RETURN_NONE;
+    const at::ScalarType type = THPVariable_Unpack(e).scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) Py_RETURN_NONE;
+    const bool bytes = args[4] != Py_None;
+    const at::ScalarType state = bytes ? at::kFloat8_e4m3fn : at::kFloat;
+    std::vector<const at::Tensor*> l[6];
+    if ((args[5] != Py_None) != bytes || !tensors(args[0], count, type, &l[0]) || !tensors(args[1], count, type, &l[1]) ||
+        !tensors(args[2], count, state, &l[2]) || !tensors(args[3], count, state, &l[3]) ||
+        (bytes && (!tensors(args[4], count, at::kFloat, &l[4]) || !tensors(args[5], count, at::kFloat, &l[5]))))
+        Py_RETURN_NONE;
+    if (!same_shapes(l[0], l[1]) || !same_shapes(l[0], l[2]) || !same_shapes(l[0], l[3])) Py_RETURN_NONE;
+    std::vector<long long> sizes(count);
+    std::vector<void*> at[6];
+    for (int i = 0; i < (bytes ? 6 : 4); ++i) {
+        at[i].resize(count);
+        for (Py_ssize_t j = 0; j < count; ++j) at[i][j] = l[i][j]->data_ptr();
+    }
+    for (Py_ssize_t j = 0; j < count; ++j) {
+        sizes[j] = l[0][j]->numel();
+        if (bytes && (l[4][j]->numel() != (sizes[j] + 255) / 256 || l[5][j]->numel() != (sizes[j] + 255) / 256)) Py_RETURN_NONE;
+    }
+    if (overlap({&l[0], &l[2], &l[3], &l[4], &l[5]}, l[1])) Py_RETURN_NONE;
+    int overflow = 0;
+    const long long step = PyLong_AsLongLongAndOverflow(args[7], &overflow);
+    if (overflow) Py_RETURN_NONE;
+    const scc_adamw_options o = {v[0], v[1], v[2], v[3], v[4], (uint64_t)PyLong_AsUnsignedLongLongMask(args[12])};
+    const int rc = launch(*l[0][0], [&](void* st) {
+        return scc_adamw_step((int)count, at[0].data(), at[1].data(), at[2].data(), at[3].data(), bytes ? (float* const*)at[4].data() : nullptr,
+                              bytes ? (float* const*)at[5].data() : nullptr, sizes.data(), &o, step, nullptr, type == at::kFloat ? SCC_F32 : SCC_BF16, st);
+    });
+    if (rc == SCC_OK || rc == SCC_ERR_LAUNCH)
+        for (int i = 0; i < 6; ++i)
+            if (i != 1) moved(l[i]);
+    return PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
 #define METHOD(name, doc) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, doc}
 PyMethodDef methods[] = {METHOD(forward, "(x, w, cg, co) -> y or None"), METHOD(backward, "(x, dy, w, cg, co) -> (dx, dw) or None"),
                          METHOD(dw_forward, "(x, kdw, w, cg, co, stride) -> y or None"),
@@ -658,6 +1068,12 @@ PyMethodDef methods[] = {METHOD(forward, "(x, w, cg, co) -> y or None"), METHOD(
                          METHOD(gated_block, "(x, w, cg, co, act) -> y under autograd, or None"),
                          METHOD(orthogonalise, "(matrices, steps, a, b, c, eps) -> list or None"),
                          METHOD(orthogonal_step, "(weights, grads, momenta, lr, momentum, weight_decay, nesterov, steps, a, b, c, eps) -> status or None"),
+                         METHOD(norm_forward, "(x, w, residual or None, eps) -> (y, h) or None"),
+                         METHOD(norm_quantised, "(x, w, residual or None, eps) -> (q, scale, h) or None"),
+                         METHOD(norm_block, "(x, w, residual or None, eps) -> (y, h) under autograd, or None"),
+                         METHOD(vocabulary_loss, "(x, w, target, reduction, ignored) -> (loss, lse) or None"),
+                         METHOD(vocabulary_block, "(x, w, target, reduction, ignored) -> loss under autograd, or None"),
+                         METHOD(adamw_step, "(weights, grads, first, second, first scales, second scales, lr, step, b1, b2, eps, weight_decay, seed) -> status or None"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -14,7 +14,7 @@ struct Shape {
     long long T() const { return (long long)N * HW; }
 };
 
-constexpr int kPad = 128;           // packed tokens, channels and pieces of the vocabulary end at multiples of this
+constexpr int kPad = 256;           // packed tokens end at a multiple of this
 inline __host__ __device__ long long padded(long long v) { return (v + kPad - 1) / kPad * kPad; }
 
 // A workspace that is handed out piece by piece; with a null base it only counts.

@@ -44,36 +44,54 @@ __device__ __forceinline__ int channel_exponent(uint32_t most)
     return m > 0.f && m <= 3.4028235e38f ? (k < -110 ? -110 : k > 110 ? 110 : k) : 0;
 }
 
-// The tokens that count, in their order; one workgroup.  lse: of the tokens of x, or null; none: losses of the others, or null.
+// The tokens that count, in their order; one workgroup, of which a wavefront takes 512 tokens at a time.  lse: of the tokens of x, or null; none, none_lse:
+// losses and lse of the others, or null; clear: room to be cleared for what follows.
 __global__ __launch_bounds__(1024) void find_tokens(const long long* __restrict__ target, long long ignored, const float* __restrict__ lse, Tokens k,
                                                     float* none, float* none_lse, uint32_t* clear, int cleared, int T)
 {
+    constexpr int kEach = 8;
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int before = 0;
     for (int i = threadIdx.x; i < cleared; i += 1024) clear[i] = 0;
-    for (int first = 0; first < T; first += 1024) {
-        const int t = first + (int)threadIdx.x;
-        const long long y = t < T ? target[t] : ignored;
-        const bool counts = y != ignored;
-        const unsigned long long there = __ballot(counts);
-        if (lane == 0) sums[wave] = __popcll(there);
+    for (int first = 0; first < T; first += 1024 * kEach) {
+        const int t0 = first + wave * 64 * kEach + lane;
+        long long y[kEach];
+        float l[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int t = t0 + e * 64;
+            y[e] = t < T ? target[t] : ignored;
+            l[e] = lse && t < T ? lse[t] : 0.f;
+        }
+        int own = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) own += __popcll(__ballot(y[e] != ignored));
+        if (lane == 0) sums[wave] = own;
         __syncthreads();
-        int at = before + __popcll(there & ((1ull << lane) - 1));
+        int at = before;
         for (int i = 0; i < 16; ++i) {
             if (i < wave) at += sums[i];
             before += sums[i];
         }
         __syncthreads();
-        if (counts) {
-            k.order[at] = t;
-            k.target[at] = y;
-            if (lse) k.lse[at] = lse[t];
-        }
-        if (t < T) {
-            k.place[t] = counts ? at : -1;
-            if (none && !counts) none[t] = 0.f;
-            if (none_lse && !counts) none_lse[t] = 0.f;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int t = t0 + e * 64;
+            const unsigned long long there = __ballot(y[e] != ignored);
+            const int place = at + __popcll(there & ((1ull << lane) - 1));
+            at += __popcll(there);
+            if (t >= T) continue;
+            const bool counts = y[e] != ignored;
+            k.place[t] = counts ? place : -1;
+            if (counts) {
+                k.order[place] = t;
+                k.target[place] = y[e];
+                if (lse) k.lse[place] = l[e];
+            } else {
+                if (none) none[t] = 0.f;
+                if (none_lse) none_lse[t] = 0.f;
+            }
         }
     }
     const int end = (int)padded(before);
@@ -106,90 +124,247 @@ struct Rows {
     const int *order, *count;
     long long rows, C, HW;
     __device__ __forceinline__ long long end() const { return order ? *count : rows; }
-    // f(row, channel, value) over 64 rows and 64 channels with 256 threads; value 0 outside.  by_row: lanes along the rows (tokens as columns)
-    __device__ __forceinline__ bool by_row() const { return HW > 1; }
-    __device__ __forceinline__ float at(long long i, long long c, long long last) const
+    // where row i's channel 0 is; channels are HW apart
+    __device__ __forceinline__ const T* row(long long i) const
     {
-        if (i >= last || c >= C) return 0.f;
-        const long long t = order ? order[i] : i, n = HW > 1 ? t / HW : t;
-        return to_f32(x[(n * C + c) * HW + (t - n * HW)]);
+        const uint32_t t = order ? (uint32_t)order[i] : (uint32_t)i, n = HW > 1 ? t / (uint32_t)HW : t;
+        return x + (long long)n * C * HW + (t - n * (uint32_t)HW);
     }
 };
 
-// most[c] = largest |value| of channel c, as the bits of a binary32 value: non-negative ones are ordered as their bits are
+__device__ __forceinline__ void raise(uint32_t* most, float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    if (b > *most) atomicMax(most, b);          // it only grows: an old value costs an atomic at most
+}
+
+// Rows whose channels are consecutive, in vectors of 8
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ void read8(const float* p, float (&v)[8])
+{
+    const u32x8 t = *(const u32x8*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(t[e]);
+}
+__device__ __forceinline__ void read8(const bf16_t* p, float (&v)[8])
+{
+    const u32x4 t = *(const u32x4*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e % 2 ? t[e / 2] & 0xffff0000u : t[e / 2] << 16);
+}
+__device__ __forceinline__ void write8(uint16_t* p, const uint16_t (&v)[8])
+{
+    u32x4 t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (uint32_t)v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
+    *(u32x4*)p = t;
+}
+
+// most[c] = largest |value| of channel c, as the bits of a binary32 value: non-negative ones are ordered as their bits are.  256 rows a workgroup,
+// 512 channels of them, eight rows of a wavefront under way.
+template <typename T>
+__global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f, uint32_t* __restrict__ most)
+{
+    constexpr int kRows = 256, kWaves = 16;
+    __shared__ float lds[kWaves][512];
+    const long long first = (long long)blockIdx.y * kRows, end = x.end();
+    if (first >= end) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long c = (long long)blockIdx.x * 512 + lane * 8;
+    float high[8] = {};
+#pragma unroll
+    for (int r = 0; r < kRows / kWaves; r += 8) {
+        float v[8][8], d[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const long long row = first + (r + i) * kWaves + wave;
+            d[i] = row < end ? f.of((int)row) : 0.f;
+            read8(x.row(row < end ? row : end - 1) + (c < x.C ? c : 0), v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) high[e] = fmaxf(high[e], fabsf(v[i][e] * d[i]));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lds[wave][e * 64 + lane] = high[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += 1024) {
+        const long long channel = (long long)blockIdx.x * 512 + (i & 63) * 8 + (i >> 6);
+        float v = lds[0][i];
+#pragma unroll
+        for (int j = 1; j < kWaves; ++j) v = fmaxf(v, lds[j][i]);
+        if (channel < x.C) raise(most + channel, v);
+    }
+}
+
+// The same for any rows: 256 rows and 64 channels a workgroup, lanes along the rows where tokens are columns
 template <typename T>
 __global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ most)
 {
-    const long long first = (long long)blockIdx.y * 256, end = x.end();
+    const long long first = (long long)blockIdx.y * 256, end = x.end(), c0 = (long long)blockIdx.x * 64;
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (x.by_row()) {
-        for (int r = 0; r < 256; r += 64) {
-            const long long i = first + r + lane;
-            const float d = i < end ? f.of((int)i) : 0.f;
-            for (int j = 0; j < 16; ++j) {
-                const long long c = (long long)blockIdx.x * 64 + wave * 16 + j;
-                float v = fabsf(x.at(i, c, end) * d);
-                for (int m = 1; m < 64; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
-                if (lane == 0 && c < x.C) atomicMax(most + c, __float_as_uint(v));
-            }
+    if (x.HW > 1) {
+        const T* row[4];
+        float d[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const long long i = first + r * 64 + lane;
+            row[r] = x.row(i < end ? i : end - 1);
+            d[r] = i < end ? f.of((int)i) : 0.f;
+        }
+        for (int j = 0; j < 16; ++j) {
+            const long long c = c0 + wave * 16 + j;
+            if (c >= x.C) break;
+            float v = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v = fmaxf(v, fabsf(to_f32(row[r][c * x.HW]) * d[r]));
+            for (int m = 1; m < 64; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
+            if (lane == 0) raise(most + c, v);
         }
     } else {
-        const long long c = (long long)blockIdx.x * 64 + lane;
+        const long long c = c0 + lane;
         float v = 0.f;
-        for (int r = wave; r < 256 && first + r < end; r += 4) v = fmaxf(v, fabsf(x.at(first + r, c, end) * f.of((int)(first + r))));
-        if (c < x.C) atomicMax(most + c, __float_as_uint(v));
+        if (c >= x.C) return;
+        for (int r = wave; r < 256 && first + r < end; r += 4) v = fmaxf(v, fabsf(to_f32(x.row(first + r)[c]) * f.of((int)(first + r))));
+        raise(most + c, v);
     }
 }
 
-// Rows into operands: `whole`, ld values a row, the value itself (PLANES 1: as bf16, 3: cut), and `scaled`, times its row's factor and its channel's
-// power of two, in fp16.  Rows up to the next multiple of `pad` and channels up to ld are zeros.
+// What the two kernels below write of a value v of row i and channel c.  whole: the value itself (PLANES 1: as bf16, 3: cut), ld values a row.  scaled: times its
+// row's factor and its channel's power of two, in fp16.  Rows up to the next multiple of `pad` and channels up to ld are zeros.
+struct Packed {
+    uint16_t *whole, *scaled;
+    long long plane;
+    const uint32_t* most;
+    int ld, pad;
+};
+
+// the powers of two of 8 channels
+__device__ __forceinline__ void units_of(const Packed& o, long long c, long long C, float (&unit)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) unit[e] = o.scaled ? power(-channel_exponent(c + e < C ? o.most[c + e] : 0)) : 0.f;
+}
+
+template <int PLANES>
+__device__ __forceinline__ void write_packed(const Packed& o, long long i, long long c, const float (&v)[8], const float (&unit)[8], float d)
+{
+    if (o.whole) {
+        uint16_t piece[8][3], line[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cut(v[e], piece[e]);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) line[e] = piece[e][p];
+            write8(o.whole + p * o.plane + i * o.ld + c, line);
+        }
+    }
+    if (o.scaled) {
+        uint16_t line[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) line[e] = half_of(v[e] == 0.f ? 0.f : v[e] * d * unit[e]);
+        write8(o.scaled + i * o.ld + c, line);
+    }
+}
+
+// Rows into operands, 8 channels a lane: 32 rows and 512 channels a workgroup
 template <typename T, int PLANES>
-__global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, uint16_t* __restrict__ whole, long long plane, uint16_t* __restrict__ scaled,
-                                            const uint32_t* __restrict__ most, int ld, int pad)
+__global__ __launch_bounds__(256) void pack_wide(Rows<T> x, Factor f, Packed o)
+{
+    const long long first = (long long)blockIdx.y * 32, end = x.end();
+    if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long c = (long long)blockIdx.x * 512 + lane * 8;
+    if (c >= o.ld) return;
+    float unit[8];
+    units_of(o, c, x.C, unit);
+#pragma unroll
+    for (int r = 0; r < 8; r += 4) {
+        float v[4][8], d[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long long i = first + (r + j) * 4 + wave;
+            const bool there = i < end && c < x.C;
+            read8(x.row(i < end ? i : 0) + (c < x.C ? c : 0), v[j]);
+            d[j] = i < end ? f.of((int)i) : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] = there ? v[j][e] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) write_packed<PLANES>(o, first + (r + j) * 4 + wave, c, v[j], unit, d[j]);
+    }
+}
+
+// The same for any rows: 64 rows and 64 channels a workgroup through LDS, read with the lanes along the tokens where these are columns
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
 {
     __shared__ float tile[64][65];
     const long long first = (long long)blockIdx.y * 64, end = x.end();
-    if (first >= (end + pad - 1) / pad * pad) return;
+    if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c0 = (long long)blockIdx.x * 64;
-    if (x.by_row()) {
-        for (int j = 0; j < 16; ++j) tile[lane][wave * 16 + j] = x.at(first + lane, c0 + wave * 16 + j, end);
+    if (x.HW > 1) {
+        const bool there = first + lane < end;
+        const T* row = there ? x.row(first + lane) : nullptr;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const long long c = c0 + wave * 16 + j;
+            tile[lane][wave * 16 + j] = there && c < x.C ? to_f32(row[c * x.HW]) : 0.f;
+        }
     } else {
-        for (int j = 0; j < 16; ++j) tile[wave * 16 + j][lane] = x.at(first + wave * 16 + j, c0 + lane, end);
+#pragma unroll 4
+        for (int j = 0; j < 16; ++j) {
+            const long long i = first + wave * 16 + j;
+            tile[wave * 16 + j][lane] = i < end && c0 + lane < x.C ? to_f32(x.row(i)[c0 + lane]) : 0.f;
+        }
     }
     __syncthreads();
-    const long long c = c0 + lane;
-    const float unit = scaled ? power(-channel_exponent(c < x.C ? most[c] : 0)) : 0.f;
-    for (int j = 0; j < 16; ++j) {
-        const long long i = first + wave * 16 + j;
-        const float v = tile[wave * 16 + j][lane];
-        if (whole) {
-            uint16_t piece[3];
-            cut(v, piece);
+    float unit[8];
+    units_of(o, c0 + (threadIdx.x % 8) * 8, x.C, unit);
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) whole[p * plane + i * ld + c] = piece[p];
-        }
-        if (scaled) scaled[i * ld + c] = half_of(v == 0.f ? 0.f : v * f.of((int)i) * unit);
+    for (int j = 0; j < 2; ++j) {
+        const int line = j * 32 + threadIdx.x / 8, at = (threadIdx.x % 8) * 8;
+        const long long i = first + line;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[line][at + e];
+        write_packed<PLANES>(o, i, c0 + at, v, unit, i < end ? f.of((int)i) : 0.f);
     }
 }
 
-// The target's logit of each packed token, a wavefront each; with `minus`, exp(known - lse) - 1 instead.  A target outside of the vocabulary: NaN.
+// The target's logit of each packed token, a wavefront each; with `minus`, exp(known - lse) - 1 instead.  A target outside of the vocabulary: NaN.  wide: w's
+// rows in vectors of 8
 template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void target_logits(const uint16_t* __restrict__ xp, long long plane, int ld, const T* __restrict__ w, Tokens k,
-                                                     bool minus, int C, int V)
+                                                     bool minus, bool wide, int C, int V)
 {
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (i >= *k.count) return;
     const long long y = k.target[i];
     const bool valid = y >= 0 && y < V;
     const T* row = w + (valid ? y : 0) * C;
+    const uint16_t* mine = xp + (long long)i * ld;
     float sum = 0.f;
-    for (int c = lane; c < C; c += 64) {
-        float v = 0.f;
+    for (int c = lane * 8; c < C; c += 512) {       // the same sums in the same order whatever w's alignment
+        float v[8] = {}, u[8] = {};
 #pragma unroll
-        for (int p = PLANES - 1; p >= 0; --p) v += to_f32((bf16_t)xp[p * plane + (long long)i * ld + c]);
-        sum = fmaf(v, to_f32(row[c]), sum);
+        for (int p = PLANES - 1; p >= 0; --p) {
+            read8((const bf16_t*)mine + p * plane + c, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += u[e];
+        }
+        if (wide) {
+            read8(row + c, u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = c + e < C ? to_f32(row[c + e]) : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(v[e], u[e], sum);
     }
     for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
     if (!valid) sum = __uint_as_float(0x7fc00000u);
@@ -219,7 +394,7 @@ int blocks_of(const Grid& g) { return ((long long)g.rows * g.columns + 7) / 8 * 
 
 // Logits of a tile: rows of the vocabulary, columns are tokens.  part[tile row][token] = (max, sum of exp(l - max))
 template <typename P>
-__global__ __launch_bounds__(256, 2) void loss_product(Operand w, Operand x, const int* __restrict__ count, float2* __restrict__ part, long long Tp,
+__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Operand w, Operand x, const int* __restrict__ count, float2* __restrict__ part, long long Tp,
                                                        int steps, int V, Grid g)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -228,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void loss_product(Operand w, Operand x, con
     if (row < 0 || column * P::kN >= *count) return;
     f32x16 acc[P::FM][P::FN];
     P::run(w, x, (long long)row * P::kM, (long long)column * P::kN, 0, steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
     const int v0 = row * P::kM + wm * 32 * P::FM + 4 * (lane >> 5);
     if (row * P::kM + P::kM > V)
 #pragma unroll
@@ -238,25 +413,27 @@ __global__ __launch_bounds__(256, 2) void loss_product(Operand w, Operand x, con
                 if (v0 + m * 32 + 8 * (r / 4) + r % 4 >= V)
 #pragma unroll
                     for (int n = 0; n < P::FN; ++n) acc[m][n][r] = -__builtin_inff();
-    float* most = (float*)lds;                  // [2][kN], then sums likewise
-    float* sums = most + 2 * P::kN;
-    float high[P::FN];
+    constexpr int kHigh = P::kM / 32 / P::FM;   // wavefronts one above the other
+    float* most = (float*)lds;                  // [kHigh][kN], then sums likewise
+    float* sums = most + kHigh * P::kN;
 #pragma unroll
     for (int n = 0; n < P::FN; ++n) {
-        high[n] = -__builtin_inff();
+        float high = -__builtin_inff();
 #pragma unroll
         for (int m = 0; m < P::FM; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) high[n] = fmaxf(high[n], acc[m][n][r]);
-        high[n] = fmaxf(high[n], __shfl_xor(high[n], 32));
-        if (lane < 32) most[wm * P::kN + (wn * P::FN + n) * 32 + lane] = high[n];
+            for (int r = 0; r < 16; ++r) high = fmaxf(high, acc[m][n][r]);
+        high = fmaxf(high, __shfl_xor(high, 32));
+        if (lane < 32) most[wm * P::kN + (wn * P::FN + n) * 32 + lane] = high;
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < P::FN; ++n) {
         const int at = (wn * P::FN + n) * 32 + (lane & 31);
-        high[n] = fmaxf(most[at], most[P::kN + at]);
-        const float shift = -high[n] * kLog2E;
+        float high = most[at];
+#pragma unroll
+        for (int i = 1; i < kHigh; ++i) high = fmaxf(high, most[i * P::kN + at]);
+        const float shift = -high * kLog2E;
         float sum = 0.f;
 #pragma unroll
         for (int m = 0; m < P::FM; ++m)
@@ -268,30 +445,45 @@ __global__ __launch_bounds__(256, 2) void loss_product(Operand w, Operand x, con
     __syncthreads();
     if (threadIdx.x < P::kN) {
         const int at = threadIdx.x;
-        part[row * Tp + column * P::kN + at] = make_float2(fmaxf(most[at], most[P::kN + at]), sums[at] + sums[P::kN + at]);
+        float high = most[at], sum = sums[at];
+#pragma unroll
+        for (int i = 1; i < kHigh; ++i) {
+            high = fmaxf(high, most[i * P::kN + at]);
+            sum += sums[i * P::kN + at];
+        }
+        part[row * Tp + column * P::kN + at] = make_float2(high, sum);
     }
 }
 
-// lse and loss of 64 packed tokens from the tiles' parts; losses: of the tokens of x
-__global__ __launch_bounds__(256) void join_parts(const float2* __restrict__ part, long long Tp, int tiles, Tokens k, float* __restrict__ losses,
-                                                  float* __restrict__ lse)
+// lse and loss of 64 packed tokens from the tiles' parts, 16 wavefronts taking the parts in turn; losses: of the tokens of x
+__global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ part, long long Tp, int tiles, Tokens k, float* __restrict__ losses,
+                                                   float* __restrict__ lse)
 {
-    __shared__ float2 lds[4][64];
+    constexpr int kWaves = 16, kAhead = 4;
+    __shared__ float2 lds[kWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, count = *k.count;
     if (blockIdx.x * 64 >= count) return;
     float high = -__builtin_inff(), sum = 0.f;
     auto join = [&](float2 p) {
         const float to = fmaxf(high, p.x);
         // a part without a finite value (-inf, 0 or NaN) has no say in the maximum
-        sum = (sum == 0.f ? 0.f : sum * exp2f((high - to) * kLog2E)) + (p.y == 0.f ? 0.f : p.y * exp2f((p.x - to) * kLog2E));
+        sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((high - to) * kLog2E)) + (p.y == 0.f ? 0.f : p.y * __builtin_amdgcn_exp2f((p.x - to) * kLog2E));
         high = to;
     };
-    for (int t = wave; t < tiles; t += 4) join(part[t * Tp + i]);
+    for (int t = wave; t < tiles; t += kWaves * kAhead) {
+        float2 p[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int at = t + e * kWaves;
+            p[e] = at < tiles ? part[at * Tp + i] : make_float2(-__builtin_inff(), 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) join(p[e]);
+    }
     lds[wave][lane] = make_float2(high, sum);
     __syncthreads();
     if (wave || i >= count) return;
-    for (int t = 1; t < 4; ++t)
-        if (t < tiles) join(lds[t][lane]);
+    for (int t = 1; t < kWaves; ++t) join(lds[t][lane]);
     const float rest = logf(sum), all = high + rest;
     const int at = k.order[i];
     // of a token that is sure of its target the loss is what is left of rest: high = known
@@ -315,7 +507,7 @@ __global__ __launch_bounds__(1024) void sum_losses(const float* __restrict__ los
 
 // p of a tile of a piece of the vocabulary: p[token][v - first]
 template <typename P>
-__global__ __launch_bounds__(256, 2) void share_product(Operand w, Operand x, Tokens k, Factor f, uint16_t* __restrict__ p, long long plane,
+__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(Operand w, Operand x, Tokens k, Factor f, uint16_t* __restrict__ p, long long plane,
                                                         int piece, int steps, int first, int V, Grid g)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -325,9 +517,9 @@ __global__ __launch_bounds__(256, 2) void share_product(Operand w, Operand x, To
     if (row < 0 || column * P::kN >= *k.count) return;
     f32x16 acc[P::FM][P::FN];
     P::run(w, x, (long long)first + row * P::kM, (long long)column * P::kN, 0, steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
     const int v0 = row * P::kM + wm * 32 * P::FM + 4 * (lane >> 5);
-    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    const bool ends = first + row * P::kM + P::kM > V;
 #pragma unroll
     for (int n = 0; n < P::FN; ++n) {
         const long long t = (long long)column * P::kN + (wn * P::FN + n) * 32 + (lane & 31);
@@ -336,43 +528,36 @@ __global__ __launch_bounds__(256, 2) void share_product(Operand w, Operand x, To
 #pragma unroll
         for (int m = 0; m < P::FM; ++m)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int v = v0 + m * 32 + 8 * q;
-                u16x4 o[P::kPlanes];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][4 * q + e], kLog2E, shift));
-                    if (first + v + e >= V) share = 0.f;
-                    if constexpr (kCut) {
-                        uint16_t c[3];
-                        cut(share * d, c);
-#pragma unroll
-                        for (int i = 0; i < 3; ++i) o[i][e] = c[i];
-                    } else {
-                        o[0][e] = half_of(share);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < P::kPlanes; ++i) *(u16x4*)(p + i * plane + t * piece + v) = o[i];
+            for (int r = 0; r < 16; ++r) {
+                float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
+                if (ends && first + v0 + m * 32 + 8 * (r / 4) + r % 4 >= V) share = 0.f;
+                acc[m][n][r] = kCut ? share * d : share;
             }
     }
-    // the target's own, from its logit: exp(l - lse) - 1
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x < P::kN) {
-        const long long t = (long long)column * P::kN + threadIdx.x;
-        const long long v = k.target[t] - first - row * P::kM;
-        if (t < *k.count && v >= 0 && v < P::kM) {
-            uint16_t* to = p + t * piece + row * P::kM + v;
+#pragma unroll
+    for (int plane_at = 0; plane_at < P::kPlanes; ++plane_at) {
+        auto piece_of = [&](float v) {
             if constexpr (kCut) {
                 uint16_t c[3];
-                cut(k.known[t] * f.of((int)t), c);
-#pragma unroll
-                for (int i = 0; i < 3; ++i) to[i * plane] = c[i];
+                cut(v, c);
+                return c[plane_at];
             } else {
-                *to = half_of(k.known[t] * (float)(1 << (int)kRaise));
+                return half_of(v);
             }
-        }
+        };
+        if (plane_at) __syncthreads();
+        Lines<P>::store(
+            lds, wm, wn, [&](int m, int n, int r) { return piece_of(acc[m][n][r]); },
+            [&]() {
+                // the target's own, from its logit: exp(l - lse) - 1
+                if (threadIdx.x >= P::kN) return;
+                const long long t = (long long)column * P::kN + threadIdx.x, v = k.target[t] - first - row * P::kM;
+                if (t < *k.count && v >= 0 && v < P::kM)
+                    *Lines<P>::place(lds, threadIdx.x, (int)v) = piece_of(k.known[t] * (kCut ? f.of((int)t) : (float)(1 << (int)kRaise)));
+            },
+            [&](int line, int at, u32x4 v) {
+                *(u32x4*)(p + plane_at * plane + ((long long)column * P::kN + line) * piece + row * P::kM + at) = v;
+            });
     }
 }
 
@@ -387,21 +572,23 @@ struct Gradients {
     int split, split_steps, steps;      // of K = piece
     bool wide, begins;                  // dw in binary32; the first piece
     Grid gx, gw;
-    int blocks_x;                       // of the grid; the others are dw's
+    int blocks_x, blocks_w;             // of the grid, the longer ones first
+    bool w_first;
 };
 
 // p W: rows are channels, columns tokens, K a part of the piece; and p^T x: rows are channels, columns the piece's rows, K the tokens
 template <typename PX, typename PW>
-__global__ __launch_bounds__(256, 2) void gradient_products(Gradients a)
+__global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_products(Gradients a)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    constexpr int kWide = PX::kN / 32 / PX::FN;     // wavefronts side by side
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / kWide, wn = wave % kWide;
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    if ((int)blockIdx.x < a.blocks_x) {
-        Grid g = a.gx;
-        const int each = a.blocks_x / a.split, part = blockIdx.x / each;
+    const int of_x = a.w_first ? (int)blockIdx.x - a.blocks_w : (int)blockIdx.x, of_w = a.w_first ? (int)blockIdx.x : (int)blockIdx.x - a.blocks_x;
+    if (of_x >= 0 && of_x < a.blocks_x) {
+        const int each = a.blocks_x / a.split, part = of_x / each;
         int row, column;
-        tile_of(blockIdx.x - part * each, g, row, column);
+        tile_of(of_x - part * each, a.gx, row, column);
         if (row < 0 || column * PX::kN >= *a.count) return;
         const int from = part * a.split_steps, left = a.steps - from;
         f32x16 acc[PX::FM][PX::FN];
@@ -410,77 +597,134 @@ __global__ __launch_bounds__(256, 2) void gradient_products(Gradients a)
 #pragma unroll
         for (int n = 0; n < PX::FN; ++n) {
             const long long t = (long long)column * PX::kN + (wn * PX::FN + n) * 32 + (lane & 31);
+            float* const to = a.dx + part * a.dx_plane + t * a.ld;
+            f32x4 before[PX::FM][4];
 #pragma unroll
             for (int m = 0; m < PX::FM; ++m)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = row * PX::kM + (wm * PX::FM + m) * 32 + 4 * (lane >> 5) + 8 * q;
-                    if (c >= a.ld) continue;
-                    f32x4* to = (f32x4*)(a.dx + part * a.dx_plane + t * a.ld + c);
-                    f32x4 v = {acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
-                    if (!a.begins) v += *to;
-                    *to = v;
+                    before[m][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (!a.begins && c < a.ld) before[m][q] = *(const f32x4*)(to + c);
+                }
+#pragma unroll
+            for (int m = 0; m < PX::FM; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = row * PX::kM + (wm * PX::FM + m) * 32 + 4 * (lane >> 5) + 8 * q;
+                    const f32x4 v = {acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
+                    if (c < a.ld) *(f32x4*)(to + c) = before[m][q] + v;
                 }
         }
         return;
     }
     int row, column;
-    tile_of(blockIdx.x - a.blocks_x, a.gw, row, column);
+    tile_of(of_w, a.gw, row, column);
     if (row < 0) return;
     f32x16 acc[PW::FM][PW::FN];
     PW::run(a.x, a.p_rows, (long long)row * PW::kM, (long long)column * PW::kN, 0, (*a.count + PW::kK - 1) / PW::kK, lds, acc);
 #pragma unroll
     for (int m = 0; m < PW::FM; ++m)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int c = row * PW::kM + (wm * PW::FM + m) * 32 + 4 * (lane >> 5) + 8 * q;
-            float unit[4];
+        for (int r = 0; r < 16; ++r) {
+            const int c = row * PW::kM + (wm * PW::FM + m) * 32 + 4 * (lane >> 5) + 8 * (r / 4) + r % 4;
+            const float unit = a.most_x && c < a.C ? power(channel_exponent(a.most_x[c]) - (int)kRaise) : 1.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                unit[e] = a.most_x && c + e < a.C ? power(channel_exponent(a.most_x[c + e]) - (int)kRaise) : 1.f;
-#pragma unroll
-            for (int n = 0; n < PW::FN; ++n) {
-                const int in = column * PW::kN + (wn * PW::FN + n) * 32 + (lane & 31);
-                const long long v = a.first + in;
-                if (v >= a.V || in >= a.piece) continue;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (c + e >= a.C) continue;
-                    const float s = acc[m][n][4 * q + e] * unit[e];
-                    if (a.wide) ((float*)a.dw)[v * a.C + c + e] = s;
-                    else ((bf16_t*)a.dw)[v * a.C + c + e] = from_f32<bf16_t>(s);
-                }
-            }
+            for (int n = 0; n < PW::FN; ++n) acc[m][n][r] *= unit;
         }
+    if (a.wide) {
+#pragma unroll
+        for (int n = 0; n < PW::FN; ++n) {
+            const int in = column * PW::kN + (wn * PW::FN + n) * 32 + (lane & 31);
+            const long long v = a.first + in;
+            if (v >= a.V || in >= a.piece) continue;
+            float* const to = (float*)a.dw + v * a.C;
+#pragma unroll
+            for (int m = 0; m < PW::FM; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = row * PW::kM + (wm * PW::FM + m) * 32 + 4 * (lane >> 5) + 8 * q;
+                    typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+                    if (c + 3 < a.C) {
+                        *(f32x4u*)(to + c) = f32x4u{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c + e < a.C) to[c + e] = acc[m][n][4 * q + e];
+                    }
+                }
+        }
+        return;
+    }
+    Lines<PW>::store(
+        lds, wm, wn, [&](int m, int n, int r) { return from_f32<bf16_t>(acc[m][n][r]); }, []() {},
+        [&](int line, int at, u32x4 v) {
+            const int in = column * PW::kN + line, c = row * PW::kM + at;
+            const long long place = a.first + in;
+            if (place >= a.V || in >= a.piece) return;
+            bf16_t* const to = (bf16_t*)a.dw + place * a.C + c;
+            typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+            if (c + 7 < a.C) {
+                *(u32x4u*)to = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < a.C) to[e] = (bf16_t)(v[e / 2] >> 16 * (e % 2));
+            }
+        });
 }
 
-// dx of 64 tokens of x and 64 channels from the parts of p W
+// dx of 64 tokens of x and 64 channels from the parts of p W, four channels a lane; through LDS where tokens are columns
 template <typename T>
 __global__ __launch_bounds__(256) void join_dx(const float* __restrict__ parts, long long plane, int split, int ld, Tokens k, Factor f,
                                                const uint32_t* __restrict__ most, T* __restrict__ dx, long long tokens, int C, long long HW)
 {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
     __shared__ float tile[64][65];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long first = (long long)blockIdx.y * 64, c = (long long)blockIdx.x * 64 + lane;
-    const float unit = most ? power(channel_exponent(c < C ? most[c] : 0) - (int)kRaise) : 1.f;
-    for (int j = 0; j < 16; ++j) {
-        const long long t = first + wave * 16 + j;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = (threadIdx.x % 16) * 4;
+    const long long first = (long long)blockIdx.y * 64, c = (long long)blockIdx.x * 64 + in;
+    float unit[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) unit[e] = most ? power(channel_exponent(c + e < C ? most[c + e] : 0) - (int)kRaise) : 1.f;
+    f32x4 sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const long long t = first + threadIdx.x / 16 + j * 16;
         const int i = t < tokens ? k.place[t] : -1;
-        float sum = 0.f;
-        if (i >= 0 && c < C) {
-            for (int s = 0; s < split; ++s) sum += parts[s * plane + (long long)i * ld + c];
-            sum *= most ? f.of(i) * unit : 1.f;
+        sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i >= 0) {
+            const float* from = parts + (long long)i * ld + c;
+            for (int s = 0; s < split; ++s) sum[j] += *(const f32x4*)(from + s * plane);
+            const float d = most ? f.of(i) : 1.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[j][e] *= most ? d * unit[e] : 1.f;
         }
-        if (HW > 1) tile[wave * 16 + j][lane] = sum;
-        else if (t < tokens && c < C) dx[t * C + c] = from_f32<T>(sum);
+        if (HW > 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[threadIdx.x / 16 + j * 16][in + e] = sum[j][e];
+        } else if (t < tokens) {
+            typedef T out __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            if (c + 3 < C) {
+                out o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(sum[j][e]);
+                *(out*)(dx + t * C + c) = o;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < C) dx[t * C + c + e] = from_f32<T>(sum[j][e]);
+            }
+        }
     }
     if (HW == 1) return;
     __syncthreads();
-    const long long t = first + lane, n = t / HW;
+    const uint32_t t = (uint32_t)first + lane, n = t / (uint32_t)HW;
     if (t >= tokens) return;
+    T* const to = dx + (long long)n * C * HW + (t - n * (uint32_t)HW);
+#pragma unroll
     for (int j = 0; j < 16; ++j) {
         const long long channel = (long long)blockIdx.x * 64 + wave * 16 + j;
-        if (channel < C) dx[(n * C + channel) * HW + (t - n * HW)] = from_f32<T>(tile[lane][wave * 16 + j]);
+        if (channel < C) to[channel * HW] = from_f32<T>(tile[lane][wave * 16 + j]);
     }
 }
 
@@ -492,19 +736,32 @@ long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
 
 template <typename T> constexpr int kPlanesOf = sizeof(T) == 4 ? 3 : 1;
 
-template <typename T, int BM, int BN> using LossProduct = Product<BM, BN, (sizeof(T) == 4 && (BM > 64)) ? 16 : 32, kPlanesOf<T>, false, false, false>;
-template <typename T, int BM, int BN> using DxProduct = Product<BM, BN, (sizeof(T) == 4 && (BM > 64)) ? 16 : 32, kPlanesOf<T>, sizeof(T) == 2, true, false>;
-template <typename T, int BM, int BN> using DwProduct = Product<BM, BN, (sizeof(T) == 4 && (BM > 64)) ? 16 : 32, kPlanesOf<T>, sizeof(T) == 2, true, true>;
+// Tiles of the products.  bf16: 128 bytes of a line at a time (K = 64), a full line of the L2; three planes: 64 bytes of each.
+template <typename T> struct Forms {
+    typedef Form<256, 256, 2, 4, 64, 2, 1> Large;
+    typedef Form<128, 128, 2, 2, 64, 2, 1> Middle;
+    typedef Form<64, 64, 2, 2, 64, 4, 1> Small;
+};
+template <> struct Forms<float> {
+    typedef Form<256, 128, 4, 2, 32, 2, 3> Large;
+    typedef Form<128, 128, 2, 2, 32, 3, 3> Middle;
+    typedef Form<64, 64, 2, 2, 32, 3, 3> Small;
+};
 
-// f(BM, BN) as constants: tiles of the product; few tokens: small ones, so that there are enough
+template <typename T, typename F> using LossProduct = Product<F, false, false, false>;
+template <typename T, typename F> using DxProduct = Product<F, sizeof(T) == 2, true, false>;
+template <typename T, typename F> using DwProduct = Product<F, sizeof(T) == 2, true, true>;
+
+// f(form) for a product of so many rows and columns: the largest tiles of which there are enough
 template <typename T, typename F>
-auto with_tiles(long long tokens, F&& f)
+auto with_form(long long rows, long long columns, F&& f)
 {
-    typedef std::integral_constant<int, 64> small;
-    typedef std::integral_constant<int, 128> middle;
-    typedef std::integral_constant<int, sizeof(T) == 4 ? 128 : 256> large;
-    if (tokens <= 64) return f(small(), small());
-    return f(large(), middle());
+    typedef typename Forms<T>::Large L;
+    typedef typename Forms<T>::Middle M;
+    auto tiles = [&](int bm, int bn) { return ((rows + bm - 1) / bm) * ((columns + bn - 1) / bn); };
+    if (columns > M::BN && rows > M::BM && tiles(L::BM, L::BN) >= 200) return f(L());
+    if (columns > 64 && rows > 64 && tiles(M::BM, M::BN) >= 200) return f(M());
+    return f(typename Forms<T>::Small());
 }
 
 template <typename T> bool direct(const T* w, const Shape& s) { return sizeof(T) == 2 && s.C % 64 == 0 && ((uintptr_t)w & 15u) == 0; }
@@ -557,23 +814,42 @@ struct Pieces {
 // Pieces of the vocabulary: at most so many values of p at a time (in the last-level cache with both of its uses), equally long
 Pieces pieces_of(const Shape& s, int planes)
 {
-    const long long Tp = padded(s.T()), Vp = round_up(s.V, kRowsPad), most = planes == 3 ? 1ll << 25 : 1ll << 26;
+    const long long Tp = padded(s.T()), Vp = round_up(s.V, kRowsPad), most = planes == 3 ? 1ll << 25 : 1ll << 27;
     long long piece = most / Tp / kRowsPad * kRowsPad;
     if (piece < 2048) piece = 2048;
     const long long count = (Vp + piece - 1) / piece;
     return {round_up((Vp + count - 1) / count, kRowsPad), (int)count};
 }
 
-template <typename T>
-int split_of(const Shape& s, long long piece, int BM, int BN)
+// The form of both gradients' products: rows are channels, columns tokens and the piece's rows
+template <typename T, typename F>
+auto with_gradient_form(const Shape& s, long long piece, F&& f)
 {
-    const long long ld = round_up(s.C, 64), Tp = padded(s.T());
-    const long long tiles = ((ld + BM - 1) / BM) * ((Tp + BN - 1) / BN), others = ((ld + BM - 1) / BM) * (piece / BN);
-    long long split = (piece + Tp - 1) / Tp;                // as many steps as the other product's
-    while (tiles * split + others < 512 && piece / split > 1024) ++split;
-    if (split > 16) split = 16;
-    while (split > 1 && piece / split < 256) --split;
-    return (int)split;
+    typedef typename Forms<T>::Large L;
+    typedef typename Forms<T>::Middle M;
+    const long long ld = round_up(s.C, 64), T_ = s.T();
+    // K of the first product can be split
+    auto blocks = [&](int bm, int bn) { return ((ld + bm - 1) / bm) * (piece / bn + (T_ + bn - 1) / bn * 8); };
+    if (ld > 128 && T_ > 128 && blocks(L::BM, L::BN) >= 200) return f(L());
+    if (ld > 64 && T_ > 64) return f(M());
+    return f(typename Forms<T>::Small());
+}
+
+// Parts of K of p W: so many that none takes longer than a CU's share of both products
+template <typename T>
+int split_of(const Shape& s, long long piece)
+{
+    return with_gradient_form<T>(s, piece, [&](auto form) {
+        typedef decltype(form) F;
+        const long long ld = round_up(s.C, 64), T_ = s.T(), high = (ld + F::BM - 1) / F::BM;
+        const long long tiles = high * ((T_ + F::BN - 1) / F::BN), others = high * (piece / F::BN);
+        const long long steps = piece / F::BK, all = tiles * steps + others * ((T_ + F::BK - 1) / F::BK);
+        const long long share = (all + 255) / 256;              // of a CU
+        long long split = (steps + share - 1) / share;          // none has more than that
+        if (split > 16) split = 16;
+        while (split > 1 && piece / split < 512) --split;
+        return (int)split;
+    });
 }
 
 struct GradientRoom {
@@ -601,7 +877,7 @@ GradientRoom take_gradients(Room& room, const Shape& s, bool direct_w)
     }
     r.pieces = pieces_of(s, planes);
     r.p = room.take<uint16_t>(planes * r.c.Tp * r.pieces.piece);
-    r.split = with_tiles<T>(s.T(), [&](auto bm, auto bn) { return split_of<T>(s, r.pieces.piece, decltype(bm)::value, decltype(bn)::value); });
+    r.split = split_of<T>(s, r.pieces.piece);
     r.parts = room.take<float>(r.split * r.c.Tp * r.c.ld);
     return r;
 }
@@ -611,6 +887,27 @@ Operand vocabulary_rows(const T* w, const uint16_t* wp, const Shape& s, long lon
 {
     if (wp) return {wp, round_up(s.V, kRowsPad) * ld, ld, round_up(s.V, kRowsPad) - 1};
     return {(const uint16_t*)w, 0, s.C, (long long)s.V - 1};
+}
+
+template <typename T> bool wide_rows(const T* p, long long C) { return C % 8 == 0 && ((uintptr_t)p & (8 * sizeof(T) - 1)) == 0; }
+
+template <typename T>
+void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* most, hipStream_t st)
+{
+    if (x.HW == 1 && wide_rows(x.x, x.C))
+        channel_maxima_wide<T><<<dim3((x.C + 511) / 512, (x.rows + 255) / 256), 1024, 0, st>>>(x, f, most);
+    else
+        channel_maxima<T><<<dim3((x.C + 63) / 64, (x.rows + 255) / 256), 256, 0, st>>>(x, f, most);
+}
+
+// rows: padded
+template <typename T>
+void launch_pack(const Rows<T>& x, const Factor& f, const Packed& o, long long rows, hipStream_t st)
+{
+    if (x.HW == 1 && wide_rows(x.x, x.C))
+        pack_wide<T, kPlanesOf<T>><<<dim3((o.ld + 511) / 512, rows / 32), 256, 0, st>>>(x, f, o);
+    else
+        pack<T, kPlanesOf<T>><<<dim3(o.ld / 64, rows / 64), 256, 0, st>>>(x, f, o);
 }
 
 template <typename K>
@@ -640,27 +937,25 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
     const long long T_ = s.T(), ld = r.c.ld, Tp = r.c.Tp;
     float* losses = reduction == NONE ? loss : r.losses;
     find_tokens<<<1, 1024, 0, st>>>(target, ignored, nullptr, k, losses, lse, nullptr, 0, (int)T_);
-    const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW};
-    pack<T, planes><<<dim3(ld / 64, Tp / 64), 256, 0, st>>>(rows, Factor{}, r.c.xp, Tp * ld, nullptr, nullptr, (int)ld, kPad);
+    launch_pack<T>({x, k.order, k.count, T_, s.C, s.HW}, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, Tp, st);
     if (r.wp) {
         const long long Vp = round_up(s.V, kRowsPad);
-        const Rows<T> all = {w, nullptr, nullptr, s.V, s.C, 1};
-        pack<T, planes><<<dim3(ld / 64, Vp / 64), 256, 0, st>>>(all, Factor{}, r.wp, Vp * ld, nullptr, nullptr, (int)ld, kRowsPad);
+        launch_pack<T>({w, nullptr, nullptr, s.V, s.C, 1}, {}, {r.wp, nullptr, Vp * ld, nullptr, (int)ld, kRowsPad}, Vp, st);
     }
-    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, false, s.C, s.V);
+    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, false, wide_rows(w, s.C), s.C, s.V);
     int tiles = 0;
-    const hipError_t e = with_tiles<T>(T_, [&](auto bm, auto bn) {
-        typedef LossProduct<T, decltype(bm)::value, decltype(bn)::value> P;
+    const hipError_t e = with_form<T>(s.V, T_, [&](auto form) {
+        typedef LossProduct<T, decltype(form)> P;
         const Grid g = {(int)((s.V + P::kM - 1) / P::kM), (int)((T_ + P::kN - 1) / P::kN)};
         tiles = g.rows;
         const hipError_t e = allow(loss_product<P>, P::kLds);
         if (e != hipSuccess) return e;
         const Operand b = {r.c.xp, Tp * ld, ld, Tp - 1};
-        loss_product<P><<<blocks_of(g), 256, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k.count, r.part, Tp, (int)(ld / P::kK), s.V, g);
+        loss_product<P><<<blocks_of(g), P::kThreads, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k.count, r.part, Tp, (int)(ld / P::kK), s.V, g);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    join_parts<<<(T_ + 63) / 64, 256, 0, st>>>(r.part, Tp, tiles, k, losses, lse);
+    join_parts<<<(T_ + 63) / 64, 1024, 0, st>>>(r.part, Tp, tiles, k, losses, lse);
     if (reduction != NONE) sum_losses<<<1, 1024, 0, st>>>(losses, k.count, reduction == MEAN, loss, (int)T_);
     return hipGetLastError();
 }
@@ -686,60 +981,66 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
     find_tokens<<<1, 1024, 0, st>>>(target, ignored, lse, k, nullptr, nullptr, r.most_x, planes == 1 ? 2 * s.C : 0, (int)T_);
     const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW}, all = {w, nullptr, nullptr, s.V, s.C, 1};
     if (planes == 1) {
-        channel_maxima<T><<<dim3(ld / 64, (T_ + 255) / 256), 256, 0, st>>>(rows, f, r.most_x);
-        channel_maxima<T><<<dim3(ld / 64, (s.V + 255) / 256), 256, 0, st>>>(all, Factor{}, r.most_w);
+        launch_maxima(rows, f, r.most_x, st);
+        launch_maxima(all, {}, r.most_w, st);
     }
-    pack<T, planes><<<dim3(ld / 64, Tp / 64), 256, 0, st>>>(rows, f, r.c.xp, Tp * ld, r.xs, r.most_x, (int)ld, kPad);
-    if (planes == 1 || r.wp)
-        pack<T, planes><<<dim3(ld / 64, Vp / 64), 256, 0, st>>>(all, Factor{}, r.wp, Vp * ld, r.ws, r.most_w, (int)ld, kRowsPad);
-    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, true, s.C, s.V);
+    launch_pack(rows, f, {r.c.xp, r.xs, Tp * ld, r.most_x, (int)ld, kPad}, Tp, st);
+    if (planes == 1 || r.wp) launch_pack(all, {}, {r.wp, r.ws, Vp * ld, r.most_w, (int)ld, kRowsPad}, Vp, st);
+    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, true, wide_rows(w, s.C), s.C, s.V);
     int parts = 1;                          // of p W: the first piece, the longest, has the most
-    const hipError_t e = with_tiles<T>(T_, [&](auto bm, auto bn) {
-        constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
-        typedef LossProduct<T, BM, BN> P;
-        typedef DxProduct<T, BM, BN> PX;
-        typedef DwProduct<T, BM, BN> PW;
-        hipError_t e = allow(share_product<P>, P::kLds);
-        if (e == hipSuccess) e = allow(gradient_products<PX, PW>, PX::kLds);
-        for (int i = 0; i < r.pieces.count && e == hipSuccess; ++i) {
-            const long long first = i * piece, length = Vp - first < piece ? Vp - first : piece;
-            if (length <= 0) break;
-            const int columns = (int)((T_ + BN - 1) / BN);
-            const Grid g = {(int)(length / BM), columns};
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < r.pieces.count && e == hipSuccess; ++i) {
+        const long long first = i * piece, length = Vp - first < piece ? Vp - first : piece;
+        if (length <= 0) break;
+        e = with_form<T>(length, T_, [&](auto form) {
+            typedef LossProduct<T, decltype(form)> P;
+            const Grid g = {(int)(length / P::kM), (int)((T_ + P::kN - 1) / P::kN)};
+            const hipError_t e = allow(share_product<P>, P::kLds);
+            if (e != hipSuccess) return e;
             const Operand b = {r.c.xp, Tp * ld, ld, Tp - 1};
-            share_product<P><<<blocks_of(g), 256, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k, f, r.p, Tp * piece, (int)piece,
-                                                               (int)(ld / P::kK), (int)first, s.V, g);
-            Gradients a = {};
-            const uint16_t *ws = planes == 3 ? r.wp : r.ws, *xs = planes == 3 ? r.c.xp : r.xs;
-            a.w = {ws + first * ld, Vp * ld, ld, ld - 8};
-            a.x = {xs, Tp * ld, ld, ld - 8};
-            a.p_tokens = {r.p, Tp * piece, piece, Tp - 1};
-            a.p_rows = {r.p, Tp * piece, piece, piece - 8};
-            a.count = k.count;
-            a.dx = r.parts;
-            a.dx_plane = Tp * ld;
-            a.dw = dw;
-            a.most_x = r.most_x;
-            a.ld = (int)ld;
-            a.C = s.C;
-            a.V = s.V;
-            a.first = (int)first;
-            a.piece = (int)length;
-            a.steps = (int)(length / PX::kK);
-            a.split = r.split;
+            share_product<P><<<blocks_of(g), P::kThreads, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k, f, r.p, Tp * piece, (int)piece,
+                                                                       (int)(ld / P::kK), (int)first, s.V, g);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) break;
+        Gradients a = {};
+        const uint16_t *ws = planes == 3 ? r.wp : r.ws, *xs = planes == 3 ? r.c.xp : r.xs;
+        a.w = {ws + first * ld, Vp * ld, ld, ld - 8};
+        a.x = {xs, Tp * ld, ld, ld - 8};
+        a.p_tokens = {r.p, Tp * piece, piece, Tp - 1};
+        a.p_rows = {r.p, Tp * piece, piece, piece - 8};
+        a.count = k.count;
+        a.dx = r.parts;
+        a.dx_plane = Tp * ld;
+        a.dw = dw;
+        a.most_x = r.most_x;
+        a.ld = (int)ld;
+        a.C = s.C;
+        a.V = s.V;
+        a.first = (int)first;
+        a.piece = (int)length;
+        a.wide = wide;
+        a.begins = i == 0;
+        e = with_gradient_form<T>(s, piece, [&](auto form) {
+            typedef decltype(form) F;
+            typedef DxProduct<T, F> PX;
+            typedef DwProduct<T, F> PW;
+            const hipError_t e = allow(gradient_products<PX, PW>, PX::kLds);
+            if (e != hipSuccess) return e;
+            a.steps = (int)(length / F::BK);
             a.split_steps = (a.steps + r.split - 1) / r.split;
             a.split = (a.steps + a.split_steps - 1) / a.split_steps;
             if (i == 0) parts = a.split;
-            a.wide = wide;
-            a.begins = i == 0;
-            a.gx = {(int)((ld + BM - 1) / BM), columns};
-            a.gw = {(int)((ld + BM - 1) / BM), (int)(length / BN)};
+            const int high = (int)((ld + F::BM - 1) / F::BM);
+            a.gx = {high, (int)((T_ + F::BN - 1) / F::BN)};
+            a.gw = {high, (int)(length / F::BN)};
             a.blocks_x = blocks_of(a.gx) * a.split;
-            gradient_products<PX, PW><<<a.blocks_x + blocks_of(a.gw), 256, PX::kLds, st>>>(a);
-            e = hipGetLastError();
-        }
-        return e;
-    });
+            a.blocks_w = blocks_of(a.gw);
+            a.w_first = T_ / F::BK > a.split_steps;
+            gradient_products<PX, PW><<<a.blocks_x + a.blocks_w, PX::kThreads, PX::kLds, st>>>(a);
+            return hipGetLastError();
+        });
+    }
     if (e != hipSuccess) return e;
     join_dx<T><<<dim3(ld / 64, (T_ + 63) / 64), 256, 0, st>>>(r.parts, Tp * ld, parts, (int)ld, k, f, r.most_w, dx, T_, s.C, s.HW);
     return hipGetLastError();

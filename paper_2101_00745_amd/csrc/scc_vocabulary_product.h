@@ -1,10 +1,9 @@
-// The matrix product of the vocabulary loss: a tile of BM x BN sums over K per workgroup of four wavefronts, on the matrix cores.
+// The matrix product of the vocabulary loss: a tile of BM x BN sums over K per workgroup, on the matrix cores.
 //
 // An operand is 16-bit, NP planes of it: one (bf16, or fp16 where HALF), or three, whose sum is a binary32 value (the exact cut of split3; six
 // of the nine products are taken).  Its K values are consecutive in memory ("along"), or its rows are ("across": the operand is K x rows
 // and is turned on its way out of LDS by ds_read_b64_tr_b16).  Tiles of BK of K go straight into LDS (global_load_lds, 16 bytes a
-// lane), three buffers in a ring: while one is multiplied the next is complete and the one after it under way, and one barrier a step is enough.
-// A wavefront has a quarter of the tile, a grid of 32 x 32 accumulators.  LDS is read without bank conflicts: in 256 bytes of LDS, which one
+// lane), into a ring of buffers: while one is multiplied the others are under way, and one barrier a step is enough.  LDS is read without bank conflicts: in 256 bytes of LDS, which one
 // phase of a read covers, 16-byte chunks (along) or 64-byte ones (across) of consecutive rows are exchanged by an exclusive or with the row.
 #pragma once
 #include "scc_common.h"
@@ -30,6 +29,15 @@ __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c)
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// A read through a restricted pointer: the compiler takes it for one that the loads under way into other buffers of LDS have nothing to do with (they
+// have not: the caller has waited for this buffer's).  Without that it waits for all of them before each: 492 TFLOP/s instead of 393.
+__device__ __forceinline__ uint64_t read_turned(const char* __restrict__ p)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lptr;
+    return __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)p));
 }
 
 // One operand's tile: R rows of it, BK values of K.
@@ -64,8 +72,6 @@ struct Tile {
     static __device__ __forceinline__ u32x4 fragment(const char* lds, int plane, int first, int f, int kk, int lane)
     {
         if constexpr (ACROSS) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4* lptr;
             typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
             constexpr int G = kChunks / 4;
             const int q = (lane >> 2) & 3, line = kk * 16 + (lane >> 5) * 8 + q;
@@ -73,8 +79,8 @@ struct Tile {
             const char* p = lds + plane * kBytes + line * (R * 2) + piece * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
             // four lines further on a line's pieces are exchanged as on this one
             const char* p4 = p + 4 * R * 2;
-            const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)p));
-            const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)p4));
+            const u32x2 a = __builtin_bit_cast(u32x2, read_turned(p));
+            const u32x2 b = __builtin_bit_cast(u32x2, read_turned(p4));
             return u32x4{a[0], a[1], b[0], b[1]};
         } else {
             constexpr int kLines = 16 / kChunks;
@@ -85,31 +91,38 @@ struct Tile {
     }
 };
 
-// BM x BN sums; the wavefront's are 32 FM x 32 FN of them: accumulator register r of lane l holds row 8 (r / 4) + 4 (l / 32) + r % 4 and column l % 32
-// of a 32 x 32 block.
-template <int BM, int BN, int BK, int NP, bool HALF, bool A_ACROSS, bool B_ACROSS>
-struct Product {
-    typedef Tile<BM, BK, NP, A_ACROSS> A;
-    typedef Tile<BN, BK, NP, B_ACROSS> B;
-    static constexpr int kM = BM, kN = BN, kK = BK, kPlanes = NP;
-    static constexpr int FM = BM / 64, FN = BN / 64;
-    static constexpr int kStage = (A::kBytes + B::kBytes) * NP, kStages = 3, kLds = kStage * kStages;
-    static constexpr int kLoadsA = A::kLoads / 4, kLoadsB = B::kLoads / 4, kLoads = kLoadsA + kLoadsB;     // of a wavefront
-    static_assert(A::kLoads % 4 == 0 && B::kLoads % 4 == 0 && BM % 64 == 0 && BN % 64 == 0, "the wavefronts load equally much");
+// BM x BN sums by WM x WN wavefronts; a wavefront's are 32 FM x 32 FN of them: accumulator register r of lane l holds row 8 (r / 4) + 4 (l / 32) + r % 4
+// and column l % 32 of a 32 x 32 block.  STAGES buffers in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int NP_>
+struct Form {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_, NP = NP_;
+};
 
-    // k: a multiple of BK, from K = begin on
+template <typename F, bool HALF, bool A_ACROSS, bool B_ACROSS>
+struct Product {
+    static constexpr int kM = F::BM, kN = F::BN, kK = F::BK, kPlanes = F::NP, kWaves = F::WM * F::WN, kThreads = kWaves * 64, kStages = F::STAGES;
+    typedef Tile<kM, kK, kPlanes, A_ACROSS> A;
+    typedef Tile<kN, kK, kPlanes, B_ACROSS> B;
+    static constexpr int FM = kM / F::WM / 32, FN = kN / F::WN / 32;
+    static constexpr int kWavesPerSimd = FM * FN > 8 ? 1 : 2;           // accumulators of one fill half of its registers
+    static constexpr int kStage = (A::kBytes + B::kBytes) * kPlanes, kLds = kStage * kStages;
+    static constexpr int kLoadsA = A::kLoads / kWaves, kLoadsB = B::kLoads / kWaves, kLoads = kLoadsA + kLoadsB;     // of a wavefront
+    static_assert(A::kLoads % kWaves == 0 && B::kLoads % kWaves == 0 && kM % (32 * F::WM) == 0 && kN % (32 * F::WN) == 0 && kLds <= 160 * 1024,
+                  "the wavefronts load and multiply equally much");
+
+    // steps tiles of kK, from K = begin, a multiple of kK, on
     static __device__ __forceinline__ void run(const Operand& a, const Operand& b, long long row, long long column, long long begin, int steps,
                                                char* lds, f32x16 (&acc)[FM][FN])
     {
         typedef const __attribute__((address_space(1))) void* gptr;
         typedef __attribute__((address_space(3))) void* lptr;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int wm = wave >> 1, wn = wave & 1;
+        const int wm = wave / F::WN, wn = wave % F::WN;
         const uint16_t *from_a[kLoadsA], *from_b[kLoadsB];
 #pragma unroll
-        for (int i = 0; i < kLoadsA; ++i) from_a[i] = A::source(a, row, wave * kLoadsA + i, lane) + begin / BK * A::step(a);
+        for (int i = 0; i < kLoadsA; ++i) from_a[i] = A::source(a, row, wave * kLoadsA + i, lane) + begin / kK * A::step(a);
 #pragma unroll
-        for (int i = 0; i < kLoadsB; ++i) from_b[i] = B::source(b, column, wave * kLoadsB + i, lane) + begin / BK * B::step(b);
+        for (int i = 0; i < kLoadsB; ++i) from_b[i] = B::source(b, column, wave * kLoadsB + i, lane) + begin / kK * B::step(b);
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
@@ -127,47 +140,122 @@ struct Product {
                 __builtin_amdgcn_global_load_lds((gptr)from_a[i], (lptr)(to + i * 1024), 16, 0, 0);
                 from_a[i] += next_a;
             }
-            to = lds + stage * kStage + A::kBytes * NP + wave * kLoadsB * 1024;
+            to = lds + stage * kStage + A::kBytes * kPlanes + wave * kLoadsB * 1024;
 #pragma unroll
             for (int i = 0; i < kLoadsB; ++i) {
                 __builtin_amdgcn_global_load_lds((gptr)from_b[i], (lptr)(to + i * 1024), 16, 0, 0);
                 from_b[i] += next_b;
             }
         };
-        request(0);
-        request(1);
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) request(i);
+        // The fragments of 16 values of K are read while the ones before them are multiplied, the first of a step during the last of the step before: that one's
+        // products wait for nothing while the next buffer is waited for and the wavefronts meet.
+        constexpr int kParts = kK / 16;
+        u32x4 fa[2][FM][kPlanes], fb[2][FN][kPlanes];
+        auto read = [&](int to, const char* at, int kk) {
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p) {
+#pragma unroll
+                for (int m = 0; m < FM; ++m) fa[to][m][p] = A::fragment(at, p, wm * 32 * FM, m, kk, lane);
+#pragma unroll
+                for (int n = 0; n < FN; ++n) fb[to][n][p] = B::fragment(at + A::kBytes * kPlanes, p, wn * 32 * FN, n, kk, lane);
+            }
+        };
+        auto products = [&](int of) {
+            // three planes: the small products first
+#pragma unroll
+            for (int sum = kPlanes - 1; sum >= 0; --sum)
+#pragma unroll
+                for (int p = sum; p >= 0; --p)
+#pragma unroll
+                    for (int m = 0; m < FM; ++m)
+#pragma unroll
+                        for (int n = 0; n < FN; ++n) acc[m][n] = multiply<HALF>(fa[of][m][p], fb[of][n][sum - p], acc[m][n]);
+        };
+        // a read after every other product or so, so that neither pipe waits for the other's burst: 155 instead of 161 us for the logits of 4096 tokens x 512 x 32000
+        auto interleave = []() {
+            constexpr int kReads = kPlanes * (FM * (A_ACROSS ? 2 : 1) + FN * (B_ACROSS ? 2 : 1)), kProducts = FM * FN * (kPlanes == 3 ? 6 : 1);
+#pragma unroll
+            for (int i = 0; i < kProducts; ++i) {
+                const int reads = kReads * (i + 1) / kProducts - kReads * i / kProducts;
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // a matrix instruction
+                if (reads == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // reads of LDS
+                if (reads == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                if (reads == 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+            }
+        };
+        // this wavefront's loads of the oldest buffer are there and it has read all that it wants of the one before; then all wavefronts' are and have
+        auto meet = [&]() {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (kStages - 2)) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        if (steps > 0) {
+            meet();
+            read(0, lds, 0);
+        }
         int stage = 0;
         for (int k = 0; k < steps; ++k) {
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-            __builtin_amdgcn_s_barrier();       // this stage is there, and what the one before it held has been read by all
-            asm volatile("" ::: "memory");
-            request(stage == 0 ? 2 : stage - 1);
             const char* at = lds + stage * kStage;
-            stage = stage == 2 ? 0 : stage + 1;
+            // the buffer of the step before has been read by all
+            request(stage == 0 ? kStages - 1 : stage - 1);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
 #pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk) {
-                u32x4 fa[FM][NP], fb[FN][NP];
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-#pragma unroll
-                    for (int m = 0; m < FM; ++m) fa[m][p] = A::fragment(at, p, wm * 32 * FM, m, kk, lane);
-#pragma unroll
-                    for (int n = 0; n < FN; ++n) fb[n][p] = B::fragment(at + A::kBytes * NP, p, wn * 32 * FN, n, kk, lane);
+            for (int kk = 0; kk < kParts; ++kk) {
+                if (kk + 1 < kParts) {
+                    read((kk + 1) & 1, at, kk + 1);
+                } else if (k + 1 < steps) {
+                    meet();
+                    read(0, lds + stage * kStage, 0);
                 }
-                // three planes: the small products first
-#pragma unroll
-                for (int sum = NP - 1; sum >= 0; --sum)
-#pragma unroll
-                    for (int p = sum; p >= 0; --p)
-#pragma unroll
-                        for (int m = 0; m < FM; ++m)
-#pragma unroll
-                            for (int n = 0; n < FN; ++n) acc[m][n] = multiply<HALF>(fa[m][p], fb[n][sum - p], acc[m][n]);
+                products(kk & 1);
+                interleave();
             }
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();           // LDS is the caller's again
         asm volatile("" ::: "memory");
+    }
+};
+
+// A tile's sums as 16-bit values to memory, rows of it (consecutive sums of a lane) along the lines there.  value(m, n, r): of an accumulator; change(line, values
+// of a line in LDS): before they leave.  In LDS a line of kM values has its 16-byte chunks exchanged by an exclusive or with the line, so that neither the
+// writes (32 lines at a time) nor the reads (a line at a time) meet in a bank.
+template <typename P>
+struct Lines {
+    static constexpr int kChunks = P::kM / 8, kBytes = P::kM * P::kN * 2;
+    static_assert(kBytes <= P::kLds, "the tile fits where the operands were");
+
+    static __device__ __forceinline__ uint16_t* place(char* lds, int line, int at)
+    {
+        return (uint16_t*)(lds + line * (P::kM * 2) + (((at >> 3) ^ line) & (kChunks - 1)) * 16 + (at & 7) * 2);
+    }
+
+    template <typename V, typename C, typename S>
+    static __device__ __forceinline__ void store(char* lds, int wm, int wn, V&& value, C&& change, S&& out)
+    {
+        typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int n = 0; n < P::FN; ++n) {
+            const int line = (wn * P::FN + n) * 32 + (lane & 31);
+#pragma unroll
+            for (int m = 0; m < P::FM; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const u16x4 v = {value(m, n, 4 * q), value(m, n, 4 * q + 1), value(m, n, 4 * q + 2), value(m, n, 4 * q + 3)};
+                    *(u16x4*)place(lds, line, (wm * P::FM + m) * 32 + 8 * q + 4 * (lane >> 5)) = v;
+                }
+        }
+        __syncthreads();
+        change();
+        __syncthreads();
+#pragma unroll 4
+        for (int i = threadIdx.x; i < P::kN * kChunks; i += P::kThreads) {
+            const int line = i / kChunks, chunk = i % kChunks;
+            out(line, chunk * 8, *(const u32x4*)place(lds, line, chunk * 8));
+        }
     }
 };
 

@@ -280,7 +280,12 @@ class ResidualNormFunction(torch.autograd.Function):
 
 
 def residual_norm(x, weight, residual=None, eps=1e-6):
-    """Functional form: (y, h) with h = x + residual and y = h / sqrt(mean over the channels of h^2 + eps) * weight; without a residual h is x."""
+    """Functional form: (y, h) with h = x + residual and y = h / sqrt(mean over the channels of h^2 + eps) * weight; without a residual h is x.
+    Plain training calls run in native code, as dw_scc's do."""
+    if not (torch.compiler.is_compiling() or _transforms_active() or _tracing_state() is not None):
+        both = (_scc._native or _scc._load_native()).norm_block(x, weight, residual, eps)
+        if both is not None:
+            return both
     if residual is None:
         return ResidualNormFunction.apply(x, None, weight, float(eps)), x
     return ResidualNormFunction.apply(x, residual, weight, float(eps))
@@ -322,7 +327,12 @@ class VocabularyLossFunction(torch.autograd.Function):
 
 def vocabulary_loss(x, weight, target, reduction="mean", ignore_index=-100):
     """Functional form: cross entropy over the vocabulary of logits[n,v,h,w] = sum_c x[n,c,h,w] weight[v,c] at target [N,H,W], float32.
-    reduction: "none", "sum" or "mean" (over the targets that are not ignore_index; 0 if there are none)."""
+    reduction: "none", "sum" or "mean" (over the targets that are not ignore_index; 0 if there are none).  Plain training calls run in native code, as
+    dw_scc's do."""
+    if not (torch.compiler.is_compiling() or _transforms_active() or _tracing_state() is not None):
+        loss = (_scc._native or _scc._load_native()).vocabulary_block(x, weight, target, _scc._reduction(reduction), ignore_index)
+        if loss is not None:
+            return loss
     return VocabularyLossFunction.apply(x, weight, target, reduction, int(ignore_index))
 
 

@@ -163,6 +163,7 @@ class _NoNative:
         return None
 
     backward = dw_forward = dw_backward = dw_block = gated_forward = gated_backward = gated_block = orthogonalise = orthogonal_step = forward
+    norm_forward = norm_quantised = norm_block = vocabulary_loss = vocabulary_block = adamw_step = forward
 
 
 def _load_native():
@@ -726,6 +727,9 @@ def _address(t):
 def scc_norm_forward(x, w, residual=None, eps=1e-6):
     """(y, h) of the residual norm in front of a feed-forward block: h = x + residual, y = h / sqrt(mean_c h^2 + eps) * w, over the channels of
     [N,C,H,W]; w [C].  Without a residual h is x itself."""
+    both = (_native or _load_native()).norm_forward(x, w, residual, eps)
+    if both is not None:
+        return both
     dev, shape = _norm_map(x, w, residual)
     y = torch.empty_like(x)
     h = None if residual is None else torch.empty_like(x)
@@ -736,6 +740,9 @@ def scc_norm_forward(x, w, residual=None, eps=1e-6):
 
 def scc_norm_quantised(x, w, residual=None, eps=1e-6):
     """(q, scale, h): the residual norm's y in 8 bits, q (float8_e4m3fn, the shape of x) * scale (float32 [N,H,W], a power of two for each pixel)."""
+    out = (_native or _load_native()).norm_quantised(x, w, residual, eps)
+    if out is not None:
+        return out
     dev, shape = _norm_map(x, w, residual)
     q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=dev)
     scale = torch.empty((shape[0], *shape[2:]), dtype=torch.float32, device=dev)
@@ -791,6 +798,9 @@ def scc_vocabulary_loss(x, w, target, reduction="mean", ignore_index=-100):
     target int64 [N,H,W].  loss: float32, [N,H,W] for "none", else one value; "mean" over the tokens whose target is not ignore_index, 0 if there
     are none.  lse: float32 [N,H,W], for scc_vocabulary_gradients."""
     code = _reduction(reduction)
+    both = (_native or _load_native()).vocabulary_loss(x, w, target, code, ignore_index)
+    if both is not None:
+        return both
     dev, shape, V, ignored = _vocabulary(x, w, target, ignore_index)
     dtype = _dtype_code(x)
     ws, ws_ptr, ws_len = _scratch(_workspace_need("scc_vocabulary_loss_workspace_bytes", *shape, V, code, dtype), dev)
@@ -856,6 +866,10 @@ def scc_adamw_step(weights, grads, first, second, lr, step, betas=(0.9, 0.999), 
     rounded at random with the stored values' expectation kept: a hash of seed, step and place.  step: from 1; or an int64 tensor of one element on
     the GPU, read when the call runs, for calls that are captured and replayed.  No weight or state may overlap another tensor of the call.  A graph that
     saved a weight cannot be run backward afterwards, as after any change in place."""
+    native = _native or _load_native()
+    status = native.adamw_step(weights, grads, first, second, first_scales, second_scales, lr, step, betas[0], betas[1], eps, weight_decay, seed)
+    if status is not None:                      # made, if it failed too: once more would move a part of the list twice
+        return _check(status)
     dev, dtype = _check_adamw(weights, grads, first, second, first_scales, second_scales)
     device_step = None
     if isinstance(step, torch.Tensor):

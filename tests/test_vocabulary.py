@@ -158,6 +158,17 @@ def test_refusals():
         N.VocabularyLoss(4, 5, reduction="median", device="cpu")
 
 
+def test_workspaces_of_many_sizes():
+    lib = S.load()
+    for T in (1, 63, 64, 65, 4096, 33000, 1 << 22, 1 << 26):
+        for C in (1, 64, 65, 513, 1 << 14, 1 << 20):
+            for V in (1, 64, 257, 5200, 70000, 1 << 26):
+                for dtype in (0, 1):
+                    assert lib.scc_vocabulary_loss_workspace_bytes(T, C, 1, 1, V, 2, dtype) > 0
+                    need = lib.scc_vocabulary_gradients_workspace_bytes(T, C, 1, 1, V, dtype)
+                    assert need >= (10 if dtype == 0 else 8) * T * C        # its copies of x and one part of dx
+
+
 @pytest.mark.gpu
 def test_refusals_of_the_binding():
     x, w, t = torch.zeros(2, 4, 3, 1, device="cuda"), torch.zeros(5, 4, device="cuda"), torch.zeros(2, 3, 1, dtype=torch.int64, device="cuda")
