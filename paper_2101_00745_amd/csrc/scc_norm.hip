@@ -40,6 +40,18 @@ struct Vec {
     }
 };
 
+// Keeps a vector as it was loaded: without it the compiler holds what it has widened for the sums until the second use, twice the registers
+template <typename T, int V>
+__device__ __forceinline__ void as_loaded(Vec<T, V>& v)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    if constexpr (V * sizeof(T) == 16) {
+        words t = __builtin_bit_cast(words, v.v);
+        asm volatile("" : "+v"(t));
+        v.v = __builtin_bit_cast(typename VecOf<T, V>::type, t);
+    }
+}
+
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
 // Squares of values beyond 2^60 leave binary32: sums that come out above this are taken again of scaled values.
@@ -264,6 +276,13 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
         if (!there) continue;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            as_loaded(xs[j]);
+            as_loaded(rs[j]);
+            as_loaded(ds[j]);
+            as_loaded(gs[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
             const int at = place(j);
             if (at >= s.C) continue;
             Vec<T, V> extra, o;
@@ -290,44 +309,59 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
 // ---- tokens as columns ----
 
 // LANES groups of V columns, THREADS / LANES channels at a time, NV times that in registers (0: any number, read again)
-template <int V, int LANES, int THREADS>
+template <int V, int LANES, int THREADS, int SUMS>
 struct Columns {
     static constexpr int kRows = THREADS / LANES, kWaves = THREADS / 64;
-    float lds[kWaves][LANES * V];
+    float lds[SUMS][kWaves][LANES * V];
 
-    // sums over all channels of each of the thread's columns
-    template <typename F>
-    __device__ __forceinline__ void reduce(float (&v)[V], F&& op)
+    // Sums (or what else op is) over all channels of each of the workgroup's columns, SUMS of them at a time; finish(column, totals) in one thread for each
+    // column, which leaves what the others are to see in totals, and says whether the sums have to be taken again; then v is that of the thread's columns.
+    // True if any column's have to.
+    template <typename F, typename G>
+    __device__ __forceinline__ bool reduce(float (&v)[SUMS][V], F&& op, G&& finish)
     {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
+        for (int i = 0; i < SUMS; ++i)
 #pragma unroll
-            for (int m = LANES; m < 64; m *= 2) v[e] = op(v[e], __shfl_xor(v[e], m));
+            for (int e = 0; e < V; ++e)
+#pragma unroll
+                for (int m = LANES; m < 64; m *= 2) v[i][e] = op(v[i][e], __shfl_xor(v[i][e], m));
         __syncthreads();
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         if (lane < LANES)
 #pragma unroll
-            for (int e = 0; e < V; ++e) lds[wave][lane * V + e] = v[e];
+            for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) lds[i][wave][lane * V + e] = v[i][e];
         __syncthreads();
+        bool again = false;
         if (threadIdx.x < LANES * V) {
-            float total = lds[0][threadIdx.x];
+            float total[SUMS];
 #pragma unroll
-            for (int i = 1; i < kWaves; ++i) total = op(total, lds[i][threadIdx.x]);
-            lds[0][threadIdx.x] = total;
+            for (int i = 0; i < SUMS; ++i) {
+                total[i] = lds[i][0][threadIdx.x];
+#pragma unroll
+                for (int j = 1; j < kWaves; ++j) total[i] = op(total[i], lds[i][j][threadIdx.x]);
+            }
+            again = finish((int)threadIdx.x, total);
+#pragma unroll
+            for (int i = 0; i < SUMS; ++i) lds[i][0][threadIdx.x] = total[i];
         }
-        __syncthreads();
+        again = __syncthreads_or(again);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = lds[0][(threadIdx.x % LANES) * V + e];
+        for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[i][e] = lds[i][0][(threadIdx.x % LANES) * V + e];
+        return again;
     }
 };
 
-template <int V>
-__device__ __forceinline__ bool any_large(const float (&sum)[V])
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> where(bool there, Vec<T, V> v)
 {
-    bool large = false;
-#pragma unroll
-    for (int e = 0; e < V; ++e) large |= !(sum[e] < kLargeSum);
-    return __syncthreads_or(large);
+    Vec<T, V> none;
+    none.clear();
+    return there ? v : none;
 }
 
 template <typename T, int V, int LANES, int THREADS, int NV, bool BYTES>
@@ -335,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__
                                                            T* __restrict__ h, void* __restrict__ y, float* __restrict__ scale, Shape s,
                                                            Groups groups)
 {
-    typedef Columns<V, LANES, THREADS> Cols;
+    typedef Columns<V, LANES, THREADS, 1> Cols;
     __shared__ Cols cols;
     const uint32_t group = blockIdx.x * LANES + threadIdx.x % LANES;
     const bool there = group < (uint32_t)groups.count;
@@ -345,65 +379,72 @@ __global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__
     const int row = threadIdx.x / LANES;
     const int count = NV ? NV : (s.C + Cols::kRows - 1) / Cols::kRows;
     Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1];
+    float gs[NV ? NV : 1];
+    // rows behind the last channel read that one and count as zeros: no load waits for a branch
     auto fetch = [&](int j, int k) {
-        const int c = row + j * Cols::kRows;
-        xs[k].clear();
-        rs[k].clear();
-        if (c < s.C) {
-            xs[k].load(x + base + (size_t)c * s.HW);
-            if (r) rs[k].load(r + base + (size_t)c * s.HW);
-        }
+        const int c = row + j * Cols::kRows, from = c < s.C ? c : s.C - 1;
+        xs[k].load(x + base + (size_t)from * s.HW);
+        if (r) rs[k].load(r + base + (size_t)from * s.HW);
+        else rs[k].clear();
+        gs[k] = to_f32(w[from]);
     };
     if constexpr (NV > 0)
 #pragma unroll
         for (int j = 0; j < NV; ++j) fetch(j, j);
-    float sum[V], rstd[V];
-    auto squares = [&](float shrink) {
+    float rstd[1][V], shrink = 1.f, kept = 0.f;
+    for (bool redo = false;;) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = 0.f;
+        for (int e = 0; e < V; ++e) rstd[0][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < count; ++j) {
+            const int k = NV ? j : 0;
+            if constexpr (NV == 0) fetch(j, 0);
+            const bool live = row + j * Cols::kRows < s.C;
+            if (NV > 0) {
+                xs[k] = where(live, xs[k]);
+                rs[k] = where(live, rs[k]);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float v = live ? (xs[k].get(e) + rs[k].get(e)) * shrink : 0.f;
+                rstd[0][e] = fmaf(v, v, rstd[0][e]);
+            }
+        }
+        const bool first = shrink == 1.f;
+        const bool again = cols.reduce(rstd, add, [&](int, float (&total)[1]) {
+            // a column whose sum left binary32 is taken again; what the others had stays
+            const bool large = first && !(total[0] < kLargeSum);
+            if (first || redo) kept = inverse_rms(total[0], shrink, s);
+            redo = large;
+            total[0] = kept;
+            return large;
+        });
+        if (!again) break;
+        shrink = kShrink;
+    }
+    if constexpr (NV > 0)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            as_loaded(xs[j]);
+            as_loaded(rs[j]);
+        }
+    auto value = [&](int k, int e) { return (xs[k].get(e) + rs[k].get(e)) * rstd[0][e] * gs[k]; };
+    float inverse[V];
+    if constexpr (BYTES) {
+        float most[1][V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) most[0][e] = 0.f;
 #pragma unroll
         for (int j = 0; j < count; ++j) {
             const int k = NV ? j : 0;
             if constexpr (NV == 0) fetch(j, 0);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float v = (xs[k].get(e) + rs[k].get(e)) * shrink;
-                sum[e] = fmaf(v, v, sum[e]);
-            }
+            for (int e = 0; e < V; ++e) most[0][e] = fmaxf(most[0][e], fabsf(value(k, e)));
         }
-        cols.reduce(sum, add);
-    };
-    squares(1.f);
-#pragma unroll
-    for (int e = 0; e < V; ++e) rstd[e] = inverse_rms(sum[e], 1.f, s);
-    if (any_large(sum)) {
-        bool large[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) large[e] = !(sum[e] < kLargeSum);
-        squares(kShrink);
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (large[e]) rstd[e] = inverse_rms(sum[e], kShrink, s);
-    }
-    auto value = [&](int k, int e, float g) { return (xs[k].get(e) + rs[k].get(e)) * rstd[e] * g; };
-    float inverse[V];
-    if constexpr (BYTES) {
-        float most[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) most[e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < count; ++j) {
-            const int k = NV ? j : 0, c = row + j * Cols::kRows;
-            if constexpr (NV == 0) fetch(j, 0);
-            if (c >= s.C) continue;
-            const float g = to_f32(w[c]);
-#pragma unroll
-            for (int e = 0; e < V; ++e) most[e] = fmaxf(most[e], fabsf(value(k, e, g)));
-        }
-        cols.reduce(most, fmaxf);
+        cols.reduce(most, fmaxf, [](int, float (&)[1]) { return false; });
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float unit = scale_of(most[e]);
+            const float unit = scale_of(most[0][e]);
             inverse[e] = 1.f / unit;
             if (there && row == 0) scale[(size_t)n * s.HW + p + e] = unit;
         }
@@ -415,16 +456,15 @@ __global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__
         if constexpr (NV == 0) fetch(j, 0);
         if (c >= s.C) continue;
         const size_t to = base + (size_t)c * s.HW;
-        const float g = to_f32(w[c]);
         Vec<T, V> o;
         if constexpr (BYTES) {
             uint32_t q[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e, g) * inverse[e]);
+            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e) * inverse[e]);
             store_bytes<V>((uint8_t*)y + to, q);
         } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) o.set(e, value(k, e, g));
+            for (int e = 0; e < V; ++e) o.set(e, value(k, e));
             o.store((T*)y + to);
         }
         if (h) {
@@ -443,7 +483,7 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
                                                             float* __restrict__ part, Shape s,
                                                             Groups groups)
 {
-    typedef Columns<V, LANES, THREADS> Cols;
+    typedef Columns<V, LANES, THREADS, 2> Cols;
     __shared__ Cols cols;
     const int row = threadIdx.x / LANES;
     const int count = NV ? NV : (s.C + Cols::kRows - 1) / Cols::kRows;
@@ -465,55 +505,61 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
         const uint32_t own = (u - n * (uint32_t)groups.per) * V - p;    // columns of this group that the one before it has
         const size_t base = (size_t)n * s.C * s.HW + p;
         Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1], ds[NV ? NV : 1];
+        float gs[NV ? NV : 1];
         auto fetch = [&](int j, int k) {
-            const int c = row + j * Cols::kRows;
-            xs[k].clear();
-            rs[k].clear();
-            ds[k].clear();
-            if (c < s.C) {
-                xs[k].load(x + base + (size_t)c * s.HW);
-                if (r) rs[k].load(r + base + (size_t)c * s.HW);
-                ds[k].load(dy + base + (size_t)c * s.HW);
-            }
+            const int c = row + j * Cols::kRows, from = c < s.C ? c : s.C - 1;
+            xs[k].load(x + base + (size_t)from * s.HW);
+            if (r) rs[k].load(r + base + (size_t)from * s.HW);
+            else rs[k].clear();
+            ds[k].load(dy + base + (size_t)from * s.HW);
+            gs[k] = to_f32(w[from]);
         };
         if constexpr (NV > 0)
 #pragma unroll
             for (int j = 0; j < NV; ++j) fetch(j, j);
-        float sum[V], dot[V], rstd[V], inner[V];
-        auto both = [&](float shrink) {
+        float both[2][V], shrink = 1.f, kept[2] = {};         // sums of h^2 and of a h, then 1 / rms and mean_c(a h / rms)
+        for (bool redo = false;;) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] = dot[e] = 0.f;
+            for (int e = 0; e < V; ++e) both[0][e] = both[1][e] = 0.f;
 #pragma unroll
             for (int j = 0; j < count; ++j) {
-                const int k = NV ? j : 0, c = row + j * Cols::kRows;
+                const int k = NV ? j : 0;
                 if constexpr (NV == 0) fetch(j, 0);
-                const float g = c < s.C ? to_f32(w[c]) : 0.f;
+                const bool live = row + j * Cols::kRows < s.C;
+                if (NV > 0) {
+                    xs[k] = where(live, xs[k]);
+                    rs[k] = where(live, rs[k]);
+                    ds[k] = where(live, ds[k]);
+                }
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float v = (xs[k].get(e) + rs[k].get(e)) * shrink;
-                    sum[e] = fmaf(v, v, sum[e]);
-                    dot[e] = fmaf(ds[k].get(e) * g, v, dot[e]);
+                    const float v = live ? (xs[k].get(e) + rs[k].get(e)) * shrink : 0.f;
+                    both[0][e] = fmaf(v, v, both[0][e]);
+                    both[1][e] = fmaf(ds[k].get(e) * gs[k], v, both[1][e]);
                 }
             }
-            cols.reduce(sum, add);
-            cols.reduce(dot, add);
-        };
-        auto finish = [&](int e, float shrink) {
-            rstd[e] = inverse_rms(sum[e], shrink, s);
-            inner[e] = dot[e] * (rstd[e] / shrink) / (float)s.C;
-        };
-        both(1.f);
-#pragma unroll
-        for (int e = 0; e < V; ++e) finish(e, 1.f);
-        if (any_large(sum)) {
-            bool large[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) large[e] = !(sum[e] < kLargeSum);
-            both(kShrink);
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (large[e]) finish(e, kShrink);
+            const bool first = shrink == 1.f;
+            const bool again = cols.reduce(both, add, [&](int, float (&total)[2]) {
+                const bool large = first && !(total[0] < kLargeSum);
+                if (first || redo) {
+                    kept[0] = inverse_rms(total[0], shrink, s);
+                    kept[1] = total[1] * (kept[0] / shrink) / (float)s.C;
+                }
+                redo = large;
+                total[0] = kept[0];
+                total[1] = kept[1];
+                return large;
+            });
+            if (!again) break;
+            shrink = kShrink;
         }
+        if constexpr (NV > 0)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                as_loaded(xs[j]);
+                as_loaded(rs[j]);
+                as_loaded(ds[j]);
+            }
 #pragma unroll
         for (int j = 0; j < count; ++j) {
             const int k = NV ? j : 0, c = row + j * Cols::kRows;
@@ -521,14 +567,13 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
             float mine = 0.f;
             if (c < s.C && there) {
                 const size_t at = base + (size_t)c * s.HW;
-                const float g = to_f32(w[c]);
                 Vec<T, V> extra, o;
                 extra.clear();
                 if (dh) extra.load(dh + at);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float hat = (xs[k].get(e) + rs[k].get(e)) * rstd[e], d = ds[k].get(e);
-                    o.set(e, fmaf(d * g - hat * inner[e], rstd[e], extra.get(e)));
+                    const float hat = (xs[k].get(e) + rs[k].get(e)) * both[0][e], d = ds[k].get(e);
+                    o.set(e, fmaf(d * gs[k] - hat * both[1][e], both[0][e], extra.get(e)));
                     if ((uint32_t)e >= own) mine = fmaf(d, hat, mine);
                 }
                 o.store(dx + at);
@@ -560,8 +605,17 @@ __global__ __launch_bounds__(1024) void weight_sums(const float* __restrict__ pa
     __shared__ float lds[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float sum = 0.f;
-    if (c < C)
-        for (int i = wave; i < rows; i += 16) sum += part[(size_t)i * C + c];
+    if (c < C) {
+        int i = wave;
+        for (; i + 7 * 16 < rows; i += 8 * 16) {        // eight rows under way
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = part[(size_t)(i + j * 16) * C + c];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[j];
+        }
+        for (; i < rows; i += 16) sum += part[(size_t)i * C + c];
+    }
     lds[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && c < C) {
@@ -593,19 +647,20 @@ hipError_t with_rows(int C, F&& f)
     return width(std::integral_constant<int, 1>());
 }
 
-// f(V, LANES, THREADS, NV) as constants for tokens as columns
+// f(V, LANES, THREADS, NV) as constants for tokens as columns: pieces of 128 bytes of a plane, 64 where the channels then still fit into registers
 template <typename T, typename F>
 hipError_t with_columns(int C, int HW, F&& f)
 {
-    auto width = [&](auto v, auto lanes) {
+    typedef std::integral_constant<int, kKept> kept;
+    auto width = [&](auto v, auto lanes, auto fewer) {
         constexpr int L = decltype(lanes)::value;
-        if (C <= 256 / L * kKept) return f(v, lanes, std::integral_constant<int, 256>(), std::integral_constant<int, kKept>());
-        if (C <= 1024 / L * kKept) return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, kKept>());
-        if (C <= 1024 / L * 8) return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+        if (C <= 256 / L * kKept) return f(v, lanes, std::integral_constant<int, 256>(), kept());
+        if (C <= 1024 / L * kKept) return f(v, lanes, std::integral_constant<int, 1024>(), kept());
+        if (C <= 2048 / L * kKept) return f(v, fewer, std::integral_constant<int, 1024>(), kept());
         return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
     };
-    if (HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>());
-    return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
+    if (HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+    return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
 }
 
 Groups groups_of(const Shape& s, int V)
