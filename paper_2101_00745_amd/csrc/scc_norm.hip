@@ -131,23 +131,23 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __rest
     const bool there = token < (size_t)s.N;
     const size_t base = (there ? token : (size_t)s.N - 1) * s.C;
     const int count = NV ? NV : (s.C + V * TPT - 1) / (V * TPT);
-    Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1];
+    Vec<T, V> xs[NV ? NV : 1], rs[NV ? NV : 1], gs[NV ? NV : 1];
     auto place = [&](int j) { return (lane + j * TPT) * V; };
     auto start = [&](int at) { return at < s.C - V ? at : s.C - V; };
+    // lanes behind the last channel read the last vector, none of which counts for them: no load waits for a branch
     auto fetch = [&](int j, int k) {
-        const int at = place(j);
-        xs[k].clear();
-        rs[k].clear();
-        if (at < s.C) {
-            xs[k].load(x + base + start(at));
-            if (r) rs[k].load(r + base + start(at));
-        }
+        const int from = start(place(j));
+        xs[k].load(x + base + from);
+        if (r) rs[k].load(r + base + from);
+        else rs[k].clear();
+        gs[k].load(w + from);
     };
     if constexpr (NV > 0)
 #pragma unroll
         for (int j = 0; j < NV; ++j) fetch(j, j);
-    auto squares = [&](float shrink) {
-        float sum = 0.f;
+    float shrink = 1.f, sum;
+    for (;;) {
+        sum = 0.f;
 #pragma unroll
         for (int j = 0; j < count; ++j) {
             const int k = NV ? j : 0;
@@ -159,28 +159,21 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __rest
                 if (start(at) + e >= at) sum = fmaf(v, v, sum);
             }
         }
-        return over_group<TPT>(sum, lds, add);
-    };
-    float shrink = 1.f, sum = squares(1.f);
-    if (!(sum < kLargeSum)) {
-        if constexpr (TPT > 64) __syncthreads();
+        sum = over_group<TPT>(sum, lds, add);
+        if (sum < kLargeSum || shrink != 1.f) break;
         shrink = kShrink;
-        sum = squares(kShrink);
     }
     const float rstd = inverse_rms(sum, shrink, s);
-    auto value = [&](int k, int e, const Vec<T, V>& g) { return (xs[k].get(e) + rs[k].get(e)) * rstd * g.get(e); };
+    auto value = [&](int k, int e) { return (xs[k].get(e) + rs[k].get(e)) * rstd * gs[k].get(e); };
     float unit = 1.f, inverse = 1.f;
     if constexpr (BYTES) {
         float most = 0.f;
 #pragma unroll
         for (int j = 0; j < count; ++j) {
-            const int k = NV ? j : 0, at = place(j);
+            const int k = NV ? j : 0;
             if constexpr (NV == 0) fetch(j, 0);
-            if (at >= s.C) continue;
-            Vec<T, V> g;
-            g.load(w + start(at));
 #pragma unroll
-            for (int e = 0; e < V; ++e) most = fmaxf(most, fabsf(value(k, e, g)));
+            for (int e = 0; e < V; ++e) most = fmaxf(most, fabsf(value(k, e)));
         }
         unit = scale_of(over_group<TPT>(most, lds, fmaxf));
         inverse = 1.f / unit;
@@ -193,16 +186,15 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __rest
         if constexpr (NV == 0) fetch(j, 0);
         if (at >= s.C) continue;
         const size_t to = base + start(at);
-        Vec<T, V> g, o;
-        g.load(w + start(at));
+        Vec<T, V> o;
         if constexpr (BYTES) {
             uint32_t q[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e, g) * inverse);
+            for (int e = 0; e < V; ++e) q[e] = e4m3(value(k, e) * inverse);
             store_bytes<V>((uint8_t*)y + to, q);
         } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) o.set(e, value(k, e, g));
+            for (int e = 0; e < V; ++e) o.set(e, value(k, e));
             o.store((T*)y + to);
         }
         if (h) {
@@ -238,38 +230,29 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
         Vec<T, V> xs[NV], rs[NV], ds[NV], gs[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int at = place(j);
-            xs[j].clear();
-            rs[j].clear();
-            ds[j].clear();
-            gs[j].clear();
-            if (at < s.C) {
-                xs[j].load(x + base + start(at));
-                if (r) rs[j].load(r + base + start(at));
-                ds[j].load(dy + base + start(at));
-                gs[j].load(w + start(at));
-            }
+            const int from = start(place(j));
+            xs[j].load(x + base + from);
+            if (r) rs[j].load(r + base + from);
+            else rs[j].clear();
+            ds[j].load(dy + base + from);
+            gs[j].load(w + from);
         }
-        auto both = [&](float shrink, float& sum, float& dot) {
+        float shrink = 1.f, sum, dot;
+        for (;;) {
             sum = dot = 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const int at = place(j);
-                    if (start(at) + e < at) continue;
-                    const float v = (xs[j].get(e) + rs[j].get(e)) * shrink;
+                    const float v = start(at) + e >= at ? (xs[j].get(e) + rs[j].get(e)) * shrink : 0.f;
                     sum = fmaf(v, v, sum);
                     dot = fmaf(ds[j].get(e) * gs[j].get(e), v, dot);
                 }
             sum = over_group<TPT>(sum, lds, add);
             dot = over_group<TPT>(dot, lds, add);
-        };
-        float shrink = 1.f, sum, dot;
-        both(1.f, sum, dot);
-        if (!(sum < kLargeSum)) {
+            if (sum < kLargeSum || shrink != 1.f) break;
             shrink = kShrink;
-            both(kShrink, sum, dot);
         }
         const float rstd = inverse_rms(sum, shrink, s);
         const float inner = dot * (rstd / shrink) / (float)s.C;      // mean_c(a h s)
@@ -638,6 +621,8 @@ hipError_t with_rows(int C, F&& f)
     auto width = [&](auto v) {
         constexpr int V = decltype(v)::value;
         if (C <= V * 16 * 2) return f(v, std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+        if (C <= V * 64) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+        if (C <= V * 64 * 2) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
         if (C <= V * 64 * kKept) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, kKept>());
         if (C <= V * 256 * kKept) return f(v, std::integral_constant<int, 256>(), std::integral_constant<int, kKept>());
         if (C <= V * 1024 * kKept) return f(v, std::integral_constant<int, 1024>(), std::integral_constant<int, kKept>());
