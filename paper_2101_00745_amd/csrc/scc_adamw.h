@@ -33,7 +33,7 @@ struct Step {
     uint64_t seed;
     float b1, b2, d1, d2;           // d = 1 - b
     float keep, lr, eps;            // keep = 1 - lr wd
-    float c1, c2;                   // 1 / (1 - b^t)
+    float c1, c2;                   // 1 / (1 - b1^t), the root of 1 / (1 - b2^t)
     uint32_t key;                   // of the step's random numbers
 };
 

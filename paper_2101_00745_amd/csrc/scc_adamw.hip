@@ -88,17 +88,22 @@ __device__ __forceinline__ void write_bytes(uint8_t* p, const uint32_t (&code)[8
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.4028235e38f; }
 
+// Magnitudes are compared as the bits of their binary32 values: in that order, and what is not finite last.
+constexpr uint32_t kInfinity = 0x7f800000u;
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
 // largest of 32 lanes' values: the lanes of a block
-__device__ __forceinline__ float over_block(float v)
+__device__ __forceinline__ uint32_t over_block(uint32_t v)
 {
 #pragma unroll
-    for (int m = 1; m < 32; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
+    for (int m = 1; m < 32; m *= 2) v = larger(v, (uint32_t)__shfl_xor((int)v, m));
     return v;
 }
 
 // k of a block's scale 2^k from its largest value, `halves`: of v, whose root is stored
-__device__ __forceinline__ int exponent_of(float most, bool halves)
+__device__ __forceinline__ int exponent_of(uint32_t bits, bool halves)
 {
+    const float most = __uint_as_float(bits);
     int e = __builtin_amdgcn_frexp_expf(most) - 1;
     e = (halves ? e >> 1 : e) - 7;
     return most > 0.f ? (e < -100 ? -100 : e > 120 ? 120 : e) : -100;
@@ -106,39 +111,30 @@ __device__ __forceinline__ int exponent_of(float most, bool halves)
 
 __device__ __forceinline__ float power(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// |m| / scale < 256 as e4m3, up with the probability that the bits behind the third say
+// |m| / scale < 256 as e4m3, up with the probability that the bits behind the third say.  Below 2^-6, where steps are of 2^-9, those bits are brought to
+// the same place.  No branches, here and below: lanes differ in which side they take.
 __device__ __forceinline__ uint32_t round_first(float m, float inverse, uint32_t random)
 {
-    const uint32_t r = (random & 0xffffu) << 4 | 8u;
     const float a = fabsf(m) * inverse;
-    const uint32_t code = a < 0.015625f ? ((uint32_t)(a * 536870912.f) + r) >> 20      // below 2^-6 steps of 2^-9
-                                        : ((__float_as_uint(a) + r) >> 20) - 960u;
-    return finite(m) ? code | (__float_as_uint(m) >> 24 & 0x80u) : 0x7fu;
+    const uint32_t below = (uint32_t)(a * 536870912.f), above = __float_as_uint(a) - (960u << 20);
+    const uint32_t code = ((a < 0.015625f ? below : above) + ((random & 0xffffu) << 4 | 8u)) >> 20;
+    return code | (__float_as_uint(m) >> 24 & 0x80u);
 }
 
-__device__ __forceinline__ float value_of(uint32_t code)
+// The root of v / scale^2 as e4m3: v lies between the squares of the neighbours low and high, and goes up with the probability that makes its expectation v.
+// Squares and differences are exact, and so is the comparison; the root itself may be rounded onto a neighbour, which moves that border by 2^-23 of it.
+// Below 2^-6 a bias of 2^-6 gives all steps the same size.
+__device__ __forceinline__ uint32_t round_second(float v, float root, float inverse, uint32_t random)
 {
-    return code < 8u ? (float)code * 0.001953125f : __uint_as_float((code + 960u) << 20);
-}
-
-// root of v / scale^2 as e4m3: the two neighbouring roots' squares have v between them.  All differences and squares are exact, so that the
-// comparison is.
-__device__ __forceinline__ uint32_t round_second(float v, float inverse, uint32_t random)
-{
-    const float q = (v * inverse) * inverse, root = __builtin_amdgcn_sqrtf(q);
-    uint32_t code = root < 0.015625f ? (uint32_t)(root * 512.f) : (__float_as_uint(root) >> 20) - 960u;
-    float low = value_of(code), high = value_of(code + 1);
-    if (low * low > q) {                    // the root was rounded onto one of them
-        high = low;
-        low = value_of(--code);
-    } else if (high * high <= q) {
-        low = high;
-        high = value_of(++code + 1);
-    }
-    const float u = (float)(random >> 8) * 5.9604644775390625e-8f;
-    const float over = fmaf(-u, high * high - low * low, q - low * low);
-    code += (over > 0.f || (code == 0u && v > 0.f)) ? 1u : 0u;
-    return finite(v) ? code : 0x7fu;
+    const float q = (v * inverse) * inverse, at = root * inverse;
+    const bool below = at < 0.015625f;
+    const float bias = below ? 0.015625f : 0.f;
+    const uint32_t bits = __float_as_uint(at + bias) & 0xfff00000u;
+    const float low = __uint_as_float(bits) - bias, high = __uint_as_float(bits + 0x100000u) - bias;
+    const float square = low * low, u = (float)(random >> 8) * 5.9604644775390625e-8f;
+    const float over = fmaf(-u, fmaf(high, high, -square), q - square);
+    const uint32_t code = (bits >> 20) - (below ? 968u : 960u);
+    return code + ((over > 0.f) | ((code == 0u) & (v > 0.f)) ? 1u : 0u);
 }
 
 template <typename T, bool BYTES>
@@ -157,13 +153,14 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
         const long long at = *s.at;
         if (threadIdx.x == 0) {
             corrections[0] = (float)(1.0 / -expm1((double)at * s.log_b1));
-            corrections[1] = (float)(1.0 / -expm1((double)at * s.log_b2));
+            corrections[1] = (float)sqrt(1.0 / -expm1((double)at * s.log_b2));
         }
         __syncthreads();
         c1 = corrections[0];
         c2 = corrections[1];
         key = step_key(s.seed, at);
     }
+    const float rate = s.lr * c1;
     key = mix(key + (b.index + (uint32_t)i) * 0x9E3779B1u);
     const uintptr_t places = (uintptr_t)t.w | (uintptr_t)t.g | (BYTES ? ((uintptr_t)t.m | (uintptr_t)t.v) << 1 : (uintptr_t)t.m | (uintptr_t)t.v);
     const bool aligned = (places & 15u) == 0;
@@ -172,7 +169,7 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
     for (int round = 0; round < kChunk / (256 * E); ++round) {
         const long long at = begin + (round * 256 + (int)threadIdx.x) * E, left = t.n - at;
         const bool whole = aligned && left >= E;
-        float w[E], g[E], m[E], v[E];
+        float w[E], g[E], m[E], v[E], root[E];
         float ms = 0.f, vs = 0.f;
         // lanes behind the end read nothing; they take part in their block's largest value as zeros
         const long long from = left > 0 ? at : 0;
@@ -189,25 +186,36 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
             read<float, E>((const float*)t.m + from, m, whole, left);
             read<float, E>((const float*)t.v + from, v, whole, left);
         }
+        // of a state in 8 bits the scale, a power of two, goes into the factor that follows: the same bits
+        const float from_m = BYTES ? ms * s.b1 : s.b1;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if constexpr (BYTES) {
-                m[e] *= ms;
                 v[e] *= vs;
                 v[e] *= v[e];
             }
-            m[e] = m[e] * s.b1 + g[e] * s.d1;
+            m[e] = m[e] * from_m + g[e] * s.d1;
             v[e] = v[e] * s.b2 + (g[e] * g[e]) * s.d2;
-            const float root = __builtin_amdgcn_sqrtf(v[e] * c2) + s.eps;
-            w[e] = w[e] * s.keep - s.lr * ((m[e] * c1) * __builtin_amdgcn_rcpf(root));
+            root[e] = __builtin_amdgcn_sqrtf(v[e]);
+            w[e] = fmaf(w[e], s.keep, -(m[e] * rate) * __builtin_amdgcn_rcpf(fmaf(root[e], c2, s.eps)));
         }
         write<T, E>((T*)t.w + from, w, whole, left);
         if constexpr (BYTES) {
-            float most_m = 0.f, most_v = 0.f;
+            uint32_t most_m = 0, most_v = 0;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                most_m = fmaxf(most_m, finite(m[e]) ? fabsf(m[e]) : 0.f);
-                most_v = fmaxf(most_v, finite(v[e]) ? v[e] : 0.f);
+                most_m = larger(most_m, __float_as_uint(m[e]) & 0x7fffffffu);
+                most_v = larger(most_v, __float_as_uint(v[e]));
+            }
+            const bool strange = __any(larger(most_m, most_v) >= kInfinity);
+            if (strange) {
+                asm volatile("");                   // a branch: rare
+                most_m = most_v = 0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    most_m = larger(most_m, finite(m[e]) ? __float_as_uint(m[e]) & 0x7fffffffu : 0u);
+                    most_v = larger(most_v, finite(v[e]) ? __float_as_uint(v[e]) : 0u);
+                }
             }
             const int km = exponent_of(over_block(most_m), false), kv = exponent_of(over_block(most_v), true);
             uint32_t qm[E], qv[E];
@@ -217,7 +225,15 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
             for (int e = 0; e < E; ++e) {
                 const uint32_t random = mix(place + (uint32_t)e);
                 qm[e] = round_first(m[e], im, random);
-                qv[e] = round_second(v[e], iv, random);
+                qv[e] = round_second(v[e], root[e], iv, random);
+            }
+            if (strange) {
+                asm volatile("");
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    qm[e] = finite(m[e]) ? qm[e] : 0x7fu;
+                    qv[e] = finite(v[e]) ? qv[e] : 0x7fu;
+                }
             }
             write_bytes((uint8_t*)t.m + from, qm, whole, left);
             write_bytes((uint8_t*)t.v + from, qv, whole, left);

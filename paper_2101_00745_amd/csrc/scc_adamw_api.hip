@@ -38,7 +38,7 @@ extern "C" int scc_adamw_step(int count, void* const* w, const void* const* g, v
     s.eps = (float)o->eps;
     if (!device_step) {
         s.c1 = (float)(1.0 / -std::expm1((double)step * s.log_b1));
-        s.c2 = (float)(1.0 / -std::expm1((double)step * s.log_b2));
+        s.c2 = (float)std::sqrt(1.0 / -std::expm1((double)step * s.log_b2));
         s.key = step_key(s.seed, step);
     }
     drop_stale_error();
