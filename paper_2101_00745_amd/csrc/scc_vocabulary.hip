@@ -45,15 +45,14 @@ __device__ __forceinline__ int channel_exponent(uint32_t most)
 }
 
 // The tokens that count, in their order; one workgroup, of which a wavefront takes 512 tokens at a time.  lse: of the tokens of x, or null; none, none_lse:
-// losses and lse of the others, or null; clear: room to be cleared for what follows.
+// losses and lse of the others, or null.
 __global__ __launch_bounds__(1024) void find_tokens(const long long* __restrict__ target, long long ignored, const float* __restrict__ lse, Tokens k,
-                                                    float* none, float* none_lse, uint32_t* clear, int cleared, int T)
+                                                    float* none, float* none_lse, int T)
 {
     constexpr int kEach = 8;
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int before = 0;
-    for (int i = threadIdx.x; i < cleared; i += 1024) clear[i] = 0;
     for (int first = 0; first < T; first += 1024 * kEach) {
         const int t0 = first + wave * 64 * kEach + lane;
         long long y[kEach];
@@ -132,12 +131,6 @@ struct Rows {
     }
 };
 
-__device__ __forceinline__ void raise(uint32_t* most, float v)
-{
-    const uint32_t b = __float_as_uint(v);
-    if (b > *most) atomicMax(most, b);          // it only grows: an old value costs an atomic at most
-}
-
 // Rows whose channels are consecutive, in vectors of 8
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ void read8(const float* p, float (&v)[8])
@@ -160,76 +153,101 @@ __device__ __forceinline__ void write8(uint16_t* p, const uint16_t (&v)[8])
     *(u32x4*)p = t;
 }
 
-// most[c] = largest |value| of channel c, as the bits of a binary32 value: non-negative ones are ordered as their bits are.  256 rows a workgroup,
-// 512 channels of them, eight rows of a wavefront under way.
+// parts[block][c] = largest |value| of channel c among 128 rows, as the bits of a binary32 value: non-negative ones are ordered as their bits are.  512 channels
+// a workgroup, a wavefront's eight rows under way.  (Atomics instead of the parts, which cross the XCDs: 37 us for 32 MB instead of 10.)
+constexpr int kMaximaRows = 128;
 template <typename T>
-__global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f, uint32_t* __restrict__ most)
+__global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f, uint32_t* __restrict__ parts, int ld)
 {
-    constexpr int kRows = 256, kWaves = 16;
+    constexpr int kWaves = 16;
     __shared__ float lds[kWaves][512];
-    const long long first = (long long)blockIdx.y * kRows, end = x.end();
+    const long long first = (long long)blockIdx.y * kMaximaRows, end = x.end();
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c = (long long)blockIdx.x * 512 + lane * 8;
-    float high[8] = {};
+    float high[8] = {}, v[8][8], d[8];
 #pragma unroll
-    for (int r = 0; r < kRows / kWaves; r += 8) {
-        float v[8][8], d[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const long long row = first + (r + i) * kWaves + wave;
-            d[i] = row < end ? f.of((int)row) : 0.f;
-            read8(x.row(row < end ? row : end - 1) + (c < x.C ? c : 0), v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) high[e] = fmaxf(high[e], fabsf(v[i][e] * d[i]));
+    for (int i = 0; i < 8; ++i) {
+        const long long row = first + i * kWaves + wave;
+        d[i] = row < end ? f.of((int)row) : 0.f;
+        read8(x.row(row < end ? row : end - 1) + (c < x.C ? c : 0), v[i]);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) high[e] = fmaxf(high[e], fabsf(v[i][e] * d[i]));
 #pragma unroll
     for (int e = 0; e < 8; ++e) lds[wave][e * 64 + lane] = high[e];
     __syncthreads();
-    for (int i = threadIdx.x; i < 512; i += 1024) {
-        const long long channel = (long long)blockIdx.x * 512 + (i & 63) * 8 + (i >> 6);
-        float v = lds[0][i];
+    if (threadIdx.x < 512) {
+        const int at = (threadIdx.x & 7) * 64 + (threadIdx.x >> 3);
+        const long long channel = (long long)blockIdx.x * 512 + threadIdx.x;
+        float most = lds[0][at];
 #pragma unroll
-        for (int j = 1; j < kWaves; ++j) v = fmaxf(v, lds[j][i]);
-        if (channel < x.C) raise(most + channel, v);
+        for (int j = 1; j < kWaves; ++j) most = fmaxf(most, lds[j][at]);
+        if (channel < ld) parts[(long long)blockIdx.y * ld + channel] = __float_as_uint(channel < x.C ? most : 0.f);
     }
 }
 
-// The same for any rows: 256 rows and 64 channels a workgroup, lanes along the rows where tokens are columns
+// The same for any rows: 64 channels a workgroup, lanes along the rows where tokens are columns
 template <typename T>
-__global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ most)
+__global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ parts, int ld)
 {
-    const long long first = (long long)blockIdx.y * 256, end = x.end(), c0 = (long long)blockIdx.x * 64;
+    __shared__ float lds[4][64];
+    const long long first = (long long)blockIdx.y * kMaximaRows, end = x.end(), c0 = (long long)blockIdx.x * 64;
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t* const to = parts + (long long)blockIdx.y * ld + c0;
     if (x.HW > 1) {
-        const T* row[4];
-        float d[4];
+        const T* row[2];
+        float d[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < 2; ++r) {
             const long long i = first + r * 64 + lane;
             row[r] = x.row(i < end ? i : end - 1);
             d[r] = i < end ? f.of((int)i) : 0.f;
         }
+#pragma unroll 4
         for (int j = 0; j < 16; ++j) {
-            const long long c = c0 + wave * 16 + j;
-            if (c >= x.C) break;
-            float v = 0.f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v = fmaxf(v, fabsf(to_f32(row[r][c * x.HW]) * d[r]));
+            const long long c = c0 + wave * 16 + j, from = (c < x.C ? c : x.C - 1) * x.HW;
+            float v = fmaxf(fabsf(to_f32(row[0][from]) * d[0]), fabsf(to_f32(row[1][from]) * d[1]));
             for (int m = 1; m < 64; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
-            if (lane == 0) raise(most + c, v);
+            if (lane == 0) to[wave * 16 + j] = __float_as_uint(c < x.C ? v : 0.f);
         }
     } else {
-        const long long c = c0 + lane;
+        const long long c = c0 + lane < x.C ? c0 + lane : x.C - 1;
         float v = 0.f;
-        if (c >= x.C) return;
-        for (int r = wave; r < 256 && first + r < end; r += 4) v = fmaxf(v, fabsf(to_f32(x.row(first + r)[c]) * f.of((int)(first + r))));
-        raise(most + c, v);
+#pragma unroll 4
+        for (int r = wave; r < kMaximaRows; r += 4)
+            if (first + r < end) v = fmaxf(v, fabsf(to_f32(x.row(first + r)[c]) * f.of((int)(first + r))));
+        lds[wave][lane] = v;
+        __syncthreads();
+        if (wave == 0) to[lane] = __float_as_uint(c0 + lane < x.C ? fmaxf(fmaxf(lds[0][lane], lds[1][lane]), fmaxf(lds[2][lane], lds[3][lane])) : 0.f);
     }
+}
+
+// most[c] of both matrices from their parts, 64 channels a workgroup
+__global__ __launch_bounds__(1024) void join_maxima(const uint32_t* __restrict__ parts_x, const int* __restrict__ tokens, uint32_t* __restrict__ most_x,
+                                                    const uint32_t* __restrict__ parts_w, int rows_w, uint32_t* __restrict__ most_w, int ld)
+{
+    __shared__ uint32_t lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    const uint32_t* parts = blockIdx.y ? parts_w : parts_x;
+    const int rows = ((blockIdx.y ? rows_w : *tokens) + kMaximaRows - 1) / kMaximaRows;
+    uint32_t most = 0;
+    for (int i = wave; i < rows; i += 64) {
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = i + j * 16 < rows ? parts[(long long)(i + j * 16) * ld + c] : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = most > v[j] ? most : v[j];
+    }
+    lds[wave][lane] = most;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = most > lds[i][lane] ? most : lds[i][lane];
+    (blockIdx.y ? most_w : most_x)[c] = most;
 }
 
 // What the two kernels below write of a value v of row i and channel c.  whole: the value itself (PLANES 1: as bf16, 3: cut), ld values a row.  scaled: times its
@@ -242,10 +260,10 @@ struct Packed {
 };
 
 // the powers of two of 8 channels
-__device__ __forceinline__ void units_of(const Packed& o, long long c, long long C, float (&unit)[8])
+__device__ __forceinline__ void units_of(const Packed& o, long long c, float (&unit)[8])
 {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) unit[e] = o.scaled ? power(-channel_exponent(c + e < C ? o.most[c + e] : 0)) : 0.f;
+    for (int e = 0; e < 8; ++e) unit[e] = o.scaled ? power(-channel_exponent(o.most[c + e])) : 0.f;
 }
 
 template <int PLANES>
@@ -280,7 +298,7 @@ __global__ __launch_bounds__(256) void pack_wide(Rows<T> x, Factor f, Packed o)
     const long long c = (long long)blockIdx.x * 512 + lane * 8;
     if (c >= o.ld) return;
     float unit[8];
-    units_of(o, c, x.C, unit);
+    units_of(o, c, unit);
 #pragma unroll
     for (int r = 0; r < 8; r += 4) {
         float v[4][8], d[4];
@@ -324,7 +342,7 @@ __global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
     }
     __syncthreads();
     float unit[8];
-    units_of(o, c0 + (threadIdx.x % 8) * 8, x.C, unit);
+    units_of(o, c0 + (threadIdx.x % 8) * 8, unit);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int line = j * 32 + threadIdx.x / 8, at = (threadIdx.x % 8) * 8;
@@ -369,6 +387,56 @@ __global__ __launch_bounds__(256) void target_logits(const uint16_t* __restrict_
     for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
     if (!valid) sum = __uint_as_float(0x7fc00000u);
     if (lane == 0) k.known[i] = minus ? expm1f(sum - k.lse[i]) : sum;
+}
+
+// find_tokens, pack and target_logits of the loss of at most 64 tokens in one: a wavefront for each packed token, all of which look at the targets
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void begin_few(Rows<T> x, const long long* __restrict__ target, long long ignored, const T* __restrict__ w, Tokens k,
+                                                 uint16_t* __restrict__ xp, long long plane, int ld, float* none, float* none_lse, bool wide_x, bool wide_w,
+                                                 int V)
+{
+    const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6), T_ = (int)x.rows, C = (int)x.C;
+    const long long y = lane < T_ ? target[lane] : ignored;
+    const unsigned long long there = __ballot(y != ignored);
+    const int count = __popcll(there), before = __popcll(there & ((1ull << lane) - 1));
+    if (i == 0) {
+        if (lane == 0) *k.count = count;
+        if (lane < T_ && y == ignored) {
+            if (none) none[lane] = 0.f;
+            if (none_lse) none_lse[lane] = 0.f;
+        }
+    }
+    uint16_t* const to = xp + (long long)i * ld;
+    if (i >= count) {           // zeros behind the last one
+        for (int c = lane * 8; c < ld; c += 512)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) *(u32x4*)(to + p * plane + c) = u32x4{0, 0, 0, 0};
+        return;
+    }
+    const uint32_t t = __ffsll(__ballot(y != ignored && before == i)) - 1, n = x.HW > 1 ? t / (uint32_t)x.HW : t;
+    const long long v = __shfl(y, (int)t);
+    const bool valid = v >= 0 && v < V;
+    const T *from = x.x + (long long)n * C * x.HW + (t - n * (uint32_t)x.HW), *row = w + (valid ? v : 0) * C;
+    float sum = 0.f;
+    for (int c = lane * 8; c < ld; c += 512) {
+        float a[8] = {}, b[8] = {}, unit[8] = {};
+        if (wide_x && c < C) read8(from + c, a);
+        if (wide_w && c < C) read8(row + c, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (!wide_x && c + e < C) a[e] = to_f32(from[(c + e) * x.HW]);
+            if (!wide_w && c + e < C) b[e] = to_f32(row[c + e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(a[e], b[e], sum);
+        write_packed<PLANES>({xp, nullptr, plane, nullptr, ld, 0}, i, c, a, unit, 1.f);
+    }
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    if (lane == 0) {
+        k.order[i] = (int)t;
+        k.target[i] = v;
+        k.known[i] = valid ? sum : __uint_as_float(0x7fc00000u);
+    }
 }
 
 // Workgroup -> tile.  Workgroups go to the XCDs in turn, and each of these takes a run of tiles: bands of four tiles of rows, all columns of a band.
@@ -459,15 +527,19 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Op
 __global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ part, long long Tp, int tiles, Tokens k, float* __restrict__ losses,
                                                    float* __restrict__ lse)
 {
-    constexpr int kWaves = 16, kAhead = 4;
+    constexpr int kWaves = 16, kAhead = 8;
     __shared__ float2 lds[kWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, count = *k.count;
     if (blockIdx.x * 64 >= count) return;
     float high = -__builtin_inff(), sum = 0.f;
-    auto join = [&](float2 p) {
-        const float to = fmaxf(high, p.x);
-        // a part without a finite value (-inf, 0 or NaN) has no say in the maximum
-        sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((high - to) * kLog2E)) + (p.y == 0.f ? 0.f : p.y * __builtin_amdgcn_exp2f((p.x - to) * kLog2E));
+    // several parts at once, so that their exponentials wait for nothing but the maximum; a part of sum 0 has no values
+    auto join = [&](const float2* p, int n) {
+        float to = high;
+#pragma unroll
+        for (int e = 0; e < n; ++e) to = fmaxf(to, p[e].x);
+        sum = sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((high - to) * kLog2E);
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum += p[e].y == 0.f ? 0.f : p[e].y * __builtin_amdgcn_exp2f((p[e].x - to) * kLog2E);
         high = to;
     };
     for (int t = wave; t < tiles; t += kWaves * kAhead) {
@@ -477,13 +549,17 @@ __global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ pa
             const int at = t + e * kWaves;
             p[e] = at < tiles ? part[at * Tp + i] : make_float2(-__builtin_inff(), 0.f);
         }
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) join(p[e]);
+        join(p, kAhead);
     }
     lds[wave][lane] = make_float2(high, sum);
     __syncthreads();
     if (wave || i >= count) return;
-    for (int t = 1; t < kWaves; ++t) join(lds[t][lane]);
+    float2 p[kWaves];
+#pragma unroll
+    for (int t = 0; t < kWaves; ++t) p[t] = lds[t][lane];
+    high = -__builtin_inff();
+    sum = 0.f;
+    join(p, kWaves);
     const float rest = logf(sum), all = high + rest;
     const int at = k.order[i];
     // of a token that is sure of its target the loss is what is left of rest: high = known
@@ -855,7 +931,7 @@ int split_of(const Shape& s, long long piece)
 struct GradientRoom {
     Common c;
     uint16_t *wp, *ws, *xs, *p;
-    uint32_t *most_x, *most_w;
+    uint32_t *most_x, *most_w, *parts_x, *parts_w;
     float* parts;
     Pieces pieces;
     int split;
@@ -872,8 +948,10 @@ GradientRoom take_gradients(Room& room, const Shape& s, bool direct_w)
     if (planes == 1) {
         r.ws = room.take<uint16_t>(rows * r.c.ld);
         r.xs = room.take<uint16_t>(r.c.Tp * r.c.ld);
-        r.most_x = room.take<uint32_t>(2 * s.C);
-        r.most_w = r.most_x + s.C;
+        r.most_x = room.take<uint32_t>(r.c.ld);
+        r.most_w = room.take<uint32_t>(r.c.ld);
+        r.parts_x = room.take<uint32_t>((s.T() + kMaximaRows - 1) / kMaximaRows * r.c.ld);
+        r.parts_w = room.take<uint32_t>((s.V + kMaximaRows - 1) / kMaximaRows * r.c.ld);
     }
     r.pieces = pieces_of(s, planes);
     r.p = room.take<uint16_t>(planes * r.c.Tp * r.pieces.piece);
@@ -892,12 +970,11 @@ Operand vocabulary_rows(const T* w, const uint16_t* wp, const Shape& s, long lon
 template <typename T> bool wide_rows(const T* p, long long C) { return C % 8 == 0 && ((uintptr_t)p & (8 * sizeof(T) - 1)) == 0; }
 
 template <typename T>
-void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* most, hipStream_t st)
+void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* parts, int ld, hipStream_t st)
 {
-    if (x.HW == 1 && wide_rows(x.x, x.C))
-        channel_maxima_wide<T><<<dim3((x.C + 511) / 512, (x.rows + 255) / 256), 1024, 0, st>>>(x, f, most);
-    else
-        channel_maxima<T><<<dim3((x.C + 63) / 64, (x.rows + 255) / 256), 256, 0, st>>>(x, f, most);
+    const int blocks = (int)((x.rows + kMaximaRows - 1) / kMaximaRows);
+    if (x.HW == 1 && wide_rows(x.x, x.C)) channel_maxima_wide<T><<<dim3((ld + 511) / 512, blocks), 1024, 0, st>>>(x, f, parts, ld);
+    else channel_maxima<T><<<dim3(ld / 64, blocks), 256, 0, st>>>(x, f, parts, ld);
 }
 
 // rows: padded
@@ -936,13 +1013,20 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
     const Tokens& k = r.c.k;
     const long long T_ = s.T(), ld = r.c.ld, Tp = r.c.Tp;
     float* losses = reduction == NONE ? loss : r.losses;
-    find_tokens<<<1, 1024, 0, st>>>(target, ignored, nullptr, k, losses, lse, nullptr, 0, (int)T_);
-    launch_pack<T>({x, k.order, k.count, T_, s.C, s.HW}, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, Tp, st);
+    const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW};
+    const bool few = T_ <= 64;
+    if (few) {
+        begin_few<T, planes><<<16, 256, 0, st>>>(rows, target, ignored, w, k, r.c.xp, Tp * ld, (int)ld, losses, lse, s.HW == 1 && wide_rows(x, s.C),
+                                                 wide_rows(w, s.C), s.V);
+    } else {
+        find_tokens<<<1, 1024, 0, st>>>(target, ignored, nullptr, k, losses, lse, (int)T_);
+        launch_pack<T>(rows, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, Tp, st);
+        target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, false, wide_rows(w, s.C), s.C, s.V);
+    }
     if (r.wp) {
         const long long Vp = round_up(s.V, kRowsPad);
         launch_pack<T>({w, nullptr, nullptr, s.V, s.C, 1}, {}, {r.wp, nullptr, Vp * ld, nullptr, (int)ld, kRowsPad}, Vp, st);
     }
-    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, false, wide_rows(w, s.C), s.C, s.V);
     int tiles = 0;
     const hipError_t e = with_form<T>(s.V, T_, [&](auto form) {
         typedef LossProduct<T, decltype(form)> P;
@@ -978,11 +1062,12 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
     const Tokens& k = r.c.k;
     const long long T_ = s.T(), ld = r.c.ld, Tp = r.c.Tp, Vp = round_up(s.V, kRowsPad), piece = r.pieces.piece;
     const Factor f = {dloss, k.order, k.count, reduction};
-    find_tokens<<<1, 1024, 0, st>>>(target, ignored, lse, k, nullptr, nullptr, r.most_x, planes == 1 ? 2 * s.C : 0, (int)T_);
+    find_tokens<<<1, 1024, 0, st>>>(target, ignored, lse, k, nullptr, nullptr, (int)T_);
     const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW}, all = {w, nullptr, nullptr, s.V, s.C, 1};
     if (planes == 1) {
-        launch_maxima(rows, f, r.most_x, st);
-        launch_maxima(all, {}, r.most_w, st);
+        launch_maxima(rows, f, r.parts_x, (int)ld, st);
+        launch_maxima(all, {}, r.parts_w, (int)ld, st);
+        join_maxima<<<dim3(ld / 64, 2), 1024, 0, st>>>(r.parts_x, k.count, r.most_x, r.parts_w, s.V, r.most_w, (int)ld);
     }
     launch_pack(rows, f, {r.c.xp, r.xs, Tp * ld, r.most_x, (int)ld, kPad}, Tp, st);
     if (planes == 1 || r.wp) launch_pack(all, {}, {r.wp, r.ws, Vp * ld, r.most_w, (int)ld, kRowsPad}, Vp, st);
