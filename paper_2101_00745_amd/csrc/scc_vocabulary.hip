@@ -439,89 +439,105 @@ __global__ __launch_bounds__(256) void begin_few(Rows<T> x, const long long* __r
     }
 }
 
-// Workgroup -> tile.  Workgroups go to the XCDs in turn, and each of these takes a run of tiles: bands of four tiles of rows, all columns of a band.
+// Workgroup -> tiles.  Workgroups go to the XCDs in turn, and each of these takes a run of tiles: bands of four tiles of rows, all columns of a band.
 struct Grid {
     int rows, columns;
 };
 
-__device__ __forceinline__ void tile_of(int block, const Grid& g, int& row, int& column)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The i'th tile of workgroup `block` of `blocks`, a multiple of 8; false if there is none
+__device__ __forceinline__ bool tile_of(int block, int blocks, int i, const Grid& g, int& row, int& column)
 {
     const int total = g.rows * g.columns, each = (total + 7) / 8;
-    const int id = (block & 7) * each + (block >> 3);
-    if ((block >> 3) >= each || id >= total) {
-        row = -1;
-        return;
-    }
+    const int in_run = (block >> 3) + i * (blocks >> 3), id = (block & 7) * each + in_run;
+    if (in_run >= each || id >= total) return false;
     const int band = id / (4 * g.columns), in = id - band * 4 * g.columns;
     const int high = g.rows - band * 4 < 4 ? g.rows - band * 4 : 4;
     column = in / high;
     row = band * 4 + in - column * high;
+    return true;
 }
 
 int blocks_of(const Grid& g) { return ((long long)g.rows * g.columns + 7) / 8 * 8; }
 
+// ... of a kernel whose workgroups walk over the tiles: as many as are resident, 256 CUs with 160 KB of LDS each
+int walkers_of(const Grid& g, int lds)
+{
+    const int all = blocks_of(g), resident = 256 * (lds <= 80 * 1024 ? 2 : 1);
+    return all < resident ? all : resident;
+}
+
 // Logits of a tile: rows of the vocabulary, columns are tokens.  part[tile row][token] = (max, sum of exp(l - max))
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Operand w, Operand x, const int* __restrict__ count, float2* __restrict__ part, long long Tp,
-                                                       int steps, int V, Grid g)
+__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Operand w, Operand x, const int* __restrict__ count,
+                                                                              float2* __restrict__ part, long long Tp, int steps, int V, int rows)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    int row, column;
-    tile_of(blockIdx.x, g, row, column);
-    if (row < 0 || column * P::kN >= *count) return;
-    f32x16 acc[P::FM][P::FN];
-    P::run(w, x, (long long)row * P::kM, (long long)column * P::kN, 0, steps, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
-    const int v0 = row * P::kM + wm * 32 * P::FM + 4 * (lane >> 5);
-    if (row * P::kM + P::kM > V)
-#pragma unroll
-        for (int m = 0; m < P::FM; ++m)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (v0 + m * 32 + 8 * (r / 4) + r % 4 >= V)
-#pragma unroll
-                    for (int n = 0; n < P::FN; ++n) acc[m][n][r] = -__builtin_inff();
     constexpr int kHigh = P::kM / 32 / P::FM;   // wavefronts one above the other
-    float* most = (float*)lds;                  // [kHigh][kN], then sums likewise
+    const Grid g = {rows, (uniform(*count) + P::kN - 1) / P::kN};
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
+    float* most = (float*)(lds + P::kLds);      // [kHigh][kN], then sums likewise
     float* sums = most + kHigh * P::kN;
+    P::walk(
+        w, x, lds,
+        [&](int i, typename P::Part& p) {
+            int row, column;
+            if (!tile_of(blockIdx.x, gridDim.x, i, g, row, column)) return false;
+            p = {(long long)row * P::kM, (long long)column * P::kN, 0, steps};
+            return true;
+        },
+        [&](const typename P::Part& p, f32x16 (&acc)[P::FM][P::FN]) {
+            const int v0 = (int)p.row + wm * 32 * P::FM + 4 * (lane >> 5);
+            if (p.row + P::kM > V)
 #pragma unroll
-    for (int n = 0; n < P::FN; ++n) {
-        float high = -__builtin_inff();
+                for (int m = 0; m < P::FM; ++m)
 #pragma unroll
-        for (int m = 0; m < P::FM; ++m)
+                    for (int r = 0; r < 16; ++r)
+                        if (v0 + m * 32 + 8 * (r / 4) + r % 4 >= V)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) high = fmaxf(high, acc[m][n][r]);
-        high = fmaxf(high, __shfl_xor(high, 32));
-        if (lane < 32) most[wm * P::kN + (wn * P::FN + n) * 32 + lane] = high;
-    }
-    __syncthreads();
+                            for (int n = 0; n < P::FN; ++n) acc[m][n][r] = -__builtin_inff();
 #pragma unroll
-    for (int n = 0; n < P::FN; ++n) {
-        const int at = (wn * P::FN + n) * 32 + (lane & 31);
-        float high = most[at];
+            for (int n = 0; n < P::FN; ++n) {
+                float high = -__builtin_inff();
 #pragma unroll
-        for (int i = 1; i < kHigh; ++i) high = fmaxf(high, most[i * P::kN + at]);
-        const float shift = -high * kLog2E;
-        float sum = 0.f;
+                for (int m = 0; m < P::FM; ++m)
 #pragma unroll
-        for (int m = 0; m < P::FM; ++m)
+                    for (int r = 0; r < 16; ++r) high = fmaxf(high, acc[m][n][r]);
+                high = fmaxf(high, __shfl_xor(high, 32));
+                if (lane < 32) most[wm * P::kN + (wn * P::FN + n) * 32 + lane] = high;
+            }
+            lds_barrier();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
-        sum += __shfl_xor(sum, 32);
-        if (lane < 32) sums[wm * P::kN + at] = sum;
-    }
-    __syncthreads();
-    if (threadIdx.x < P::kN) {
-        const int at = threadIdx.x;
-        float high = most[at], sum = sums[at];
+            for (int n = 0; n < P::FN; ++n) {
+                const int at = (wn * P::FN + n) * 32 + (lane & 31);
+                float high = most[at];
 #pragma unroll
-        for (int i = 1; i < kHigh; ++i) {
-            high = fmaxf(high, most[i * P::kN + at]);
-            sum += sums[i * P::kN + at];
-        }
-        part[row * Tp + column * P::kN + at] = make_float2(high, sum);
-    }
+                for (int i = 1; i < kHigh; ++i) high = fmaxf(high, most[i * P::kN + at]);
+                const float shift = -high * kLog2E;
+                float sum = 0.f;
+#pragma unroll
+                for (int m = 0; m < P::FM; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
+                sum += __shfl_xor(sum, 32);
+                if (lane < 32) sums[wm * P::kN + at] = sum;
+            }
+            lds_barrier();
+            if (threadIdx.x < P::kN) {
+                const int at = threadIdx.x;
+                float high = most[at], sum = sums[at];
+#pragma unroll
+                for (int i = 1; i < kHigh; ++i) {
+                    high = fmaxf(high, most[i * P::kN + at]);
+                    sum += sums[i * P::kN + at];
+                }
+                part[p.row / P::kM * Tp + p.column + at] = make_float2(high, sum);
+            }
+            lds_barrier();                      // most is written again
+        });
 }
+template <typename P> constexpr int kLossLds = P::kLds + 2 * (P::kM / 32 / P::FM) * P::kN * 4;
 
 // lse and loss of 64 packed tokens from the tiles' parts, 16 wavefronts taking the parts in turn; losses: of the tokens of x
 __global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ part, long long Tp, int tiles, Tokens k, float* __restrict__ losses,
@@ -581,59 +597,95 @@ __global__ __launch_bounds__(1024) void sum_losses(const float* __restrict__ los
     *out = (float)(mean ? sum / (double)(*count > 0 ? *count : 1) : sum);
 }
 
-// p of a tile of a piece of the vocabulary: p[token][v - first]
+// p of a tile of a piece of the vocabulary: p[token][v - first].  Three planes: workgroups walk over the tiles, and a tile's values leave through 16 KB beside
+// the operands' buffers while the next tile's are loaded (177 -> 162 us a launch of 2000 tokens x 512 x 16000).  One plane: a tile a workgroup, whose
+// values leave through all of the buffers' room in one go (4096 x 512 x 32000: 193 us, walking 230: eight pieces, and no registers left).
+template <typename P> constexpr bool kWalks = P::kPlanes == 3;
+template <typename P> constexpr bool kTwoRooms = P::kLds + 2 * Lines<P>::kPiece <= 160 * 1024;
+template <typename P> constexpr int kShareLds = P::kLds + (kWalks<P> ? (kTwoRooms<P> ? 2 : 1) * Lines<P>::kPiece : 0);
+
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(Operand w, Operand x, Tokens k, Factor f, uint16_t* __restrict__ p, long long plane,
-                                                        int piece, int steps, int first, int V, Grid g)
+__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(Operand w, Operand x, Tokens k, Factor f, uint16_t* __restrict__ p,
+                                                                               long long plane, int piece, int steps, int first, int V, int rows)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     constexpr bool kCut = P::kPlanes == 3;
-    int row, column;
-    tile_of(blockIdx.x, g, row, column);
-    if (row < 0 || column * P::kN >= *k.count) return;
-    f32x16 acc[P::FM][P::FN];
-    P::run(w, x, (long long)first + row * P::kM, (long long)column * P::kN, 0, steps, lds, acc);
+    const int count = uniform(*k.count);
+    const Grid g = {rows, (count + P::kN - 1) / P::kN};
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
-    const int v0 = row * P::kM + wm * 32 * P::FM + 4 * (lane >> 5);
-    const bool ends = first + row * P::kM + P::kM > V;
+    auto at = [&](int i, typename P::Part& part) {
+        int row, column;
+        if (!tile_of(blockIdx.x, gridDim.x, i, g, row, column)) return false;
+        part = {(long long)first + row * P::kM, (long long)column * P::kN, 0, steps};
+        return true;
+    };
+    // logits into p, which a token's gradient is part of where it is cut
+    auto shares = [&](const typename P::Part& part, f32x16 (&acc)[P::FM][P::FN]) {
+        const int v0 = (int)part.row + wm * 32 * P::FM + 4 * (lane >> 5);
+        const bool ends = part.row + P::kM > V;
 #pragma unroll
-    for (int n = 0; n < P::FN; ++n) {
-        const long long t = (long long)column * P::kN + (wn * P::FN + n) * 32 + (lane & 31);
-        const float shift = (kCut ? 0.f : kRaise) - k.lse[t] * kLog2E;
-        const float d = kCut ? f.of((int)t) : 1.f;
+        for (int n = 0; n < P::FN; ++n) {
+            const long long t = part.column + (wn * P::FN + n) * 32 + (lane & 31);
+            const float shift = (kCut ? 0.f : kRaise) - k.lse[t] * kLog2E;
+            const float d = kCut ? f.of((int)t) : 1.f;
 #pragma unroll
-        for (int m = 0; m < P::FM; ++m)
+            for (int m = 0; m < P::FM; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
-                if (ends && first + v0 + m * 32 + 8 * (r / 4) + r % 4 >= V) share = 0.f;
-                acc[m][n][r] = kCut ? share * d : share;
+                for (int r = 0; r < 16; ++r) {
+                    float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
+                    if (ends && v0 + m * 32 + 8 * (r / 4) + r % 4 >= V) share = 0.f;
+                    acc[m][n][r] = kCut ? share * d : share;
+                }
+        }
+    };
+    // the place of token t's target among a tile's rows, -1: elsewhere
+    auto own_place = [&](const typename P::Part& part, long long t) {
+        const long long v = k.target[t] - part.row;
+        return t < count && v >= 0 && v < P::kM ? (int)v : -1;
+    };
+    if constexpr (kWalks<P>) {
+        P::walk(w, x, lds, at, [&](const typename P::Part& part, f32x16 (&acc)[P::FM][P::FN]) {
+            shares(part, acc);
+            float own[P::FN];                   // the target's value, exp(l - lse) - 1, and its place if it is among this wavefront's rows of the vocabulary
+            int own_at[P::FN];
+#pragma unroll
+            for (int n = 0; n < P::FN; ++n) {
+                const long long t = part.column + (wn * P::FN + n) * 32 + (lane & 31);
+                const int v = own_place(part, t);
+                own_at[n] = lane < 32 && v / (32 * P::FM) == wm ? v : -1;
+                own[n] = k.known[t] * f.of((int)t);
             }
-    }
 #pragma unroll
-    for (int plane_at = 0; plane_at < P::kPlanes; ++plane_at) {
-        auto piece_of = [&](float v) {
-            if constexpr (kCut) {
-                uint16_t c[3];
-                cut(v, c);
-                return c[plane_at];
-            } else {
-                return half_of(v);
+            for (int plane_at = 0; plane_at < P::kPlanes; ++plane_at) {
+                auto piece_of = [&](float v) {
+                    uint16_t c[3];
+                    cut(v, c);
+                    return c[plane_at];
+                };
+                Lines<P>::template stream<kTwoRooms<P>>(
+                    lds + P::kLds, wm, wn, [&](int m, int n, int r) { return piece_of(acc[m][n][r]); },
+                    [&](char* room, int n) {
+                        // after the wavefront's own writes of the same line
+                        if (own_at[n] >= 0) *Lines<P>::place(room, lane, own_at[n]) = piece_of(own[n]);
+                    },
+                    [&](int line, int at, u32x4 v) { *(u32x4*)(p + plane_at * plane + (part.column + line) * piece + (part.row - first) + at) = v; });
             }
-        };
-        if (plane_at) __syncthreads();
+        });
+    } else {
+        typename P::Part part;
+        if (!at(0, part)) return;
+        f32x16 acc[P::FM][P::FN];
+        P::run(w, x, part, lds, acc);
+        shares(part, acc);
         Lines<P>::store(
-            lds, wm, wn, [&](int m, int n, int r) { return piece_of(acc[m][n][r]); },
+            lds, wm, wn, [&](int m, int n, int r) { return half_of(acc[m][n][r]); },
             [&]() {
-                // the target's own, from its logit: exp(l - lse) - 1
                 if (threadIdx.x >= P::kN) return;
-                const long long t = (long long)column * P::kN + threadIdx.x, v = k.target[t] - first - row * P::kM;
-                if (t < *k.count && v >= 0 && v < P::kM)
-                    *Lines<P>::place(lds, threadIdx.x, (int)v) = piece_of(k.known[t] * (kCut ? f.of((int)t) : (float)(1 << (int)kRaise)));
+                const long long t = part.column + threadIdx.x;
+                const int v = own_place(part, t);
+                if (v >= 0) *Lines<P>::place(lds, threadIdx.x, v) = half_of(k.known[t] * (float)(1 << (int)kRaise));
             },
-            [&](int line, int at, u32x4 v) {
-                *(u32x4*)(p + plane_at * plane + ((long long)column * P::kN + line) * piece + row * P::kM + at) = v;
-            });
+            [&](int line, int at, u32x4 v) { *(u32x4*)(p + (part.column + line) * piece + (part.row - first) + at) = v; });
     }
 }
 
@@ -664,12 +716,11 @@ __global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_prod
     if (of_x >= 0 && of_x < a.blocks_x) {
         const int each = a.blocks_x / a.split, part = of_x / each;
         int row, column;
-        tile_of(of_x - part * each, a.gx, row, column);
-        if (row < 0 || column * PX::kN >= *a.count) return;
+        if (!tile_of(of_x - part * each, each, 0, {a.gx.rows, (uniform(*a.count) + PX::kN - 1) / PX::kN}, row, column)) return;
         const int from = part * a.split_steps, left = a.steps - from;
         f32x16 acc[PX::FM][PX::FN];
-        PX::run(a.w, a.p_tokens, (long long)row * PX::kM, (long long)column * PX::kN, (long long)from * PX::kK,
-                left < a.split_steps ? left : a.split_steps, lds, acc);
+        PX::run(a.w, a.p_tokens, {(long long)row * PX::kM, (long long)column * PX::kN, (long long)from * PX::kK, left < a.split_steps ? left : a.split_steps}, lds,
+                acc);
 #pragma unroll
         for (int n = 0; n < PX::FN; ++n) {
             const long long t = (long long)column * PX::kN + (wn * PX::FN + n) * 32 + (lane & 31);
@@ -695,10 +746,9 @@ __global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_prod
         return;
     }
     int row, column;
-    tile_of(of_w, a.gw, row, column);
-    if (row < 0) return;
+    if (!tile_of(of_w, a.blocks_w, 0, a.gw, row, column)) return;
     f32x16 acc[PW::FM][PW::FN];
-    PW::run(a.x, a.p_rows, (long long)row * PW::kM, (long long)column * PW::kN, 0, (*a.count + PW::kK - 1) / PW::kK, lds, acc);
+    PW::run(a.x, a.p_rows, {(long long)row * PW::kM, (long long)column * PW::kN, 0, (uniform(*a.count) + PW::kK - 1) / PW::kK}, lds, acc);
 #pragma unroll
     for (int m = 0; m < PW::FM; ++m)
 #pragma unroll
@@ -1032,10 +1082,11 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
         typedef LossProduct<T, decltype(form)> P;
         const Grid g = {(int)((s.V + P::kM - 1) / P::kM), (int)((T_ + P::kN - 1) / P::kN)};
         tiles = g.rows;
-        const hipError_t e = allow(loss_product<P>, P::kLds);
+        const hipError_t e = allow(loss_product<P>, kLossLds<P>);
         if (e != hipSuccess) return e;
         const Operand b = {r.c.xp, Tp * ld, ld, Tp - 1};
-        loss_product<P><<<blocks_of(g), P::kThreads, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k.count, r.part, Tp, (int)(ld / P::kK), s.V, g);
+        loss_product<P><<<walkers_of(g, kLossLds<P>), P::kThreads, kLossLds<P>, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k.count, r.part, Tp,
+                                                                                      (int)(ld / P::kK), s.V, g.rows);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
@@ -1080,11 +1131,11 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
         e = with_form<T>(length, T_, [&](auto form) {
             typedef LossProduct<T, decltype(form)> P;
             const Grid g = {(int)(length / P::kM), (int)((T_ + P::kN - 1) / P::kN)};
-            const hipError_t e = allow(share_product<P>, P::kLds);
+            const hipError_t e = allow(share_product<P>, kShareLds<P>);
             if (e != hipSuccess) return e;
             const Operand b = {r.c.xp, Tp * ld, ld, Tp - 1};
-            share_product<P><<<blocks_of(g), P::kThreads, P::kLds, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k, f, r.p, Tp * piece, (int)piece,
-                                                                       (int)(ld / P::kK), (int)first, s.V, g);
+            share_product<P><<<kWalks<P> ? walkers_of(g, kShareLds<P>) : blocks_of(g), P::kThreads, kShareLds<P>, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k, f, r.p, Tp * piece,
+                                                                                            (int)piece, (int)(ld / P::kK), (int)first, s.V, g.rows);
             return hipGetLastError();
         });
         if (e != hipSuccess) break;

@@ -110,58 +110,66 @@ struct Product {
     static_assert(A::kLoads % kWaves == 0 && B::kLoads % kWaves == 0 && kM % (32 * F::WM) == 0 && kN % (32 * F::WN) == 0 && kLds <= 160 * 1024,
                   "the wavefronts load and multiply equally much");
 
-    // steps tiles of kK, from K = begin, a multiple of kK, on
-    static __device__ __forceinline__ void run(const Operand& a, const Operand& b, long long row, long long column, long long begin, int steps,
-                                               char* lds, f32x16 (&acc)[FM][FN])
+    // What a workgroup multiplies: a tile of rows and columns over `steps` times kK values of K, from K = begin, a multiple of kK, on
+    struct Part {
+        long long row, column, begin;
+        int steps;
+    };
+
+    // at(i, part): the workgroup's i'th part, false behind the last one (steps > 0 in all); done(part, acc): its sums.  The loads run on from one part into the next: while
+    // done() works on a part's sums the next part's first buffers are under way, so it leaves the kLds bytes alone.
+    template <typename At, typename Done>
+    static __device__ __forceinline__ void walk(const Operand& a, const Operand& b, char* lds, At&& at, Done&& done)
     {
         typedef const __attribute__((address_space(1))) void* gptr;
         typedef __attribute__((address_space(3))) void* lptr;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wm = wave / F::WN, wn = wave % F::WN;
         const uint16_t *from_a[kLoadsA], *from_b[kLoadsB];
+        Part ahead;
+        int asked = 0, left = 0;                // parts that are asked for, steps of the last of them that are not
+        if (!at(0, ahead)) return;
+        auto begin_part = [&]() {
 #pragma unroll
-        for (int i = 0; i < kLoadsA; ++i) from_a[i] = A::source(a, row, wave * kLoadsA + i, lane) + begin / kK * A::step(a);
+            for (int i = 0; i < kLoadsA; ++i) from_a[i] = A::source(a, ahead.row, wave * kLoadsA + i, lane) + ahead.begin / kK * A::step(a);
 #pragma unroll
-        for (int i = 0; i < kLoadsB; ++i) from_b[i] = B::source(b, column, wave * kLoadsB + i, lane) + begin / kK * B::step(b);
-#pragma unroll
-        for (int m = 0; m < FM; ++m)
-#pragma unroll
-            for (int n = 0; n < FN; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
-        // the last steps ask for the last tile again, so that the number of loads under way is always the same
-        int asked = 0;
+            for (int i = 0; i < kLoadsB; ++i) from_b[i] = B::source(b, ahead.column, wave * kLoadsB + i, lane) + ahead.begin / kK * B::step(b);
+            left = ahead.steps;
+            ++asked;
+        };
+        begin_part();
+        // behind the last part its last tile is asked for again, so that the number of loads under way is always the same
         auto request = [&](int stage) {
             char* to = lds + stage * kStage + wave * kLoadsA * 1024;
-            const bool more = ++asked < steps;
-            const long long next_a = more ? A::step(a) : 0, next_b = more ? B::step(b) : 0;
 #pragma unroll
-            for (int i = 0; i < kLoadsA; ++i) {
-                __builtin_amdgcn_global_load_lds((gptr)from_a[i], (lptr)(to + i * 1024), 16, 0, 0);
-                from_a[i] += next_a;
-            }
+            for (int i = 0; i < kLoadsA; ++i) __builtin_amdgcn_global_load_lds((gptr)from_a[i], (lptr)(to + i * 1024), 16, 0, 0);
             to = lds + stage * kStage + A::kBytes * kPlanes + wave * kLoadsB * 1024;
 #pragma unroll
-            for (int i = 0; i < kLoadsB; ++i) {
-                __builtin_amdgcn_global_load_lds((gptr)from_b[i], (lptr)(to + i * 1024), 16, 0, 0);
-                from_b[i] += next_b;
+            for (int i = 0; i < kLoadsB; ++i) __builtin_amdgcn_global_load_lds((gptr)from_b[i], (lptr)(to + i * 1024), 16, 0, 0);
+            if (--left > 0) {
+                const long long next_a = A::step(a), next_b = B::step(b);
+#pragma unroll
+                for (int i = 0; i < kLoadsA; ++i) from_a[i] += next_a;
+#pragma unroll
+                for (int i = 0; i < kLoadsB; ++i) from_b[i] += next_b;
+            } else if (left == 0 && at(asked, ahead)) {
+                begin_part();
             }
         };
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) request(i);
         // The fragments of 16 values of K are read while the ones before them are multiplied, the first of a step during the last of the step before: that one's
         // products wait for nothing while the next buffer is waited for and the wavefronts meet.
         constexpr int kParts = kK / 16;
         u32x4 fa[2][FM][kPlanes], fb[2][FN][kPlanes];
-        auto read = [&](int to, const char* at, int kk) {
+        auto read = [&](int to, const char* from, int kk) {
 #pragma unroll
             for (int p = 0; p < kPlanes; ++p) {
 #pragma unroll
-                for (int m = 0; m < FM; ++m) fa[to][m][p] = A::fragment(at, p, wm * 32 * FM, m, kk, lane);
+                for (int m = 0; m < FM; ++m) fa[to][m][p] = A::fragment(from, p, wm * 32 * FM, m, kk, lane);
 #pragma unroll
-                for (int n = 0; n < FN; ++n) fb[to][n][p] = B::fragment(at + A::kBytes * kPlanes, p, wn * 32 * FN, n, kk, lane);
+                for (int n = 0; n < FN; ++n) fb[to][n][p] = B::fragment(from + A::kBytes * kPlanes, p, wn * 32 * FN, n, kk, lane);
             }
         };
+        f32x16 acc[FM][FN];
         auto products = [&](int of) {
             // three planes: the small products first
 #pragma unroll
@@ -185,39 +193,81 @@ struct Product {
                 if (reads == 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
             }
         };
-        // this wavefront's loads of the oldest buffer are there and it has read all that it wants of the one before; then all wavefronts' are and have
-        auto meet = [&]() {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (kStages - 2)) : "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        };
-        if (steps > 0) {
-            meet();
-            read(0, lds, 0);
-        }
-        int stage = 0;
-        for (int k = 0; k < steps; ++k) {
-            const char* at = lds + stage * kStage;
-            // the buffer of the step before has been read by all
-            request(stage == 0 ? kStages - 1 : stage - 1);
-            stage = stage == kStages - 1 ? 0 : stage + 1;
 #pragma unroll
-            for (int kk = 0; kk < kParts; ++kk) {
-                if (kk + 1 < kParts) {
-                    read((kk + 1) & 1, at, kk + 1);
-                } else if (k + 1 < steps) {
-                    meet();
-                    read(0, lds + stage * kStage, 0);
+        for (int i = 0; i < kStages; ++i) request(i);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (kStages - 1)) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(0, lds, 0);
+        int stage = 0;
+        Part now, next;
+        bool more = at(0, now);
+        for (int i = 0; more; ++i) {
+            more = at(i + 1, next);
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int n = 0; n < FN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[m][n][r] = 0.f;
+            for (int k = 0; k < now.steps; ++k) {
+                const char* from = lds + stage * kStage;
+#pragma unroll
+                for (int kk = 0; kk < kParts; ++kk) {
+                    if (kk + 1 < kParts) {
+                        read((kk + 1) & 1, from, kk + 1);
+                    } else if (more || k + 1 < now.steps) {
+                        // this wavefront's loads of the next buffer are there and it has read all of this one; then all wavefronts' are and have
+                        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads * (kStages - 2)) : "memory");
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                        request(stage);
+                        stage = stage == kStages - 1 ? 0 : stage + 1;
+                        read(0, lds + stage * kStage, 0);
+                    }
+                    products(kk & 1);
+                    interleave();
                 }
-                products(kk & 1);
-                interleave();
             }
+            done(now, acc);
+            now = next;
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();           // LDS is the caller's again
+        __builtin_amdgcn_s_barrier();           // nothing is under way to LDS any more
         asm volatile("" ::: "memory");
     }
+
+    // One part; steps may be 0.  LDS is the caller's again afterwards.
+    static __device__ __forceinline__ void run(const Operand& a, const Operand& b, const Part& part, char* lds, f32x16 (&sums)[FM][FN])
+    {
+#pragma unroll
+        for (int m = 0; m < FM; ++m)
+#pragma unroll
+            for (int n = 0; n < FN; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sums[m][n][r] = 0.f;
+        walk(
+            a, b, lds,
+            [&](int i, Part& p) {
+                p = part;
+                return i == 0 && part.steps > 0;
+            },
+            [&](const Part&, f32x16 (&acc)[FM][FN]) {
+#pragma unroll
+                for (int m = 0; m < FM; ++m)
+#pragma unroll
+                    for (int n = 0; n < FN; ++n) sums[m][n] = acc[m][n];
+            });
+    }
 };
+
+// Barrier for what wavefronts hand each other in LDS; loads and stores of memory go on
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 // A tile's sums as 16-bit values to memory, rows of it (consecutive sums of a lane) along the lines there.  value(m, n, r): of an accumulator; change(line, values
 // of a line in LDS): before they leave.  In LDS a line of kM values has its 16-byte chunks exchanged by an exclusive or with the line, so that neither the
@@ -256,6 +306,41 @@ struct Lines {
             const int line = i / kChunks, chunk = i % kChunks;
             out(line, chunk * 8, *(const u32x4*)place(lds, line, chunk * 8));
         }
+    }
+
+    // The same in pieces of 32 lines through a room of kPiece bytes (and another one, where `two`, which saves half of the barriers), for a tile whose operands'
+    // buffers are in use.  change(n, first): the wavefronts that hold the 32 lines from `first` on have written them.
+    static constexpr int kPiece = P::kM * 32 * 2;
+    template <bool TWO, typename V, typename C, typename S>
+    static __device__ __forceinline__ void stream(char* room, int wm, int wn, V&& value, C&& change, S&& out)
+    {
+        typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+        constexpr int kColumns = P::kN / 32 / P::FN;
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kColumns * P::FN; ++i) {
+            const int n = i % P::FN;                // of the wavefronts in column i / FN
+            char* const lds = room + (TWO ? i & 1 : 0) * kPiece;
+            if (wn == i / P::FN) {
+                const int line = lane & 31;
+#pragma unroll
+                for (int m = 0; m < P::FM; ++m)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const u16x4 v = {value(m, n, 4 * q), value(m, n, 4 * q + 1), value(m, n, 4 * q + 2), value(m, n, 4 * q + 3)};
+                        *(u16x4*)place(lds, line, (wm * P::FM + m) * 32 + 8 * q + 4 * (lane >> 5)) = v;
+                    }
+                change(lds, n);
+            }
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < (32 * kChunks + P::kThreads - 1) / P::kThreads; ++j) {
+                const int at = threadIdx.x + j * P::kThreads, line = at / kChunks, chunk = at % kChunks;
+                if (32 * kChunks % P::kThreads == 0 || line < 32) out(i * 32 + line, chunk * 8, *(const u32x4*)place(lds, line, chunk * 8));
+            }
+            if (!TWO) lds_barrier();
+        }
+        if (TWO) lds_barrier();
     }
 };
 
