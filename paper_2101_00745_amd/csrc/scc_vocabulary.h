@@ -34,7 +34,7 @@ struct Tokens {
     int *order, *place;             // of a packed token in x; of a token of x among the packed ones, -1: ignored
     int* count;                     // one value
     long long* target;
-    float *known, *lse;             // the target's logit; log-sum-exp
+    float *known, *lse;             // the target's logit (of the loss); log-sum-exp
 };
 
 template <typename T>

@@ -86,6 +86,7 @@ __global__ __launch_bounds__(1024) void find_tokens(const long long* __restrict_
             if (counts) {
                 k.order[place] = t;
                 k.target[place] = y[e];
+                k.known[place] = __uint_as_float(0x7fc00000u);          // until the target's tile writes it: never, if it is outside of the vocabulary
                 if (lse) k.lse[place] = l[e];
             } else {
                 if (none) none[t] = 0.f;
@@ -354,46 +355,10 @@ __global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
     }
 }
 
-// The target's logit of each packed token, a wavefront each; with `minus`, exp(known - lse) - 1 instead.  A target outside of the vocabulary: NaN.  wide: w's
-// rows in vectors of 8
+// find_tokens and pack for the loss of at most 64 tokens in one: a wavefront for each packed token, all of which look at the targets
 template <typename T, int PLANES>
-__global__ __launch_bounds__(256) void target_logits(const uint16_t* __restrict__ xp, long long plane, int ld, const T* __restrict__ w, Tokens k,
-                                                     bool minus, bool wide, int C, int V)
-{
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= *k.count) return;
-    const long long y = k.target[i];
-    const bool valid = y >= 0 && y < V;
-    const T* row = w + (valid ? y : 0) * C;
-    const uint16_t* mine = xp + (long long)i * ld;
-    float sum = 0.f;
-    for (int c = lane * 8; c < C; c += 512) {       // the same sums in the same order whatever w's alignment
-        float v[8] = {}, u[8] = {};
-#pragma unroll
-        for (int p = PLANES - 1; p >= 0; --p) {
-            read8((const bf16_t*)mine + p * plane + c, u);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += u[e];
-        }
-        if (wide) {
-            read8(row + c, u);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = c + e < C ? to_f32(row[c + e]) : 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(v[e], u[e], sum);
-    }
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-    if (!valid) sum = __uint_as_float(0x7fc00000u);
-    if (lane == 0) k.known[i] = minus ? expm1f(sum - k.lse[i]) : sum;
-}
-
-// find_tokens, pack and target_logits of the loss of at most 64 tokens in one: a wavefront for each packed token, all of which look at the targets
-template <typename T, int PLANES>
-__global__ __launch_bounds__(256) void begin_few(Rows<T> x, const long long* __restrict__ target, long long ignored, const T* __restrict__ w, Tokens k,
-                                                 uint16_t* __restrict__ xp, long long plane, int ld, float* none, float* none_lse, bool wide_x, bool wide_w,
-                                                 int V)
+__global__ __launch_bounds__(256) void begin_few(Rows<T> x, const long long* __restrict__ target, long long ignored, Tokens k,
+                                                 uint16_t* __restrict__ xp, long long plane, int ld, float* none, float* none_lse, bool wide)
 {
     const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6), T_ = (int)x.rows, C = (int)x.C;
     const long long y = lane < T_ ? target[lane] : ignored;
@@ -415,27 +380,19 @@ __global__ __launch_bounds__(256) void begin_few(Rows<T> x, const long long* __r
     }
     const uint32_t t = __ffsll(__ballot(y != ignored && before == i)) - 1, n = x.HW > 1 ? t / (uint32_t)x.HW : t;
     const long long v = __shfl(y, (int)t);
-    const bool valid = v >= 0 && v < V;
-    const T *from = x.x + (long long)n * C * x.HW + (t - n * (uint32_t)x.HW), *row = w + (valid ? v : 0) * C;
-    float sum = 0.f;
+    const T* const from = x.x + (long long)n * C * x.HW + (t - n * (uint32_t)x.HW);
     for (int c = lane * 8; c < ld; c += 512) {
-        float a[8] = {}, b[8] = {}, unit[8] = {};
-        if (wide_x && c < C) read8(from + c, a);
-        if (wide_w && c < C) read8(row + c, b);
+        float a[8] = {}, unit[8] = {};
+        if (wide && c < C) read8(from + c, a);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (!wide_x && c + e < C) a[e] = to_f32(from[(c + e) * x.HW]);
-            if (!wide_w && c + e < C) b[e] = to_f32(row[c + e]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(a[e], b[e], sum);
+        for (int e = 0; e < 8; ++e)
+            if (!wide && c + e < C) a[e] = to_f32(from[(c + e) * x.HW]);
         write_packed<PLANES>({xp, nullptr, plane, nullptr, ld, 0}, i, c, a, unit, 1.f);
     }
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
     if (lane == 0) {
         k.order[i] = (int)t;
         k.target[i] = v;
-        k.known[i] = valid ? sum : __uint_as_float(0x7fc00000u);
+        k.known[i] = __uint_as_float(0x7fc00000u);
     }
 }
 
@@ -468,14 +425,34 @@ int walkers_of(const Grid& g, int lds)
     return all < resident ? all : resident;
 }
 
-// Logits of a tile: rows of the vocabulary, columns are tokens.  part[tile row][token] = (max, sum of exp(l - max))
+// f(m, n, r) for the accumulator that holds the target of the lane's token, in the lane that has it; first: row of the vocabulary with which the tile begins
+template <typename P, typename F>
+__device__ __forceinline__ void at_targets(const Tokens& k, int count, int V, long long first, long long column, int wm, int wn, F&& f)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < P::FN; ++n) {
+        const long long t = column + (wn * P::FN + n) * 32 + (lane & 31), y = k.target[t], v = y - first - wm * 32 * P::FM;
+        const int in = t < count && y < V && v >= 0 && v < 32 * P::FM && ((int)v >> 2 & 1) == lane >> 5 ? (int)v & ~4 : -1;
+        if (!__any(in >= 0)) continue;              // seldom: a token's target is in one of the vocabulary's many tiles
+#pragma unroll
+        for (int m = 0; m < P::FM; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (in == m * 32 + 8 * (r / 4) + r % 4) f(t, m, n, r);
+    }
+}
+
+// Logits of a tile: rows of the vocabulary, columns are tokens.  part[tile row][token] = (max, sum of exp(l - max)); and the targets' own: the loss is a difference
+// of the same sums
 template <typename P>
-__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Operand w, Operand x, const int* __restrict__ count,
+__global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Operand w, Operand x, Tokens k,
                                                                               float2* __restrict__ part, long long Tp, int steps, int V, int rows)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     constexpr int kHigh = P::kM / 32 / P::FM;   // wavefronts one above the other
-    const Grid g = {rows, (uniform(*count) + P::kN - 1) / P::kN};
+    const int count = uniform(*k.count);
+    const Grid g = {rows, (count + P::kN - 1) / P::kN};
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (P::kN / 32 / P::FN), wn = wave % (P::kN / 32 / P::FN);
     float* most = (float*)(lds + P::kLds);      // [kHigh][kN], then sums likewise
     float* sums = most + kHigh * P::kN;
@@ -489,6 +466,7 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Op
         },
         [&](const typename P::Part& p, f32x16 (&acc)[P::FM][P::FN]) {
             const int v0 = (int)p.row + wm * 32 * P::FM + 4 * (lane >> 5);
+            at_targets<P>(k, count, V, p.row, p.column, wm, wn, [&](long long t, int m, int n, int r) { k.known[t] = acc[m][n][r]; });
             if (p.row + P::kM > V)
 #pragma unroll
                 for (int m = 0; m < P::FM; ++m)
@@ -637,24 +615,12 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(O
                     acc[m][n][r] = kCut ? share * d : share;
                 }
         }
-    };
-    // the place of token t's target among a tile's rows, -1: elsewhere
-    auto own_place = [&](const typename P::Part& part, long long t) {
-        const long long v = k.target[t] - part.row;
-        return t < count && v >= 0 && v < P::kM ? (int)v : -1;
+        at_targets<P>(k, count, V, part.row, part.column, wm, wn,
+                      [&](long long t, int m, int n, int r) { acc[m][n][r] -= kCut ? f.of((int)t) : (float)(1 << (int)kRaise); });
     };
     if constexpr (kWalks<P>) {
         P::walk(w, x, lds, at, [&](const typename P::Part& part, f32x16 (&acc)[P::FM][P::FN]) {
             shares(part, acc);
-            float own[P::FN];                   // the target's value, exp(l - lse) - 1, and its place if it is among this wavefront's rows of the vocabulary
-            int own_at[P::FN];
-#pragma unroll
-            for (int n = 0; n < P::FN; ++n) {
-                const long long t = part.column + (wn * P::FN + n) * 32 + (lane & 31);
-                const int v = own_place(part, t);
-                own_at[n] = lane < 32 && v / (32 * P::FM) == wm ? v : -1;
-                own[n] = k.known[t] * f.of((int)t);
-            }
 #pragma unroll
             for (int plane_at = 0; plane_at < P::kPlanes; ++plane_at) {
                 auto piece_of = [&](float v) {
@@ -664,10 +630,6 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(O
                 };
                 Lines<P>::template stream<kTwoRooms<P>>(
                     lds + P::kLds, wm, wn, [&](int m, int n, int r) { return piece_of(acc[m][n][r]); },
-                    [&](char* room, int n) {
-                        // after the wavefront's own writes of the same line
-                        if (own_at[n] >= 0) *Lines<P>::place(room, lane, own_at[n]) = piece_of(own[n]);
-                    },
                     [&](int line, int at, u32x4 v) { *(u32x4*)(p + plane_at * plane + (part.column + line) * piece + (part.row - first) + at) = v; });
             }
         });
@@ -679,12 +641,6 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(O
         shares(part, acc);
         Lines<P>::store(
             lds, wm, wn, [&](int m, int n, int r) { return half_of(acc[m][n][r]); },
-            [&]() {
-                if (threadIdx.x >= P::kN) return;
-                const long long t = part.column + threadIdx.x;
-                const int v = own_place(part, t);
-                if (v >= 0) *Lines<P>::place(lds, threadIdx.x, v) = half_of(k.known[t] * (float)(1 << (int)kRaise));
-            },
             [&](int line, int at, u32x4 v) { *(u32x4*)(p + (part.column + line) * piece + (part.row - first) + at) = v; });
     }
 }
@@ -783,7 +739,7 @@ __global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_prod
         return;
     }
     Lines<PW>::store(
-        lds, wm, wn, [&](int m, int n, int r) { return from_f32<bf16_t>(acc[m][n][r]); }, []() {},
+        lds, wm, wn, [&](int m, int n, int r) { return from_f32<bf16_t>(acc[m][n][r]); },
         [&](int line, int at, u32x4 v) {
             const int in = column * PW::kN + line, c = row * PW::kM + at;
             const long long place = a.first + in;
@@ -1066,12 +1022,10 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
     const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW};
     const bool few = T_ <= 64;
     if (few) {
-        begin_few<T, planes><<<16, 256, 0, st>>>(rows, target, ignored, w, k, r.c.xp, Tp * ld, (int)ld, losses, lse, s.HW == 1 && wide_rows(x, s.C),
-                                                 wide_rows(w, s.C), s.V);
+        begin_few<T, planes><<<16, 256, 0, st>>>(rows, target, ignored, k, r.c.xp, Tp * ld, (int)ld, losses, lse, s.HW == 1 && wide_rows(x, s.C));
     } else {
         find_tokens<<<1, 1024, 0, st>>>(target, ignored, nullptr, k, losses, lse, (int)T_);
         launch_pack<T>(rows, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, Tp, st);
-        target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, false, wide_rows(w, s.C), s.C, s.V);
     }
     if (r.wp) {
         const long long Vp = round_up(s.V, kRowsPad);
@@ -1085,7 +1039,7 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
         const hipError_t e = allow(loss_product<P>, kLossLds<P>);
         if (e != hipSuccess) return e;
         const Operand b = {r.c.xp, Tp * ld, ld, Tp - 1};
-        loss_product<P><<<walkers_of(g, kLossLds<P>), P::kThreads, kLossLds<P>, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k.count, r.part, Tp,
+        loss_product<P><<<walkers_of(g, kLossLds<P>), P::kThreads, kLossLds<P>, st>>>(vocabulary_rows(w, r.wp, s, ld), b, k, r.part, Tp,
                                                                                       (int)(ld / P::kK), s.V, g.rows);
         return hipGetLastError();
     });
@@ -1122,7 +1076,6 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
     }
     launch_pack(rows, f, {r.c.xp, r.xs, Tp * ld, r.most_x, (int)ld, kPad}, Tp, st);
     if (planes == 1 || r.wp) launch_pack(all, {}, {r.wp, r.ws, Vp * ld, r.most_w, (int)ld, kRowsPad}, Vp, st);
-    target_logits<T, planes><<<(T_ + 3) / 4, 256, 0, st>>>(r.c.xp, Tp * ld, (int)ld, w, k, true, wide_rows(w, s.C), s.C, s.V);
     int parts = 1;                          // of p W: the first piece, the longest, has the most
     hipError_t e = hipSuccess;
     for (int i = 0; i < r.pieces.count && e == hipSuccess; ++i) {

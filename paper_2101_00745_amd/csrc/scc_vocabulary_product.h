@@ -269,8 +269,7 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-// A tile's sums as 16-bit values to memory, rows of it (consecutive sums of a lane) along the lines there.  value(m, n, r): of an accumulator; change(line, values
-// of a line in LDS): before they leave.  In LDS a line of kM values has its 16-byte chunks exchanged by an exclusive or with the line, so that neither the
+// A tile's sums as 16-bit values to memory, rows of it (consecutive sums of a lane) along the lines there.  value(m, n, r): of an accumulator.  In LDS a line of kM values has its 16-byte chunks exchanged by an exclusive or with the line, so that neither the
 // writes (32 lines at a time) nor the reads (a line at a time) meet in a bank.
 template <typename P>
 struct Lines {
@@ -282,8 +281,8 @@ struct Lines {
         return (uint16_t*)(lds + line * (P::kM * 2) + (((at >> 3) ^ line) & (kChunks - 1)) * 16 + (at & 7) * 2);
     }
 
-    template <typename V, typename C, typename S>
-    static __device__ __forceinline__ void store(char* lds, int wm, int wn, V&& value, C&& change, S&& out)
+    template <typename V, typename S>
+    static __device__ __forceinline__ void store(char* lds, int wm, int wn, V&& value, S&& out)
     {
         typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
         const int lane = threadIdx.x & 63;
@@ -299,8 +298,6 @@ struct Lines {
                 }
         }
         __syncthreads();
-        change();
-        __syncthreads();
 #pragma unroll 4
         for (int i = threadIdx.x; i < P::kN * kChunks; i += P::kThreads) {
             const int line = i / kChunks, chunk = i % kChunks;
@@ -309,10 +306,10 @@ struct Lines {
     }
 
     // The same in pieces of 32 lines through a room of kPiece bytes (and another one, where `two`, which saves half of the barriers), for a tile whose operands'
-    // buffers are in use.  change(n, first): the wavefronts that hold the 32 lines from `first` on have written them.
+    // buffers are in use.
     static constexpr int kPiece = P::kM * 32 * 2;
-    template <bool TWO, typename V, typename C, typename S>
-    static __device__ __forceinline__ void stream(char* room, int wm, int wn, V&& value, C&& change, S&& out)
+    template <bool TWO, typename V, typename S>
+    static __device__ __forceinline__ void stream(char* room, int wm, int wn, V&& value, S&& out)
     {
         typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
         constexpr int kColumns = P::kN / 32 / P::FN;
@@ -330,7 +327,6 @@ struct Lines {
                         const u16x4 v = {value(m, n, 4 * q), value(m, n, 4 * q + 1), value(m, n, 4 * q + 2), value(m, n, 4 * q + 3)};
                         *(u16x4*)place(lds, line, (wm * P::FM + m) * 32 + 8 * q + 4 * (lane >> 5)) = v;
                     }
-                change(lds, n);
             }
             lds_barrier();
 #pragma unroll
