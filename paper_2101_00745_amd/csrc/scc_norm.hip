@@ -85,6 +85,9 @@ __device__ __forceinline__ void store_bytes(uint8_t* to, const uint32_t (&q)[V])
 {
     if constexpr (V == 1) {
         *to = (uint8_t)q[0];
+    } else if constexpr (V == 2) {
+        typedef uint16_t both __attribute__((aligned(1)));
+        *(both*)to = (uint16_t)(q[0] | q[1] << 8);
     } else {
         typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(1)));
         words o;
@@ -291,6 +294,16 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
 
 // ---- tokens as columns ----
 
+// The i'th tile of workgroup `block` of `blocks`, a multiple of 8; -1: none.  Workgroups go to the XCDs in turn, and with `runs` each of these takes a run of
+// tiles: where planes do not end at a line of the L2 neighbouring tiles share lines (8 x 512 x 2000 bf16: backward 24.2 -> 19.8 us; where they do, it is 261
+// instead of 242 for 128 x 512 x 32x32 fp32).
+__device__ __forceinline__ long long tile_of(uint32_t block, uint32_t blocks, uint32_t i, uint32_t tiles, bool runs)
+{
+    if (!runs) return block + (long long)i * blocks < tiles ? block + (long long)i * blocks : -1;
+    const uint32_t each = (tiles + 7) / 8, in_run = (block >> 3) + i * (blocks >> 3), tile = (block & 7) * each + in_run;
+    return in_run < each && tile < tiles ? (long long)tile : -1;
+}
+
 // LANES groups of V columns, THREADS / LANES channels at a time, NV times that in registers (0: any number, read again)
 template <int V, int LANES, int THREADS, int SUMS>
 struct Columns {
@@ -354,7 +367,9 @@ __global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__
 {
     typedef Columns<V, LANES, THREADS, 1> Cols;
     __shared__ Cols cols;
-    const uint32_t group = blockIdx.x * LANES + threadIdx.x % LANES;
+    const long long tile = tile_of(blockIdx.x, gridDim.x, 0, ((uint32_t)groups.count + LANES - 1) / LANES, true);
+    if (tile < 0) return;
+    const uint32_t group = (uint32_t)tile * LANES + threadIdx.x % LANES;
     const bool there = group < (uint32_t)groups.count;
     uint32_t n, p;
     column_of_group(there ? group : (uint32_t)groups.count - 1, groups, n, p);
@@ -479,8 +494,12 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
         for (int m = 1; m < LANES; m *= 2) v += __shfl_xor(v, m);
         return v;
     };
-    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint32_t group = tile * LANES + threadIdx.x % LANES;
+    const bool runs = s.HW * (int)sizeof(T) % 128 != 0;
+    long long tile = tile_of(blockIdx.x, gridDim.x, 0, tiles, runs);
+    if (NV == 0 && tile < 0)                    // a row of sums all the same
+        for (int c = threadIdx.x; c < s.C; c += THREADS) part[(size_t)blockIdx.x * s.C + c] = 0.f;
+    for (uint32_t i = 0; tile >= 0; tile = tile_of(blockIdx.x, gridDim.x, ++i, tiles, runs)) {
+        const uint32_t group = (uint32_t)tile * LANES + threadIdx.x % LANES;
         const bool there = group < (uint32_t)groups.count;
         const uint32_t u = there ? group : (uint32_t)groups.count - 1;
         uint32_t n, p;
@@ -567,7 +586,7 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
                 mine = over_lanes(mine);
                 if (threadIdx.x % LANES == 0 && c < s.C) {
                     float* to = part + (size_t)blockIdx.x * s.C + c;
-                    *to = tile == blockIdx.x ? mine : *to + mine;
+                    *to = i == 0 ? mine : *to + mine;
                 }
             }
         }
@@ -632,28 +651,48 @@ hipError_t with_rows(int C, F&& f)
     return width(std::integral_constant<int, 1>());
 }
 
-// f(V, LANES, THREADS, NV) as constants for tokens as columns: pieces of 128 bytes of a plane, 64 where the channels then still fit into registers
-template <typename T, typename F>
-hipError_t with_columns(int C, int HW, F&& f)
-{
-    typedef std::integral_constant<int, kKept> kept;
-    auto width = [&](auto v, auto lanes, auto fewer) {
-        constexpr int L = decltype(lanes)::value;
-        if (C <= 256 / L * kKept) return f(v, lanes, std::integral_constant<int, 256>(), kept());
-        if (C <= 1024 / L * kKept) return f(v, lanes, std::integral_constant<int, 1024>(), kept());
-        if (C <= 2048 / L * kKept) return f(v, fewer, std::integral_constant<int, 1024>(), kept());
-        return f(v, lanes, std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
-    };
-    if (HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
-    return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
-}
-
 Groups groups_of(const Shape& s, int V)
 {
     Problem p = {};
     p.N = s.N;
     p.HW = s.HW;
     return column_groups(p, V);
+}
+
+// f(V, LANES, THREADS, NV) as constants for tokens as columns.  V: 16 bytes of a plane, less where it has less.  A workgroup's piece of a plane is 128 bytes, of
+// channels that do not fit into registers too, which are then read twice, the second time out of the last-level cache (64 x 1000 x 16x16 fp32: 4.4 TB/s
+// forward, in pieces of 64 bytes that fit 4.2; 26 x 2016: 4.4, in pieces of 32 bytes 2.1); 64 or 32 bytes only where there were not 64 workgroups otherwise.
+template <typename T, typename F>
+hipError_t with_columns(const Shape& s, F&& f)
+{
+    auto width = [&](auto v, auto whole) {
+        constexpr int V = decltype(v)::value, L = decltype(whole)::value;
+        typedef std::integral_constant<int, L / 2> half;
+        typedef std::integral_constant<int, L / 4> quarter;
+        typedef std::integral_constant<int, 256> few;
+        typedef std::integral_constant<int, 1024> all;
+        typedef std::integral_constant<int, kKept> kept;
+        typedef std::integral_constant<int, 0> again;
+        const long long groups = groups_of(s, V).count;
+        auto enough = [&](int lanes) { return (groups + lanes - 1) / lanes >= 64; };
+        auto fits = [&](int lanes) { return s.C <= 1024 / lanes * kKept; };
+        if (s.C <= 256 / L * kKept) return f(v, whole, few(), kept());
+        if (fits(L) && (enough(L) || s.C < 2048 / L)) return f(v, whole, all(), kept());
+        if constexpr (V > 1) {
+            if (enough(L)) return f(v, whole, all(), again());
+            if (fits(L / 2) && (enough(L / 2) || s.C < 4096 / L)) return f(v, half(), all(), kept());
+            if (enough(L / 2)) return f(v, half(), all(), again());
+            if (fits(L / 4)) return f(v, quarter(), all(), kept());
+            return f(v, quarter(), all(), again());
+        } else if (fits(L)) {
+            return f(v, whole, all(), kept());
+        }
+        return f(v, whole, all(), again());
+    };
+    if (s.HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>());
+    if (kWide<T> > 4 && s.HW >= 4) return width(std::integral_constant<int, 4>(), std::integral_constant<int, 16>());
+    if (s.HW >= 2) return width(std::integral_constant<int, 2>(), std::integral_constant<int, sizeof(T) == 4 ? 16 : 32>());
+    return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
 }
 
 constexpr int kSumRows = 1024;      // most rows of dw's sums, one for each group of lanes
@@ -678,10 +717,10 @@ Grid backward_grid(const Shape& s)
             return hipSuccess;
         });
     } else {
-        (void)with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto) {
+        (void)with_columns<T>(s, [&](auto v, auto lanes, auto threads, auto) {
             const long long tiles = (groups_of(s, decltype(v)::value).count + decltype(lanes)::value - 1) / decltype(lanes)::value;
             const int wanted = decltype(threads)::value == 256 ? kSumRows : 512;
-            g.blocks = g.rows = (int)(tiles < wanted ? tiles : wanted);
+            g.blocks = g.rows = (int)(tiles < wanted ? (tiles + 7) / 8 * 8 : wanted);
             return hipSuccess;
         });
     }
@@ -701,10 +740,10 @@ hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, flo
             else forward_rows<T, V, TPT, NV, false><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
             return hipGetLastError();
         });
-    return with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto nv) {
+    return with_columns<T>(s, [&](auto v, auto lanes, auto threads, auto nv) {
         constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
         const Groups g = groups_of(s, V);
-        const int blocks = (int)((g.count + L - 1) / L);
+        const int blocks = (int)((g.count + L - 1) / L + 7) / 8 * 8;
         if (scale) forward_columns<T, V, L, TH, NV, true><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
         else forward_columns<T, V, L, TH, NV, false><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
         return hipGetLastError();
@@ -730,7 +769,7 @@ hipError_t launch_backward(const T* x, const T* r, const T* w, const T* dy, cons
             return hipGetLastError();
         });
     else
-        e = with_columns<T>(s.C, s.HW, [&](auto v, auto lanes, auto threads, auto nv) {
+        e = with_columns<T>(s, [&](auto v, auto lanes, auto threads, auto nv) {
             constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
             backward_columns<T, V, L, TH, NV><<<g.blocks, TH, 0, st>>>(x, r, w, dy, dh, dx, part, s, groups_of(s, V));
             return hipGetLastError();

@@ -658,6 +658,9 @@ struct Gradients {
     Grid gx, gw;
     int blocks_x, blocks_w;             // of the grid, the longer ones first
     bool w_first;
+    int split_w;                        // of K = tokens; more than one: sums to dw_parts, [split][row of the piece][ld]
+    float* dw_parts;
+    long long dw_plane;
 };
 
 // p W: rows are channels, columns tokens, K a part of the piece; and p^T x: rows are channels, columns the piece's rows, K the tokens
@@ -701,10 +704,13 @@ __global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_prod
         }
         return;
     }
+    const int each = a.blocks_w / a.split_w, part = of_w / each;
     int row, column;
-    if (!tile_of(of_w, a.blocks_w, 0, a.gw, row, column)) return;
+    if (!tile_of(of_w - part * each, each, 0, a.gw, row, column)) return;
+    const int steps = (uniform(*a.count) + PW::kK - 1) / PW::kK, own = (steps + a.split_w - 1) / a.split_w, from = part * own;
     f32x16 acc[PW::FM][PW::FN];
-    PW::run(a.x, a.p_rows, {(long long)row * PW::kM, (long long)column * PW::kN, 0, (uniform(*a.count) + PW::kK - 1) / PW::kK}, lds, acc);
+    PW::run(a.x, a.p_rows,
+            {(long long)row * PW::kM, (long long)column * PW::kN, (long long)from * PW::kK, steps - from < own ? (steps > from ? steps - from : 0) : own}, lds, acc);
 #pragma unroll
     for (int m = 0; m < PW::FM; ++m)
 #pragma unroll
@@ -714,6 +720,22 @@ __global__ __launch_bounds__(PX::kThreads, PX::kWavesPerSimd) void gradient_prod
 #pragma unroll
             for (int n = 0; n < PW::FN; ++n) acc[m][n][r] *= unit;
         }
+    if (a.split_w > 1) {
+#pragma unroll
+        for (int n = 0; n < PW::FN; ++n) {
+            const long long in = column * PW::kN + (wn * PW::FN + n) * 32 + (lane & 31);
+            float* const to = a.dw_parts + part * a.dw_plane + in * a.ld;
+#pragma unroll
+            for (int m = 0; m < PW::FM; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = row * PW::kM + (wm * PW::FM + m) * 32 + 4 * (lane >> 5) + 8 * q;
+                    if (c < a.ld && in < a.piece)
+                        *(f32x4*)(to + c) = f32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]};
+                }
+        }
+        return;
+    }
     if (a.wide) {
 #pragma unroll
         for (int n = 0; n < PW::FN; ++n) {
@@ -808,6 +830,23 @@ __global__ __launch_bounds__(256) void join_dx(const float* __restrict__ parts, 
         const long long channel = (long long)blockIdx.x * 64 + wave * 16 + j;
         if (channel < C) to[channel * HW] = from_f32<T>(tile[lane][wave * 16 + j]);
     }
+}
+
+// dw of a piece from the parts of p^T x, four channels a thread
+__global__ __launch_bounds__(256) void join_dw(const float* __restrict__ parts, long long plane, int split, int ld, void* __restrict__ dw, bool wide, int rows, int C)
+{
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, v = at / (ld / 4);
+    const int c = (int)(at - v * (ld / 4)) * 4;
+    if (v >= rows || c >= C) return;
+    f32x4 sum = *(const f32x4*)(parts + v * ld + c);
+    for (int s = 1; s < split; ++s) sum += *(const f32x4*)(parts + s * plane + v * ld + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < C) {
+            if (wide) ((float*)dw)[v * C + c + e] = sum[e];
+            else ((bf16_t*)dw)[v * C + c + e] = from_f32<bf16_t>(sum[e]);
+        }
 }
 
 // ---- sizes ----
@@ -917,20 +956,26 @@ auto with_gradient_form(const Shape& s, long long piece, F&& f)
     return f(typename Forms<T>::Small());
 }
 
-// Parts of K of p W: so many that none takes longer than a CU's share of both products
+// Parts of K of p W and of p^T x: so many that none takes longer than a CU's share of both products, and none of fewer than 512 values of K
+struct Splits {
+    int x, w;
+};
+
 template <typename T>
-int split_of(const Shape& s, long long piece)
+Splits splits_of(const Shape& s, long long piece)
 {
     return with_gradient_form<T>(s, piece, [&](auto form) {
         typedef decltype(form) F;
         const long long ld = round_up(s.C, 64), T_ = s.T(), high = (ld + F::BM - 1) / F::BM;
-        const long long tiles = high * ((T_ + F::BN - 1) / F::BN), others = high * (piece / F::BN);
-        const long long steps = piece / F::BK, all = tiles * steps + others * ((T_ + F::BK - 1) / F::BK);
-        const long long share = (all + 255) / 256;              // of a CU
-        long long split = (steps + share - 1) / share;          // none has more than that
-        if (split > 16) split = 16;
-        while (split > 1 && piece / split < 512) --split;
-        return (int)split;
+        const long long tiles_x = high * ((T_ + F::BN - 1) / F::BN), tiles_w = high * (piece / F::BN);
+        const long long steps_x = piece / F::BK, steps_w = (T_ + F::BK - 1) / F::BK;
+        const long long share = (tiles_x * steps_x + tiles_w * steps_w + 255) / 256;
+        auto split = [&](long long steps, long long k) {
+            long long n = (steps + share - 1) / share;
+            n = n > 16 ? 16 : n;
+            return (int)(n > k / 512 ? (k / 512 > 1 ? k / 512 : 1) : n);
+        };
+        return Splits{split(steps_x, piece), split(steps_w, T_)};
     });
 }
 
@@ -940,7 +985,8 @@ struct GradientRoom {
     uint32_t *most_x, *most_w, *parts_x, *parts_w;
     float* parts;
     Pieces pieces;
-    int split;
+    Splits split;
+    float* dw_parts;
 };
 
 template <typename T>
@@ -961,8 +1007,9 @@ GradientRoom take_gradients(Room& room, const Shape& s, bool direct_w)
     }
     r.pieces = pieces_of(s, planes);
     r.p = room.take<uint16_t>(planes * r.c.Tp * r.pieces.piece);
-    r.split = split_of<T>(s, r.pieces.piece);
-    r.parts = room.take<float>(r.split * r.c.Tp * r.c.ld);
+    r.split = splits_of<T>(s, r.pieces.piece);
+    r.parts = room.take<float>(r.split.x * r.c.Tp * r.c.ld);
+    r.dw_parts = r.split.w > 1 ? room.take<float>(r.split.w * r.pieces.piece * r.c.ld) : nullptr;
     return r;
 }
 
@@ -1117,16 +1164,24 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
             const hipError_t e = allow(gradient_products<PX, PW>, PX::kLds);
             if (e != hipSuccess) return e;
             a.steps = (int)(length / F::BK);
-            a.split_steps = (a.steps + r.split - 1) / r.split;
+            a.split_steps = (a.steps + r.split.x - 1) / r.split.x;
             a.split = (a.steps + a.split_steps - 1) / a.split_steps;
             if (i == 0) parts = a.split;
             const int high = (int)((ld + F::BM - 1) / F::BM);
             a.gx = {high, (int)((T_ + F::BN - 1) / F::BN)};
             a.gw = {high, (int)(length / F::BN)};
             a.blocks_x = blocks_of(a.gx) * a.split;
-            a.blocks_w = blocks_of(a.gw);
-            a.w_first = T_ / F::BK > a.split_steps;
+            a.split_w = r.split.w;
+            a.dw_parts = r.dw_parts;
+            a.dw_plane = piece * ld;
+            a.blocks_w = blocks_of(a.gw) * a.split_w;
+            a.w_first = T_ / F::BK / a.split_w > a.split_steps;
             gradient_products<PX, PW><<<a.blocks_x + a.blocks_w, PX::kThreads, PX::kLds, st>>>(a);
+            if (a.split_w > 1) {
+                const long long rows = s.V - first < length ? s.V - first : length;
+                void* const to = (char*)dw + first * s.C * (wide ? 4 : 2);
+                if (rows > 0) join_dw<<<(rows * (ld / 4) + 255) / 256, 256, 0, st>>>(r.dw_parts, piece * ld, a.split_w, (int)ld, to, wide, (int)rows, s.C);
+            }
             return hipGetLastError();
         });
     }

@@ -110,7 +110,7 @@ def test_refusals_of_the_binding():
 SHAPES = [(1, 512, 1, 1), (5, 1, 1, 1), (3, 7, 1, 1), (70, 8, 1, 1), (33, 100, 1, 1), (9, 257, 1, 1), (300, 512, 1, 1), (2, 1030, 1, 1), (17, 2048, 1, 1),
           (3, 5003, 1, 1), (2, 12000, 1, 1), (1, 40001, 1, 1), (2000, 64, 1, 1), (2, 3, 2, 1), (3, 16, 2, 2), (2, 60, 7, 1), (4, 33, 3, 3), (1, 128, 8, 1),
           (2, 130, 5, 3), (3, 512, 7, 7), (2, 200, 1, 33), (2, 513, 50, 1), (2, 1000, 9, 2), (1, 1500, 11, 1), (1, 3000, 4, 4), (64, 24, 16, 16), (1, 5, 300, 7),
-          (2, 96, 1000, 1)]
+          (2, 96, 1000, 1), (1, 9000, 40, 1), (2, 5000, 3, 1), (40, 1100, 6, 1), (300, 2050, 16, 1), (3, 700, 40, 1)]
 IDS = ["x".join(map(str, s)) for s in SHAPES]
 
 

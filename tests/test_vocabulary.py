@@ -218,6 +218,18 @@ def test_split_sums_over_a_long_vocabulary(dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape,V", [((9000, 40, 1, 1), 70), ((3, 150, 40, 50), 300), ((2600, 200, 1, 1), 500)])
+def test_split_sums_over_many_tokens(shape, V, dtype):
+    x, w, target = inputs(shape, V, dtype, ignored=0.4)
+    lse = check_loss(x, w, target)
+    check_gradients(x, w, target, lse, "mean", torch.tensor(1.0, device="cuda"))
+    target.fill_(IGNORED)
+    dx, dw = S.scc_vocabulary_gradients(x, w, target, lse, torch.tensor(1.0, device="cuda"))
+    assert (dx == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", [(40, 64, 1, 1), (2, 48, 100, 1)])
 def test_no_token_counts(shape, dtype):
     x, w, target = inputs(shape, 333, dtype)
