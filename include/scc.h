@@ -476,7 +476,7 @@ int scc_vocabulary_loss(const void* x, const void* w, const long long* target, f
  * bits between the products, and so is d_t x_tc; of a channel's values those below 2^-31 of its largest lose bits.
  * workspace, for both: at least the query's bytes, 256-byte aligned, owned by the caller, contents undefined before and after (0 for invalid
  * arguments).  It holds a copy of w (three bf16 pieces for each value of binary32) and, for the gradients, one piece's p.
- * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W or V over 2^26, C over 2^20), SCC_ERR_DTYPE, SCC_ERR_OPTION (reduction),
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W or V over 2^26, their product over 2^45, C over 2^20), SCC_ERR_DTYPE, SCC_ERR_OPTION (reduction),
  * SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH.
  */
 size_t scc_vocabulary_gradients_workspace_bytes(int N, int C, int H, int W, int V, scc_dtype dtype);

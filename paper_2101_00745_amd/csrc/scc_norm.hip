@@ -494,7 +494,7 @@ __global__ __launch_bounds__(THREADS) void backward_columns(const T* __restrict_
         for (int m = 1; m < LANES; m *= 2) v += __shfl_xor(v, m);
         return v;
     };
-    const bool runs = s.HW * (int)sizeof(T) % 128 != 0;
+    const bool runs = (size_t)s.HW * sizeof(T) % 128 != 0;
     long long tile = tile_of(blockIdx.x, gridDim.x, 0, tiles, runs);
     if (NV == 0 && tile < 0)                    // a row of sums all the same
         for (int c = threadIdx.x; c < s.C; c += THREADS) part[(size_t)blockIdx.x * s.C + c] = 0.f;

@@ -162,10 +162,10 @@ __global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f,
 {
     constexpr int kWaves = 16;
     __shared__ float lds[kWaves][512];
-    const long long first = (long long)blockIdx.y * kMaximaRows, end = x.end();
+    const long long first = (long long)blockIdx.x * kMaximaRows, end = x.end();
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.x * 512 + lane * 8;
+    const long long c = (long long)blockIdx.y * 512 + lane * 8;
     float high[8] = {}, v[8][8], d[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -182,11 +182,11 @@ __global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f,
     __syncthreads();
     if (threadIdx.x < 512) {
         const int at = (threadIdx.x & 7) * 64 + (threadIdx.x >> 3);
-        const long long channel = (long long)blockIdx.x * 512 + threadIdx.x;
+        const long long channel = (long long)blockIdx.y * 512 + threadIdx.x;
         float most = lds[0][at];
 #pragma unroll
         for (int j = 1; j < kWaves; ++j) most = fmaxf(most, lds[j][at]);
-        if (channel < ld) parts[(long long)blockIdx.y * ld + channel] = __float_as_uint(channel < x.C ? most : 0.f);
+        if (channel < ld) parts[(long long)blockIdx.x * ld + channel] = __float_as_uint(channel < x.C ? most : 0.f);
     }
 }
 
@@ -195,10 +195,10 @@ template <typename T>
 __global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ parts, int ld)
 {
     __shared__ float lds[4][64];
-    const long long first = (long long)blockIdx.y * kMaximaRows, end = x.end(), c0 = (long long)blockIdx.x * 64;
+    const long long first = (long long)blockIdx.x * kMaximaRows, end = x.end(), c0 = (long long)blockIdx.y * 64;
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t* const to = parts + (long long)blockIdx.y * ld + c0;
+    uint32_t* const to = parts + (long long)blockIdx.x * ld + c0;
     if (x.HW > 1) {
         const T* row[2];
         float d[2];
@@ -293,10 +293,10 @@ __device__ __forceinline__ void write_packed(const Packed& o, long long i, long 
 template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void pack_wide(Rows<T> x, Factor f, Packed o)
 {
-    const long long first = (long long)blockIdx.y * 32, end = x.end();
+    const long long first = (long long)blockIdx.x * 32, end = x.end();
     if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.x * 512 + lane * 8;
+    const long long c = (long long)blockIdx.y * 512 + lane * 8;
     if (c >= o.ld) return;
     float unit[8];
     units_of(o, c, unit);
@@ -322,10 +322,10 @@ template <typename T, int PLANES>
 __global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
 {
     __shared__ float tile[64][65];
-    const long long first = (long long)blockIdx.y * 64, end = x.end();
+    const long long first = (long long)blockIdx.x * 64, end = x.end();
     if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c0 = (long long)blockIdx.x * 64;
+    const long long c0 = (long long)blockIdx.y * 64;
     if (x.HW > 1) {
         const bool there = first + lane < end;
         const T* row = there ? x.row(first + lane) : nullptr;
@@ -786,7 +786,7 @@ __global__ __launch_bounds__(256) void join_dx(const float* __restrict__ parts, 
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     __shared__ float tile[64][65];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = (threadIdx.x % 16) * 4;
-    const long long first = (long long)blockIdx.y * 64, c = (long long)blockIdx.x * 64 + in;
+    const long long first = (long long)blockIdx.x * 64, c = (long long)blockIdx.y * 64 + in;
     float unit[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) unit[e] = most ? power(channel_exponent(c + e < C ? most[c + e] : 0) - (int)kRaise) : 1.f;
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(256) void join_dx(const float* __restrict__ parts, 
     T* const to = dx + (long long)n * C * HW + (t - n * (uint32_t)HW);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-        const long long channel = (long long)blockIdx.x * 64 + wave * 16 + j;
+        const long long channel = (long long)blockIdx.y * 64 + wave * 16 + j;
         if (channel < C) to[channel * HW] = from_f32<T>(tile[lane][wave * 16 + j]);
     }
 }
@@ -917,12 +917,14 @@ struct LossRoom {
 };
 
 // direct: w is read where it is
-LossRoom take_loss(Room& room, const Shape& s, int planes, bool direct_w, int reduction)
+template <typename T>
+LossRoom take_loss(Room& room, const Shape& s, bool direct_w, int reduction)
 {
+    constexpr int planes = kPlanesOf<T>;
     LossRoom r;
     r.c = take_common(room, s, planes);
     r.wp = direct_w ? nullptr : room.take<uint16_t>(planes * round_up(s.V, kRowsPad) * r.c.ld);
-    r.part = room.take<float2>(round_up(s.V, 64) / 64 * r.c.Tp);
+    r.part = room.take<float2>(with_form<T>(s.V, s.T(), [&](auto form) { return (s.V + decltype(form)::BM - 1) / decltype(form)::BM; }) * r.c.Tp);
     r.losses = reduction == NONE ? nullptr : room.take<float>(s.T());
     return r;
 }
@@ -1026,8 +1028,8 @@ template <typename T>
 void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* parts, int ld, hipStream_t st)
 {
     const int blocks = (int)((x.rows + kMaximaRows - 1) / kMaximaRows);
-    if (x.HW == 1 && wide_rows(x.x, x.C)) channel_maxima_wide<T><<<dim3((ld + 511) / 512, blocks), 1024, 0, st>>>(x, f, parts, ld);
-    else channel_maxima<T><<<dim3(ld / 64, blocks), 256, 0, st>>>(x, f, parts, ld);
+    if (x.HW == 1 && wide_rows(x.x, x.C)) channel_maxima_wide<T><<<dim3(blocks, (ld + 511) / 512), 1024, 0, st>>>(x, f, parts, ld);
+    else channel_maxima<T><<<dim3(blocks, ld / 64), 256, 0, st>>>(x, f, parts, ld);
 }
 
 // rows: padded
@@ -1035,9 +1037,9 @@ template <typename T>
 void launch_pack(const Rows<T>& x, const Factor& f, const Packed& o, long long rows, hipStream_t st)
 {
     if (x.HW == 1 && wide_rows(x.x, x.C))
-        pack_wide<T, kPlanesOf<T>><<<dim3((o.ld + 511) / 512, rows / 32), 256, 0, st>>>(x, f, o);
+        pack_wide<T, kPlanesOf<T>><<<dim3(rows / 32, (o.ld + 511) / 512), 256, 0, st>>>(x, f, o);
     else
-        pack<T, kPlanesOf<T>><<<dim3(o.ld / 64, rows / 64), 256, 0, st>>>(x, f, o);
+        pack<T, kPlanesOf<T>><<<dim3(rows / 64, o.ld / 64), 256, 0, st>>>(x, f, o);
 }
 
 template <typename K>
@@ -1051,7 +1053,8 @@ hipError_t allow(K* kernel, int bytes)
 size_t loss_workspace(const Shape& s, int es, bool aligned, int reduction)
 {
     Room room = {nullptr};
-    (void)take_loss(room, s, es == 4 ? 3 : 1, es == 2 && s.C % 64 == 0 && aligned, reduction);
+    if (es == 4) (void)take_loss<float>(room, s, false, reduction);
+    else (void)take_loss<bf16_t>(room, s, s.C % 64 == 0 && aligned, reduction);
     return room.used;
 }
 
@@ -1062,7 +1065,7 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
     constexpr int planes = kPlanesOf<T>;
     Room room = {workspace};
     const bool at_place = direct(w, s);
-    const LossRoom r = take_loss(room, s, planes, at_place, reduction);
+    const LossRoom r = take_loss<T>(room, s, at_place, reduction);
     const Tokens& k = r.c.k;
     const long long T_ = s.T(), ld = r.c.ld, Tp = r.c.Tp;
     float* losses = reduction == NONE ? loss : r.losses;
@@ -1186,7 +1189,7 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
         });
     }
     if (e != hipSuccess) return e;
-    join_dx<T><<<dim3(ld / 64, (T_ + 63) / 64), 256, 0, st>>>(r.parts, Tp * ld, parts, (int)ld, k, f, r.most_w, dx, T_, s.C, s.HW);
+    join_dx<T><<<dim3((T_ + 63) / 64, ld / 64), 256, 0, st>>>(r.parts, Tp * ld, parts, (int)ld, k, f, r.most_w, dx, T_, s.C, s.HW);
     return hipGetLastError();
 }
 

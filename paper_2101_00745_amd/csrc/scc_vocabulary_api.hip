@@ -10,8 +10,8 @@ int check(int N, int C, int H, int W, int V, scc_dtype dtype, scc_reduction redu
 {
     if (N < 1 || C < 1 || H < 1 || W < 1 || V < 1) return SCC_ERR_SHAPE;
     const long long HW = (long long)H * W, T = HW * N;
-    // tokens are counted in 32 bits, also padded, and so are tiles; K steps of a product are at most 2^31 / 32
-    if (HW > 0x7fffffff || T > 1 << 26 || C > 1 << 20 || V > 1 << 26) return SCC_ERR_SHAPE;
+    // tokens are counted in 32 bits, also padded, and so are the tiles of a product, of 2^15 logits or more where there are so many
+    if (HW > 0x7fffffff || T > 1 << 26 || C > 1 << 20 || V > 1 << 26 || T * V > 1ll << 45) return SCC_ERR_SHAPE;
     if (!dtype_ok(dtype)) return SCC_ERR_DTYPE;
     if (reduction != SCC_NONE && reduction != SCC_SUM && reduction != SCC_MEAN) return SCC_ERR_OPTION;
     *s = {N, C, (int)HW, V};

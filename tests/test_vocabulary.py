@@ -163,6 +163,9 @@ def test_workspaces_of_many_sizes():
     for T in (1, 63, 64, 65, 4096, 33000, 1 << 22, 1 << 26):
         for C in (1, 64, 65, 513, 1 << 14, 1 << 20):
             for V in (1, 64, 257, 5200, 70000, 1 << 26):
+                if T * V > 1 << 45:
+                    assert lib.scc_vocabulary_gradients_workspace_bytes(T, C, 1, 1, V, 0) == 0
+                    continue
                 for dtype in (0, 1):
                     assert lib.scc_vocabulary_loss_workspace_bytes(T, C, 1, 1, V, 2, dtype) > 0
                     need = lib.scc_vocabulary_gradients_workspace_bytes(T, C, 1, 1, V, dtype)
@@ -206,6 +209,26 @@ def test_several_pieces_of_the_vocabulary(dtype):
     x, w, target = inputs((33000, 16, 1, 1), 5200, dtype, ignored=0.1)
     lse = check_loss(x, w, target)
     check_gradients(x, w, target, lse, "mean", torch.tensor(1.0, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_more_tokens_than_a_grid_has_rows():
+    """Three million tokens, of which a few thousand count; what they are not part of stays zero."""
+    T, C, V = 3_000_000, 8, 40
+    x, w, target = inputs((T, C, 1, 1), V, torch.bfloat16)
+    target.fill_(IGNORED)
+    some = torch.arange(0, T, 700, device="cuda")
+    target[some] = torch.randint(V, (some.numel(), 1, 1), device="cuda")
+    picked = x[some].contiguous()
+    want, want_lse = S.scc_vocabulary_loss(picked, w, target[some].contiguous(), "none")
+    got, lse = S.scc_vocabulary_loss(x, w, target, "none")
+    assert torch.equal(got[some], want) and torch.equal(lse[some], want_lse) and int((got != 0).sum()) == int((want != 0).sum())
+    d = torch.tensor(1.0, device="cuda")
+    dx, dw = S.scc_vocabulary_gradients(x, w, target, lse, d, "sum")
+    want_dx, want_dw, dx_size, dw_size = gradients(picked, w, target[some], torch.ones_like(want))
+    assert int((dx != 0).any(1).sum()) == some.numel()
+    assert ((dx[some].double() - want_dx).abs() <= 2.0 ** -8 * want_dx.abs() + 2.0 ** -9 * dx_size).all()
+    assert ((dw.double() - want_dw).abs() <= 2.0 ** -9 * dw_size).all()
 
 
 @pytest.mark.gpu
