@@ -1167,7 +1167,7 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
             const hipError_t e = allow(gradient_products<PX, PW>, PX::kLds);
             if (e != hipSuccess) return e;
             a.steps = (int)(length / F::BK);
-            a.split_steps = (a.steps + r.split.x - 1) / r.split.x;
+            a.split_steps = (int)((piece / F::BK + r.split.x - 1) / r.split.x);     // of a whole piece, so that no later one has more parts than the first
             a.split = (a.steps + a.split_steps - 1) / a.split_steps;
             if (i == 0) parts = a.split;
             const int high = (int)((ld + F::BM - 1) / F::BM);
