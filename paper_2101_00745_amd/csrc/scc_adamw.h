@@ -11,6 +11,7 @@ namespace adamw {
 constexpr int kBatch = 60;          // weights of one launch: their descriptions are kernel arguments (4 KB at most)
 constexpr int kBlock = 256;         // elements of a scale
 constexpr int kChunk = 2048;        // elements of a workgroup
+constexpr long long kMostChunks = 1 << 23;      // of a launch, whose lanes are counted in 32 bits
 
 struct Weight {
     void* w;

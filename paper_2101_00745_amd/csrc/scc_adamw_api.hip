@@ -16,7 +16,7 @@ extern "C" int scc_adamw_step(int count, void* const* w, const void* const* g, v
     if (count < 1) return SCC_ERR_SHAPE;
     for (int i = 0; i < count; ++i) {
         if (!w[i] || !g[i] || !first[i] || !second[i] || (bytes && (!first_scales[i] || !second_scales[i]))) return SCC_ERR_NULL;
-        if (sizes[i] < 1 || sizes[i] > 1ll << 40) return SCC_ERR_SHAPE;
+        if (sizes[i] < 1 || sizes[i] > kMostChunks * kChunk) return SCC_ERR_SHAPE;
     }
     if (!dtype_ok(dtype)) return SCC_ERR_DTYPE;
     for (const double v : {o->lr, o->eps, o->weight_decay})
@@ -57,7 +57,7 @@ extern "C" int scc_adamw_step(int count, void* const* w, const void* const* g, v
     };
     for (int i = 0; i < count; ++i) {
         const long long own = (sizes[i] + kChunk - 1) / kChunk;
-        if (b.count == kBatch || (b.count && chunks + own > 0x7fffffff)) {
+        if (b.count == kBatch || (b.count && chunks + own > kMostChunks)) {
             const int rc = launch();
             if (rc != SCC_OK) return rc;
         }

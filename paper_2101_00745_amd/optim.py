@@ -115,6 +115,29 @@ class AdamW(torch.optim.Optimizer):
                     state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
         return state
 
+    def _resting(self, group):
+        """The numbers on the GPU of the weights that have no gradient in this step."""
+        steps = (self.state[p].get("step") for p in group["params"] if p.grad is None and p in self.state)
+        return {id(step) for step in steps if isinstance(step, torch.Tensor)}
+
+    def _part(self, group, moving):
+        """Weights that have aged together and of which some rest now: the others go on with a number of their own."""
+        resting, fresh = self._resting(group), {}
+        for p in moving if resting else ():
+            step = self.state[p].get("step")
+            if id(step) in resting:
+                if id(step) not in fresh:
+                    fresh[id(step)] = step.clone()
+                self.state[p]["step"] = fresh[id(step)]
+
+    def _check_capture(self, group, moving):
+        """A replay repeats what the captured call did: it neither counts on the host nor makes states."""
+        if not group["capturable"] or any(not isinstance(self.state.get(p, {}).get("step"), torch.Tensor) for p in moving):
+            raise RuntimeError("a captured step wants capturable=True, and a step of the same weights before the capture")
+        resting = self._resting(group)
+        if any(id(self.state[p]["step"]) in resting for p in moving):
+            raise RuntimeError("make a step with gradients for the same weights before the capture")
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
@@ -123,9 +146,11 @@ class AdamW(torch.optim.Optimizer):
                 loss = closure()
         for group in self.param_groups:
             lists, begun, raised = {}, {}, set()
-            for p in group["params"]:
-                if p.grad is None or p.numel() == 0:
-                    continue
+            moving = [p for p in group["params"] if p.grad is not None and p.numel()]
+            if any(p.is_cuda for p in moving) and torch.cuda.is_current_stream_capturing():
+                self._check_capture(group, moving)
+            self._part(group, moving)
+            for p in moving:
                 state = self._begin(p, group, begun)
                 small = "first_scales" in state
                 if isinstance(state["step"], torch.Tensor):

@@ -72,7 +72,7 @@ def test_refusals():
     for name in ("w", "g", "m", "v"):
         assert call(**{name: none}) == -1
     assert call(options=False) == -1 and call(ms=ptr) == -1 and call(vs=ptr) == -1 and call(ms=ptr, vs=none) == -1 and call(ms=none, vs=ptr) == -1
-    assert call(count=0) == -2 and call(sizes=(ctypes.c_longlong * 1)(0)) == -2 and call(sizes=(ctypes.c_longlong * 1)((1 << 40) + 1)) == -2
+    assert call(count=0) == -2 and call(sizes=(ctypes.c_longlong * 1)(0)) == -2 and call(sizes=(ctypes.c_longlong * 1)((1 << 34) + 1)) == -2
     assert call(dtype=2) == -4 and call(step=0) == -8
     for o in (dict(lr=math.nan), dict(eps=-1.0), dict(eps=math.inf), dict(beta1=1.0), dict(beta2=-0.1), dict(beta2=math.nan), dict(weight_decay=math.inf)):
         assert call(**o) == -8
@@ -358,3 +358,36 @@ def test_a_graph_over_moved_weights_is_an_error():
     opt.step()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+@pytest.mark.gpu
+def test_weights_that_rest_keep_their_age_on_the_gpu():
+    params = [torch.nn.Parameter(torch.randn(n, device="cuda")) for n in (30, 500, 7)]
+    copies = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    ours, plain = optim.AdamW(params, lr=LR, capturable=True), optim.AdamW(copies, lr=LR)
+    for moving in ((0, 1, 2), (0, 1, 2), (1,), (0, 2), (1, 2), (0, 1, 2)):
+        for i, (p, q) in enumerate(zip(params, copies)):
+            p.grad = torch.randn_like(p) if i in moving else None
+            q.grad = None if p.grad is None else p.grad.clone()
+        ours.step()
+        plain.step()
+        for p, q in zip(params, copies):
+            assert int(ours.state[p]["step"]) == plain.state[q]["step"]
+            assert ((p - q).abs() <= 6 * 4 * LR * 4 * ULP + 4 * ULP * q.abs()).all()
+
+
+@pytest.mark.gpu
+def test_captures_that_would_not_count_are_refused():
+    params = [torch.nn.Parameter(torch.randn(n, device="cuda")) for n in (30, 500)]
+    for p in params:
+        p.grad = torch.ones_like(p)
+    on_host, fresh, parted = (optim.AdamW(params, lr=LR, capturable=c) for c in (False, True, True))
+    on_host.step()
+    parted.step()
+    before = [p.detach().clone() for p in params]
+    params[1].grad = None
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        for opt in (on_host, fresh, parted):
+            with pytest.raises(RuntimeError, match="before the capture|capturable"):
+                opt.step()
+    assert not fresh.state and int(parted.state[params[0]]["step"]) == 1 and all(torch.equal(p, q) for p, q in zip(params, before))
