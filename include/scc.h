@@ -434,7 +434,7 @@ int scc_orthogonal_step(int count, void* const* w, const void* const* g, float* 
  * scc_norm_quantised writes y in 8 bits: q[n][c][h][w] * scale[n][h][w], q e4m3 (of the OCP's 8-bit formats the one without infinities), rounded to
  * nearest even, scale the smallest power of two that brings the pixel's largest |y| to 448 or less (between 2^-120 and 2^120; 1 for a pixel of zeros).
  * Outputs must not alias inputs or each other.
- * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W >= 2^31), SCC_ERR_DTYPE, SCC_ERR_OPTION (eps not positive and finite), SCC_ERR_LAUNCH.
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W >= 2^31, C over 2^26), SCC_ERR_DTYPE, SCC_ERR_OPTION (eps not positive and finite), SCC_ERR_LAUNCH.
  */
 int scc_norm_forward(const void* x, const void* residual, const void* w, void* h, void* y, int N, int C, int H, int W, float eps,
                      scc_dtype dtype, void* stream);
@@ -498,7 +498,7 @@ int scc_vocabulary_gradients(const void* x, const void* w, const long long* targ
  * changed; values below 1 are not refused there).
  * The arrays of pointers and sizes are HOST arrays, read before the call returns; the tensors are device memory.  No tensor that is written may
  * overlap another tensor of the call, which is not checked here.
- * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count < 1, a size < 1 or over 2^40), SCC_ERR_DTYPE, SCC_ERR_OPTION (a beta outside [0, 1), eps < 0, a value
+ * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count < 1, a size < 1 or over 2^34), SCC_ERR_DTYPE, SCC_ERR_OPTION (a beta outside [0, 1), eps < 0, a value
  * that is not finite, step < 1), SCC_ERR_LAUNCH (some of the list may have moved, so the call is not to be made again).
  */
 typedef struct {

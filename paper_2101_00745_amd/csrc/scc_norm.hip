@@ -100,6 +100,11 @@ __device__ __forceinline__ void store_bytes(uint8_t* to, const uint32_t (&q)[V])
     }
 }
 
+// The forward pass has a workgroup for each of up to 2^31 tokens or tiles of columns, while a side of a grid has at most 2^32 lanes: two sides
+constexpr int kGridSide = 1 << 20;
+dim3 grid_of(long long blocks) { return blocks <= kGridSide ? dim3((uint32_t)blocks) : dim3(kGridSide, (uint32_t)((blocks + kGridSide - 1) / kGridSide)); }
+__device__ __forceinline__ uint32_t block_of_grid() { return blockIdx.y * kGridSide + blockIdx.x; }
+
 // ---- tokens as rows ----
 
 template <int TPT, typename F>
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __rest
 {
     __shared__ float lds[TPT > 64 ? kRowThreads<TPT> / 64 : 1];
     const int lane = threadIdx.x % TPT;
-    const size_t token = (size_t)blockIdx.x * (kRowThreads<TPT> / TPT) + threadIdx.x / TPT;
+    const size_t token = (size_t)block_of_grid() * (kRowThreads<TPT> / TPT) + threadIdx.x / TPT;
     const bool there = token < (size_t)s.N;
     const size_t base = (there ? token : (size_t)s.N - 1) * s.C;
     const int count = NV ? NV : (s.C + V * TPT - 1) / (V * TPT);
@@ -367,7 +372,7 @@ __global__ __launch_bounds__(THREADS) void forward_columns(const T* __restrict__
 {
     typedef Columns<V, LANES, THREADS, 1> Cols;
     __shared__ Cols cols;
-    const long long tile = tile_of(blockIdx.x, gridDim.x, 0, ((uint32_t)groups.count + LANES - 1) / LANES, true);
+    const long long tile = tile_of(block_of_grid(), 8, 0, ((uint32_t)groups.count + LANES - 1) / LANES, true);
     if (tile < 0) return;
     const uint32_t group = (uint32_t)tile * LANES + threadIdx.x % LANES;
     const bool there = group < (uint32_t)groups.count;
@@ -711,7 +716,7 @@ Grid backward_grid(const Shape& s)
     if (rows) {
         (void)with_rows<T>(s.C, [&](auto, auto tpt, auto) {
             constexpr int TPT = decltype(tpt)::value, G = kRowThreads<TPT> / TPT;
-            const int most = (s.N + G - 1) / G, wanted = kSumRows / G;
+            const int most = (int)(((long long)s.N + G - 1) / G), wanted = kSumRows / G;
             g.blocks = most < wanted ? most : wanted;
             g.rows = g.blocks * G;
             return hipSuccess;
@@ -735,7 +740,7 @@ hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, flo
     if (s.HW == 1)
         return with_rows<T>(s.C, [&](auto v, auto tpt, auto nv) {
             constexpr int V = decltype(v)::value, TPT = decltype(tpt)::value, NV = decltype(nv)::value, G = kRowThreads<TPT> / TPT;
-            const int blocks = (s.N + G - 1) / G;
+            const dim3 blocks = grid_of(((long long)s.N + G - 1) / G);
             if (scale) forward_rows<T, V, TPT, NV, true><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
             else forward_rows<T, V, TPT, NV, false><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
             return hipGetLastError();
@@ -743,7 +748,7 @@ hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, flo
     return with_columns<T>(s, [&](auto v, auto lanes, auto threads, auto nv) {
         constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
         const Groups g = groups_of(s, V);
-        const int blocks = (int)((g.count + L - 1) / L + 7) / 8 * 8;
+        const dim3 blocks = grid_of((((long long)g.count + L - 1) / L + 7) / 8 * 8);
         if (scale) forward_columns<T, V, L, TH, NV, true><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
         else forward_columns<T, V, L, TH, NV, false><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
         return hipGetLastError();

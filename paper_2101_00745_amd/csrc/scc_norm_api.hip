@@ -11,7 +11,7 @@ namespace {
 int check(const void* x, const void* w, int N, int C, int H, int W, float eps, scc_dtype dtype, norm::Shape* s)
 {
     if (!x || !w) return SCC_ERR_NULL;
-    if (N < 1 || C < 1 || H < 1 || W < 1 || (long long)H * W > 0x7fffffff || (long long)N * H * W > 0x7fffffff) return SCC_ERR_SHAPE;
+    if (N < 1 || C < 1 || C > 1 << 26 || H < 1 || W < 1 || (long long)H * W > 0x7fffffff || (long long)N * H * W > 0x7fffffff) return SCC_ERR_SHAPE;
     if (!dtype_ok(dtype)) return SCC_ERR_DTYPE;
     if (!(eps > 0.f) || !std::isfinite(eps)) return SCC_ERR_OPTION;
     *s = {N, C, H * W, eps};

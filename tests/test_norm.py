@@ -267,3 +267,20 @@ def test_captured_and_on_another_stream(shape):
         torch.cuda.synchronize()
         assert torch.equal(y, want_y) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         assert torch.equal(q[0].view(torch.uint8), want_q[0].view(torch.uint8)) and torch.equal(q[1], want_q[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [((1 << 28) + 100, 1, 1, 1), (1, 1, 1 << 15, (1 << 15) + 8)])
+def test_more_lanes_than_a_side_of_a_grid_has(shape):
+    """One channel: y is x's sign, 1 / sqrt(1 + 1e-6) being 1 in bfloat16."""
+    x = torch.ones(shape, dtype=torch.bfloat16, device="cuda")
+    x.view(-1)[::3] = -1.0
+    y, h = S.scc_norm_forward(x, torch.ones(1, dtype=torch.bfloat16, device="cuda"))
+    assert h is x and torch.equal(y, x)
+
+
+def test_more_channels_than_are_taken():
+    lib = S.load()
+    one = 1 << 20
+    assert lib.scc_norm_forward(one, None, one, None, one, 1, (1 << 26) + 1, 1, 1, 1e-6, 0, None) == -2
+    assert lib.scc_norm_backward_workspace_bytes(1, (1 << 26) + 1, 1, 1, 0) == 0 < lib.scc_norm_backward_workspace_bytes(1, 1 << 26, 1, 1, 0)
