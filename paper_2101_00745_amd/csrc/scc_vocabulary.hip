@@ -517,14 +517,15 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void loss_product(Op
 }
 template <typename P> constexpr int kLossLds = P::kLds + 2 * (P::kM / 32 / P::FM) * P::kN * 4;
 
-// lse and loss of 64 packed tokens from the tiles' parts, 16 wavefronts taking the parts in turn; losses: of the tokens of x
+// lse and loss of 16 packed tokens from the tiles' parts, which 64 groups of lanes take in turn; losses: of the tokens of x.  (64 tokens and 16 groups: 6.1 us
+// instead of 3.6 for 48 tokens and 500 parts each, 7.9 instead of 10.1 for 16000 and 251.)
 __global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ part, long long Tp, int tiles, Tokens k, float* __restrict__ losses,
                                                    float* __restrict__ lse)
 {
-    constexpr int kWaves = 16, kAhead = 8;
-    __shared__ float2 lds[kWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, count = *k.count;
-    if (blockIdx.x * 64 >= count) return;
+    constexpr int TOKENS = 16, kWaves = 16, kAhead = 8, kSets = 1024 / TOKENS;
+    __shared__ float2 lds[kWaves][TOKENS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * TOKENS + lane % TOKENS, count = *k.count;
+    if ((int)blockIdx.x * TOKENS >= count) return;
     float high = -__builtin_inff(), sum = 0.f;
     // several parts at once, so that their exponentials wait for nothing but the maximum; a part of sum 0 has no values
     auto join = [&](const float2* p, int n) {
@@ -536,18 +537,23 @@ __global__ __launch_bounds__(1024) void join_parts(const float2* __restrict__ pa
         for (int e = 0; e < n; ++e) sum += p[e].y == 0.f ? 0.f : p[e].y * __builtin_amdgcn_exp2f((p[e].x - to) * kLog2E);
         high = to;
     };
-    for (int t = wave; t < tiles; t += kWaves * kAhead) {
+    for (int t = threadIdx.x / TOKENS; t < tiles; t += kSets * kAhead) {
         float2 p[kAhead];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
-            const int at = t + e * kWaves;
+            const int at = t + e * kSets;
             p[e] = at < tiles ? part[at * Tp + i] : make_float2(-__builtin_inff(), 0.f);
         }
         join(p, kAhead);
     }
-    lds[wave][lane] = make_float2(high, sum);
+#pragma unroll
+    for (int m = TOKENS; m < 64; m *= 2) {
+        const float2 other = make_float2(__shfl_xor(high, m), __shfl_xor(sum, m));
+        join(&other, 1);
+    }
+    if (lane < TOKENS) lds[wave][lane] = make_float2(high, sum);
     __syncthreads();
-    if (wave || i >= count) return;
+    if (wave || lane >= TOKENS || i >= count) return;
     float2 p[kWaves];
 #pragma unroll
     for (int t = 0; t < kWaves; ++t) p[t] = lds[t][lane];
@@ -1094,7 +1100,7 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    join_parts<<<(T_ + 63) / 64, 1024, 0, st>>>(r.part, Tp, tiles, k, losses, lse);
+    join_parts<<<(T_ + 15) / 16, 1024, 0, st>>>(r.part, Tp, tiles, k, losses, lse);
     if (reduction != NONE) sum_losses<<<1, 1024, 0, st>>>(losses, k.count, reduction == MEAN, loss, (int)T_);
     return hipGetLastError();
 }
