@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void forward_rows(const T* __rest
     }
 }
 
-// One row of dw's sums for each group of lanes, which takes every gridDim.x * groups'th token.
+// A group of lanes takes every gridDim.x * groups'th token; one row of dw's sums for each workgroup.
 template <typename T, int V, int TPT, int NV>
 __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __restrict__ x, const T* __restrict__ r, const T* __restrict__ w,
                                                                   const T* __restrict__ dy, const T* __restrict__ dh, T* __restrict__ dx, float* __restrict__ part,
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
     constexpr int kGroups = kRowThreads<TPT> / TPT;
     __shared__ float lds[TPT > 64 ? kRowThreads<TPT> / 64 : 1];
     const int lane = threadIdx.x % TPT;
-    const size_t group = (size_t)blockIdx.x * kGroups + threadIdx.x / TPT, groups = (size_t)gridDim.x * kGroups;
+    const size_t groups = (size_t)gridDim.x * kGroups;
     auto place = [&](int j) { return (lane + j * TPT) * V; };
     auto start = [&](int at) { return at < s.C - V ? at : s.C - V; };
     float sums[NV][V];
@@ -288,13 +288,25 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
             o.store(dx + base + start(at));
         }
     }
+    constexpr int kMost = V * TPT * NV;         // channels
+    __shared__ float rows[kGroups > 1 ? kGroups * kMost : 1];
+    float* const to = kGroups > 1 ? rows + threadIdx.x / TPT * kMost : part + (size_t)blockIdx.x * s.C;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const int at = place(j);
-            if (at < s.C && start(at) + e >= at) part[group * s.C + start(at) + e] = sums[j][e];
+            if (at < s.C && start(at) + e >= at) to[start(at) + e] = sums[j][e];
         }
+    if constexpr (kGroups > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < s.C; c += kRowThreads<TPT>) {
+            float sum = rows[c];
+#pragma unroll
+            for (int i = 1; i < kGroups; ++i) sum += rows[i * kMost + c];
+            part[(size_t)blockIdx.x * s.C + c] = sum;
+        }
+    }
 }
 
 // ---- tokens as columns ----
@@ -636,24 +648,36 @@ __global__ __launch_bounds__(1024) void weight_sums(const float* __restrict__ pa
 // Vectors that a token's channels (or a plane's pixels) are read in: 16 bytes where there are as many.
 template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
 
-constexpr int kKept = 4;            // vectors of a lane that stay in registers
+constexpr int kKept = 4;            // most vectors of a lane that stay in registers
 
-// f(V, TPT, NV) as constants for tokens as rows
+// f(V, TPT, NV) as constants for tokens as rows: as few lanes a token as keep its channels in one or two vectors of a lane, so that a wavefront or four sum without the
+// others, and up to 1024 tokens, where a token's time counts, one vector of as many lanes as it takes.  bf16, forward / backward in us: 1024 channels, 64 tokens: 256 lanes
+// 2.6 / 6.4, 64 lanes 2.9 / 6.1; 32768 tokens: 42 / 69 and 39 / 55.  4096 channels, one token: 1024 lanes 2.9 / 7.5, 256 lanes 3.0 / 8.0; 4096 tokens: 23 / 55 and 21 / 44.
 template <typename T, typename F>
-hipError_t with_rows(int C, F&& f)
+hipError_t with_rows(const Shape& s, F&& f)
 {
+    typedef std::integral_constant<int, 1> one;
+    typedef std::integral_constant<int, 2> two;
+    typedef std::integral_constant<int, kKept> kept;
+    typedef std::integral_constant<int, 16> quarter;
+    typedef std::integral_constant<int, 64> wave;
+    typedef std::integral_constant<int, 256> four;
+    typedef std::integral_constant<int, 1024> all;
+    const int C = s.C;
+    const bool few = s.N <= 1024;
     auto width = [&](auto v) {
         constexpr int V = decltype(v)::value;
-        if (C <= V * 16 * 2) return f(v, std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
-        if (C <= V * 64) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-        if (C <= V * 64 * 2) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-        if (C <= V * 64 * kKept) return f(v, std::integral_constant<int, 64>(), std::integral_constant<int, kKept>());
-        if (C <= V * 256 * kKept) return f(v, std::integral_constant<int, 256>(), std::integral_constant<int, kKept>());
-        if (C <= V * 1024 * kKept) return f(v, std::integral_constant<int, 1024>(), std::integral_constant<int, kKept>());
-        return f(v, std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
+        if (C <= V * 16) return f(v, quarter(), one());
+        if (C <= V * 32 && !few) return f(v, quarter(), two());
+        if (C <= V * 64) return f(v, wave(), one());
+        if (C <= V * 128 && !few) return f(v, wave(), two());
+        if (C <= V * 256) return f(v, four(), one());
+        if (C <= V * 1024) return few ? f(v, all(), one()) : f(v, four(), kept());
+        if (C <= V * 1024 * kKept) return f(v, all(), kept());
+        return f(v, all(), std::integral_constant<int, 0>());
     };
     if (C >= kWide<T>) return width(std::integral_constant<int, kWide<T>>());
-    return width(std::integral_constant<int, 1>());
+    return width(one());
 }
 
 Groups groups_of(const Shape& s, int V)
@@ -700,7 +724,7 @@ hipError_t with_columns(const Shape& s, F&& f)
     return width(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
 }
 
-constexpr int kSumRows = 1024;      // most rows of dw's sums, one for each group of lanes
+constexpr int kSumRows = 1024;      // most rows of dw's sums, one for each workgroup
 
 // Workgroups of the backward pass and the rows of sums that they leave
 struct Grid {
@@ -714,11 +738,10 @@ Grid backward_grid(const Shape& s)
     // tokens as rows, of too many channels for registers: as planes of one pixel
     const bool rows = s.HW == 1 && s.C <= kWide<T> * 1024 * kKept && s.C >= kWide<T>;
     if (rows) {
-        (void)with_rows<T>(s.C, [&](auto, auto tpt, auto) {
+        (void)with_rows<T>(s, [&](auto, auto tpt, auto) {
             constexpr int TPT = decltype(tpt)::value, G = kRowThreads<TPT> / TPT;
-            const int most = (int)(((long long)s.N + G - 1) / G), wanted = kSumRows / G;
-            g.blocks = most < wanted ? most : wanted;
-            g.rows = g.blocks * G;
+            const int most = (int)(((long long)s.N + G - 1) / G);
+            g.blocks = g.rows = most < kSumRows ? most : kSumRows;
             return hipSuccess;
         });
     } else {
@@ -738,7 +761,7 @@ template <typename T>
 hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, float* scale, const Shape& s, hipStream_t st)
 {
     if (s.HW == 1)
-        return with_rows<T>(s.C, [&](auto v, auto tpt, auto nv) {
+        return with_rows<T>(s, [&](auto v, auto tpt, auto nv) {
             constexpr int V = decltype(v)::value, TPT = decltype(tpt)::value, NV = decltype(nv)::value, G = kRowThreads<TPT> / TPT;
             const dim3 blocks = grid_of(((long long)s.N + G - 1) / G);
             if (scale) forward_rows<T, V, TPT, NV, true><<<blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, h, y, scale, s);
@@ -767,7 +790,7 @@ hipError_t launch_backward(const T* x, const T* r, const T* w, const T* dy, cons
     const Grid g = backward_grid<T>(s);
     hipError_t e;
     if (s.HW == 1 && s.C <= kWide<T> * 1024 * kKept && s.C >= kWide<T>)
-        e = with_rows<T>(s.C, [&](auto v, auto tpt, auto nv) {
+        e = with_rows<T>(s, [&](auto v, auto tpt, auto nv) {
             constexpr int V = decltype(v)::value, TPT = decltype(tpt)::value, NV = decltype(nv)::value;
             if constexpr (NV > 0 && V > 1)
                 backward_rows<T, V, TPT, NV><<<g.blocks, kRowThreads<TPT>, 0, st>>>(x, r, w, dy, dh, dx, part, s);

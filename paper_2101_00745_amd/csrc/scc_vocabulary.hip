@@ -879,7 +879,8 @@ template <typename T, typename F> using LossProduct = Product<F, false, false, f
 template <typename T, typename F> using DxProduct = Product<F, sizeof(T) == 2, true, false>;
 template <typename T, typename F> using DwProduct = Product<F, sizeof(T) == 2, true, true>;
 
-// f(form) for a product of so many rows and columns: the largest tiles of which there are enough
+// f(form) for a product of so many rows and columns: the largest tiles of which there are enough.  Losses of C = 512 bf16: 300 x 16000 (126 large tiles) 32.3 us in the large form,
+// 26.6 in the middle one; 1000 x 16000 (252) 36, 39; 4096 x 32000 166, 193; 100 x 16000 (125 middle tiles) 23.3 in the middle form, 21.1 in the small one
 template <typename T, typename F>
 auto with_form(long long rows, long long columns, F&& f)
 {
@@ -940,17 +941,19 @@ struct Pieces {
     int count;
 };
 
-// Pieces of the vocabulary: at most so many values of p at a time (in the last-level cache with both of its uses), equally long
+// Pieces of the vocabulary, equally long: at most 2^28 values of p at a time, 2^26 of three planes, some 0.5 GB; a piece costs a round of dx's sums and the ends of three
+// launches.  16000 x 1024 x 64001 bf16, gradients: 2^26 7.1 ms, 2^27 6.5, 2^28 6.2, 2^29 6.1; 1340 x 512 x 32000 binary32: 2^24 934 us, 2^25 916, 2^26 834, 2^27 858
 Pieces pieces_of(const Shape& s, int planes)
 {
-    const long long Tp = padded(s.T()), Vp = round_up(s.V, kRowsPad), most = planes == 3 ? 1ll << 25 : 1ll << 27;
+    const long long Tp = padded(s.T()), Vp = round_up(s.V, kRowsPad), most = planes == 3 ? 1ll << 26 : 1ll << 28;
     long long piece = most / Tp / kRowsPad * kRowsPad;
     if (piece < 2048) piece = 2048;
     const long long count = (Vp + piece - 1) / piece;
     return {round_up((Vp + count - 1) / count, kRowsPad), (int)count};
 }
 
-// The form of both gradients' products: rows are channels, columns tokens and the piece's rows
+// The form of both gradients' products: rows are channels, columns tokens and the piece's rows.  Gradients of 512 x 32000 bf16: 512 tokens (282 blocks) 172 us in the large
+// form, 156 in the middle one; 1000 (314) 222, 212; 2000 (378) 321, 357; 4096 (506) 543, 697
 template <typename T, typename F>
 auto with_gradient_form(const Shape& s, long long piece, F&& f)
 {
@@ -959,12 +962,13 @@ auto with_gradient_form(const Shape& s, long long piece, F&& f)
     const long long ld = round_up(s.C, 64), T_ = s.T();
     // K of the first product can be split
     auto blocks = [&](int bm, int bn) { return ((ld + bm - 1) / bm) * (piece / bn + (T_ + bn - 1) / bn * 8); };
-    if (ld > 128 && T_ > 128 && blocks(L::BM, L::BN) >= 200) return f(L());
+    if (ld > 128 && T_ > 128 && blocks(L::BM, L::BN) >= 350) return f(L());
     if (ld > 64 && T_ > 64) return f(M());
     return f(typename Forms<T>::Small());
 }
 
-// Parts of K of p W and of p^T x: so many that none takes longer than a CU's share of both products, and none of fewer than 512 values of K
+// Parts of K of p W and of p^T x: so many that none takes longer than a CU's share of both products, and none of fewer than 512 values of K (in one part each the gradients
+// of 48 tokens x 512 x 32000 take 186 us instead of 119, of 4096 tokens 985 instead of 543)
 struct Splits {
     int x, w;
 };

@@ -32,7 +32,8 @@ __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c)
 }
 
 // A read through a restricted pointer: the compiler takes it for one that the loads under way into other buffers of LDS have nothing to do with (they
-// have not: the caller has waited for this buffer's).  Without that it waits for all of them before each: 492 TFLOP/s instead of 393.
+// have not: the caller has waited for this buffer's).  Without that it waits for all of them before each: 275 instead of 219 us for the
+// gradients of 4096 tokens x 512 and a piece of 16128.
 __device__ __forceinline__ uint64_t read_turned(const char* __restrict__ p)
 {
     typedef short s16x4 __attribute__((ext_vector_type(4)));

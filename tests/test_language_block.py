@@ -143,4 +143,4 @@ def test_a_step_is_captured():
         torch.cuda.synchronize()
         assert abs(float(loss) - float(want)) <= 1e-5 * math.fabs(float(want))
         for p, q in zip((sides[0][0].weight, sides[0][1].weight), (sides[1][0].weight, sides[1][1].weight)):
-            assert float((p - q).abs().max()) <= 1e-5
+            assert float((p - q).detach().abs().max()) <= 1e-5
