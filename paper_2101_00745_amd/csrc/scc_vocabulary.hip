@@ -797,18 +797,26 @@ __global__ __launch_bounds__(256) void join_dx(const float* __restrict__ parts, 
 #pragma unroll
     for (int e = 0; e < 4; ++e) unit[e] = most ? power(channel_exponent(c + e < C ? most[c + e] : 0) - (int)kRaise) : 1.f;
     f32x4 sum[4];
+    const float* from[4];
+    int place[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const long long t = first + threadIdx.x / 16 + j * 16;
-        const int i = t < tokens ? k.place[t] : -1;
+        place[j] = t < tokens ? k.place[t] : -1;
+        from[j] = parts + (long long)(place[j] < 0 ? 0 : place[j]) * ld + c;
         sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (i >= 0) {
-            const float* from = parts + (long long)i * ld + c;
-            for (int s = 0; s < split; ++s) sum[j] += *(const f32x4*)(from + s * plane);
-            const float d = most ? f.of(i) : 1.f;
+    }
+    if (place[0] >= 0 || place[1] >= 0 || place[2] >= 0 || place[3] >= 0)
+#pragma unroll 4
+        for (int s = 0; s < split; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[j][e] *= most ? d * unit[e] : 1.f;
-        }
+            for (int j = 0; j < 4; ++j) sum[j] += *(const f32x4*)(from[j] + s * plane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const long long t = first + threadIdx.x / 16 + j * 16;
+        const float d = place[j] < 0 ? 0.f : most ? f.of(place[j]) : 1.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[j][e] = place[j] < 0 ? 0.f : sum[j][e] * (most ? d * unit[e] : 1.f);
         if (HW > 1) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) tile[threadIdx.x / 16 + j * 16][in + e] = sum[j][e];
