@@ -876,11 +876,13 @@ template <typename T> struct Forms {
     typedef Form<256, 256, 2, 4, 64, 2, 1> Large;
     typedef Form<128, 128, 2, 2, 64, 2, 1> Middle;
     typedef Form<64, 64, 2, 2, 64, 4, 1> Small;
+    typedef Form<64, 64, 2, 2, 64, 2, 1> Few;
 };
 template <> struct Forms<float> {
     typedef Form<256, 128, 4, 2, 32, 2, 3> Large;
     typedef Form<128, 128, 2, 2, 32, 3, 3> Middle;
     typedef Form<64, 64, 2, 2, 32, 3, 3> Small;
+    typedef Form<64, 64, 2, 2, 32, 2, 3> Few;
 };
 
 template <typename T, typename F> using LossProduct = Product<F, false, false, false>;
@@ -961,7 +963,9 @@ Pieces pieces_of(const Shape& s, int planes)
 }
 
 // The form of both gradients' products: rows are channels, columns tokens and the piece's rows.  Gradients of 512 x 32000 bf16: 512 tokens (282 blocks) 172 us in the large
-// form, 156 in the middle one; 1000 (314) 222, 212; 2000 (378) 321, 357; 4096 (506) 543, 697
+// form, 156 in the middle one; 1000 (314) 222, 212; 2000 (378) 321, 357; 4096 (506) 543, 697.
+// Few tokens make most tiles one or two steps long: two buffers, so that more of them share a CU; 48 tokens 98 us, in the small form 112, 100 tokens 109, in the middle one 113; 200
+// tokens 135 and 122; 4096 x 64 x 32000 302, in the small form 252
 template <typename T, typename F>
 auto with_gradient_form(const Shape& s, long long piece, F&& f)
 {
@@ -971,7 +975,8 @@ auto with_gradient_form(const Shape& s, long long piece, F&& f)
     // K of the first product can be split
     auto blocks = [&](int bm, int bn) { return ((ld + bm - 1) / bm) * (piece / bn + (T_ + bn - 1) / bn * 8); };
     if (ld > 128 && T_ > 128 && blocks(L::BM, L::BN) >= 350) return f(L());
-    if (ld > 64 && T_ > 64) return f(M());
+    if (T_ <= 128) return f(typename Forms<T>::Few());
+    if (ld > 64) return f(M());
     return f(typename Forms<T>::Small());
 }
 
