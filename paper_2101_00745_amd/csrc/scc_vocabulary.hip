@@ -158,14 +158,13 @@ __device__ __forceinline__ void write8(uint16_t* p, const uint16_t (&v)[8])
 // a workgroup, a wavefront's eight rows under way.  (Atomics instead of the parts, which cross the XCDs: 37 us for 32 MB instead of 10.)
 constexpr int kMaximaRows = 128;
 template <typename T>
-__global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f, uint32_t* __restrict__ parts, int ld)
+__device__ __forceinline__ void maxima_wide(const Rows<T>& x, const Factor& f, uint32_t* __restrict__ parts, int ld, int block, int group, float* lds)
 {
     constexpr int kWaves = 16;
-    __shared__ float lds[kWaves][512];
-    const long long first = (long long)blockIdx.x * kMaximaRows, end = x.end();
+    const long long first = (long long)block * kMaximaRows, end = x.end();
     if (first >= end) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.y * 512 + lane * 8;
+    const long long c = (long long)group * 512 + lane * 8;
     float high[8] = {}, v[8][8], d[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -178,28 +177,28 @@ __global__ __launch_bounds__(1024) void channel_maxima_wide(Rows<T> x, Factor f,
 #pragma unroll
         for (int e = 0; e < 8; ++e) high[e] = fmaxf(high[e], fabsf(v[i][e] * d[i]));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) lds[wave][e * 64 + lane] = high[e];
+    for (int e = 0; e < 8; ++e) lds[wave * 512 + e * 64 + lane] = high[e];
     __syncthreads();
     if (threadIdx.x < 512) {
         const int at = (threadIdx.x & 7) * 64 + (threadIdx.x >> 3);
-        const long long channel = (long long)blockIdx.y * 512 + threadIdx.x;
-        float most = lds[0][at];
+        const long long channel = (long long)group * 512 + threadIdx.x;
+        float most = lds[at];
 #pragma unroll
-        for (int j = 1; j < kWaves; ++j) most = fmaxf(most, lds[j][at]);
-        if (channel < ld) parts[(long long)blockIdx.x * ld + channel] = __float_as_uint(channel < x.C ? most : 0.f);
+        for (int j = 1; j < kWaves; ++j) most = fmaxf(most, lds[j * 512 + at]);
+        if (channel < ld) parts[(long long)block * ld + channel] = __float_as_uint(channel < x.C ? most : 0.f);
     }
 }
 
-// The same for any rows: 64 channels a workgroup, lanes along the rows where tokens are columns
+// The same for any rows: 256 channels a workgroup, four wavefronts for each 64 of them, lanes along the rows where tokens are columns
 template <typename T>
-__global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ parts, int ld)
+__device__ __forceinline__ void maxima_any(const Rows<T>& x, const Factor& f, uint32_t* __restrict__ parts, int ld, int block, int group, float* lds)
 {
-    __shared__ float lds[4][64];
-    const long long first = (long long)blockIdx.x * kMaximaRows, end = x.end(), c0 = (long long)blockIdx.y * 64;
+    const long long first = (long long)block * kMaximaRows, end = x.end(), c0 = (long long)group * 256 + (threadIdx.x >> 8) * 64;
     if (first >= end) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t* const to = parts + (long long)blockIdx.x * ld + c0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6 & 3;
+    uint32_t* const to = parts + (long long)block * ld + c0;
     if (x.HW > 1) {
+        if (c0 >= ld) return;
         const T* row[2];
         float d[2];
 #pragma unroll
@@ -221,10 +220,26 @@ __global__ __launch_bounds__(256) void channel_maxima(Rows<T> x, Factor f, uint3
 #pragma unroll 4
         for (int r = wave; r < kMaximaRows; r += 4)
             if (first + r < end) v = fmaxf(v, fabsf(to_f32(x.row(first + r)[c]) * f.of((int)(first + r))));
-        lds[wave][lane] = v;
+        float* const own = lds + (threadIdx.x >> 8) * 256 + lane;
+        own[wave * 64] = v;
         __syncthreads();
-        if (wave == 0) to[lane] = __float_as_uint(c0 + lane < x.C ? fmaxf(fmaxf(lds[0][lane], lds[1][lane]), fmaxf(lds[2][lane], lds[3][lane])) : 0.f);
+        if (wave == 0 && c0 < ld) to[lane] = __float_as_uint(c0 + lane < x.C ? fmaxf(fmaxf(own[0], own[64]), fmaxf(own[128], own[192])) : 0.f);
     }
+}
+
+// Of both matrices in one launch: workgroups from `blocks_x` on are the second's
+template <typename T>
+__global__ __launch_bounds__(1024) void channel_maxima(Rows<T> x, Factor f, uint32_t* __restrict__ parts_x, int blocks_x, bool wide_x, Rows<T> w,
+                                                       uint32_t* __restrict__ parts_w, bool wide_w, int ld)
+{
+    __shared__ float lds[16 * 512];
+    const bool first = (int)blockIdx.x < blocks_x, wide = first ? wide_x : wide_w;
+    const int i = first ? blockIdx.x : blockIdx.x - blocks_x, groups = wide ? (ld + 511) / 512 : (ld + 255) / 256, block = i / groups, group = i % groups;
+    const Rows<T> m = first ? x : w;
+    const Factor own = first ? f : Factor{};
+    uint32_t* const parts = first ? parts_x : parts_w;
+    if (wide) maxima_wide(m, own, parts, ld, block, group, lds);
+    else maxima_any(m, own, parts, ld, block, group, lds);
 }
 
 // most[c] of both matrices from their parts, 64 channels a workgroup
@@ -291,12 +306,12 @@ __device__ __forceinline__ void write_packed(const Packed& o, long long i, long 
 
 // Rows into operands, 8 channels a lane: 32 rows and 512 channels a workgroup
 template <typename T, int PLANES>
-__global__ __launch_bounds__(256) void pack_wide(Rows<T> x, Factor f, Packed o)
+__device__ __forceinline__ void pack_wide(const Rows<T>& x, const Factor& f, const Packed& o, int block, int group)
 {
-    const long long first = (long long)blockIdx.x * 32, end = x.end();
+    const long long first = (long long)block * 32, end = x.end();
     if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.y * 512 + lane * 8;
+    const long long c = (long long)group * 512 + lane * 8;
     if (c >= o.ld) return;
     float unit[8];
     units_of(o, c, unit);
@@ -319,13 +334,12 @@ __global__ __launch_bounds__(256) void pack_wide(Rows<T> x, Factor f, Packed o)
 
 // The same for any rows: 64 rows and 64 channels a workgroup through LDS, read with the lanes along the tokens where these are columns
 template <typename T, int PLANES>
-__global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
+__device__ __forceinline__ void pack_any(const Rows<T>& x, const Factor& f, const Packed& o, int block, int group, float (&tile)[64][65])
 {
-    __shared__ float tile[64][65];
-    const long long first = (long long)blockIdx.x * 64, end = x.end();
+    const long long first = (long long)block * 64, end = x.end();
     if (first >= (end + o.pad - 1) / o.pad * o.pad) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c0 = (long long)blockIdx.y * 64;
+    const long long c0 = (long long)group * 64;
     if (x.HW > 1) {
         const bool there = first + lane < end;
         const T* row = there ? x.row(first + lane) : nullptr;
@@ -353,6 +367,20 @@ __global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed o)
         for (int e = 0; e < 8; ++e) v[e] = tile[line][at + e];
         write_packed<PLANES>(o, i, c0 + at, v, unit, i < end ? f.of((int)i) : 0.f);
     }
+}
+
+// Both matrices in one launch: workgroups from `blocks_x` on are the second's
+template <typename T, int PLANES>
+__global__ __launch_bounds__(256) void pack(Rows<T> x, Factor f, Packed to_x, int blocks_x, bool wide_x, Rows<T> w, Packed to_w, bool wide_w)
+{
+    __shared__ float tile[64][65];
+    const bool first = (int)blockIdx.x < blocks_x, wide = first ? wide_x : wide_w;
+    const Rows<T> m = first ? x : w;
+    const Factor own = first ? f : Factor{};
+    const Packed o = first ? to_x : to_w;
+    const int i = first ? blockIdx.x : blockIdx.x - blocks_x, groups = wide ? (o.ld + 511) / 512 : o.ld / 64, block = i / groups, group = i % groups;
+    if (wide) pack_wide<T, PLANES>(m, own, o, block, group);
+    else pack_any<T, PLANES>(m, own, o, block, group, tile);
 }
 
 // find_tokens and pack for the loss of at most 64 tokens in one: a wavefront for each packed token, all of which look at the targets
@@ -1047,22 +1075,22 @@ Operand vocabulary_rows(const T* w, const uint16_t* wp, const Shape& s, long lon
 
 template <typename T> bool wide_rows(const T* p, long long C) { return C % 8 == 0 && ((uintptr_t)p & (8 * sizeof(T) - 1)) == 0; }
 
+template <typename T> bool wide(const Rows<T>& m) { return m.HW == 1 && wide_rows(m.x, m.C); }
+
 template <typename T>
-void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* parts, int ld, hipStream_t st)
+void launch_maxima(const Rows<T>& x, const Factor& f, uint32_t* parts_x, const Rows<T>& w, uint32_t* parts_w, int ld, hipStream_t st)
 {
-    const int blocks = (int)((x.rows + kMaximaRows - 1) / kMaximaRows);
-    if (x.HW == 1 && wide_rows(x.x, x.C)) channel_maxima_wide<T><<<dim3(blocks, (ld + 511) / 512), 1024, 0, st>>>(x, f, parts, ld);
-    else channel_maxima<T><<<dim3(blocks, ld / 64), 256, 0, st>>>(x, f, parts, ld);
+    auto blocks = [&](const Rows<T>& m) { return (int)((m.rows + kMaximaRows - 1) / kMaximaRows) * (wide(m) ? (ld + 511) / 512 : (ld + 255) / 256); };
+    channel_maxima<T><<<blocks(x) + blocks(w), 1024, 0, st>>>(x, f, parts_x, blocks(x), wide(x), w, parts_w, wide(w), ld);
 }
 
-// rows: padded
+// rows: padded, 0 for a matrix that is not packed
 template <typename T>
-void launch_pack(const Rows<T>& x, const Factor& f, const Packed& o, long long rows, hipStream_t st)
+void launch_pack(const Rows<T>& x, const Factor& f, const Packed& to_x, long long rows_x, const Rows<T>& w, const Packed& to_w, long long rows_w, hipStream_t st)
 {
-    if (x.HW == 1 && wide_rows(x.x, x.C))
-        pack_wide<T, kPlanesOf<T>><<<dim3(rows / 32, (o.ld + 511) / 512), 256, 0, st>>>(x, f, o);
-    else
-        pack<T, kPlanesOf<T>><<<dim3(rows / 64, o.ld / 64), 256, 0, st>>>(x, f, o);
+    auto blocks = [&](const Rows<T>& m, const Packed& o, long long rows) { return (int)(wide(m) ? rows / 32 * ((o.ld + 511) / 512) : rows / 64 * (o.ld / 64)); };
+    const int of_x = blocks(x, to_x, rows_x), all = of_x + blocks(w, to_w, rows_w);
+    if (all) pack<T, kPlanesOf<T>><<<all, 256, 0, st>>>(x, f, to_x, of_x, wide(x), w, to_w, wide(w));
 }
 
 template <typename K>
@@ -1094,16 +1122,13 @@ hipError_t launch_loss(const T* x, const T* w, const long long* target, long lon
     float* losses = reduction == NONE ? loss : r.losses;
     const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW};
     const bool few = T_ <= 64;
-    if (few) {
-        begin_few<T, planes><<<16, 256, 0, st>>>(rows, target, ignored, k, r.c.xp, Tp * ld, (int)ld, losses, lse, s.HW == 1 && wide_rows(x, s.C));
-    } else {
+    const long long Vp = round_up(s.V, kRowsPad);
+    if (few)
+        begin_few<T, planes><<<16, 256, 0, st>>>(rows, target, ignored, k, r.c.xp, Tp * ld, (int)ld, losses, lse, wide(rows));
+    else
         find_tokens<<<1, 1024, 0, st>>>(target, ignored, nullptr, k, losses, lse, (int)T_);
-        launch_pack<T>(rows, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, Tp, st);
-    }
-    if (r.wp) {
-        const long long Vp = round_up(s.V, kRowsPad);
-        launch_pack<T>({w, nullptr, nullptr, s.V, s.C, 1}, {}, {r.wp, nullptr, Vp * ld, nullptr, (int)ld, kRowsPad}, Vp, st);
-    }
+    launch_pack<T>(rows, {}, {r.c.xp, nullptr, Tp * ld, nullptr, (int)ld, kPad}, few ? 0 : Tp, {w, nullptr, nullptr, s.V, s.C, 1},
+                   {r.wp, nullptr, Vp * ld, nullptr, (int)ld, kRowsPad}, r.wp ? Vp : 0, st);
     int tiles = 0;
     const hipError_t e = with_form<T>(s.V, T_, [&](auto form) {
         typedef LossProduct<T, decltype(form)> P;
@@ -1142,13 +1167,12 @@ hipError_t launch_gradients(const T* x, const T* w, const long long* target, lon
     const Factor f = {dloss, k.order, k.count, reduction};
     find_tokens<<<1, 1024, 0, st>>>(target, ignored, lse, k, nullptr, nullptr, (int)T_);
     const Rows<T> rows = {x, k.order, k.count, T_, s.C, s.HW}, all = {w, nullptr, nullptr, s.V, s.C, 1};
-    if (planes == 1) {
-        launch_maxima(rows, f, r.parts_x, (int)ld, st);
-        launch_maxima(all, {}, r.parts_w, (int)ld, st);
+    if constexpr (planes == 1) {
+        launch_maxima(rows, f, r.parts_x, all, r.parts_w, (int)ld, st);
         join_maxima<<<dim3(ld / 64, 2), 1024, 0, st>>>(r.parts_x, k.count, r.most_x, r.parts_w, s.V, r.most_w, (int)ld);
     }
-    launch_pack(rows, f, {r.c.xp, r.xs, Tp * ld, r.most_x, (int)ld, kPad}, Tp, st);
-    if (planes == 1 || r.wp) launch_pack(all, {}, {r.wp, r.ws, Vp * ld, r.most_w, (int)ld, kRowsPad}, Vp, st);
+    launch_pack(rows, f, {r.c.xp, r.xs, Tp * ld, r.most_x, (int)ld, kPad}, Tp, all, {r.wp, r.ws, Vp * ld, r.most_w, (int)ld, kRowsPad},
+                planes == 1 || r.wp ? Vp : 0, st);
     int parts = 1;                          // of p W: the first piece, the longest, has the most
     hipError_t e = hipSuccess;
     for (int i = 0; i < r.pieces.count && e == hipSuccess; ++i) {
