@@ -690,7 +690,8 @@ Groups groups_of(const Shape& s, int V)
 
 // f(V, LANES, THREADS, NV) as constants for tokens as columns.  V: 16 bytes of a plane, less where it has less.  A workgroup's piece of a plane is 128 bytes, of
 // channels that do not fit into registers too, which are then read twice, the second time out of the last-level cache (64 x 1000 x 16x16 fp32: 4.4 TB/s
-// forward, in pieces of 64 bytes that fit 4.2; 26 x 2016: 4.4, in pieces of 32 bytes 2.1); 64 or 32 bytes only where there were not 64 workgroups otherwise.
+// forward, in pieces of 64 bytes that fit 4.2; 26 x 2016: 4.4, in pieces of 32 bytes 2.1); 64 or 32 bytes only where there were not 64 workgroups otherwise, 64 bytes read again
+// only for 128 (8 x 2048 x 250 fp32, 126 of these: 37 us forward, 51 backward; 32 bytes that stay: 21 and 32).
 template <typename T, typename F>
 hipError_t with_columns(const Shape& s, F&& f)
 {
@@ -703,14 +704,14 @@ hipError_t with_columns(const Shape& s, F&& f)
         typedef std::integral_constant<int, kKept> kept;
         typedef std::integral_constant<int, 0> again;
         const long long groups = groups_of(s, V).count;
-        auto enough = [&](int lanes) { return (groups + lanes - 1) / lanes >= 64; };
+        auto enough = [&](int lanes, int blocks = 64) { return (groups + lanes - 1) / lanes >= blocks; };
         auto fits = [&](int lanes) { return s.C <= 1024 / lanes * kKept; };
         if (s.C <= 256 / L * kKept) return f(v, whole, few(), kept());
         if (fits(L) && (enough(L) || s.C < 2048 / L)) return f(v, whole, all(), kept());
         if constexpr (V > 1) {
             if (enough(L)) return f(v, whole, all(), again());
             if (fits(L / 2) && (enough(L / 2) || s.C < 4096 / L)) return f(v, half(), all(), kept());
-            if (enough(L / 2)) return f(v, half(), all(), again());
+            if (enough(L / 2, 128)) return f(v, half(), all(), again());
             if (fits(L / 4)) return f(v, quarter(), all(), kept());
             return f(v, quarter(), all(), again());
         } else if (fits(L)) {
