@@ -375,3 +375,45 @@ def test_captured_and_on_another_stream(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_several_pieces_of_the_vocabulary_for_more_tokens():
+    """p of 140000 tokens in bfloat16 in three pieces; dx adds up over them."""
+    x, w, target = inputs((140000, 16, 1, 1), 5200, torch.bfloat16, ignored=0.02)
+    lse = check_loss(x, w, target)
+    check_gradients(x, w, target, lse, "mean", torch.tensor(1.0, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_offsets_of_more_than_32_bits():
+    """A vocabulary of 2^25 + 300 rows of 128 channels, all zeros but a few, the targets' among them: every other row has exp(0) in the sum."""
+    V, C = (1 << 25) + 300, 128
+    w = torch.zeros(V, C, dtype=torch.bfloat16, device="cuda")
+    special = torch.tensor([0, 1 << 24, 1 << 25, V - 1], device="cuda")
+    w[special] = torch.randn(4, C, device="cuda").bfloat16()
+    x = (torch.randn(3, C, 1, 1, device="cuda") + 1.5 * w[special[1:]].float()[:, :, None, None]).bfloat16()
+    target = special[1:].view(3, 1, 1).contiguous()
+    rows_, some = x.double().view(3, C), w[special].double()
+    l = rows_ @ some.t()
+    total = torch.exp(l).sum(1) + (V - 4)
+    loss, lse = S.scc_vocabulary_loss(x, w, target, "none")
+    # logits as in the other tests; the sum's 2^25 equal terms and its 500000 tiles' joins stay below 64 roundings of the whole
+    assert ((lse.double().view(3) - torch.log(total)).abs() <= 1e-5 * l.abs().amax() + 64 * ULP * torch.log(total)).all()
+    assert ((loss.double().view(3) - (torch.log(total) - l[torch.arange(3), torch.arange(1, 4)])).abs() <= 1e-5 * l.abs().amax() + 64 * ULP * torch.log(total)).all()
+    dx, dw = S.scc_vocabulary_gradients(x, w, target, lse, torch.tensor(1.0, device="cuda"), "sum")
+    p = torch.exp(l) / total[:, None]
+    size = p.clone()
+    p[torch.arange(3), torch.arange(1, 4)] -= 1
+    size[torch.arange(3), torch.arange(1, 4)] += 1
+    # p is 1 for a sure token, and what is left of p - 1 is the error of its exponent l - lse: of a logit (twice, the lse has it too), of eight roundings of numbers of
+    # the lse's size, and of p as it is stored; in relation to p + [target].  As in check_gradients.
+    off = (2 * logit_bar(x, w[special]) + 8 * ULP * (1 + torch.log(total)) + 2.0 ** -11).view(3, 1)
+    want = p @ some
+    assert ((dx.double().view(3, C) - want).abs() <= 2.0 ** -8 * want.abs() + (off * size) @ some.abs()).all()
+    want = p.t() @ rows_
+    assert ((dw[special].double() - want).abs() <= ((off + 2.0 ** -11) * size).t() @ rows_.abs() + 2.0 ** -37 * rows_.abs().amax()).all()
+    # a row of zeros: p = 1 / total for each token, stored as fp16 times 2^14: 2^-11 of it, or all of what is below 2^-25
+    want = (rows_ / total[:, None]).sum(0)
+    for v in (1, (1 << 24) + 1, (1 << 25) + 1, V - 2):
+        assert ((dw[v].double() - want).abs() <= 2.0 ** -9 * (rows_.abs() / total[:, None]).sum(0) + 2.0 ** -37 * rows_.abs().amax()).all()
