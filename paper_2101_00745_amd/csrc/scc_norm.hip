@@ -665,19 +665,17 @@ hipError_t with_rows(const Shape& s, F&& f)
     typedef std::integral_constant<int, 1024> all;
     const int C = s.C;
     const bool few = s.N <= 1024;
-    auto width = [&](auto v) {
-        constexpr int V = decltype(v)::value;
-        if (C <= V * 16) return f(v, quarter(), one());
-        if (C <= V * 32 && !few) return f(v, quarter(), two());
-        if (C <= V * 64) return f(v, wave(), one());
-        if (C <= V * 128 && !few) return f(v, wave(), two());
-        if (C <= V * 256) return f(v, four(), one());
-        if (C <= V * 1024) return few ? f(v, all(), one()) : f(v, four(), kept());
-        if (C <= V * 1024 * kKept) return f(v, all(), kept());
-        return f(v, all(), std::integral_constant<int, 0>());
-    };
-    if (C >= kWide<T>) return width(std::integral_constant<int, kWide<T>>());
-    return width(one());
+    constexpr int V = kWide<T>;
+    const std::integral_constant<int, V> v;
+    if (C < V) return f(one(), quarter(), one());
+    if (C <= V * 16) return f(v, quarter(), one());
+    if (C <= V * 32 && !few) return f(v, quarter(), two());
+    if (C <= V * 64) return f(v, wave(), one());
+    if (C <= V * 128 && !few) return f(v, wave(), two());
+    if (C <= V * 256) return f(v, four(), one());
+    if (C <= V * 1024) return few ? f(v, all(), one()) : f(v, four(), kept());
+    if (C <= V * 1024 * kKept) return f(v, all(), kept());
+    return f(v, all(), std::integral_constant<int, 0>());
 }
 
 Groups groups_of(const Shape& s, int V)
@@ -707,17 +705,16 @@ hipError_t with_columns(const Shape& s, F&& f)
         auto enough = [&](int lanes, int blocks = 64) { return (groups + lanes - 1) / lanes >= blocks; };
         auto fits = [&](int lanes) { return s.C <= 1024 / lanes * kKept; };
         if (s.C <= 256 / L * kKept) return f(v, whole, few(), kept());
-        if (fits(L) && (enough(L) || s.C < 2048 / L)) return f(v, whole, all(), kept());
         if constexpr (V > 1) {
+            if (fits(L) && (enough(L) || s.C < 2048 / L)) return f(v, whole, all(), kept());
             if (enough(L)) return f(v, whole, all(), again());
             if (fits(L / 2) && (enough(L / 2) || s.C < 4096 / L)) return f(v, half(), all(), kept());
             if (enough(L / 2, 128)) return f(v, half(), all(), again());
             if (fits(L / 4)) return f(v, quarter(), all(), kept());
             return f(v, quarter(), all(), again());
-        } else if (fits(L)) {
-            return f(v, whole, all(), kept());
+        } else {
+            return f(v, whole, all(), again());     // single pixels come here with few channels or with more than as rows fit, both backward
         }
-        return f(v, whole, all(), again());
     };
     if (s.HW >= kWide<T>) return width(std::integral_constant<int, kWide<T>>(), std::integral_constant<int, 8>());
     if (kWide<T> > 4 && s.HW >= 4) return width(std::integral_constant<int, 4>(), std::integral_constant<int, 16>());
@@ -771,11 +768,13 @@ hipError_t launch_forward(const T* x, const T* r, const T* w, T* h, void* y, flo
         });
     return with_columns<T>(s, [&](auto v, auto lanes, auto threads, auto nv) {
         constexpr int V = decltype(v)::value, L = decltype(lanes)::value, TH = decltype(threads)::value, NV = decltype(nv)::value;
-        const Groups g = groups_of(s, V);
-        const dim3 blocks = grid_of((((long long)g.count + L - 1) / L + 7) / 8 * 8);
-        if (scale) forward_columns<T, V, L, TH, NV, true><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
-        else forward_columns<T, V, L, TH, NV, false><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
-        return hipGetLastError();
+        if constexpr (V > 1) {
+            const Groups g = groups_of(s, V);
+            const dim3 blocks = grid_of((((long long)g.count + L - 1) / L + 7) / 8 * 8);
+            if (scale) forward_columns<T, V, L, TH, NV, true><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
+            else forward_columns<T, V, L, TH, NV, false><<<blocks, TH, 0, st>>>(x, r, w, h, y, scale, s, g);
+        }
+        return hipGetLastError();           // single pixels are rows
     });
 }
 
