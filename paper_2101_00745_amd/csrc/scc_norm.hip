@@ -54,6 +54,17 @@ __device__ __forceinline__ void as_loaded(Vec<T, V>& v)
 
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
+// Sum of a power of two of values as a tree: log N roundings behind one another instead of N
+template <int N>
+__device__ __forceinline__ float in_pairs(float (&v)[N])
+{
+#pragma unroll
+    for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] += v[i + n];
+    return v[0];
+}
+
 // Squares of values beyond 2^60 leave binary32: sums that come out above this are taken again of scaled values.
 constexpr float kLargeSum = 1e37f;
 constexpr float kShrink = 8.077935669463161e-28f;    // 2^-90: the square of the largest value times 2^31 channels fits
@@ -301,10 +312,10 @@ __global__ __launch_bounds__(kRowThreads<TPT>) void backward_rows(const T* __res
     if constexpr (kGroups > 1) {
         __syncthreads();
         for (int c = threadIdx.x; c < s.C; c += kRowThreads<TPT>) {
-            float sum = rows[c];
+            float v[kGroups];
 #pragma unroll
-            for (int i = 1; i < kGroups; ++i) sum += rows[i * kMost + c];
-            part[(size_t)blockIdx.x * s.C + c] = sum;
+            for (int i = 0; i < kGroups; ++i) v[i] = rows[i * kMost + c];
+            part[(size_t)blockIdx.x * s.C + c] = in_pairs(v);
         }
     }
 }
@@ -624,22 +635,22 @@ __global__ __launch_bounds__(1024) void weight_sums(const float* __restrict__ pa
     __shared__ float lds[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float sum = 0.f;
-    if (c < C) {
-        int i = wave;
-        for (; i + 7 * 16 < rows; i += 8 * 16) {        // eight rows under way
+    if (c < C)
+        for (int i = wave; i < rows; i += 8 * 16) {     // eight rows under way
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = part[(size_t)(i + j * 16) * C + c];
+            for (int j = 0; j < 8; ++j) v[j] = part[(size_t)(i + j * 16 < rows ? i + j * 16 : rows - 1) * C + c];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[j];
+            for (int j = 0; j < 8; ++j) v[j] = i + j * 16 < rows ? v[j] : 0.f;
+            sum += in_pairs(v);
         }
-        for (; i < rows; i += 16) sum += part[(size_t)i * C + c];
-    }
     lds[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && c < C) {
-        for (int i = 1; i < 16; ++i) sum += lds[i][lane];
-        dw[c] = from_f32<D>(sum);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = lds[i][lane];
+        dw[c] = from_f32<D>(in_pairs(v));
     }
 }
 
