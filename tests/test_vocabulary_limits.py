@@ -1,0 +1,63 @@
+"""The vocabulary loss where its exponents are large.
+
+Logits here are exact: x has one channel that is not 0, w one that is 1 for the target.  So what is off is the loss's own."""
+import math
+
+import pytest
+import torch
+
+import paper_2101_00745_amd as S
+from tests.test_vocabulary import DTYPES, ULP
+
+C, V, Y = 64, 2000, 777
+
+
+def sure(dtype, tokens):
+    """Tokens whose target's logit is between 12 and 20000 and whose other logits are 0."""
+    x = torch.zeros(tokens, C, 1, 1, device="cuda")
+    x[:, 5, 0, 0] = torch.exp2(torch.linspace(math.log2(12.0), math.log2(20000.0), tokens, device="cuda"))
+    w = torch.zeros(V, C, device="cuda")
+    w[Y, 5] = 1.0
+    return x.to(dtype), w.to(dtype), torch.full((tokens, 1, 1), Y, device="cuda")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [40, 500, 3000])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_token_that_is_sure_of_its_target(tokens, dtype):
+    """total = 1 + (V - 1) exp(-l).  The 1 is exact, so the loss is never below 0, and it is 0 from l = 40 on, where the rest is less than half a
+    step of the 1.  Below that: a lane adds up to 64 terms (64 roundings of a sum near 1), some 24 more join them, the exponents l log2(e) are rounded
+    by 2^-24 l, which the term exp(-l) makes at most 12 exp(-12) V of it, and the logarithm is rounded: 96 * 2^-24."""
+    x, w, target = sure(dtype, tokens)
+    l = x[:, 5, 0, 0].double()
+    want = torch.log1p((V - 1) * torch.exp(-l))
+    for reduction in ("none", "sum"):
+        loss, lse = S.scc_vocabulary_loss(x, w, target, reduction)
+        if reduction == "none":
+            loss = loss.double().flatten()
+            assert (loss >= 0).all()
+            assert (loss[l >= 40] == 0).all()
+            assert ((loss - want).abs() <= 96 * ULP).all()
+        # half a step of the lse on top
+        assert ((lse.double().flatten() - l - want).abs() <= 96 * ULP + ULP * (l + want)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("offset", [0, 100, 100000])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_what_all_logits_of_a_token_have_in_common(dtype, offset):
+    """Logits offset + 0 .. 15: the loss is that of 0 .. 15, whatever the offset.  Sums of at most 64 terms of a lane and a dozen joins, exponents of at most 15
+    log2(e), whose terms are the small ones: 110 * 2^-24 of the whole."""
+    x = torch.zeros(300, C, 1, 1, device="cuda")
+    x[:, 0] = 1.0
+    x[:, 1:3] = 256.0
+    w = torch.zeros(V, C, device="cuda")
+    w[:, 0] = torch.arange(V, device="cuda") % 16
+    # both factors in bfloat16: 100 = 256 * 0.390625, 100000 = 256 * (390 + 0.625)
+    w[:, 1], w[:, 2] = (offset // 256) & ~1, offset / 256 - ((offset // 256) & ~1)
+    target = torch.randint(V, (300, 1, 1), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    logits = w[:, 0].double()
+    want = torch.logsumexp(logits, 0) - logits[target.flatten()]
+    loss = S.scc_vocabulary_loss(x.to(dtype), w.to(dtype), target, "none")[0].double().flatten()
+    assert torch.equal(w.to(dtype).float(), w)
+    assert ((loss - want).abs() <= 110 * ULP * (1 + want)).all()
