@@ -640,13 +640,14 @@ __global__ __launch_bounds__(P::kThreads, P::kWavesPerSimd) void share_product(O
 #pragma unroll
         for (int n = 0; n < P::FN; ++n) {
             const long long t = part.column + (wn * P::FN + n) * 32 + (lane & 31);
-            const float shift = (kCut ? 0.f : kRaise) - k.lse[t] * kLog2E;
+            // lse off first, as in loss_product: what p is off by as a whole is half a step of lse (2^-24 of it) and, raised, of 14 (3e-7)
+            const float lse = k.lse[t];
             const float d = kCut ? f.of((int)t) : 1.f;
 #pragma unroll
             for (int m = 0; m < P::FM; ++m)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][r], kLog2E, shift));
+                    float share = __builtin_amdgcn_exp2f(fmaf(acc[m][n][r] - lse, kLog2E, kCut ? 0.f : kRaise));
                     if (ends && v0 + m * 32 + 8 * (r / 4) + r % 4 >= V) share = 0.f;
                     acc[m][n][r] = kCut ? share * d : share;
                 }
