@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
         }
         // of a state in 8 bits the scale, a power of two, goes into the factor that follows: the same bits
         const float from_m = BYTES ? ms * s.b1 : s.b1;
+        bool small = false;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if constexpr (BYTES) {
@@ -198,8 +199,17 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, Step s)
             m[e] = m[e] * from_m + g[e] * s.d1;
             v[e] = v[e] * s.b2 + (g[e] * g[e]) * s.d2;
             root[e] = __builtin_amdgcn_sqrtf(v[e]);
-            w[e] = fmaf(w[e], s.keep, -(m[e] * rate) * __builtin_amdgcn_rcpf(fmaf(root[e], c2, s.eps)));
+            small |= __float_as_uint(v[e]) - 1u < 0x7fffffu;
         }
+        if (__any(small)) {
+            asm volatile("");                   // a branch: rare
+            // the instruction takes what is below 2^-126 for 0; the root of it is no less than 2^-75
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (__float_as_uint(v[e]) - 1u < 0x7fffffu) root[e] = __builtin_amdgcn_sqrtf(v[e] * 18446744073709551616.f) * 2.3283064365386963e-10f;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = fmaf(w[e], s.keep, -(m[e] * rate) * __builtin_amdgcn_rcpf(fmaf(root[e], c2, s.eps)));
         write<T, E>((T*)t.w + from, w, whole, left);
         if constexpr (BYTES) {
             uint32_t most_m = 0, most_v = 0;
