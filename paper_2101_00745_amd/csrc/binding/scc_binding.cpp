@@ -1011,49 +1011,78 @@ bool tensors(PyObject* o, Py_ssize_t count, at::ScalarType type, std::vector<con
     return true;
 }
 
+// What a step works on: weights, gradients, states and, in 8 bits, their scales
+struct AdamwLists {
+    std::vector<const at::Tensor*> l[6];
+    at::ScalarType type;
+    bool bytes;
+};
+
+// (weights, grads, first, second, first scales or None, second scales or None); false where they are not plain or do not fit together
+bool adamw_lists(PyObject* const* args, AdamwLists* o)
+{
+    if (!no_modes() || !PyList_CheckExact(args[0]) || PyList_GET_SIZE(args[0]) < 1 || PyList_GET_SIZE(args[0]) > INT_MAX) return false;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    PyObject* e = PyList_GET_ITEM(args[0], 0);
+    if (!THPVariable_CheckExact(e)) return false;
+    const at::ScalarType type = THPVariable_Unpack(e).scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) return false;
+    const bool bytes = args[4] != Py_None;
+    const at::ScalarType state = bytes ? at::kFloat8_e4m3fn : at::kFloat;
+    std::vector<const at::Tensor*>(&l)[6] = o->l;
+    if ((args[5] != Py_None) != bytes || !tensors(args[0], count, type, &l[0]) || !tensors(args[1], count, type, &l[1]) ||
+        !tensors(args[2], count, state, &l[2]) || !tensors(args[3], count, state, &l[3]) ||
+        (bytes && (!tensors(args[4], count, at::kFloat, &l[4]) || !tensors(args[5], count, at::kFloat, &l[5]))))
+        return false;
+    if (!same_shapes(l[0], l[1]) || !same_shapes(l[0], l[2]) || !same_shapes(l[0], l[3])) return false;
+    for (Py_ssize_t j = 0; bytes && j < count; ++j) {
+        const int64_t blocks = (l[0][j]->numel() + 255) / 256;
+        if (l[4][j]->numel() != blocks || l[5][j]->numel() != blocks) return false;
+    }
+    o->type = type;
+    o->bytes = bytes;
+    return !overlap({&l[0], &l[2], &l[3], &l[4], &l[5]}, l[1]);
+}
+
+// The same arguments -> True where a step on them is made here, or None
+PyObject* adamw_fits(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    AdamwLists a;
+    if (n != 6 || !adamw_lists(args, &a)) Py_RETURN_NONE;
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 // (weights, grads, first, second, first scales or None, second scales or None, lr, step, b1, b2, eps, weight_decay, seed) -> the library's status, or
 // None where the call is not plain; as orthogonal_step
 PyObject* adamw_step(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     double v[5];
-    if (n != 13 || !no_modes() || !PyList_CheckExact(args[0]) || PyList_GET_SIZE(args[0]) < 1 || PyList_GET_SIZE(args[0]) > INT_MAX) Py_RETURN_NONE;
-    if (!PyLong_CheckExact(args[7]) || !PyLong_CheckExact(args[12]) || !numbers(args + 6, 1, v) || !numbers(args + 8, 4, v + 1)) Py_RETURN_NONE;
-    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
-    PyObject* e = PyList_GET_ITEM(args[0], 0);
-    if (!THPVariable_CheckExact(e)) Py_RETURN_NONE;
-    const at::ScalarType type = THPVariable_Unpack(e).scalar_type();
-    if (type != at::kFloat && type != at::kBFloat16) Py_RETURN_NONE;
-    const bool bytes = args[4] != Py_None;
-    const at::ScalarType state = bytes ? at::kFloat8_e4m3fn : at::kFloat;
-    std::vector<const at::Tensor*> l[6];
-    if ((args[5] != Py_None) != bytes || !tensors(args[0], count, type, &l[0]) || !tensors(args[1], count, type, &l[1]) ||
-        !tensors(args[2], count, state, &l[2]) || !tensors(args[3], count, state, &l[3]) ||
-        (bytes && (!tensors(args[4], count, at::kFloat, &l[4]) || !tensors(args[5], count, at::kFloat, &l[5]))))
+    AdamwLists a;
+    if (n != 13 || !PyLong_CheckExact(args[7]) || !PyLong_CheckExact(args[12]) || !numbers(args + 6, 1, v) || !numbers(args + 8, 4, v + 1) ||
+        !adamw_lists(args, &a))
         Py_RETURN_NONE;
-    if (!same_shapes(l[0], l[1]) || !same_shapes(l[0], l[2]) || !same_shapes(l[0], l[3])) Py_RETURN_NONE;
+    const size_t count = a.l[0].size();
     std::vector<long long> sizes(count);
     std::vector<void*> at[6];
-    for (int i = 0; i < (bytes ? 6 : 4); ++i) {
+    for (int i = 0; i < (a.bytes ? 6 : 4); ++i) {
         at[i].resize(count);
-        for (Py_ssize_t j = 0; j < count; ++j) at[i][j] = l[i][j]->data_ptr();
+        for (size_t j = 0; j < count; ++j) at[i][j] = a.l[i][j]->data_ptr();
     }
-    for (Py_ssize_t j = 0; j < count; ++j) {
-        sizes[j] = l[0][j]->numel();
-        if (bytes && (l[4][j]->numel() != (sizes[j] + 255) / 256 || l[5][j]->numel() != (sizes[j] + 255) / 256)) Py_RETURN_NONE;
-    }
-    if (overlap({&l[0], &l[2], &l[3], &l[4], &l[5]}, l[1])) Py_RETURN_NONE;
+    for (size_t j = 0; j < count; ++j) sizes[j] = a.l[0][j]->numel();
     int overflow = 0;
     const long long step = PyLong_AsLongLongAndOverflow(args[7], &overflow);
     if (overflow) Py_RETURN_NONE;
     const scc_adamw_options o = {v[0], v[1], v[2], v[3], v[4], (uint64_t)PyLong_AsUnsignedLongLongMask(args[12])};
-    const int rc = launch(*l[0][0], [&](void* st) {
-        return scc_adamw_step((int)count, at[0].data(), at[1].data(), at[2].data(), at[3].data(), bytes ? (float* const*)at[4].data() : nullptr,
-                              bytes ? (float* const*)at[5].data() : nullptr, sizes.data(), &o, step, nullptr, type == at::kFloat ? SCC_F32 : SCC_BF16, st);
+    const int rc = launch(*a.l[0][0], [&](void* st) {
+        return scc_adamw_step((int)count, at[0].data(), at[1].data(), at[2].data(), at[3].data(), a.bytes ? (float* const*)at[4].data() : nullptr,
+                              a.bytes ? (float* const*)at[5].data() : nullptr, sizes.data(), &o, step, nullptr, a.type == at::kFloat ? SCC_F32 : SCC_BF16, st);
     });
     if (rc == SCC_OK || rc == SCC_ERR_LAUNCH)
         for (int i = 0; i < 6; ++i)
-            if (i != 1) moved(l[i]);
+            if (i != 1) moved(a.l[i]);
     return PyLong_FromLong(rc);
     END_HANDLE_TH_ERRORS
 }
@@ -1073,6 +1102,7 @@ PyMethodDef methods[] = {METHOD(forward, "(x, w, cg, co) -> y or None"), METHOD(
                          METHOD(norm_block, "(x, w, residual or None, eps) -> (y, h) under autograd, or None"),
                          METHOD(vocabulary_loss, "(x, w, target, reduction, ignored) -> (loss, lse) or None"),
                          METHOD(vocabulary_block, "(x, w, target, reduction, ignored) -> loss under autograd, or None"),
+                         METHOD(adamw_fits, "(weights, grads, first, second, first scales, second scales) -> True or None"),
                          METHOD(adamw_step, "(weights, grads, first, second, first scales, second scales, lr, step, b1, b2, eps, weight_decay, seed) -> status or None"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -95,10 +95,11 @@ class AdamW(torch.optim.Optimizer):
                 return other
         return step
 
-    def _begin(self, p, group, begun):
-        """The weight's state; begun: the numbers on the GPU of the weights that begin in this step."""
+    def _begin(self, p, group, begun, fresh):
+        """The weight's state; begun: the numbers on the GPU of the weights that begin in this step; fresh: gets the weights whose states are made here."""
         state = self.state[p]
         if not state:
+            fresh.append(p)
             if group["capturable"]:
                 if p.device not in begun:
                     begun[p.device] = torch.zeros((), dtype=torch.int64, device=p.device)
@@ -114,6 +115,30 @@ class AdamW(torch.optim.Optimizer):
                 for name in ("first", "second"):
                     state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
         return state
+
+    def _gather(self, group, moving, fresh):
+        """The lists of the group's calls, each of one device, type, width of states and age: [weights, gradients, states and their scales]."""
+        lists, begun = {}, {}
+        for p in moving:
+            state = self._begin(p, group, begun, fresh)
+            step, scales = state["step"], [state.get("first_scales"), state.get("second_scales")]
+            key = (p.device, p.dtype, scales[0] is None, id(step) if isinstance(step, torch.Tensor) else step)
+            own = lists.setdefault(key, ([], [], [], [], *([None] * 2 if scales[0] is None else ([], []))))
+            for to, t in zip(own, (p, p.grad.contiguous(), state["first"], state["second"], *scales)):
+                if to is not None:
+                    to.append(t)
+        return list(lists.values())
+
+    def _age(self, moving, by):
+        seen = set()
+        for p in moving:
+            state = self.state[p]
+            step = state["step"]
+            if not isinstance(step, torch.Tensor):
+                state["step"] = step + by
+            elif id(step) not in seen:
+                seen.add(id(step))
+                step.add_(by)
 
     def _resting(self, group):
         """The numbers on the GPU of the weights that have no gradient in this step."""
@@ -140,32 +165,34 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None):
+        """Every call is looked at before one is made (the first one by itself: it is refused before it moves anything), so that a step that is refused leaves
+        ages, weights and states as they were."""
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        for group in self.param_groups:
-            lists, begun, raised = {}, {}, set()
-            moving = [p for p in group["params"] if p.grad is not None and p.numel()]
-            if any(p.is_cuda for p in moving) and torch.cuda.is_current_stream_capturing():
-                self._check_capture(group, moving)
-            self._part(group, moving)
-            for p in moving:
-                state = self._begin(p, group, begun)
-                small = "first_scales" in state
-                if isinstance(state["step"], torch.Tensor):
-                    age = state["step"].data_ptr()
-                    if age not in raised:
-                        state["step"].add_(1)
-                        raised.add(age)
-                else:
-                    state["step"] += 1
-                    age = state["step"]
-                own = lists.setdefault((p.device, p.dtype, small, age), (state["step"], [], [], [], [], [], []))
-                for to, t in zip(own[1:], (p, p.grad.contiguous(), state["first"], state["second"], state.get("first_scales"), state.get("second_scales"))):
-                    to.append(t)
-            for (_, _, small, _), (step, ws, gs, ms, vs, mss, vss) in lists.items():
-                _scc.scc_adamw_step(ws, gs, ms, vs, group["lr"], step, betas=group["betas"], eps=group["eps"],
-                                    weight_decay=group["weight_decay"], first_scales=mss if small else None,
-                                    second_scales=vss if small else None, seed=group["seed"])
+        groups = [(group, [p for p in group["params"] if p.grad is not None and p.numel()]) for group in self.param_groups]
+        if any(p.is_cuda for _, moving in groups for p in moving) and torch.cuda.is_current_stream_capturing():
+            for group, moving in groups:
+                if moving:
+                    self._check_capture(group, moving)
+        fresh, raised = [], False
+        try:
+            calls = [(group, lists) for group, moving in groups for lists in self._gather(group, moving, fresh)]
+            for group, lists in calls[1:]:
+                _scc._refuse_adamw(*lists, group["lr"], self.state[lists[0][0]]["step"], group["betas"], group["eps"], group["weight_decay"])
+            for group, moving in groups:
+                self._part(group, moving)
+                self._age(moving, 1)
+            raised = True
+            for i, (group, (ws, gs, ms, vs, mss, vss)) in enumerate(calls):
+                _scc.scc_adamw_step(ws, gs, ms, vs, group["lr"], self.state[ws[0]]["step"], betas=group["betas"], eps=group["eps"],
+                                    weight_decay=group["weight_decay"], first_scales=mss, second_scales=vss, seed=group["seed"])
+        except Exception as e:
+            if not raised or (i == 0 and getattr(e, "status", None) != _scc.SCC_ERR_LAUNCH):
+                for _, moving in groups if raised else ():
+                    self._age(moving, -1)
+                for p in fresh:
+                    del self.state[p]
+            raise
         return loss

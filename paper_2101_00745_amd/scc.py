@@ -8,6 +8,7 @@ GPU the call raises.
 """
 import ctypes
 import functools
+import math
 import os
 
 import torch
@@ -16,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libscc_hip.so")
 
 SCC_F32, SCC_BF16 = 0, 1
-SCC_ERR_LAUNCH = -6
+SCC_ERR_SHAPE, SCC_ERR_LAUNCH, SCC_ERR_OPTION = -2, -6, -8
 SYMBOLS = ("scc_window_params", "scc_forward", "scc_forward_workspace_bytes", "scc_forward_ws", "scc_backward_input",
            "scc_backward_input_workspace_bytes", "scc_backward_input_ws",
            "scc_backward_weight_workspace_bytes", "scc_backward_weight", "scc_backward_weight_static",
@@ -33,6 +34,7 @@ SYMBOLS = ("scc_window_params", "scc_forward", "scc_forward_workspace_bytes", "s
 ACTIVATIONS = {"silu": 0, "gelu": 1}    # scc_activation of include/scc.h
 REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}    # scc_reduction of include/scc.h
 STATE_BLOCK = 256                       # elements of a scale of AdamW's states in 8 bits
+MOST_ADAMW = 1 << 34                    # elements of a weight that scc_adamw_step takes
 STATIC_SCRATCH_BYTES = 32 << 20    # SCC_STATIC_SCRATCH_BYTES of include/scc.h
 
 _lib = None
@@ -163,7 +165,7 @@ class _NoNative:
         return None
 
     backward = dw_forward = dw_backward = dw_block = gated_forward = gated_backward = gated_block = orthogonalise = orthogonal_step = forward
-    norm_forward = norm_quantised = norm_block = vocabulary_loss = vocabulary_block = adamw_step = forward
+    norm_forward = norm_quantised = norm_block = vocabulary_loss = vocabulary_block = adamw_step = adamw_fits = forward
 
 
 def _load_native():
@@ -858,6 +860,23 @@ def _check_adamw(weights, grads, first, second, first_scales, second_scales):
     return dev, _dtype_code(weights[0])
 
 
+def _check_step(step, dev):
+    if step.dtype != torch.int64 or step.numel() != 1 or step.device != dev:
+        raise ValueError("step must be a number, or an int64 tensor of one element on the weights' device")
+
+
+def _refuse_adamw(weights, grads, first, second, first_scales, second_scales, lr, step, betas, eps, weight_decay):
+    """Raises what scc_adamw_step would refuse these arguments with."""
+    if not (_native or _load_native()).adamw_fits(weights, grads, first, second, first_scales, second_scales):
+        _check_adamw(weights, grads, first, second, first_scales, second_scales)
+    if any(w.numel() > MOST_ADAMW for w in weights):
+        _check(SCC_ERR_SHAPE)
+    if not (all(math.isfinite(v) for v in (lr, eps, weight_decay)) and eps >= 0 and all(0 <= b < 1 for b in betas)):
+        _check(SCC_ERR_OPTION)
+    if isinstance(step, torch.Tensor):
+        _check_step(step, weights[0].device)
+
+
 def scc_adamw_step(weights, grads, first, second, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, first_scales=None,
                    second_scales=None, seed=0):
     """A step of AdamW on a list of weights of any shapes, in place: m <- b1 m + (1 - b1) g, v <- b2 v + (1 - b2) g^2, w <- (1 - lr weight_decay) w -
@@ -873,8 +892,7 @@ def scc_adamw_step(weights, grads, first, second, lr, step, betas=(0.9, 0.999), 
     dev, dtype = _check_adamw(weights, grads, first, second, first_scales, second_scales)
     device_step = None
     if isinstance(step, torch.Tensor):
-        if step.dtype != torch.int64 or step.numel() != 1 or step.device != dev:
-            raise ValueError("step must be a number, or an int64 tensor of one element on the weights' device")
+        _check_step(step, dev)
         device_step, step = step.data_ptr(), 1
     count = len(weights)
     lists = [weights, grads, first, second, first_scales, second_scales]
