@@ -250,7 +250,7 @@ struct FirstOrder : torch::autograd::Function<FirstOrder> {
 
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, torch::autograd::variable_list)
     {
-        TORCH_CHECK(false, "sliding-channel convolution has no second derivative");
+        TORCH_CHECK(false, "this operator has no second derivative");
     }
 };
 
@@ -414,7 +414,7 @@ struct FirstOrderPair : torch::autograd::Function<FirstOrderPair> {
 
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, torch::autograd::variable_list)
     {
-        TORCH_CHECK(false, "sliding-channel convolution has no second derivative");
+        TORCH_CHECK(false, "this operator has no second derivative");
     }
 };
 
@@ -661,7 +661,7 @@ struct FirstOrderOf : torch::autograd::Function<FirstOrderOf> {
 
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext*, torch::autograd::variable_list)
     {
-        TORCH_CHECK(false, "sliding-channel convolution has no second derivative");
+        TORCH_CHECK(false, "this operator has no second derivative");
     }
 };
 

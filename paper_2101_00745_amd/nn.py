@@ -32,7 +32,7 @@ class _FirstOrder(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        raise RuntimeError("sliding-channel convolution has no second derivative")
+        raise RuntimeError("this operator has no second derivative")
 
 
 def _first_order(grads, *used):
