@@ -460,7 +460,7 @@ int scc_norm_backward(const void* x, const void* residual, const void* w, const 
  * x: N*C*H*W.  w: V*C, one row for each element of the vocabulary, the type of x.  target: N*H*W.  lse: out, N*H*W (0 where ignored).  loss: out, N*H*W
  * values (SCC_NONE), or one: their sum (SCC_SUM) or that divided by the number of tokens that are not ignored (SCC_MEAN; 0 if there are
  * none).  A target that is neither `ignored` nor in 0 .. V-1 gives a NaN for its token; nothing is read there.  Logits are binary32 sums (products as in
- * scc_forward).  Non-finite inputs as for scc_forward.
+ * scc_forward).  Of each the largest is taken off before the exponential, so no loss is below 0.  Non-finite inputs as for scc_forward.
  */
 typedef enum { SCC_NONE = 0, SCC_SUM = 1, SCC_MEAN = 2 } scc_reduction;
 size_t scc_vocabulary_loss_workspace_bytes(int N, int C, int H, int W, int V, scc_reduction reduction, scc_dtype dtype);
@@ -471,11 +471,15 @@ int scc_vocabulary_loss(const void* x, const void* w, const long long* target, f
  * Its gradients, the logits computed again in pieces of the vocabulary: with p_tv = exp(l_tv - lse_t) - [v = y_t] and d_t the gradient of token t's
  * loss (dloss[t], or dloss[0], or dloss[0] / count; 0 where ignored),
  *     dx_tc = d_t sum_v p_tv w_vc,   dw_vc = sum_t d_t p_tv x_tc
- * lse: as scc_vocabulary_loss wrote it, from the same x, w, target and `ignored`.  dx: out, as x.  dw: out, V*C values of the type `grad` (SCC_F32, or
+ * lse: as scc_vocabulary_loss wrote it, from the same x, w, target and `ignored`; the half step that it is rounded by, up to 2^-24 of it, puts all
+ * p of a token off by as much.  dx: out, as x.  dw: out, V*C values of the type `grad` (SCC_F32, or
  * SCC_BF16 for bf16 tensors).  Sums are binary32, in a fixed order: two calls give bitwise identical results.  In bf16 p is rounded to 11
- * bits between the products, and so is d_t x_tc; of a channel's values those below 2^-31 of its largest lose bits.
+ * bits between the products (below 2^-28 to steps of 2^-38, so that p below 2^-39 is 0), and so is d_t x_tc: terms are off by 2^-12 each, in dw as binary32 too; of a
+ * channel's values those below 2^-31 of its largest lose bits.
  * workspace, for both: at least the query's bytes, 256-byte aligned, owned by the caller, contents undefined before and after (0 for invalid
- * arguments).  It holds a copy of w (three bf16 pieces for each value of binary32) and, for the gradients, one piece's p.
+ * arguments).  It holds the tokens that count as rows and a copy of w (three bf16 pieces for each value of binary32; the loss reads aligned bf16 rows of a multiple of 64
+ * channels where they are) and, for the gradients in bf16, both once more in fp16; one piece's p, 0.5 GB or 2048 values a token, whichever is more (three times 2 bytes each in
+ * binary32); 1 to 16 parts of dx in binary32, and where a piece's rows of dw are summed in parts up to 16 of those.
  * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (a size < 1, N*H*W or V over 2^26, their product over 2^45, C over 2^20), SCC_ERR_DTYPE, SCC_ERR_OPTION (reduction),
  * SCC_ERR_WORKSPACE, SCC_ERR_LAUNCH.
  */
@@ -500,6 +504,9 @@ int scc_vocabulary_gradients(const void* x, const void* w, const long long* targ
  * overlap another tensor of the call, which is not checked here.
  * Errors: SCC_ERR_NULL, SCC_ERR_SHAPE (count < 1, a size < 1 or over 2^34), SCC_ERR_DTYPE, SCC_ERR_OPTION (a beta outside [0, 1), eps < 0, a value
  * that is not finite, step < 1), SCC_ERR_LAUNCH (some of the list may have moved, so the call is not to be made again).
+ * The options are read before the call returns: a captured call replays with the lr, betas and weight_decay that it was captured with.  The numbers of two
+ * lists of one seed and t are the same ones, from i = 0 on.  All arithmetic is binary32's, subnormal numbers included: a v that is 0 there (of gradients below 2^-70; in 8 bits also where
+ * a block's largest root is below 2^-58 and an element's far below that) leaves m over eps, and with an eps of 0 what m / 0 is.
  */
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay;

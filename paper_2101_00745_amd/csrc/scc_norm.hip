@@ -1,7 +1,7 @@
 // Root-mean-square norm over the channels with the residual's addition, its 8-bit output and its gradients.
 //
 // All of it is bound by memory: forward reads x and r and writes h and y, backward reads x, r, dy and dh and writes dx, each
-// element once (128 x 512 x 32x32 fp32: 194 us forward, 5.5 TB/s, 246 backward, 4.4; 4096 x 512 tokens bf16, in the last-level cache: 4.1 and 10.2).  So a
+// element once (128 x 512 x 32x32 fp32: 195 us forward, 5.5 TB/s, 246 backward, 4.4; 4096 x 512 tokens bf16, in the last-level cache: 4.5, and 6.3 with 5.5 for dw's sums).  So a
 // token's channels stay in registers between the sum over them and their second use, as they were loaded (bf16 pairs are not widened
 // before they are used).  Two layouts: tokens as rows (H*W = 1: the channels of a token are consecutive; a group of 16 to 1024 lanes per token)
 // and tokens as columns (a workgroup has some consecutive columns and all their channels: lanes along the pixels, so that a channel's load

@@ -4,11 +4,13 @@
 // vocabulary for each token; these are joined per token.  The gradients: the vocabulary in pieces; for each piece the product again, whose
 // tiles leave p = exp(l - lse) - [target] in the workspace, and then both p W and p^T x in one launch.  Four products of 2 T C V operations,
 // where keeping the logits would take three and T V values of memory.  Bound by the matrix instructions, of which our loop alone reaches 1.39 PFLOP/s in bf16: 16000 tokens x 1024
-// x 64001 1.9 ms for the logits (1.1), 2.4 for p and 3.9 for both gradients (1.07); 4096 x 512 x 32000, K of eight steps, 155, 200 and 275 us (0.87, 0.67, 0.98).
+// x 64001 1.94 ms for the logits (1.08), 2.34 for p (0.89) and 3.74 for both gradients (1.12); 4096 x 512 x 32000, K of eight steps, 158, 205 and 271 us (0.85, 0.65, 0.99).
 //
 // bf16 tensors: the logits' products are exact in binary32.  The gradients' products are of fp16 values: p, in [-1, 1], as 2^14 p, and x and w
-// with a power of two for each channel, which leaves the sum over tokens (the vocabulary) as a factor.  fp16 keeps 3 bits more of p than bf16,
-// so that the gradients are rounded once in effect, at their end; of x and w it keeps all bits from 2^-31 of a channel's largest value up.
+// with a power of two for each channel, which leaves the sum over tokens (the vocabulary) as a factor.  fp16 keeps 3 bits more of p than bf16 from 2^-28
+// up (below that steps are of 2^-38: fewer bits than bf16's below 2^-31, nothing below 2^-39), so that bf16 gradients are rounded once in effect, at their
+// end (16000 x 1024 x 64001, dw: 0.00168 in norm, with p and d x in binary32 0.00166); gradients asked for in binary32 are off by 2^-12 of their terms.  Of x and w
+// fp16 keeps all bits from 2^-31 of a channel's largest value up.
 // binary32 tensors: all factors are cut exactly into three bf16 pieces, and six of nine products are taken (as in scc_forward).
 #include "scc_vocabulary.h"
 #include "scc_vocabulary_product.h"
@@ -982,8 +984,9 @@ struct Pieces {
     int count;
 };
 
-// Pieces of the vocabulary, equally long: at most 2^28 values of p at a time, 2^26 of three planes, some 0.5 GB; a piece costs a round of dx's sums and the ends of three
-// launches.  16000 x 1024 x 64001 bf16, gradients: 2^26 7.1 ms, 2^27 6.5, 2^28 6.2, 2^29 6.1; 1340 x 512 x 32000 binary32: 2^24 934 us, 2^25 916, 2^26 834, 2^27 858
+// Pieces of the vocabulary, equally long: at most 2^28 values of p at a time, 2^26 of three planes, some 0.5 GB, or 2048 rows of the vocabulary where that is more (beyond 131072
+// tokens in bf16 and 32768 in binary32: 262144 tokens keep 1.1 or 3.2 GB); a piece costs a round of dx's sums and the ends of three launches.  16000 x 1024 x
+// 64001 bf16, gradients: 2^26 7.1 ms, 2^27 6.5, 2^28 6.2, 2^29 6.1; 1340 x 512 x 32000 binary32: 2^24 934 us, 2^25 916, 2^26 834, 2^27 858
 Pieces pieces_of(const Shape& s, int planes)
 {
     const long long Tp = padded(s.T()), Vp = round_up(s.V, kRowsPad), most = planes == 3 ? 1ll << 26 : 1ll << 28;

@@ -61,8 +61,10 @@ class OrthogonalMomentum(torch.optim.Optimizer):
 class AdamW(torch.optim.Optimizer):
     """AdamW for the weights that ``OrthogonalMomentum`` does not take, or for all (``scc_adamw_step``): one call, in launches of 60 weights, for all weights of
     a group, dtype and age.  state_bits: 32, or 8 for states of e4m3 with a scale for each 256 elements, rounded at random (a hash of ``seed``, the
-    step and the place, so that a run repeats).  capturable: the step's number is kept on the GPU, so that a captured step can be replayed; make one
-    step before the capture, which allocates the states."""
+    step and the place, so that a run repeats; lists of one step round by the same numbers).  capturable: the step's number is kept on the GPU, so that a captured
+    step can be replayed; make one step before the capture, which allocates the states.  A replay has the lr, betas, eps and weight_decay of the capture: where a
+    schedule moves them, capture again.  bfloat16 weights are rounded to nearest: a step of less than half of theirs (2^-9 to 2^-8 of a weight; around
+    1 that is two to four of the default lr) leaves them where they are."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, seed=0, capturable=False):
         if lr < 0.0 or not all(0.0 <= b < 1.0 for b in betas) or eps < 0.0 or weight_decay < 0.0:

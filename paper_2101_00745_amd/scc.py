@@ -814,7 +814,8 @@ def scc_vocabulary_loss(x, w, target, reduction="mean", ignore_index=-100):
 
 
 def scc_vocabulary_gradients(x, w, target, lse, dloss, reduction="mean", ignore_index=-100):
-    """(dx, dw) of scc_vocabulary_loss from the lse that it returned: dx like x, dw [V,C] float32; dloss: the loss's gradient, float32 of its shape."""
+    """(dx, dw) of scc_vocabulary_loss from the lse that it returned: dx like x, dw [V,C] float32; dloss: the loss's gradient, float32 of its shape.  Of bfloat16
+    tensors the softmax and dloss x are rounded to 11 bits between the products, so dw's terms are off by 2^-12 each."""
     return _vocabulary_gradients(x, w, target, lse, dloss, _reduction(reduction), ignore_index, False)
 
 
@@ -883,7 +884,7 @@ def scc_adamw_step(weights, grads, first, second, lr, step, betas=(0.9, 0.999), 
     lr (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps).  weights and grads: float32 or bfloat16, one dtype for all.  States: float32, or with
     first_scales and second_scales (float32, one for each 256 elements of a weight) float8_e4m3fn, m = first * scale, v = (second * scale)^2,
     rounded at random with the stored values' expectation kept: a hash of seed, step and place.  step: from 1; or an int64 tensor of one element on
-    the GPU, read when the call runs, for calls that are captured and replayed.  No weight or state may overlap another tensor of the call.  A graph that
+    the GPU, read when the call runs, for calls that are captured and replayed (lr, betas, eps and weight_decay are read at the capture).  No weight or state may overlap another tensor of the call.  A graph that
     saved a weight cannot be run backward afterwards, as after any change in place."""
     native = _native or _load_native()
     status = native.adamw_step(weights, grads, first, second, first_scales, second_scales, lr, step, betas[0], betas[1], eps, weight_decay, seed)
